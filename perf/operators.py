@@ -1,0 +1,468 @@
+"""Operators of a transformer block around the packed attention, as measurable cases.
+
+Three operators, each as a user's program calls it, forward alone (inference) or forward and backward (training):
+
+  norm_pack       the norm in front of a block: the selected tokens' rows are normed on their way into packed order; backward:
+                  the gradient at token positions, added to that of the residual path
+  norm_residual   the norm behind a block with the token's gate and the residual scale, scattered back onto the residual
+                  stream; backward: through the norm, and on into the gate that scored the tokens
+  bias_attention  attention inside every image's packed segment with a learned bias by the bucket of the relative position
+                  of two tokens on the image's grid; backward: with the gradient of the bias table
+
+Shapes are those of the framework's workloads (ViT-S / ViT-B at 14 x 14 tokens, detection at 50 x 84, the first stage of the
+hierarchy at 56 x 56, the two-image fp32 batch) and odd grids beside them.  A program keeps its launches, buffers and plans
+(`prepare`); the inputs of a pass are read from the buffers anew each time.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+EPS = 1e-6
+LOSS_SCALE = 1e-3
+
+
+def _case(name, op, train, B, h, w, C, H, lo, hi, dtype="bf16", norm="layer", buckets="exact"):
+    return dict(name=name, op=op, train=train, B=B, h=h, w=w, C=C, H=H, lo=lo, hi=hi, dtype=dtype, norm=norm, buckets=buckets)
+
+
+def listed():
+    return [
+        # one classification image at a time, as an online service does: the smallest call, bound by latency
+        _case("norm_pack_one_image", "norm_pack", False, 1, 14, 14, 384, 6, 0.10, 0.90),
+        # the norm of a ViT-B-shaped training step
+        _case("norm_pack_vit_b_train", "norm_pack", True, 64, 14, 14, 768, 12, 0.05, 0.95),
+        # a ragged batch in fp32 with the norm that keeps the mean
+        _case("norm_pack_ragged_f32_train", "norm_pack", True, 23, 17, 23, 448, 7, 0.05, 0.95, dtype="f32", norm="rms"),
+        # a large detection batch, training
+        _case("norm_pack_det_train", "norm_pack", True, 32, 50, 84, 256, 8, 0.05, 0.40, norm="rms"),
+        # one classification image
+        _case("norm_residual_one_image", "norm_residual", False, 1, 14, 14, 384, 6, 0.10, 0.90),
+        # a large detection batch, inference
+        _case("norm_residual_det", "norm_residual", False, 32, 50, 84, 256, 8, 0.05, 0.40),
+        # ViT-B-shaped training step, on into the gate
+        _case("norm_residual_vit_b_train", "norm_residual", True, 64, 14, 14, 768, 12, 0.05, 0.95),
+        # first stage of a hierarchy: many narrow rows
+        _case("norm_residual_stage_train", "norm_residual", True, 16, 56, 56, 96, 3, 0.10, 0.60, norm="rms"),
+        # two small images in fp32, a bias of its own for every offset
+        _case("bias_attention_tiny_f32_train", "bias_attention", True, 2, 14, 14, 64, 2, 0.20, 0.40, dtype="f32"),
+        # ViT-B-shaped training step, a bias for every offset (27 x 27 of them)
+        _case("bias_attention_vit_b_train", "bias_attention", True, 64, 14, 14, 768, 12, 0.05, 0.95),
+        # detection batch, inference, offsets in buckets that widen with the distance
+        _case("bias_attention_det", "bias_attention", False, 8, 50, 84, 256, 8, 0.05, 0.40, buckets="log"),
+        # first stage of a hierarchy, training, a bias for every offset (111 x 111): the largest
+        _case("bias_attention_stage_train", "bias_attention", True, 16, 56, 56, 96, 3, 0.10, 0.60),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    most = max(_cost(c) for c in listed())
+    while True:
+        op = rng.choice(["norm_pack", "norm_residual", "bias_attention", "bias_attention"])
+        long = rng.random() < 0.4
+        h = _log_int(rng, 17, 64) if long else rng.randint(1, 16)
+        w = _log_int(rng, 17, 96) if long else rng.randint(2, 20)
+        B, H, Dh = _log_int(rng, 1, 128), _log_int(rng, 1, 16), rng.choice([32, 64])
+        C = H * Dh if op == "bias_attention" else rng.choice([H * Dh, 8 * _log_int(rng, 4, 128)])
+        lo = round(rng.uniform(0.0, 0.4), 2)
+        hi = round(rng.uniform(lo + 0.05, 0.95), 2)
+        dtype = "f32" if rng.random() < 0.2 else "bf16"
+        c = _case("", op, rng.random() < 0.5, B, h, w, C, H, lo, hi, dtype, rng.choice(["layer", "rms"]), rng.choice(["exact", "log"]))
+        del c["name"]
+        if C <= 1024 and B * h * w <= 140_000 and _cost(c) <= most and not (dtype == "f32" and B * h * w > 12_000):
+            return c
+
+
+# ---------------------------------------------------------------------------------- inputs
+def _axis_buckets(n, near=4, levels=4):
+    """Bucket of every offset -(n-1) .. n-1 along an axis: one each up to `near`, then `levels` that widen with the
+    distance up to n, each sign its own."""
+    d = np.arange(-(n - 1), n)
+    a = np.abs(d)
+    far = near + np.floor(np.log(np.maximum(a, near) / near) / np.log(max(n, near + 1) / near) * levels)
+    b = np.where(a < near, a, np.minimum(far, near + levels - 1)).astype(np.int64)
+    return np.where(d < 0, b + near + levels, b), 2 * (near + levels)
+
+
+def _buckets(c):
+    if c["buckets"] == "exact":
+        n = (2 * c["h"] - 1) * (2 * c["w"] - 1)
+        return np.arange(n), n
+    (rows, nr), (cols, nc) = _axis_buckets(c["h"]), _axis_buckets(c["w"])
+    return (rows[:, None] * nc + cols[None, :]).reshape(-1), nr * nc
+
+
+def _selection(c, g):
+    """Per image a disc of the tokens around a random centre, lo .. hi of them, with some tokens flipped."""
+    B, h, w = c["B"], c["h"], c["w"]
+    N = h * w
+    at = torch.rand(B, 2, generator=g, device="cuda")
+    frac = c["lo"] + (c["hi"] - c["lo"]) * torch.rand(B, generator=g, device="cuda")
+    t = torch.arange(N, device="cuda")
+    dist = (t // w - at[:, :1] * h) ** 2 + (t % w - at[:, 1:] * w) ** 2
+    rank = dist.argsort(1).argsort(1)
+    flip = torch.rand(B, N, generator=g, device="cuda") < 0.02
+    return ((rank < (frac * N)[:, None]) ^ flip).to(torch.uint8)
+
+
+def prepare(case, seed):
+    c = case
+    B, N, C, H = c["B"], c["h"] * c["w"], c["C"], c["H"]
+    cap, td = B * N, torch.bfloat16 if c["dtype"] == "bf16" else torch.float32
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    zeros = lambda *s, dtype=td: torch.zeros(*s, dtype=dtype, device="cuda")
+    f32 = dict(dtype=torch.float32)
+    mask = _selection(c, g)
+    lens = mask.sum(1, dtype=torch.int64)
+    chosen = mask.view(-1).nonzero().view(-1)
+    T = chosen.numel()
+    gather_idx, inv_pos = zeros(cap, dtype=torch.int32), torch.full((cap,), -1, dtype=torch.int32, device="cuda")
+    gather_idx[:T] = chosen.int()
+    inv_pos[chosen] = torch.arange(T, dtype=torch.int32, device="cuda")
+    cu = zeros(B + 1, dtype=torch.int32)
+    cu[1:] = lens.cumsum(0)
+    s = dict(c, N=N, cap=cap, T=T, n_max=int(lens.max()), mask=mask, gather_idx=gather_idx, inv_pos=inv_pos, cu=cu,
+             total=torch.tensor([T], dtype=torch.int32, device="cuda"))
+    if c["op"] == "bias_attention":
+        buckets, nb = _buckets(c)
+        s.update(qkv=rnd(cap, 3 * C).to(td), dout=rnd(cap, C).to(td), table=(0.5 * rnd(H, nb)).to(td), nb=nb,
+                 buckets=torch.from_numpy(buckets.astype(np.int32)).cuda())
+    else:
+        s.update(x=(rnd(B, N, C) + 0.3 * rnd(B, N, 1)).to(td), gamma=(1 + 0.2 * rnd(C)).to(td),
+                 beta=(0.2 * rnd(C)).to(td) if c["norm"] == "layer" else None, dy=rnd(B, N, C).to(td))
+    if c["op"] == "norm_pack":
+        s.update(d_packed=rnd(cap, C).to(td))
+    if c["op"] == "norm_residual":
+        s.update(z=rnd(cap, C).to(td), scale=(0.5 * rnd(C)).to(td), gate_w=(rnd(C) / C ** 0.5).to(td),
+                 scores=torch.where(mask.bool(), 1.0, -1.0) * (0.2 + rnd(B, N).abs()),
+                 labels=(mask ^ (torch.rand(B, N, generator=g, device="cuda") < 0.05)).to(torch.uint8))
+    if own:
+        _prepare_own(s, zeros, f32)
+        s["outputs"] = _given(s["outputs"])
+    return s
+
+
+def _prepare_own(s, zeros, f32):
+    """What a program keeps: result buffers, workspaces, and the launches of the pass bound to them."""
+    from paper_2410_23608_amd import spa
+    B, N, C, H, cap, td = s["B"], s["N"], s["C"], s["H"], s["cap"], s["x"].dtype if "x" in s else s["qkv"].dtype
+    code = spa.SPA_BF16 if td == torch.bfloat16 else spa.SPA_F32
+    ws = lambda n: torch.empty(max(n, 256), dtype=torch.uint8, device="cuda")
+    if s["op"] == "bias_attention":
+        Dh, grid = C // H, (s["h"], s["w"])
+        q, k, v = (s["qkv"][:, i * C:(i + 1) * C] for i in range(3))
+        out, lse = zeros(cap, C), zeros(H, cap, **f32)
+        # (for the backward's row sums: what rounding took from out)
+        low = zeros(cap, C) if s["train"] and td == torch.bfloat16 else None
+        s["outputs"] = dict(out=out, lse=lse)
+        s["launches"] = [spa.spa_packed_attention_bias(q, k, v, s["cu"], s["gather_idx"], s["table"], s["buckets"], grid, B, N, H,
+                                                       Dh, out, low, lse, prepare=True)]
+        if s["train"]:
+            dqkv, d_table = zeros(cap, 3 * C), zeros(H, s["nb"], **f32)
+            dq, dk, dv = (dqkv[:, i * C:(i + 1) * C] for i in range(3))
+            s["outputs"].update(dqkv=dqkv, d_table=d_table)
+            s["launches"].append(spa.spa_packed_attention_bias_bwd(
+                q, k, v, out, low, s["dout"], lse, s["cu"], s["gather_idx"], s["table"], s["buckets"], grid, B, N, H, Dh, dq, dk, dv,
+                d_table, ws(spa.spa_attention_bias_bwd_workspace_bytes(B, N, H, Dh, *grid, code)), prepare=True))
+        return
+    kind = spa.SPA_NORM_LAYER if s["norm"] == "layer" else spa.SPA_NORM_RMS
+    stats = zeros(2, cap, **f32) if s["train"] else None
+    dgamma, dbeta = zeros(C, **f32), zeros(C, **f32) if s["beta"] is not None else None
+    ws_norm = ws(spa.spa_norm_bwd_workspace_bytes(cap, C, code))
+    if s["op"] == "norm_pack":
+        packed = zeros(cap, C)
+        s["outputs"] = dict(packed=packed)
+        s["launches"] = [spa.spa_norm_packed(s["x"], s["gather_idx"], s["total"], s["gamma"], s["beta"], kind, EPS, packed, stats,
+                                             prepare=True)]
+        if s["train"]:
+            dx = zeros(B, N, C)
+            s["outputs"].update(dx=dx, dgamma=dgamma, dbeta=dbeta)
+            s["launches"].append(spa.spa_norm_packed_bwd(s["d_packed"], s["x"], s["gather_idx"], s["inv_pos"], s["total"], s["gamma"],
+                                                         kind, stats, s["dy"], dx, dgamma, dbeta, ws_norm, prepare=True))
+        return
+    y = zeros(B, N, C)
+    s["outputs"] = dict(y=y)
+    s["launches"] = [spa.spa_norm_residual_unpack(s["z"], s["inv_pos"], s["x"], s["gamma"], s["beta"], s["scale"], s["scores"], kind,
+                                                  EPS, y, stats, prepare=True)]
+    if s["train"]:
+        dz, d_scores, dscale = zeros(cap, C), zeros(B, N, **f32), zeros(C, **f32)
+        dx, dw, db, loss = zeros(B, N, C), zeros(C, **f32), zeros(1, **f32), zeros(1, **f32)
+        s["outputs"].update(dz=dz, d_scores=d_scores, dgamma=dgamma, dbeta=dbeta, dscale=dscale, dx=dx, dw=dw, db=db, loss=loss)
+        s["launches"] += [
+            spa.spa_norm_residual_unpack_bwd(s["dy"], s["z"], s["gather_idx"], s["inv_pos"], s["total"], s["gamma"], s["beta"],
+                                             s["scale"], s["scores"], kind, stats, dz, d_scores, dgamma, dbeta, dscale, ws_norm,
+                                             prepare=True),
+            spa.spa_gate_bwd_scores(s["x"], s["gate_w"], 0.0, s["scores"], None, s["labels"], d_scores, s["dy"], LOSS_SCALE, loss, dx, dw,
+                                    db, ws(spa.spa_gate_bwd_workspace_bytes(B, N, C, code)), prepare=True)]
+
+
+# ---------------------------------------------------------------------------------- the pass
+def run(state):
+    if own:
+        for launch in state["launches"]:
+            launch()
+        return state["outputs"]
+    return _given({"norm_pack": _norm_pack, "norm_residual": _norm_residual, "bias_attention": _bias_attention}[state["op"]](state))
+
+
+def _given(outputs):
+    """Without the results that the norm at hand does not have (no offset, no gradient of one)."""
+    return {name: t for name, t in outputs.items() if t is not None}
+
+
+def _normed(x, norm):
+    """The rows of x (fp32) without their scale and offset, and the factor that did it."""
+    if norm == "layer":
+        x = x - x.mean(-1, keepdim=True)
+    r = torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS)
+    return x * r, r
+
+
+def _norm_grad(g, xh, r, norm):
+    """Gradient of the rows from that of the normed rows."""
+    if norm == "layer":
+        g = g - g.mean(-1, keepdim=True)
+    return (g - xh * (g * xh).mean(-1, keepdim=True)) * r
+
+
+def _norm_pack(s):
+    td, sel, flat = s["x"].dtype, s["gather_idx"][:s["T"]].long(), s["x"].view(s["cap"], -1)
+    gamma = s["gamma"].float()
+    xh, r = _normed(flat[sel].float(), s["norm"])
+    a = xh * gamma
+    if s["beta"] is not None:
+        a = a + s["beta"].float()
+    packed = torch.zeros_like(flat)
+    packed[:s["T"]] = a.to(td)
+    out = dict(packed=packed)
+    if s["train"]:
+        da = s["d_packed"][:s["T"]].float()
+        dx = s["dy"].float().view(s["cap"], -1).clone()
+        dx[sel] += _norm_grad(da * gamma, xh, r, s["norm"])
+        out.update(dx=dx.to(td).view_as(s["x"]), dgamma=(da * xh).sum(0, dtype=torch.float64).float(),
+                   dbeta=da.sum(0, dtype=torch.float64).float() if s["beta"] is not None else None)
+    return out
+
+
+def _norm_residual(s):
+    td, T, sel, cap = s["x"].dtype, s["T"], s["gather_idx"][:s["T"]].long(), s["cap"]
+    gamma, scale = s["gamma"].float(), s["scale"].float()
+    x = s["x"].float().view(cap, -1)
+    zh, r = _normed(s["z"][:T].float(), s["norm"])
+    u = zh * gamma
+    if s["beta"] is not None:
+        u = u + s["beta"].float()
+    p_all = 1 / (1 + torch.exp(-s["scores"].view(-1)))
+    p = p_all[sel][:, None]
+    y = x.clone()
+    y[sel] += p * scale * u
+    out = dict(y=y.to(td).view_as(s["x"]))
+    if s["train"]:
+        dy_all = s["dy"].float().view(cap, -1)
+        dy = dy_all[sel]
+        h = p * scale * dy
+        dz = torch.zeros_like(s["z"])
+        dz[:T] = _norm_grad(h * gamma, zh, r, s["norm"]).to(td)
+        d_scores = torch.zeros(cap, device="cuda")
+        d_scores[sel] = (dy * scale * u).sum(1) * (p * (1 - p))[:, 0]
+        sums = lambda v: v.sum(0, dtype=torch.float64).float()
+        sc, lab = s["scores"].view(-1), s["labels"].view(-1).float()
+        ds = LOSS_SCALE * (p_all - lab) + d_scores
+        bce = torch.clamp(sc, min=0) - lab * sc + torch.log1p(torch.exp(-sc.abs()))
+        out.update(dz=dz, d_scores=d_scores.view_as(s["scores"]), dgamma=sums(h * zh),
+                   dbeta=sums(h) if s["beta"] is not None else None, dscale=sums(p * dy * u),
+                   dx=(dy_all + ds[:, None] * s["gate_w"].float()).to(td).view_as(s["x"]), dw=sums(ds[:, None] * x),
+                   db=sums(ds[:, None]), loss=LOSS_SCALE * sums(bce[:, None]))
+    return out
+
+
+def _bias_attention(s):
+    B, N, C, H, T, n = s["B"], s["N"], s["C"], s["H"], s["T"], max(s["n_max"], 1)
+    Dh, td, cap, w = C // H, s["qkv"].dtype, s["cap"], s["w"]
+    cu = s["cu"].long()
+    at = torch.arange(n, device="cuda")
+    ok = at < (cu[1:] - cu[:-1])[:, None]                                     # [B, n]: rows of the padded batch
+    rows = torch.where(ok, cu[:-1, None] + at, 0)
+    padded = lambda t: torch.where(ok[..., None], t[rows].float(), 0.0).view(B, n, H, Dh).transpose(1, 2).contiguous()
+    q, k, v = (padded(s["qkv"][:, i * C:(i + 1) * C]) for i in range(3))
+    tok = torch.where(ok, s["gather_idx"].long()[rows] % N, 0)
+    p = tok // w * (2 * w - 1) + tok % w
+    offset = p[:, :, None] - p[:, None, :] + (s["h"] - 1) * (2 * w - 1) + w - 1    # [B, n, n]
+    bias = s["table"].float()[:, s["buckets"].long()]                         # [H, offsets]
+    S = torch.matmul(q, k.transpose(2, 3).contiguous()) * Dh ** -0.5 + bias[:, offset].transpose(0, 1)
+    S = torch.where(ok[:, None, None, :], S, float("-inf"))
+    m = torch.where(ok.any(1)[:, None, None, None], S.amax(3, keepdim=True), 0.0)
+    P = torch.exp(S - m)
+    l = P.sum(3, keepdim=True)
+    P = P / torch.where(l > 0, l, 1.0)
+    O = torch.matmul(P, v)
+    unpad = lambda t: t.transpose(1, 2).reshape(B, n, -1)[ok]
+    out, lse = torch.zeros(cap, C, dtype=td, device="cuda"), torch.zeros(H, cap, device="cuda")
+    out[:T] = unpad(O).to(td)
+    lse[:, :T] = unpad((m + torch.log(torch.where(l > 0, l, 1.0)))).transpose(0, 1)
+    res = dict(out=out, lse=lse)
+    if s["train"]:
+        dO = padded(s["dout"])
+        dP = torch.matmul(dO, v.transpose(2, 3).contiguous())
+        dS = P * (dP - (dO * O).sum(3, keepdim=True)) * ok[:, None, :, None]
+        Pt, dSt = (P * ok[:, None, :, None]).transpose(2, 3).contiguous(), dS.transpose(2, 3).contiguous()
+        dqkv = torch.zeros(cap, 3 * C, dtype=td, device="cuda")
+        for i, t in enumerate((torch.matmul(dS, k) * Dh ** -0.5, torch.matmul(dSt, q) * Dh ** -0.5, torch.matmul(Pt, dO))):
+            dqkv[:T, i * C:(i + 1) * C] = unpad(t).to(td)
+        # dS of every pair of positions, then along the diagonals of equal offset (a padded row's position is N)
+        h, nn = s["h"], N + 1
+        pairs = torch.zeros(H, nn * nn, dtype=torch.float64, device="cuda")
+        pos = torch.where(ok, tok, N)
+        for b in range(B):
+            pairs.index_add_(1, (pos[b][:, None] * nn + pos[b]).view(-1), dS[b].reshape(H, -1).double())
+        pairs = pairs.view(H, nn, nn)[:, :N, :N].transpose(1, 2).contiguous().view(H, N, h, w)       # [H, key, query's row, column]
+        by_offset = torch.zeros(H, 2 * h - 1, 2 * w - 1, dtype=torch.float64, device="cuda")
+        for j in range(N):
+            r, col = h - 1 - j // w, w - 1 - j % w
+            by_offset[:, r:r + h, col:col + w] += pairs[:, j]
+        d_table = torch.zeros(H, s["nb"], dtype=torch.float64, device="cuda").index_add_(1, s["buckets"].long(), by_offset.view(H, -1))
+        res.update(dqkv=dqkv, d_table=d_table.float())
+    return res
+
+
+# ------------------------------------------------------------------------------ in 64 bits
+def exact(case, seed):
+    """The results in 64 bits, from the definitions, image by image over the lists of its tokens."""
+    return _given(_exact(prepare(case, seed)))
+
+
+def _exact(s):
+    f = {k: v.double() if torch.is_tensor(v) and v.is_floating_point() else v for k, v in s.items()}
+    B, N, C, cap = s["B"], s["N"], s["C"], s["cap"]
+    tokens = [torch.nonzero(s["mask"][b]).view(-1) for b in range(B)]
+    starts = [0]
+    for t in tokens:
+        starts.append(starts[-1] + t.numel())
+    if s["op"] == "bias_attention":
+        return _exact_attention(s, f, tokens, starts)
+    gamma, beta = f["gamma"], f["beta"] if f["beta"] is not None else torch.zeros_like(f["gamma"])
+    full = lambda: torch.zeros(cap, C, dtype=torch.float64, device="cuda")
+    total = lambda: torch.zeros(C, dtype=torch.float64, device="cuda")
+    dgamma, dbeta, dscale = total(), total(), total()
+
+    def moments(rows):
+        mu = rows.sum(1, keepdim=True) / C if s["norm"] == "layer" else torch.zeros_like(rows[:, :1])
+        sd = torch.sqrt(((rows - mu) ** 2).sum(1, keepdim=True) / C + EPS)
+        return (rows - mu) / sd, sd
+
+    def back(g, hat, sd):
+        inner = g - hat * (g * hat).sum(1, keepdim=True) / C
+        return (inner - g.sum(1, keepdim=True) / C if s["norm"] == "layer" else inner) / sd
+
+    if s["op"] == "norm_pack":
+        packed, dx = full(), f["dy"].clone()
+        for b, t in enumerate(tokens):
+            j = slice(starts[b], starts[b + 1])
+            hat, sd = moments(f["x"][b, t])
+            packed[j] = hat * gamma + beta
+            da = f["d_packed"][j]
+            dx[b, t] += back(da * gamma, hat, sd)
+            dgamma += (da * hat).sum(0)
+            dbeta += da.sum(0)
+        res = dict(packed=packed)
+        if s["train"]:
+            res.update(dx=dx, dgamma=dgamma, dbeta=dbeta if s["beta"] is not None else None)
+        return res
+    y, dz, d_scores = f["x"].clone(), full(), torch.zeros_like(f["scores"])
+    prob = torch.sigmoid(f["scores"])
+    for b, t in enumerate(tokens):
+        j = slice(starts[b], starts[b + 1])
+        hat, sd = moments(f["z"][j])
+        u, p, dy = hat * gamma + beta, prob[b, t][:, None], f["dy"][b, t]
+        y[b, t] += p * f["scale"] * u
+        g = dy * p * f["scale"]
+        dz[j] = back(g * gamma, hat, sd)
+        dgamma += (g * hat).sum(0)
+        dbeta += g.sum(0)
+        dscale += (dy * p * u).sum(0)
+        d_scores[b, t] = ((dy * f["scale"] * u).sum(1, keepdim=True) * p * (1 - p))[:, 0]
+    res = dict(y=y)
+    if s["train"]:
+        lab = s["labels"].double()
+        ds = LOSS_SCALE * (prob - lab) + d_scores
+        loss = -LOSS_SCALE * (lab * torch.nn.functional.logsigmoid(f["scores"])
+                              + (1 - lab) * torch.nn.functional.logsigmoid(-f["scores"])).sum()
+        res.update(dz=dz, d_scores=d_scores, dgamma=dgamma, dbeta=dbeta if s["beta"] is not None else None, dscale=dscale,
+                   dx=f["dy"] + ds[..., None] * f["gate_w"], dw=(ds[..., None] * f["x"]).sum((0, 1)), db=ds.sum().view(1),
+                   loss=loss.view(1))
+    return res
+
+
+def _exact_attention(s, f, tokens, starts):
+    C, H, w = s["C"], s["H"], s["w"]
+    Dh, cap = C // H, s["cap"]
+    zeros = lambda *shape: torch.zeros(*shape, dtype=torch.float64, device="cuda")
+    out, lse, dqkv, d_table = zeros(cap, C), zeros(H, cap), zeros(cap, 3 * C), np.zeros((H, s["nb"]))
+    for b, t in enumerate(tokens):
+        j, n = slice(starts[b], starts[b + 1]), t.numel()
+        if n == 0:
+            continue
+        dr, dc = t[:, None] // w - t[None, :] // w, t[:, None] % w - t[None, :] % w
+        bucket = s["buckets"].long()[(dr + s["h"] - 1) * (2 * w - 1) + dc + w - 1]
+        for h in range(H):
+            col = slice(h * Dh, (h + 1) * Dh)
+            q, k, v = (f["qkv"][j, i * C:(i + 1) * C][:, col] for i in range(3))
+            S = q @ k.T / math.sqrt(Dh) + f["table"][h][bucket]
+            lse[h, j] = torch.logsumexp(S, 1)
+            P = torch.exp(S - lse[h, j][:, None])
+            out[j, col] = P @ v
+            if s["train"]:
+                dO = f["dout"][j, col]
+                dP = dO @ v.T
+                dS = P * (dP - (P * dP).sum(1, keepdim=True))
+                dqkv[j, h * Dh:(h + 1) * Dh] = dS @ k / math.sqrt(Dh)
+                dqkv[j, C + h * Dh:C + (h + 1) * Dh] = dS.T @ q / math.sqrt(Dh)
+                dqkv[j, 2 * C + h * Dh:2 * C + (h + 1) * Dh] = P.T @ dO
+                d_table[h] += np.bincount(bucket.view(-1).cpu().numpy(), dS.reshape(-1).cpu().numpy(), s["nb"])
+    res = dict(out=out, lse=lse)
+    if s["train"]:
+        res.update(dqkv=dqkv, d_table=torch.from_numpy(d_table))
+    return res
+
+
+# ----------------------------------------------------------------------- what a pass cannot do without
+def work(case):
+    c = case
+    B, N, C, H, e = c["B"], c["h"] * c["w"], c["C"], c["H"], 2 if c["dtype"] == "bf16" else 4
+    f1, f2 = (c["lo"] + c["hi"]) / 2, (c["lo"] ** 2 + c["lo"] * c["hi"] + c["hi"] ** 2) / 3
+    cap, T, n2 = B * N, B * N * f1, B * N * N * f2
+    full, sel = cap * C * e, T * C * e
+    if c["op"] == "norm_pack":
+        nbytes, flops = 2 * sel + 4 * T + 2 * C * e, 8.0 * T * C                # rows in and out, their index
+        if c["train"]:
+            nbytes += sel + 2 * full + 4 * cap + 8 * C                          # their gradient; that of the residual path, dx
+            flops += 12.0 * T * C + cap * C
+    elif c["op"] == "norm_residual":
+        nbytes, flops = 2 * full + sel + 4 * cap + 4 * T + 3 * C * e, 10.0 * T * C
+        if c["train"]:
+            # dy, dz; the gate's scores, labels and gradients; dx
+            nbytes += full + sel + 4 * cap + cap + 4 * cap + full + 20 * C
+            flops += 20.0 * T * C + 6.0 * cap * C
+    else:
+        nb = _buckets(c)[1] if c["buckets"] == "log" else (2 * c["h"] - 1) * (2 * c["w"] - 1)
+        nbytes, flops = 4 * sel + 4 * T + 4 * H * T + H * nb * e + 4 * (2 * c["h"] - 1) * (2 * c["w"] - 1), 4.0 * C * n2
+        if c["train"]:
+            nbytes += 4 * sel + 4 * H * nb                                      # dout in; dq, dk, dv, d_table out
+            flops += 10.0 * C * n2
+    return {"bytes": float(nbytes), "flops": flops}
+
+
+def _cost(c):
+    """Rough seconds of a pass, to keep drawn cases within the largest listed one."""
+    w = work(c)
+    return w["bytes"] / 3e12 + w["flops"] / (20e12 if c["dtype"] == "f32" else 200e12)
