@@ -187,7 +187,7 @@ def _prepare_own(s, zeros, f32):
         if s["train"]:
             dx = zeros(B, N, C)
             s["outputs"].update(dx=dx, dgamma=dgamma, dbeta=dbeta)
-            s["launches"].append(spa.spa_norm_packed_bwd(s["d_packed"], s["x"], s["gather_idx"], s["inv_pos"], s["total"], s["gamma"],
+            s["launches"].append(spa.spa_norm_packed_bwd(s["d_packed"], s["x"], s["inv_pos"], s["total"], s["gamma"],
                                                          kind, stats, s["dy"], dx, dgamma, dbeta, ws_norm, prepare=True))
         return
     y = zeros(B, N, C)
