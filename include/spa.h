@@ -481,6 +481,37 @@ int spa_linear_packed_unpack(const void* x, const int32_t* total, const void* W,
                              int K, int N_out, int dtype, const int32_t* gather_idx, const int32_t* inv_pos,
                              int64_t rows, const void* residual, void* y, void* stream);
 
+/*
+ * The norm in front of a block on packed tokens: the rows of the selected tokens are normed on their way into packed order
+ * (a block of Section 3.2 inside a transformer: norm, projections, attention, and the residual add around them).
+ *   packed[j,:] = gamma * xh + beta,  xh = (x_i - mu_i) r_i,  i = gather_idx[j] (j when NULL),   j < min(*total, M_cap)
+ *   SPA_NORM_LAYER: mu = mean(x_i), r = 1 / sqrt(mean((x_i - mu)^2) + eps)
+ *   SPA_NORM_RMS:   mu = 0,         r = 1 / sqrt(mean(x_i^2) + eps)
+ * Moments in fp32, the variance from the deviations; one rounding, at the store.
+ * in:  x [*, C] dtype; gather_idx [>= rows used] int32 or NULL; total [1] int32 (device) or NULL (= M_cap rows);
+ *      gamma, beta [C] dtype, each NULL for 1 and 0; eps >= 0 (host float); C <= 8192.
+ * out: packed [M_cap, C] dtype (later rows are not written); stats [2, M_cap] fp32 or NULL: mu (SPA_NORM_LAYER only) and r
+ *      of the packed rows, for the backward.
+ */
+#define SPA_NORM_LAYER 0
+#define SPA_NORM_RMS 1
+int spa_norm_packed(const void* x, const int32_t* gather_idx, const int32_t* total, const void* gamma, const void* beta,
+                    int kind, float eps, int M_cap, int C, int dtype, void* packed, float* stats, void* stream);
+
+/*
+ * The norm behind a block, with the token's gate and the residual scale, and the scatter back onto the residual stream
+ * (Section 3.2: unselected tokens bypass the block, Sigmoid(s) weighs what a selected one gets from it):
+ *   y[i,:] = residual[i,:] + Sigmoid(gate_scores[i]) * scale * (gamma * zh_j + beta),  j = inv_pos[i], where 0 <= j < M_cap
+ *   y[i,:] = residual[i,:]                                                              elsewhere,  i < rows
+ * zh_j: row j of z normed as in spa_norm_packed.  One rounding, at the store.
+ * in:  z [M_cap, C] dtype; inv_pos [rows] int32 from spa_pack or NULL (j = i); residual [rows, C] dtype or NULL (0); gamma,
+ *      beta, scale [C] dtype, each may be NULL (1, 0, 1); gate_scores [rows] fp32 or NULL (weight 1); kind, eps as above.
+ * out: y [rows, C] dtype; may be residual itself: the unselected rows are then not touched.  stats [2, M_cap] fp32 or NULL.
+ */
+int spa_norm_residual_unpack(const void* z, const int32_t* inv_pos, const void* residual, const void* gamma, const void* beta,
+                             const void* scale, const float* gate_scores, int kind, float eps, int M_cap, int64_t rows, int C,
+                             int dtype, void* y, float* stats, void* stream);
+
 /* ----------------------------------------------------------------- training ---- */
 
 /*
@@ -683,6 +714,52 @@ int spa_gate_bwd_straight_through(const void* x, const void* w, float bias, cons
                                   float temperature, int B, int N, int C, int dtype, float* loss,
                                   void* dx, float* dw, float* db, void* workspace,
                                   size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace the two calls below need: rows = B*N for spa_norm_packed_bwd, M_cap for the other. Host. */
+size_t spa_norm_bwd_workspace_bytes(int64_t rows, int C, int dtype);
+
+/*
+ * Backward of spa_norm_packed, at the token positions and onto the gradient that comes by the residual path: with
+ * da = d_packed[inv_pos[i],:], g = da * gamma,
+ *   dx[i,:] = d_residual[i,:] + r (g - mean(g) - xh mean(g xh))      where 0 <= inv_pos[i] < min(*total, M_cap)
+ *   dx[i,:] = d_residual[i,:]                                         elsewhere,  i < rows
+ *   dgamma = sum_j da xh,  dbeta = sum_j da                           (SPA_NORM_RMS: without mean(g))
+ * in:  d_packed [M_cap, C], x [rows, C] dtype; inv_pos [rows] int32 or NULL (row i is packed row i); total as in the
+ *      forward; gamma or NULL; stats of the forward; d_residual [rows, C] dtype or NULL (0); workspace (device, 16-byte
+ *      aligned) of spa_norm_bwd_workspace_bytes(rows, C, dtype) bytes.
+ * out: dx [rows, C] dtype, may be d_residual itself; dgamma, dbeta [C] fp32, each may be NULL.  Run-to-run bit-stable.
+ */
+int spa_norm_packed_bwd(const void* d_packed, const void* x, const int32_t* inv_pos, const int32_t* total, const void* gamma,
+                        int kind, const float* stats, const void* d_residual, int M_cap, int64_t rows, int C, int dtype, void* dx,
+                        float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Backward of spa_norm_residual_unpack (the gradient of residual is dy itself).  i = gather_idx[j], p = Sigmoid(gate_scores[i]),
+ * g = p dy_i * scale * gamma:
+ *   dz[j,:] = r (g - mean(g) - zh mean(g zh)),   j < min(*total, M_cap)       (SPA_NORM_RMS: without mean(g))
+ *   d_scores[i] = p (1 - p) <dy_i, scale * (gamma * zh + beta)>, 0 for tokens that were not selected
+ *   dgamma = scale * sum_j p dy_i zh,  dbeta = scale * sum_j p dy_i,  dscale = sum_j p dy_i (gamma zh + beta)
+ * in:  dy [rows, C], z [M_cap, C] dtype; gather_idx [M_cap], inv_pos [rows] int32 from spa_pack, or both NULL (row j is token
+ *      j; d_scores is then written for those rows alone); total [1] int32 (device) or NULL; the rest as in the forward;
+ *      workspace (device, 16-byte aligned) of spa_norm_bwd_workspace_bytes(M_cap, C, dtype) bytes.
+ * out: dz [M_cap, C] dtype (later rows are not written); d_scores [rows] fp32 or NULL (needs gate_scores), for
+ *      spa_gate_bwd_scores; dgamma, dbeta, dscale [C] fp32, each may be NULL.  Run-to-run bit-stable.
+ */
+int spa_norm_residual_unpack_bwd(const void* dy, const void* z, const int32_t* gather_idx, const int32_t* inv_pos,
+                                 const int32_t* total, const void* gamma, const void* beta, const void* scale,
+                                 const float* gate_scores, int kind, const float* stats, int M_cap, int64_t rows, int C, int dtype,
+                                 void* dz, float* d_scores, float* dgamma, float* dbeta, float* dscale, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * spa_gate_bwd where the rest of the block has formed the gradients of the scores and of x itself (a gate behind the
+ * block's norm): as there, with
+ *   ds_i = loss_scale (p_i - y_i) + d_scores[i],   dx_i = d_x[i,:] + own_i ds_i w
+ * in:  as spa_gate_bwd; d_scores [B,N] fp32; d_x [B,N,C] dtype or NULL (0).   out: as spa_gate_bwd; dx may be d_x itself.
+ */
+int spa_gate_bwd_scores(const void* x, const void* w, float bias, const float* scores, const float* s_up, const uint8_t* labels,
+                        const float* d_scores, const void* d_x, float loss_scale, int B, int N, int C, int dtype, float* loss,
+                        void* dx, float* dw, float* db, void* workspace, size_t workspace_bytes, void* stream);
 
 /* -------------------------------------------------- comparison baseline -------- */
 

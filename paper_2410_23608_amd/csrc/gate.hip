@@ -7,72 +7,13 @@
 #include <mutex>
 
 #include "group.h"
+#include "row_groups.h"
 #include "spa_common.h"
 
 namespace spa {
 
 constexpr int kGateThreads = 256;
 constexpr int kMaxGateC = 8192;
-
-template <typename T> struct Vec16;
-template <> struct Vec16<float> {
-  static constexpr int kElems = 4;
-  // dx is the last thing the backward pass writes and nothing here reads it again: non-temporal
-  __device__ static __forceinline__ void store(float* p, const float (&f)[4]) {
-    floatx4 v = {f[0], f[1], f[2], f[3]};
-    __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(p));
-  }
-};
-template <> struct Vec16<__bf16> {
-  static constexpr int kElems = 8;
-  __device__ static __forceinline__ void store(__bf16* p, const float (&f)[8]) {
-    floatx8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = f[i];
-    __builtin_nontemporal_store(float_to_bf16x8(v), reinterpret_cast<bf16x8*>(p));
-  }
-};
-
-template <typename T> struct Raw16;
-template <> struct Raw16<float> { using type = floatx4; };
-template <> struct Raw16<__bf16> { using type = bf16x8; };
-__device__ __forceinline__ void widen(floatx4 v, float (&f)[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = v[i];
-}
-__device__ __forceinline__ void widen(bf16x8 v, float (&f)[8]) {
-  const floatx8 w = bf16x8_to_float(v);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = w[i];
-}
-
-// Sum over groups of G neighbouring lanes, in every lane, in the order of exchanges with lane ^ G/2, ^ G/4, ... ^ 1, in the
-// vector ALU: the two halves and the two 16-lane rows of a half by the lane swaps, ^ 8 as a rotation of the row by 8, ^ 4 as
-// one by 4 once both halves of a row hold the same (groups of 8: as two shifts), ^ 2 and ^ 1 inside a quad.  An
-// exchange through LDS takes 85 cycles, one of these 8 to 16, and the dot products wait for each of them.
-__device__ __forceinline__ float add_lane_xor32(float v) {
-  const unsigned u = __builtin_bit_cast(unsigned, v);
-  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  const unsigned a = r[0], b = r[1];
-  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
-}
-__device__ __forceinline__ float add_lane_xor16(float v) {
-  const unsigned u = __builtin_bit_cast(unsigned, v);
-  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  const unsigned a = r[0], b = r[1];
-  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
-}
-template <int G>
-__device__ __forceinline__ float group_sum(float v) {
-  constexpr int kRor = 0x120;
-  if (G > 32) v = add_lane_xor32(v);
-  if (G > 16) v = add_lane_xor16(v);
-  if (G > 8) v += dpp_move<kRor + 8>(v);
-  if (G > 8) v += dpp_move<kRor + 4>(v);
-  else v += lane_xor<4>(v);
-  v += lane_xor<2>(v);
-  return v + lane_xor<1>(v);
-}
 
 // Lanes per token: by the row's 16-byte chunks (the same for every launch of the gate)
 __host__ __device__ constexpr int gate_lanes(int chunks) { return chunks <= 8 ? 8 : chunks <= 64 ? 16 : chunks <= 256 ? 32 : 64; }
@@ -532,8 +473,10 @@ struct GateBwdArgs {
   int ntok, C;
   T* dx;
   float* partial;
+  const float* d_scores;       // kScores: a gradient of the scores that the caller formed, added to that of the loss;
+                               // d_rg is then the gradient of x by other ways (or null), added to dx as it is
 };
-template <typename T, int G, int IT, int U>
+template <typename T, int G, int IT, int U, bool kScores = false>
 __device__ __forceinline__ void gate_bwd_block(const GateBwdArgs<T>& a, unsigned block, unsigned blocks, float* lds) {
   constexpr int VE = Vec16<T>::kElems, kGroups = kGateThreads / G, kWaves = kGateThreads / kWave;
   using Raw = typename Raw16<T>::type;
@@ -549,7 +492,7 @@ __device__ __forceinline__ void gate_bwd_block(const GateBwdArgs<T>& a, unsigned
 
   const int grp = threadIdx.x / G, gl = threadIdx.x % G;
   const int chunks = C / VE;
-  const bool scaled = gate_scaled != 0 && d_rg != nullptr;
+  const bool scaled = kScores ? d_rg != nullptr : gate_scaled != 0 && d_rg != nullptr;
   float wv[IT][VE], dwa[IT][VE];
 #pragma unroll
   for (int it = 0; it < IT; ++it) {
@@ -566,7 +509,7 @@ __device__ __forceinline__ void gate_bwd_block(const GateBwdArgs<T>& a, unsigned
   const long t0 = block * per, t1 = min((long)ntok, t0 + per);
   for (long base = t0 + grp; base < t1; base += kGroups * U) {
     Raw xr[U][IT], dr[U][IT];
-    float s[U], up[U], nz[U];
+    float s[U], up[U], nz[U], given[U];
     uint8_t lab[U], sel[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -586,6 +529,7 @@ __device__ __forceinline__ void gate_bwd_block(const GateBwdArgs<T>& a, unsigned
       up[u] = s_up != nullptr ? s_up[tok] : 0.f;
       sel[u] = st.mask != nullptr ? st.mask[tok] : 0;
       nz[u] = st.noise != nullptr ? st.noise[tok] : 0.f;
+      if (kScores) given[u] = a.d_scores[tok];
     }
     float s_mine = 0.f, y_mine = 0.f, d_mine = 0.f;          // lane u of the group keeps the loss of its token u
 #pragma unroll
@@ -598,9 +542,9 @@ __device__ __forceinline__ void gate_bwd_block(const GateBwdArgs<T>& a, unsigned
         widen(xr[u][it], xf[it]);
         widen(dr[u][it], df[it]);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) dot = fmaf(df[it][e], xf[it][e], dot);
+        for (int e = 0; e < VE && !kScores; ++e) dot = fmaf(df[it][e], xf[it][e], dot);
       }
-      dot = group_sum<G>(dot);
+      if (!kScores) dot = group_sum<G>(dot);
       bool own = tok < t1;
       if (s_up != nullptr) {                             // (uniform) did the up-scale score win the max? (see gate_chains)
         float g = 0.f;
@@ -613,7 +557,9 @@ __device__ __forceinline__ void gate_bwd_block(const GateBwdArgs<T>& a, unsigned
       const float p = sigmoidf_dev(s[u]);
       const float y = lab[u] != 0 ? 1.f : 0.f;
       float ds = loss_scale * (p - y);
-      if (scaled) {
+      if (kScores) {
+        ds += given[u];
+      } else if (scaled) {
         float coef = p * (1.f - p);                      // through r_g = sigmoid(s) . r
         if (sel[u] != 0) {                               // through the relaxed selection weight: <d_rg, r_g> = p dot
           const float pt = sigmoidf_dev((s[u] + nz[u]) * st.inv_temperature);
@@ -622,7 +568,7 @@ __device__ __forceinline__ void gate_bwd_block(const GateBwdArgs<T>& a, unsigned
         ds = fmaf(coef, dot, ds);
       }
       const float dsg = own ? ds : 0.f;                  // (w, b) get no gradient where the up-scale score won
-      const float pg = scaled ? p : 0.f;
+      const float pg = scaled ? (kScores ? 1.f : p) : 0.f;
 #pragma unroll
       for (int it = 0; it < IT; ++it) {
         const int ch = gl + it * G;
@@ -685,10 +631,10 @@ __device__ __forceinline__ void gate_bwd_block(const GateBwdArgs<T>& a, unsigned
 }
 
 // LDS: 4 rows of C floats
-template <typename T, int G, int IT, int U>
+template <typename T, int G, int IT, int U, bool kScores>
 __global__ void __launch_bounds__(kGateThreads) gate_bwd_kernel(const GateBwdArgs<T> a) {
   extern __shared__ float lds[];
-  gate_bwd_block<T, G, IT, U>(a, blockIdx.x, gridDim.x, lds);
+  gate_bwd_block<T, G, IT, U, kScores>(a, blockIdx.x, gridDim.x, lds);
 }
 // Several calls in one launch (launch groups): the forms of launch_gate_bwd, up to 1024 columns
 __global__ void __launch_bounds__(kGateThreads) gate_bwd_group_kernel(const Members<GateBwdArgs<__bf16>> m) {
@@ -934,21 +880,21 @@ extern "C" size_t spa_gate_bwd_workspace_bytes(int B, int N, int C, int dtype) {
   return (size_t)gate_bwd_parts((long)B * N) * (size_t)(C + 2) * sizeof(float);
 }
 
-template <typename T>
+template <typename T, bool kScores = false>
 static int launch_gate_bwd(const void* x, const void* w, float bias, const float* scores, const float* s_up,
                            const uint8_t* labels, const void* d_rg, int gate_scaled, float loss_scale,
                            StraightThrough stt, long ntok, int C, float* loss, void* dx, float* dw, float* db,
-                           float* partial, hipStream_t st) {
+                           float* partial, hipStream_t st, const float* d_scores = nullptr) {
   constexpr int VE = Vec16<T>::kElems;
   const int chunks = C / VE;
   const int parts = gate_bwd_parts(ntok);
   const size_t lds = (size_t)(kGateThreads / kWave) * C * sizeof(float);      // at most 64 KB (C <= 4096)
   const GateBwdArgs<T> args = {static_cast<const T*>(x), static_cast<const T*>(w), bias, scores, s_up, labels,
                                static_cast<const T*>(d_rg), gate_scaled, loss_scale, stt, (int)ntok, C, static_cast<T*>(dx),
-                               partial};
+                               partial, d_scores};
   const GateReduceArgs rargs = {partial, parts, C, loss_scale, loss, dw, db};
   const unsigned rblocks = (C + 2 + 15) / 16;
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 2 && !kScores) {
     if (group_open()) {
       SPA_REQUIRE(C <= 1024, SPA_ERR_UNSUPPORTED, "spa_gate_bwd: C = %d > 1024 cannot be part of a group", C);
       if (int rc = g_noted_bwd.add("spa_gate_bwd", args, parts)) return rc;
@@ -956,7 +902,7 @@ static int launch_gate_bwd(const void* x, const void* w, float bias, const float
     }
   }
   SPA_REQUIRE(!group_open(), SPA_ERR_UNSUPPORTED, "spa_gate_bwd: fp32 calls cannot be part of a group");
-#define SPA_GB(G, IT, U) hipLaunchKernelGGL((gate_bwd_kernel<T, G, IT, U>), dim3(parts), dim3(kGateThreads), lds, st, args)
+#define SPA_GB(G, IT, U) hipLaunchKernelGGL((gate_bwd_kernel<T, G, IT, U, kScores>), dim3(parts), dim3(kGateThreads), lds, st, args)
   // (up to 512 shares a share is 16 tokens, one per group of 16 lanes, two per group of 32: no more taken at a time)
   const bool few = ntok <= 16L * kGateBwdMaxParts;
   if (chunks <= 16 && few) SPA_GB(16, 1, 1);
@@ -977,7 +923,8 @@ static int launch_gate_bwd(const void* x, const void* w, float bias, const float
 static int gate_bwd_common(const char* fn, const void* x, const void* w, float bias, const float* scores,
                            const float* s_up, const uint8_t* labels, const void* d_rg, int gate_scaled,
                            float loss_scale, StraightThrough stt, int B, int N, int C, int dtype, float* loss,
-                           void* dx, float* dw, float* db, void* workspace, size_t workspace_bytes, void* stream) {
+                           void* dx, float* dw, float* db, void* workspace, size_t workspace_bytes, void* stream,
+                           const float* d_scores = nullptr) {
   SPA_REQUIRE(x && w && scores && labels && loss && dx && dw && db, SPA_ERR_INVALID_ARG, "%s: null pointer", fn);
   SPA_REQUIRE(B >= 1 && N >= 1 && C >= 1, SPA_ERR_INVALID_ARG, "%s: B, N, C must be >= 1", fn);
   SPA_REQUIRE((long)B * N < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*N must be < 2^31", fn);
@@ -993,6 +940,12 @@ static int gate_bwd_common(const char* fn, const void* x, const void* w, float b
               "%s: workspace of %zu bytes needed, %zu given", fn, need, workspace_bytes);
   hipStream_t st = as_stream(stream);
   float* partial = static_cast<float*>(workspace);
+  if (d_scores != nullptr && dtype == SPA_F32)
+    return launch_gate_bwd<float, true>(x, w, bias, scores, s_up, labels, d_rg, gate_scaled, loss_scale, stt, (long)B * N,
+                                        C, loss, dx, dw, db, partial, st, d_scores);
+  if (d_scores != nullptr)
+    return launch_gate_bwd<__bf16, true>(x, w, bias, scores, s_up, labels, d_rg, gate_scaled, loss_scale, stt, (long)B * N,
+                                         C, loss, dx, dw, db, partial, st, d_scores);
   if (dtype == SPA_F32)
     return launch_gate_bwd<float>(x, w, bias, scores, s_up, labels, d_rg, gate_scaled, loss_scale, stt, (long)B * N,
                                   C, loss, dx, dw, db, partial, st);
@@ -1007,6 +960,17 @@ extern "C" int spa_gate_bwd(const void* x, const void* w, float bias, const floa
   return gate_bwd_common("spa_gate_bwd", x, w, bias, scores, s_up, labels, d_rg, gate_scaled, loss_scale,
                          StraightThrough{nullptr, nullptr, 1.f}, B, N, C, dtype, loss, dx, dw, db, workspace,
                          workspace_bytes, stream);
+}
+
+extern "C" int spa_gate_bwd_scores(const void* x, const void* w, float bias, const float* scores, const float* s_up,
+                                   const uint8_t* labels, const float* d_scores, const void* d_x, float loss_scale, int B, int N,
+                                   int C, int dtype, float* loss, void* dx, float* dw, float* db, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  SPA_REFUSE_IN_GROUP("spa_gate_bwd_scores");
+  SPA_REQUIRE(d_scores != nullptr, SPA_ERR_INVALID_ARG, "spa_gate_bwd_scores: d_scores is null");
+  return gate_bwd_common("spa_gate_bwd_scores", x, w, bias, scores, s_up, labels, d_x, 0, loss_scale,
+                         StraightThrough{nullptr, nullptr, 1.f}, B, N, C, dtype, loss, dx, dw, db, workspace,
+                         workspace_bytes, stream, d_scores);
 }
 
 // ---- the gate backward for callers that cannot allocate --------------------------------

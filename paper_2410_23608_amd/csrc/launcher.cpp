@@ -74,6 +74,8 @@ const Entry kEntries[] = {
     ENTRY(spa_linear_packed_scatter), ENTRY(spa_linear_packed_unpack), ENTRY(spa_linear_packed_bwd_input), ENTRY(spa_linear_packed_bwd_weight),
     ENTRY(spa_unpack), ENTRY(spa_unpack_bwd), ENTRY(spa_pack_bwd), ENTRY(spa_packed_attention_bwd),
     ENTRY(spa_packed_attention_bwd_tokens), ENTRY(spa_gate_bwd), ENTRY(spa_gate_bwd_static), ENTRY(spa_padded_attention),
+    ENTRY(spa_norm_packed), ENTRY(spa_norm_packed_bwd), ENTRY(spa_norm_residual_unpack), ENTRY(spa_norm_residual_unpack_bwd),
+    ENTRY(spa_gate_bwd_scores),
 };
 
 PyObject* g_on_error = nullptr;      // called with the return code of a failing C call; raises

@@ -112,6 +112,15 @@ _SIGNATURES = {
                              _P, _P, _P, _P, _P, c_size_t, _P]),
     "spa_gate_bwd_static": (c_int, [_P, _P, c_float, _P, _P, _P, _P, c_int, c_float, c_int, c_int, c_int, c_int,
                                     _P, _P, _P, _P, _P]),
+    "spa_norm_packed": (c_int, [_P, _P, _P, _P, _P, c_int, c_float, c_int, c_int, c_int, _P, _P, _P]),
+    "spa_norm_residual_unpack": (c_int, [_P, _P, _P, _P, _P, _P, _P, c_int, c_float, c_int, c_int64, c_int, c_int, _P, _P, _P]),
+    "spa_norm_bwd_workspace_bytes": (c_size_t, [c_int64, c_int, c_int]),
+    "spa_norm_packed_bwd": (c_int, [_P, _P, _P, _P, _P, c_int, _P, _P, c_int, c_int64, c_int, c_int, _P, _P, _P, _P, c_size_t,
+                                    _P]),
+    "spa_norm_residual_unpack_bwd": (c_int, [_P, _P, _P, _P, _P, _P, _P, _P, _P, c_int, _P, c_int, c_int64, c_int, c_int, _P, _P,
+                                             _P, _P, _P, _P, c_size_t, _P]),
+    "spa_gate_bwd_scores": (c_int, [_P, _P, c_float, _P, _P, _P, _P, _P, c_float, c_int, c_int, c_int, c_int, _P, _P, _P, _P, _P,
+                                    c_size_t, _P]),
     "spa_padded_attention": (c_int, [_P, _P, _P, c_int64, _P, c_int, c_int, c_int, c_int, c_int, c_float, _P, _P]),
 }
 for _name, (_res, _args) in _SIGNATURES.items():
@@ -980,6 +989,115 @@ def spa_gate_bwd_straight_through(x, w, bias, scores, s_up, labels, d_rg, loss_s
                      (_ptr(x), _ptr(w), _num(bias), _ptr(scores), _ptr(s_up), _ptr(labels), _ptr(d_rg),
                       _num(loss_scale), _ptr(mask), _ptr(noise), _num(temperature), B, N, C, code,
                       _ptr(loss), _ptr(dx), _ptr(dw), _ptr(db), _ptr(workspace), ws_bytes, _stream(),), _keep, prepare)
+
+
+def spa_gate_bwd_scores(x, w, bias, scores, s_up, labels, d_scores, d_x, loss_scale, loss, dx, dw, db, workspace,
+                        prepare=False):
+    """spa_gate_bwd with the gradient of the scores given (d_scores [B,N] f32, added to that of the loss) and that of x by
+    other ways (d_x [B,N,C] or None, added to dx; dx may be d_x itself)."""
+    fn = "spa_gate_bwd_scores"
+    B, N, C, code = _gate_bwd_checks(fn, x, w, scores, s_up, labels, d_x, None, None, loss, dx, dw, db)
+    _typed(fn, torch.float32, d_scores=d_scores)
+    _holds(fn, d_scores=(d_scores, B * N))
+    _keep = (x, w, scores, s_up, labels, d_scores, d_x, loss, dx, dw, db, workspace,)
+    _contig(*_keep)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return _dispatch(lib.spa_gate_bwd_scores,
+                     (_ptr(x), _ptr(w), _num(bias), _ptr(scores), _ptr(s_up), _ptr(labels), _ptr(d_scores), _ptr(d_x),
+                      _num(loss_scale), B, N, C, code, _ptr(loss), _ptr(dx), _ptr(dw), _ptr(db), _ptr(workspace), ws_bytes,
+                      _stream(),), _keep, prepare)
+
+
+SPA_NORM_LAYER, SPA_NORM_RMS = 0, 1
+
+
+def spa_norm_packed(x, gather_idx, total, gamma, beta, kind, eps, packed, stats=None, prepare=False):
+    """packed[j] = gamma * norm(x[gather_idx[j]]) + beta for j < *total.  x [*, C] (any leading shape), packed [rows, C];
+    gather_idx, total, gamma, beta may be None; stats [2, rows] f32: kept for the backward."""
+    fn = "spa_norm_packed"
+    C, M = x.shape[-1], packed.shape[0]
+    code = _features(fn, x=x, gamma=gamma, beta=beta, packed=packed)
+    _typed(fn, torch.int32, gather_idx=gather_idx, total=total)
+    _typed(fn, torch.float32, stats=stats)
+    _rows(fn, C, packed=(packed, 1))
+    # (without an index packed row j is row j of x; total may say that fewer are wanted)
+    _holds(fn, x=(x, M * C if gather_idx is None else C), gather_idx=(gather_idx, M), total=(total, 1), gamma=(gamma, C), beta=(beta, C),
+           stats=(stats, 2 * M))
+    _keep = (x, gather_idx, total, gamma, beta, packed, stats,)
+    _contig(*_keep)
+    return _dispatch(lib.spa_norm_packed,
+                     (_ptr(x), _ptr(gather_idx), _ptr(total), _ptr(gamma), _ptr(beta), int(kind), _num(eps), M, C, code,
+                      _ptr(packed), _ptr(stats), _stream(),), _keep, prepare)
+
+
+def spa_norm_residual_unpack(z, inv_pos, residual, gamma, beta, scale, gate_scores, kind, eps, y, stats=None, prepare=False):
+    """y[i] = residual[i] + sigmoid(gate_scores[i]) * scale * (gamma * norm(z[inv_pos[i]]) + beta), residual[i] where
+    inv_pos[i] < 0.  z [M, C] packed, y / residual [*, C] (any leading shape); y may be residual itself."""
+    fn = "spa_norm_residual_unpack"
+    M, C = z.shape
+    rows = y.numel() // C
+    if y.shape[-1] != C or (residual is not None and residual.shape != y.shape):
+        raise ValueError(f"{fn}: y (and residual) must be [..., C = {C}]")
+    code = _features(fn, z=z, residual=residual, gamma=gamma, beta=beta, scale=scale, y=y)
+    _typed(fn, torch.int32, inv_pos=inv_pos)
+    _typed(fn, torch.float32, gate_scores=gate_scores, stats=stats)
+    _holds(fn, inv_pos=(inv_pos, rows), gamma=(gamma, C), beta=(beta, C), scale=(scale, C), gate_scores=(gate_scores, rows),
+           stats=(stats, 2 * M))
+    _keep = (z, inv_pos, residual, gamma, beta, scale, gate_scores, y, stats,)
+    _contig(*_keep)
+    return _dispatch(lib.spa_norm_residual_unpack,
+                     (_ptr(z), _ptr(inv_pos), _ptr(residual), _ptr(gamma), _ptr(beta), _ptr(scale), _ptr(gate_scores), int(kind),
+                      _num(eps), M, rows, C, code, _ptr(y), _ptr(stats), _stream(),), _keep, prepare)
+
+
+def spa_norm_bwd_workspace_bytes(rows, C, dtype) -> int:
+    return int(lib.spa_norm_bwd_workspace_bytes(int(rows), int(C), int(dtype)))
+
+
+def spa_norm_packed_bwd(d_packed, x, inv_pos, total, gamma, kind, stats, d_residual, dx, dgamma, dbeta, workspace, prepare=False):
+    """dx[i] = d_residual[i] + the gradient of x[i] through spa_norm_packed (rows with inv_pos[i] >= 0); dgamma, dbeta [C] f32
+    (each may be None).  d_packed [M, C], x / dx / d_residual [*, C]; dx may be d_residual itself."""
+    fn = "spa_norm_packed_bwd"
+    M, C = d_packed.shape
+    rows = dx.numel() // C
+    if dx.shape[-1] != C or x.shape[-1] != C or (d_residual is not None and d_residual.shape != dx.shape):
+        raise ValueError(f"{fn}: x, dx (and d_residual) must be [..., C = {C}]")
+    code = _features(fn, d_packed=d_packed, x=x, gamma=gamma, d_residual=d_residual, dx=dx)
+    _typed(fn, torch.int32, inv_pos=inv_pos, total=total)
+    _typed(fn, torch.float32, stats=stats, dgamma=dgamma, dbeta=dbeta)
+    _holds(fn, x=(x, rows * C), inv_pos=(inv_pos, rows), total=(total, 1), gamma=(gamma, C), stats=(stats, 2 * M),
+           dgamma=(dgamma, C), dbeta=(dbeta, C))
+    _keep = (d_packed, x, inv_pos, total, gamma, stats, d_residual, dx, dgamma, dbeta, workspace,)
+    _contig(*_keep)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return _dispatch(lib.spa_norm_packed_bwd,
+                     (_ptr(d_packed), _ptr(x), _ptr(inv_pos), _ptr(total), _ptr(gamma), int(kind), _ptr(stats), _ptr(d_residual),
+                      M, rows, C, code, _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), ws_bytes, _stream(),), _keep, prepare)
+
+
+def spa_norm_residual_unpack_bwd(dy, z, gather_idx, inv_pos, total, gamma, beta, scale, gate_scores, kind, stats, dz, d_scores,
+                                 dgamma, dbeta, dscale, workspace, prepare=False):
+    """The backward of spa_norm_residual_unpack: dz [M, C] packed, d_scores [*] f32 at token positions (for
+    spa_gate_bwd_scores), dgamma, dbeta, dscale [C] f32 (each of the last four may be None); the gradient of residual is dy."""
+    fn = "spa_norm_residual_unpack_bwd"
+    M, C = z.shape
+    rows = dy.numel() // C
+    if dy.shape[-1] != C or dz.shape != z.shape:
+        raise ValueError(f"{fn}: dy must be [..., C = {C}] and dz of z's shape")
+    code = _features(fn, dy=dy, z=z, gamma=gamma, beta=beta, scale=scale, dz=dz)
+    _typed(fn, torch.int32, gather_idx=gather_idx, inv_pos=inv_pos, total=total)
+    _typed(fn, torch.float32, gate_scores=gate_scores, stats=stats, d_scores=d_scores, dgamma=dgamma, dbeta=dbeta, dscale=dscale)
+    _holds(fn, gather_idx=(gather_idx, M), inv_pos=(inv_pos, rows), total=(total, 1), gamma=(gamma, C), beta=(beta, C),
+           scale=(scale, C), gate_scores=(gate_scores, rows), stats=(stats, 2 * M), d_scores=(d_scores, rows), dgamma=(dgamma, C),
+           dbeta=(dbeta, C), dscale=(dscale, C))
+    _keep = (dy, z, gather_idx, inv_pos, total, gamma, beta, scale, gate_scores, stats, dz, d_scores, dgamma, dbeta, dscale,
+             workspace,)
+    _contig(*_keep)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return _dispatch(lib.spa_norm_residual_unpack_bwd,
+                     (_ptr(dy), _ptr(z), _ptr(gather_idx), _ptr(inv_pos), _ptr(total), _ptr(gamma), _ptr(beta), _ptr(scale),
+                      _ptr(gate_scores), int(kind), _ptr(stats), M, rows, C, code, _ptr(dz), _ptr(d_scores), _ptr(dgamma),
+                      _ptr(dbeta), _ptr(dscale), _ptr(workspace), ws_bytes, _stream(),), _keep, prepare)
 
 
 def spa_padded_attention(q, k, v, seqlens, B, n_pad, H, Dh, out, softmax_scale=0.0, prepare=False):
