@@ -162,17 +162,15 @@ def _prepare_own(s, zeros, f32):
         Dh, grid = C // H, (s["h"], s["w"])
         q, k, v = (s["qkv"][:, i * C:(i + 1) * C] for i in range(3))
         out, lse = zeros(cap, C), zeros(H, cap, **f32)
-        # (for the backward's row sums: what rounding took from out)
-        low = zeros(cap, C) if s["train"] and td == torch.bfloat16 else None
         s["outputs"] = dict(out=out, lse=lse)
         s["launches"] = [spa.spa_packed_attention_bias(q, k, v, s["cu"], s["gather_idx"], s["table"], s["buckets"], grid, B, N, H,
-                                                       Dh, out, low, lse, prepare=True)]
+                                                       Dh, out, lse, prepare=True)]
         if s["train"]:
             dqkv, d_table = zeros(cap, 3 * C), zeros(H, s["nb"], **f32)
             dq, dk, dv = (dqkv[:, i * C:(i + 1) * C] for i in range(3))
             s["outputs"].update(dqkv=dqkv, d_table=d_table)
             s["launches"].append(spa.spa_packed_attention_bias_bwd(
-                q, k, v, out, low, s["dout"], lse, s["cu"], s["gather_idx"], s["table"], s["buckets"], grid, B, N, H, Dh, dq, dk, dv,
+                q, k, v, out, s["dout"], lse, s["cu"], s["gather_idx"], s["table"], s["buckets"], grid, B, N, H, Dh, dq, dk, dv,
                 d_table, ws(spa.spa_attention_bias_bwd_workspace_bytes(B, N, H, Dh, *grid, code)), prepare=True))
         return
     kind = spa.SPA_NORM_LAYER if s["norm"] == "layer" else spa.SPA_NORM_RMS
