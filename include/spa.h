@@ -307,6 +307,24 @@ int spa_packed_attention_running_max(const void* q, const void* k, const void* v
                                      float* lse, void* stream);
 
 /*
+ * spa_packed_attention with a learned bias by the bucket of the relative position (a Swin-like backbone around the blocks
+ * of Section 3.2).  The token of packed row j sits at n = gather_idx[j] mod (grid_h*grid_w) of its image's map, in row
+ * n / grid_w and column n mod grid_w (gather_idx NULL: row j of a segment is token j of the map).  For rows i, j of a segment and
+ * o = (row_i - row_j + grid_h - 1) (2 grid_w - 1) + column_i - column_j + grid_w - 1, one of (2 grid_h - 1)(2 grid_w - 1) offsets,
+ *   S_ij = softmax_scale <q_i, k_j> + table[h, buckets[o]],   O = softmax(S) V,   lse = log sum_j exp(S_ij)
+ * A bucket outside 0 .. n_buckets-1 stands for no bias.  An entry of -inf leaves its pairs out (the rows of q, k and v have
+ * to be finite there all the same); a row whose scores are all -inf gives out = 0, lse = -inf and no gradient.
+ * in:  q, k, v, strides, cu_seqlens, max_seqlen, softmax_scale as in spa_packed_attention, max_seqlen <= grid_h*grid_w;
+ *      table [H, n_buckets] dtype; buckets [(2 grid_h - 1)(2 grid_w - 1)] int32, or NULL: a bucket per offset (n_buckets is
+ *      their number); sequences without a second axis: grid_h = 1.
+ * out: out, lse as in spa_packed_attention.
+ */
+int spa_packed_attention_bias(const void* q, const void* k, const void* v, int64_t q_row_stride, int64_t k_row_stride,
+                              int64_t v_row_stride, const int32_t* cu_seqlens, const int32_t* gather_idx, const void* table,
+                              const int32_t* buckets, int n_buckets, int grid_h, int grid_w, int B, int max_seqlen, int H, int Dh,
+                              int dtype, float softmax_scale, void* out, float* lse, void* stream);
+
+/*
  * Scatter back (Section 3.2: positive tokens undergo attention, negative tokens go on
  * directly).  y[i,:] = packed_out[inv_pos[i],:] if inv_pos[i] >= 0 else 0; with base given,
  * y[i,:] = base[i,:] (+ packed_out[inv_pos[i],:] on selected rows).
@@ -653,6 +671,28 @@ int spa_gated_attention_bwd_tokens_spread(const void* q, const void* k, const vo
                                           const int32_t* gather_idx, const int32_t* inv_pos, int64_t rows, void* dq,
                                           void* dk, void* d_rg, int64_t dq_row_stride, int64_t dk_row_stride,
                                           int64_t d_rg_row_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace spa_packed_attention_bias_bwd needs. Host. */
+size_t spa_attention_bias_bwd_workspace_bytes(int B, int max_seqlen, int H, int Dh, int grid_h, int grid_w, int dtype);
+
+/*
+ * Backward of spa_packed_attention_bias: dq, dk, dv as in spa_packed_attention_bwd, and
+ *   d_table[h, b] = sum of dS_ij over the pairs (i, j) whose offset is in bucket b,   dS = P (dP - D)
+ * D_i is sum_d dO_id O_id from the rounded out for dq; for d_table (and dk) what the row's dS then still add up to, which is the
+ * error of that D, is taken off, so that d_table is good to fp32 from bf16 rows too.
+ * in:  as in the forward, with its out and lse; dout [>= T, H*Dh] dtype contiguous; workspace (device, 256-byte aligned) of at least spa_attention_bias_bwd_workspace_bytes bytes, contents
+ *      of no account.
+ * out: dq, dk, dv as in spa_packed_attention_bwd (rows >= T are not written); d_table [H, n_buckets] fp32 or NULL: added in
+ *      integers finer than 2^-30 of the largest dS a head can have, in any order the same.  All results run-to-run
+ *      bit-stable.  A head with a gradient, value or score that is not a finite number (-inf scores aside) has NaN in its row
+ *      of d_table.
+ */
+int spa_packed_attention_bias_bwd(const void* q, const void* k, const void* v, int64_t q_row_stride, int64_t k_row_stride,
+                                  int64_t v_row_stride, const void* out, const void* dout, const float* lse,
+                                  const int32_t* cu_seqlens, const int32_t* gather_idx, const void* table, const int32_t* buckets,
+                                  int n_buckets, int grid_h, int grid_w, int B, int max_seqlen, int H, int Dh, int dtype,
+                                  float softmax_scale, void* dq, void* dk, void* dv, int64_t dq_row_stride, int64_t dk_row_stride,
+                                  int64_t dv_row_stride, float* d_table, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Bytes of workspace spa_gate_bwd needs. Host. */
 size_t spa_gate_bwd_workspace_bytes(int B, int N, int C, int dtype);

@@ -41,7 +41,7 @@ template <> struct Kind<int64_t> { static constexpr char c = 'l'; static int64_t
 template <> struct Kind<size_t> { static constexpr char c = 'z'; static size_t get(const Value& v) { return v.z; } };
 template <> struct Kind<float> { static constexpr char c = 'f'; static float get(const Value& v) { return v.f; } };
 
-constexpr int kMaxArgs = 32;
+constexpr int kMaxArgs = 33;
 
 template <class F> struct Signature;
 template <class... A> struct Signature<int (*)(A...)> {
@@ -75,7 +75,7 @@ const Entry kEntries[] = {
     ENTRY(spa_unpack), ENTRY(spa_unpack_bwd), ENTRY(spa_pack_bwd), ENTRY(spa_packed_attention_bwd),
     ENTRY(spa_packed_attention_bwd_tokens), ENTRY(spa_gate_bwd), ENTRY(spa_gate_bwd_static), ENTRY(spa_padded_attention),
     ENTRY(spa_norm_packed), ENTRY(spa_norm_packed_bwd), ENTRY(spa_norm_residual_unpack), ENTRY(spa_norm_residual_unpack_bwd),
-    ENTRY(spa_gate_bwd_scores),
+    ENTRY(spa_gate_bwd_scores), ENTRY(spa_packed_attention_bias), ENTRY(spa_packed_attention_bias_bwd),
 };
 
 PyObject* g_on_error = nullptr;      // called with the return code of a failing C call; raises

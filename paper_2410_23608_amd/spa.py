@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import copy
 import ctypes
+import math
 import os
 import threading
 from ctypes import c_char_p, c_double, c_float, c_int, c_int64, c_size_t, c_void_p
@@ -112,6 +113,12 @@ _SIGNATURES = {
                              _P, _P, _P, _P, _P, c_size_t, _P]),
     "spa_gate_bwd_static": (c_int, [_P, _P, c_float, _P, _P, _P, _P, c_int, c_float, c_int, c_int, c_int, c_int,
                                     _P, _P, _P, _P, _P]),
+    "spa_packed_attention_bias": (c_int, [_P, _P, _P, c_int64, c_int64, c_int64, _P, _P, _P, _P, c_int, c_int, c_int, c_int, c_int,
+                                          c_int, c_int, c_int, c_float, _P, _P, _P]),
+    "spa_attention_bias_bwd_workspace_bytes": (c_size_t, [c_int, c_int, c_int, c_int, c_int, c_int, c_int]),
+    "spa_packed_attention_bias_bwd": (c_int, [_P, _P, _P, c_int64, c_int64, c_int64, _P, _P, _P, _P, _P, _P, _P, c_int, c_int,
+                                              c_int, c_int, c_int, c_int, c_int, c_int, c_float, _P, _P, _P, c_int64, c_int64,
+                                              c_int64, _P, _P, c_size_t, _P]),
     "spa_norm_packed": (c_int, [_P, _P, _P, _P, _P, c_int, c_float, c_int, c_int, c_int, _P, _P, _P]),
     "spa_norm_residual_unpack": (c_int, [_P, _P, _P, _P, _P, _P, _P, c_int, c_float, c_int, c_int64, c_int, c_int, _P, _P, _P]),
     "spa_norm_bwd_workspace_bytes": (c_size_t, [c_int64, c_int, c_int]),
@@ -936,6 +943,73 @@ def spa_gated_attention_bwd_tokens(q, k, x, scores, out, dy, lse, cu_seqlens, B,
                       _ptr(gather_idx), _ptr(inv_pos), rows, _ptr(dq), _ptr(dk), _ptr(d_rg), _row_stride(dq),
                       _row_stride(dk), _row_stride(d_rg), _ptr(workspace), ws_bytes, *(() if y is None else (_ptr(y),)),
                       _stream(),), _keep, prepare)
+
+
+def relative_position_buckets(grid_h, grid_w, near=8, levels=8, far=None):
+    """A bucket map of the offsets on a grid_h x grid_w map for spa_packed_attention_bias, and the number of its buckets.  Along
+    each axis offsets up to `near` have buckets of their own, larger ones `levels` buckets that widen with the distance up to
+    `far` (default: the axis) and the last beyond it, either sign apart; the bucket of an offset is the pair of its axes'."""
+    def axis(n):
+        top = max(n if far is None else int(far), near + 1)
+        out = []
+        for d in range(-(n - 1), n):
+            a = abs(d)
+            b = a if a < near else near + min(levels - 1, int(math.log(a / near) / math.log(top / near) * levels))
+            out.append(b + (near + levels if d < 0 else 0))
+        return torch.tensor(out, dtype=torch.int32), 2 * (near + levels)
+    if grid_h < 1 or grid_w < 1 or near < 1 or levels < 1:
+        raise ValueError("relative_position_buckets: sizes must be >= 1")
+    (rows, _), (cols, n_cols) = axis(int(grid_h)), axis(int(grid_w))
+    return (rows[:, None] * n_cols + cols[None, :]).reshape(-1).contiguous(), n_cols * n_cols
+
+
+def _bias_checks(fn, q, k, v, out, lse, cu_seqlens, gather_idx, table, buckets, grid, B, max_seqlen, H, Dh, **more):
+    C, (gh, gw) = H * Dh, (int(n) for n in grid)
+    code = _features(fn, q=q, k=k, v=v, table=table, out=out, **more)
+    _typed(fn, torch.int32, cu_seqlens=cu_seqlens, gather_idx=gather_idx, buckets=buckets)
+    _typed(fn, torch.float32, lse=lse)
+    _rows(fn, C, q=(q, 1), k=(k, 1), v=(v, 1), out=(out, 1), **{name: (t, 1) for name, t in more.items()})
+    if table.dim() != 2 or table.shape[0] != H:
+        raise ValueError(f"{fn}: table must be [H = {H}, n_buckets], got {tuple(table.shape)}")
+    _holds(fn, cu_seqlens=(cu_seqlens, B + 1), lse=(lse, H * B * max_seqlen), buckets=(buckets, (2 * gh - 1) * (2 * gw - 1)))
+    _contig(out, lse, cu_seqlens, gather_idx, table, buckets)
+    return code, gh, gw
+
+
+def spa_packed_attention_bias(q, k, v, cu_seqlens, gather_idx, table, buckets, grid, B, max_seqlen, H, Dh, out, lse=None,
+                               softmax_scale=0.0, prepare=False):
+    """spa_packed_attention with table[h, buckets[offset]] added to the scores (table [H, n_buckets]; grid = (grid_h, grid_w);
+    buckets None: a bucket per offset).  gather_idx [rows] says where a packed row sits on the map (None: row j of a segment
+    is token j)."""
+    fn = "spa_packed_attention_bias"
+    code, gh, gw = _bias_checks(fn, q, k, v, out, lse, cu_seqlens, gather_idx, table, buckets, grid, B, max_seqlen, H, Dh)
+    _keep = (q, k, v, cu_seqlens, gather_idx, table, buckets, out, lse,)
+    return _dispatch(lib.spa_packed_attention_bias,
+                     (_ptr(q), _ptr(k), _ptr(v), _row_stride(q), _row_stride(k), _row_stride(v), _ptr(cu_seqlens), _ptr(gather_idx),
+                      _ptr(table), _ptr(buckets), table.shape[1], gh, gw, B, max_seqlen, H, Dh, code, _num(softmax_scale), _ptr(out),
+                      _ptr(lse), _stream(),), _keep, prepare)
+
+
+def spa_attention_bias_bwd_workspace_bytes(B, max_seqlen, H, Dh, grid_h, grid_w, dtype) -> int:
+    return int(lib.spa_attention_bias_bwd_workspace_bytes(B, max_seqlen, H, Dh, int(grid_h), int(grid_w), dtype))
+
+
+def spa_packed_attention_bias_bwd(q, k, v, out, dout, lse, cu_seqlens, gather_idx, table, buckets, grid, B, max_seqlen, H,
+                                  Dh, dq, dk, dv, d_table, workspace, softmax_scale=0.0, prepare=False):
+    """The backward of spa_packed_attention_bias; d_table [H, n_buckets] f32 (None: not wanted)."""
+    fn = "spa_packed_attention_bias_bwd"
+    code, gh, gw = _bias_checks(fn, q, k, v, out, lse, cu_seqlens, gather_idx, table, buckets, grid, B, max_seqlen, H, Dh,
+                                dout=dout, dq=dq, dk=dk, dv=dv)
+    _typed(fn, torch.float32, d_table=d_table)
+    _holds(fn, d_table=(d_table, table.numel()))
+    _contig(dout, d_table, workspace)
+    _keep = (q, k, v, out, dout, lse, cu_seqlens, gather_idx, table, buckets, dq, dk, dv, d_table, workspace,)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return _dispatch(lib.spa_packed_attention_bias_bwd,
+                     (_ptr(q), _ptr(k), _ptr(v), _row_stride(q), _row_stride(k), _row_stride(v), _ptr(out), _ptr(dout),
+                      _ptr(lse), _ptr(cu_seqlens), _ptr(gather_idx), _ptr(table), _ptr(buckets), table.shape[1], gh, gw, B, max_seqlen,
+                      H, Dh, code, _num(softmax_scale), _ptr(dq), _ptr(dk), _ptr(dv), _row_stride(dq), _row_stride(dk),
+                      _row_stride(dv), _ptr(d_table), _ptr(workspace), ws_bytes, _stream(),), _keep, prepare)
 
 
 def spa_gate_bwd_workspace_bytes(B, N, C, dtype) -> int:
