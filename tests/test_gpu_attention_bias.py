@@ -220,6 +220,20 @@ def test_steep_rows_and_zero_bias_is_the_plain_attention(spa):
     assert bool(((got["out"][:c.T].cpu().double() - out[:c.T].cpu().double()).abs() <= 2 * tol).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_entries_of_the_types_lowest_value(spa, dtype):
+    """A mask written with the type's lowest number: such pairs weigh nothing beside any other, and share a row that has no other."""
+    c = Case([70, 1, 33, 150], (15, 15), 2, 32, dtype, seed=15, buckets="random")
+    c.buckets.clamp_(0, c.nb - 1)
+    c.map = c.buckets.long()
+    low = torch.finfo(TD[dtype]).min
+    c.table[0, ::2], c.table[1] = low, low
+    c.qkv[:, :c.C] = 0                                        # (scores beside such an entry are below its last place)
+    got = c.run(spa)
+    c.check(got, ("out", "dq", "dk", "dv"))
+    assert bool(torch.isfinite(got["d_table"]).all())
+
+
 def test_without_the_table_gradient_the_rest_is_the_same(spa):
     c = Case([100, 300, 9], (20, 20), 2, 32, "bf16", seed=7)
     a, b = c.run(spa), c.run(spa, want_table=False)
