@@ -44,6 +44,7 @@ __device__ __forceinline__ int bias_position(const BiasMap& m, int token) {
   return (int)(n + r * (m.gw.d - 1));                         // r (2 gw - 1) + n - r gw
 }
 __device__ __forceinline__ int bias_position(const BiasMap& m, long row, int j) { return bias_position(m, bias_token(m, row, j)); }
+typedef int intx4 __attribute__((ext_vector_type(4)));
 template <typename T>
 __device__ __forceinline__ float bias_at(const BiasMap& m, int h, int offset) {
   const int b = m.buckets != nullptr ? m.buckets[offset] : offset;
@@ -150,6 +151,7 @@ __device__ __forceinline__ int wave_pick(int v) {
 // copied as it lies in memory, 16 bytes at a time (shift: where it starts in its first 16); through one, a row of up to
 // kTableLds entries is brought to LDS first, and the map comes in 16-byte pieces too where `base` allows.
 constexpr int kTableLds = 1024;
+template <int THREADS = kBiasThreads>
 __device__ __forceinline__ int load_window(const BiasMap& m, int h, int base, int n, uint16_t* win, uint16_t* row_lds) {
   const uint16_t* row = static_cast<const uint16_t*>(m.table) + (long)h * m.nb;
   n = min(n, m.offsets - base);
@@ -159,14 +161,14 @@ __device__ __forceinline__ int load_window(const BiasMap& m, int h, int base, in
     const int shift = (int)(at & 15) / 2, first = (8 - shift) & 7;              // entries in front of the first whole piece
     const int whole = n > first ? (n - first) / 8 : 0;
     constexpr int U = 8;
-    for (int i0 = tid; i0 < whole; i0 += U * kBiasThreads) {
+    for (int i0 = tid; i0 < whole; i0 += U * THREADS) {
       uintx4 v[U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        v[u] = *reinterpret_cast<const uintx4*>(row + base + first + 8 * min(i0 + u * kBiasThreads, whole - 1));
+        v[u] = *reinterpret_cast<const uintx4*>(row + base + first + 8 * min(i0 + u * THREADS, whole - 1));
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (i0 + u * kBiasThreads < whole) *reinterpret_cast<uintx4*>(win + shift + first + 8 * (i0 + u * kBiasThreads)) = v[u];
+        if (i0 + u * THREADS < whole) *reinterpret_cast<uintx4*>(win + shift + first + 8 * (i0 + u * THREADS)) = v[u];
     }
     if (tid < min(first, n)) win[shift + tid] = row[base + tid];
     const int rest = first + 8 * whole + tid;                                   // behind the last whole piece
@@ -175,25 +177,24 @@ __device__ __forceinline__ int load_window(const BiasMap& m, int h, int base, in
   }
   const bool in_lds = m.nb <= kTableLds;
   if (in_lds) {
-    for (int i = tid; i < m.nb; i += kBiasThreads) row_lds[i] = row[i];
+    for (int i = tid; i < m.nb; i += THREADS) row_lds[i] = row[i];
     __syncthreads();
   }
   const uint16_t* from = in_lds ? row_lds : row;
   auto entry = [&](int b) -> uint16_t { return (unsigned)b < (unsigned)m.nb ? from[b] : (uint16_t)0; };
-  typedef int intx4 __attribute__((ext_vector_type(4)));
   const int quads = (base & 3) == 0 ? n / 4 : 0;
   constexpr int U = 8;
-  for (int i0 = tid; i0 < quads; i0 += U * kBiasThreads) {
+  for (int i0 = tid; i0 < quads; i0 += U * THREADS) {
     intx4 b[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) b[u] = *reinterpret_cast<const intx4*>(m.buckets + base + 4 * min(i0 + u * kBiasThreads, quads - 1));
+    for (int u = 0; u < U; ++u) b[u] = *reinterpret_cast<const intx4*>(m.buckets + base + 4 * min(i0 + u * THREADS, quads - 1));
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uintx2 w = {(uint32_t)entry(b[u][0]) | (uint32_t)entry(b[u][1]) << 16, (uint32_t)entry(b[u][2]) | (uint32_t)entry(b[u][3]) << 16};
-      if (i0 + u * kBiasThreads < quads) *reinterpret_cast<uintx2*>(win + 4 * (i0 + u * kBiasThreads)) = w;
+      if (i0 + u * THREADS < quads) *reinterpret_cast<uintx2*>(win + 4 * (i0 + u * THREADS)) = w;
     }
   }
-  for (int i = 4 * quads + tid; i < n; i += kBiasThreads) win[i] = entry(m.buckets[base + i]);
+  for (int i = 4 * quads + tid; i < n; i += THREADS) win[i] = entry(m.buckets[base + i]);
   return 0;
 }
 
@@ -240,7 +241,7 @@ struct BiasTiles {
 // The workgroup's block: (segment, head, rows from r0), longest segments first where they can be ranked.
 struct BiasBlock {
   Segment seg;
-  int h, r0;
+  int img, h, r0;
   bool valid;
 };
 template <int DH>
@@ -250,12 +251,12 @@ __device__ __forceinline__ BiasBlock bias_block(BiasTiles<DH>& l, const int32_t*
     LiveTile* slot = reinterpret_cast<LiveTile*>(l.s_live);
     const LiveTile t = live_tiles_apply(H, B) ? live_tile_block<1>(xcd, j, H, B, cu, kBiasRows, nblk, slot)
                                               : class_tile_block<1>(xcd, j, H, B, cu, kBiasRows, nblk, slot);
-    return {{t.row0, t.len, t.len}, t.h, t.qb * kBiasRows, t.valid};
+    return {{t.row0, t.len, t.len}, t.img, t.h, t.qb * kBiasRows, t.valid};
   }
   const TileId t = xcd_tile_at(xcd, j, nblk, H, B);
-  if (!t.valid) return {{0, 0, 0}, 0, 0, false};
+  if (!t.valid) return {{0, 0, 0}, 0, 0, 0, false};
   const Segment seg = segment_of(t.rank, cu, nullptr, 0);
-  return {seg, t.h, t.qb * kBiasRows, t.qb * kBiasRows < seg.nq};
+  return {seg, t.rank, t.h, t.qb * kBiasRows, t.qb * kBiasRows < seg.nq};
 }
 
 struct BiasFwd {
@@ -275,7 +276,6 @@ struct BiasFwd {
 template <int SIGN>
 __device__ __forceinline__ void add_bias(floatx16 (&s)[2], const int* pos, int own, bool in_window, const BiasMap& m, int h,
                                          const uint16_t* win, float scale, int hh) {
-  typedef int intx4 __attribute__((ext_vector_type(4)));
 #pragma unroll
   for (int sb = 0; sb < 2; ++sb) {
     float b[16];
@@ -441,94 +441,597 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_fwd_kernel(const BiasF
 }
 
 // ------------------------------------------------------------------------------- backward
-constexpr int kBiasParts = 32;                 // shares of the rows whose largest |dO| and |V| are found apart
-
-// The largest |dO| and |V| of every head and share of the rows (as bits, which order like the magnitudes, a NaN above all; a
-// row whose lse or D is not a number counts as one), and the cleared sums.
-struct BiasPrep {
-  const void *out, *dout, *v;
-  long vs;
-  const float* lse;
-  long lse_stride;
-  const int32_t* cu;
-  int B, H;
-  uint32_t* largest;              // [H][kBiasParts][2]
-  unsigned long long* sums;       // [H][offsets]
-  long nsums;
-};
-template <typename T, int DH>
-__global__ void __launch_bounds__(256) attn_bias_prep_kernel(const BiasPrep a) {
-  const long T_rows = a.cu[a.B], C = (long)a.H * DH;
-  const int h = blockIdx.y;
-  const long threads = (long)gridDim.x * gridDim.y * 256;
-  for (long i = ((long)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x; i < a.nsums; i += threads) a.sums[i] = 0;
-  uint32_t mo = 0, mv = 0;
-  for (long row = (long)blockIdx.x * 256 + threadIdx.x; row < T_rows; row += (long)gridDim.x * 256) {
-    float D = 0.f;
-    for (int d = 0; d < DH; ++d) {
-      const float g = (float)static_cast<const T*>(a.dout)[row * C + h * DH + d];
-      D = fmaf(g, (float)static_cast<const T*>(a.out)[row * C + h * DH + d], D);
-      mo = max(mo, __builtin_bit_cast(uint32_t, g) & 0x7fffffffu);
-      mv = max(mv, __builtin_bit_cast(uint32_t, (float)static_cast<const T*>(a.v)[row * a.vs + h * DH + d]) & 0x7fffffffu);
-    }
-    const float l = a.lse[h * a.lse_stride + row];
-    if (!(l < INFINITY) || !(fabsf(D) < INFINITY)) mo = 0x7fffffffu;
-  }
-  __shared__ uint32_t s[2];
-  if (threadIdx.x < 2) s[threadIdx.x] = 0;
-  __syncthreads();
-  atomicMax(&s[0], mo);
-  atomicMax(&s[1], mv);
-  __syncthreads();
-  if (threadIdx.x < 2) a.largest[(h * kBiasParts + blockIdx.x) * 2 + threadIdx.x] = s[threadIdx.x];
-}
-
-// The power of two above every |dS| of a head; `bad`: a gradient or a value of it is not finite, or the bound is beyond fp32.
-struct DsBound {
-  int e;
-  bool bad;
-};
-template <int DH>
-__device__ __forceinline__ DsBound ds_bound(const uint32_t* largest, int h) {
-  uint32_t mo = 0, mv = 0;
-  for (int i = 0; i < kBiasParts; ++i) {
-    mo = max(mo, largest[(h * kBiasParts + i) * 2]);
-    mv = max(mv, largest[(h * kBiasParts + i) * 2 + 1]);
-  }
-  // |x| < 2^(exponent + 1), exponent = (bits >> 23) - 127 (subnormals: below 2^-126); Dh products, dP and D
-  const int e = (int)(mo >> 23) - 126 + (int)(mv >> 23) - 126 + (DH == 32 ? 5 : 6) + 2;
-  return {e, mo >= 0x7f800000u || mv >= 0x7f800000u || e > 126};
-}
+// Bits of an integer dS below the power of two above every |dS|: the sum of a workgroup's, one per offset and row it goes over,
+// stays inside 64 bits for up to 2^22 rows (and |dS| cannot add up to more than its rows' |dP|).
+constexpr int kDsBits = 40;
 __device__ __forceinline__ double power_of_two(int e) { return __builtin_bit_cast(double, (uint64_t)(e + 1023) << 52); }
-// x / 2^(e - shift) rounded to an integer: the low bits of the sum with 1.5 2^52, whose own bits are taken off again
+// x factor, a power of two, rounded to an integer: the low bits of the sum with 1.5 2^52, whose own bits are taken off again
 __device__ __forceinline__ unsigned long long ds_integer(float x, double factor) {
   const double magic = 6755399441055744.0;
   return __builtin_bit_cast(uint64_t, fma((double)x, factor, magic)) - __builtin_bit_cast(uint64_t, magic);
 }
 
+// ------------------------------------------------------------------------- bf16 backward
+// Two launches and the sums behind them (fp32: one thread per row in each, below).  The dq launch walks the keys for 128 queries a workgroup, as the forward does, with D
+// from the rounded out, and leaves what the second launch needs: the corrected D of every row, and for every
+// block of queries a number that no |dS| of its rows exceeds in that launch.  The dk / dv launch walks the queries for the
+// keys of a workgroup, S and dP un-transposed (a lane is a key), so that P and dS are operands in registers again.
+// There dS goes into a histogram over the offsets in LDS, 64-bit integers: 32 lanes hold 32 keys against one query, so
+// that the lanes of an instruction have offsets of their own.  A workgroup keeps its histogram over all the blocks it
+// takes, of one head, and writes it once, as fp32; the sum over the workgroups has a fixed order.  Maps with more offsets than LDS
+// has room for are taken in slices: the first pass over the blocks does everything but the offsets of later slices, the
+// others only go over the tiles that have offsets in theirs.
+template <typename T>
 struct BiasBwd {
-  const void *q, *k, *v, *out, *dout;
+  const T *q, *k, *v, *out, *dout;
   long qs, ks, vs;
   const float* lse;
-  float* dvec;                    // D of every (head, row): the query side writes it, the key side reads it
+  float* dvec;
   long lse_stride;
   const int32_t* cu;
-  int H;
-  float scale;
   BiasMap m;
-  void *dq, *dk, *dv;
+  int H, B, nblk;                 // nblk: blocks of kBiasRows rows of the longest possible segment
+  float scale;
+  T *dq, *dk, *dv;
   long dqs, dks, dvs;
-  const uint32_t* largest;
-  unsigned long long* sums;
-  int shift;
+  uint32_t* most;                 // [H][B * nblk]: what no |dS| of a block of queries exceeds
+  float* partial;                 // [H][groups][offsets] or null
+  int groups, slice;              // dk / dv: workgroups a head; offsets of a histogram
+  int kblk;                       // dk / dv: blocks of 32 NW keys of the longest possible segment
 };
 
-// One thread per row: a query (dq, and D), or a key (dk, dv, and dS into the sums); the other side streams through LDS.
-// D from the rounded out is off by a share of that rounding.  sum_j dS_ij = sum_j P_ij dP_ij - D_i is what it is off by: the query
-// side adds it to the D that the key side takes.
-template <typename T, int DH, bool kKeySide>
-__global__ void __launch_bounds__(kRowThreads) attn_bias_bwd_rows_kernel(const BiasBwd a) {
-  __shared__ float As[kRowTile * DH], Bs[kRowTile * DH], lses[kRowTile], Ds[kRowTile];
+template <int DH, bool WHOLE>
+__global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBwd<__bf16> a) {
+  constexpr int RS = DH + 8, KK = DH / 16, DB = DH / 32, BN = kBiasBN;
+  extern __shared__ __attribute__((aligned(16))) uint16_t win[];
+  __shared__ BiasTiles<DH> l;
+  __shared__ float s_most[2][kBiasThreads / kWave];
+  const BiasBlock blk = bias_block<DH>(l, a.cu, a.H, a.B, a.nblk);
+  if (!blk.valid) return;
+  const Segment seg = blk.seg;
+  const int h = blk.h, n = seg.nk, lane = threadIdx.x & 63, wv = threadIdx.x >> 6, l32 = lane & 31, hh = lane >> 5;
+  const int qi = blk.r0 + wv * 32 + l32, last = n - 1;
+  const bool wave_live = blk.r0 + wv * 32 < n, q_ok = qi < n;
+  const long C = (long)a.H * DH, q_row = seg.row0 + min(qi, last);
+
+  PairStage<DH, kBiasThreads, BN, false, false> st(threadIdx.x);
+  st.gi = nullptr;
+  st.last = last;
+  st.source(0, a.k + h * DH, a.ks, seg.row0);
+  st.source(1, a.v + h * DH, a.vs, seg.row0);
+  int token = 0;
+  auto load_tile = [&](int kt) {
+    st.load(kt);
+    const int j = min(kt + lane, last);
+    if (threadIdx.x < BN) token = bias_token(a.m, seg.row0 + j, j);
+  };
+  float v_most = 0.f;                                         // of |V|, of the rows this thread stages
+  auto store_tile = [&](int buf, auto clear) {
+    st.template store<clear>(l.A[buf], l.B[buf]);
+    put_positions(l.p, buf, a.m, token, !WHOLE);
+#pragma unroll
+    for (int t = 0; t < decltype(st)::CPT; ++t) {
+      const floatx8 f = bf16x8_to_float(st.v[1][t]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v_most = __builtin_elementwise_maximum(v_most, fabsf(f[e]));
+    }
+  };
+  load_tile(0);
+  bf16x8 qf[KK], dof[KK];
+  float D = 0.f, l1 = 0.f;                                    // <dO, out> and sum |dO| of the lane's row
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    const int col = h * DH + kk * 16 + hh * 8;
+    qf[kk] = *reinterpret_cast<const bf16x8*>(a.q + q_row * a.qs + col);
+    dof[kk] = *reinterpret_cast<const bf16x8*>(a.dout + q_row * C + col);
+    const floatx8 g = bf16x8_to_float(dof[kk]), o = bf16x8_to_float(*reinterpret_cast<const bf16x8*>(a.out + q_row * C + col));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      D = fmaf(g[e], o[e], D);
+      l1 += fabsf(g[e]);
+    }
+  }
+  D = sum_across_halves(D);
+  l1 = sum_across_halves(l1);
+  const float lse = a.lse[h * a.lse_stride + q_row];
+  const bool far = __ballot(fabsf(lse) >= kFarScore && lse != -INFINITY) != 0;
+  const float lse2 = lse == -INFINITY || !q_ok ? INFINITY : lse * kLog2e;      // (no score, or no row: probability 0)
+  const int own = bias_position(a.m, q_row, min(qi, last)) + a.m.centre;
+  const uint16_t* at0 = win;
+  if (!WHOLE) {
+    const int lo = wave_pick<false>(own), hi = wave_pick<true>(own);
+    if (lane == 0) {
+      l.p.own[wv][0] = lo;
+      l.p.own[wv][1] = hi;
+    }
+  } else {
+    at0 = win + load_window(a.m, h, 0, a.m.offsets, win, l.row);
+  }
+  floatx16 acc[DB], negD;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    negD[r] = -D;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[d][r] = 0.f;
+  }
+  float left = 0.f, most = 0.f;
+  store_tile(0, std::true_type{});
+  __syncthreads();
+  const Range mine = WHOLE ? Range{0, 0} : own_range(l.p);
+  int base = -0x40000000;
+  const int nt = (n + BN - 1) / BN;
+  walk_tiles(nt, [&](int t, auto at) {
+    constexpr bool end = decltype(at)::value == kTileLast;
+    const int buf = t & 1, kt = t * BN;
+    if (!end) load_tile(kt + BN);
+    bool in_window = true;
+    if (!WHOLE) {
+      const int lo = mine.lo - l.p.range[buf][1], hi = mine.hi - l.p.range[buf][0];
+      in_window = hi - lo < kWindow - 3;
+      if (in_window && (lo < base || hi >= base + kWindow)) {
+        base = max(hi - kWindow + 4, 0) & ~3;
+        at0 = win + load_window(a.m, h, base, kWindow, win, l.row) - base;
+        __syncthreads();
+      }
+    }
+    if (wave_live) {
+      floatx16 s[2], dp[2];
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[sb][r] = 0.f;
+        dp[sb] = negD;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          const int at_row = (sb * 32 + l32) * RS + kk * 16 + hh * 8;
+          s[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&l.A[buf][at_row]), qf[kk], s[sb], 0, 0, 0);
+          dp[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&l.B[buf][at_row]), dof[kk], dp[sb], 0, 0, 0);
+        }
+      }
+      if (WHOLE || in_window) add_bias<1>(s, l.p.pos[buf], own, true, a.m, h, at0, a.scale, hh);
+      else add_bias<1>(s, l.p.pos[buf], own, false, a.m, h, at0, a.scale, hh);
+      if (end) {
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (kt + sb * 32 + acc_row(r, hh) >= n) s[sb][r] = -INFINITY;
+      }
+      if (!far) {
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[sb][r] = __builtin_amdgcn_exp2f(fmaf(s[sb][r], kLog2e, -lse2));
+      } else {
+        const float ref = lse2 == INFINITY ? INFINITY : lse;
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[sb][r] = __builtin_amdgcn_exp2f((s[sb][r] - ref) * kLog2e);
+      }
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+        for (int mf = 0; mf < 2; ++mf) {
+          floatx8 f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            f[j] = s[sb][8 * mf + j] * dp[sb][8 * mf + j];
+            left += f[j];
+            most = __builtin_elementwise_maximum(most, fabsf(f[j]));
+          }
+          const bf16x8 dsb = float_to_bf16x8(f);
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+            acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_frag_rowmajor<RS>(l.A[buf], d, sb * 32, mf, lane), dsb, acc[d], 0, 0, 0);
+        }
+    }
+    if (!end) {
+      store_tile(buf ^ 1, std::bool_constant<decltype(at)::value == kTileBeforeLast>{});
+      __syncthreads();
+    }
+  });
+  store_rows<DH>(acc, a.scale, a.dq + q_row * a.dqs + h * DH, q_ok, hh);
+  left = sum_across_halves(left);
+  if (q_ok && hh == 0) a.dvec[h * a.lse_stride + q_row] = D + left;
+  // |dS| of the other launch: of this one, plus what D moves by, plus what the order of Dh products in dP can make (at most
+  // Dh U sum|dO V| in either launch)
+  v_most = __builtin_bit_cast(float, wave_pick<true>((int)(__builtin_bit_cast(uint32_t, v_most) & 0x7fffffffu)));
+  if (lane == 0) s_most[0][wv] = v_most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kBiasThreads / kWave; ++w) v_most = __builtin_elementwise_maximum(v_most, s_most[0][w]);
+  const float bound = q_ok ? most + fabsf(left) + l1 * v_most * 0x1p-16f : 0.f;
+  const int bits = wave_pick<true>((int)(__builtin_bit_cast(uint32_t, bound) & 0x7fffffffu));      // (a NaN above all)
+  if (lane == 0) s_most[1][wv] = __builtin_bit_cast(float, bits);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t all = 0;
+#pragma unroll
+    for (int w = 0; w < kBiasThreads / kWave; ++w) all = max(all, __builtin_bit_cast(uint32_t, s_most[1][w]));
+    a.most[((long)h * a.B + blk.img) * a.nblk + blk.r0 / kBiasRows] = all;
+  }
+}
+
+// The head's blocks of keys in the order in which the workgroups take them: up to 256 segments by length, longest first,
+// blocks that exist numbered through; more segments in index order, with blocks of the longest possible one each.
+struct KeyBlocks {
+  int img[kLptMaxB], len[kLptMaxB], upto[kLptMaxB];           // by rank; blocks up to and including the rank's
+  int all;
+};
+template <int THREADS>
+__device__ __forceinline__ void list_key_blocks(KeyBlocks& k, const int32_t* cu, int B, int rows, int kblk) {
+  if (B > kLptMaxB) {
+    if (threadIdx.x == 0) k.all = B * kblk;
+    __syncthreads();
+    return;
+  }
+  for (int b = threadIdx.x; b < B; b += THREADS) k.upto[b] = max(cu[b + 1] - cu[b], 0);
+  __syncthreads();
+  for (int b = threadIdx.x; b < B; b += THREADS) {
+    const int mine = k.upto[b];
+    int rank = 0;
+    for (int i = 0; i < B; ++i) rank += k.upto[i] > mine || (k.upto[i] == mine && i < b);
+    k.img[rank] = b;
+    k.len[rank] = mine;
+  }
+  __syncthreads();
+  if (threadIdx.x < kWave) {
+    int before = 0;
+    for (int r0 = 0; r0 < B; r0 += kWave) {
+      const int r = r0 + threadIdx.x, nb = r < B ? min((k.len[r] + rows - 1) / rows, kblk) : 0, to = before + wave_scan(nb);
+      if (r < B) k.upto[r] = to;
+      before = __builtin_amdgcn_readlane(to, 63);
+    }
+    if (threadIdx.x == 0) k.all = before;
+  }
+  __syncthreads();
+}
+struct KeyBlock {
+  long row0;
+  int n, k0;
+};
+__device__ __forceinline__ KeyBlock key_block(const KeyBlocks& k, const int32_t* cu, int B, int rows, int kblk, int i) {
+  int img, at;
+  if (B > kLptMaxB) {
+    img = i / kblk;
+    at = i % kblk;
+  } else {
+    int lo = 0, hi = B - 1;                                   // the first rank with upto > i
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (k.upto[mid] > i) hi = mid;
+      else lo = mid + 1;
+    }
+    img = k.img[lo];
+    at = i - (lo > 0 ? k.upto[lo - 1] : 0);
+  }
+  img = __builtin_amdgcn_readfirstlane(img);
+  const int from = cu[img];
+  return {from, cu[img + 1] - from, __builtin_amdgcn_readfirstlane(at) * rows};
+}
+
+// The scale of a head's integers: 2^e is above twice what the dq launch found (its blocks that exist); `unit` NaN: some dS of
+// the head is not a finite number.  All threads call it.
+struct DsScale {
+  int e;
+  double factor;
+  float unit;
+};
+template <int THREADS>
+__device__ __forceinline__ DsScale ds_scale(const uint32_t* most_h, const int32_t* cu, int B, int nblk, uint32_t* s_most) {
+  uint32_t most = 0;
+  for (int i = threadIdx.x; i < B * nblk; i += THREADS) {
+    const int img = i / nblk;
+    if ((i - img * nblk) * kBiasRows < cu[img + 1] - cu[img]) most = max(most, most_h[i]);
+  }
+  most = (uint32_t)wave_pick<true>((int)most);
+  if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < THREADS / kWave; ++w) most = max(most, s_most[w]);
+  const int e = __builtin_amdgcn_readfirstlane((int)(most >> 23) - 126 + 1);
+  const bool bad = most >= 0x7f800000u || e > 126;
+  return {e, bad ? 0. : power_of_two(kDsBits - e), bad ? NAN : 0.f};
+}
+// A workgroup's histogram of offsets from .. from + slice of its head, as fp32; all threads call it, behind the last add.
+template <int THREADS>
+__device__ __forceinline__ void write_partial(const unsigned long long* hist, const DsScale& s, int slice, int from, int offsets, float* out) {
+  __syncthreads();
+  const double quantum = power_of_two(s.e - kDsBits);
+  for (int i = threadIdx.x; i < min(slice, offsets - from); i += THREADS) out[from + i] = s.unit + (float)((double)(long long)hist[i] * quantum);
+  __syncthreads();
+}
+
+template <int DH, int NW>
+struct DkdvTiles {
+  static constexpr int RS = DH + 8;
+  __attribute__((aligned(16))) __bf16 Q[2][kBiasBN * RS];
+  __attribute__((aligned(16))) __bf16 G[2][kBiasBN * RS];     // dO
+  __attribute__((aligned(16))) float lse[2][kBiasBN];         // +inf: no score, or no row (probability 0)
+  __attribute__((aligned(16))) float lse2[2][kBiasBN];        // times log2 e
+  __attribute__((aligned(16))) float negD[2][kBiasBN];
+  __attribute__((aligned(16))) int pos[2][kBiasBN];
+  int range[2][2], far[2];
+  int own[NW][2];
+  uint32_t most[NW];
+  uint16_t row[kTableLds];
+  KeyBlocks blocks;
+};
+
+template <int DH, int NW, bool WHOLE, bool HIST>
+__global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<__bf16> a) {
+  constexpr int RS = DH + 8, KK = DH / 16, DB = DH / 32, BN = kBiasBN, THREADS = 64 * NW, ROWS = 32 * NW;
+  static_assert(NW >= 4, "the first four waves stage");
+  extern __shared__ __attribute__((aligned(16))) unsigned long long hist[];       // [slice], then the window of biases
+  __shared__ DkdvTiles<DH, NW> l;
+  const int h = blockIdx.x % a.H, group = blockIdx.x / a.H;
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, l32 = lane & 31, hh = lane >> 5;
+  const bool stages = tid < kBiasThreads;
+  const long C = (long)a.H * DH;
+  uint16_t* win = reinterpret_cast<uint16_t*>(hist + (HIST ? a.slice : 0));
+  const float* lse_h = a.lse + h * a.lse_stride;
+  const float* d_h = a.dvec + h * a.lse_stride;
+
+  list_key_blocks<THREADS>(l.blocks, a.cu, a.B, ROWS, a.kblk);
+  DsScale scale = {0, 0., 0.f};
+  if (HIST) scale = ds_scale<THREADS>(a.most + (long)h * a.B * a.nblk, a.cu, a.B, a.nblk, l.most);
+  const uint16_t* at0 = win;
+  if (WHOLE) at0 = win + load_window<THREADS>(a.m, h, 0, a.m.offsets, win, l.row);
+
+  const int passes = HIST ? (a.m.offsets + a.slice - 1) / a.slice : 1;
+  for (int pass = 0; pass < passes; ++pass) {
+    const int from = pass * a.slice;
+    if (HIST) {
+      for (int i = tid; i < a.slice; i += THREADS) hist[i] = 0;
+      // (in front of the first add there is the barrier behind a block's first tile)
+    }
+    for (int round = 0;; ++round) {
+      const int item = round * a.groups + (round & 1 ? a.groups - 1 - group : group);
+      if (item >= l.blocks.all) break;
+      const KeyBlock kb = key_block(l.blocks, a.cu, a.B, ROWS, a.kblk, item);
+      if (kb.k0 >= kb.n) continue;
+      const int n = kb.n, last = n - 1, ki = kb.k0 + wv * 32 + l32;
+      const bool wave_live = kb.k0 + wv * 32 < n, k_ok = ki < n;
+      const long k_row = kb.row0 + min(ki, last);
+      PairStage<DH, kBiasThreads, BN, false, false> st(tid);
+      st.gi = nullptr;
+      st.last = last;
+      st.source(0, a.q + h * DH, a.qs, kb.row0);
+      st.source(1, a.dout + h * DH, C, kb.row0);
+      int token = 0;
+      float lse_t = 0.f, d_t = 0.f;
+      auto load_tile = [&](int qt) {
+        if (stages) st.load(qt);
+        const int j = min(qt + lane, last);
+        if (tid < BN) {
+          token = bias_token(a.m, kb.row0 + j, j);
+          lse_t = lse_h[kb.row0 + j];
+          d_t = d_h[kb.row0 + j];
+        }
+      };
+      auto store_tile = [&](int buf, int qt, auto clear) {
+        if (stages) st.template store<clear>(l.Q[buf], l.G[buf]);
+        if (tid < BN) {
+          const bool none = lse_t == -INFINITY || qt + tid >= n;
+          l.lse[buf][tid] = none ? INFINITY : lse_t;
+          l.lse2[buf][tid] = none ? INFINITY : lse_t * kLog2e;
+          l.negD[buf][tid] = -d_t;
+          const int p = bias_position(a.m, token) + a.m.centre;
+          l.pos[buf][tid] = p;
+          const bool any = __ballot(!none && fabsf(lse_t) >= kFarScore) != 0;
+          const int lo = !WHOLE || passes > 1 ? wave_pick<false>(p) : 0, hi = !WHOLE || passes > 1 ? wave_pick<true>(p) : 0;
+          if (tid == 0) {
+            l.range[buf][0] = lo;
+            l.range[buf][1] = hi;
+            l.far[buf] = any;
+          }
+        }
+      };
+      load_tile(0);
+      bf16x8 kf[KK], vf[KK];
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const int col = h * DH + kk * 16 + hh * 8;
+        kf[kk] = *reinterpret_cast<const bf16x8*>(a.k + k_row * a.ks + col);
+        vf[kk] = *reinterpret_cast<const bf16x8*>(a.v + k_row * a.vs + col);
+      }
+      const int own = bias_position(a.m, k_row, min(ki, last));
+      __syncthreads();                                        // every wave is past its last read of the tiles before
+      if (!WHOLE || passes > 1) {
+        const int lo = wave_pick<false>(own), hi = wave_pick<true>(own);
+        if (lane == 0) {
+          l.own[wv][0] = lo;
+          l.own[wv][1] = hi;
+        }
+      }
+      floatx16 dka[DB], dva[DB];
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dka[d][r] = dva[d][r] = 0.f;
+      store_tile(0, 0, std::true_type{});
+      __syncthreads();
+      Range mine = {0, 0};
+      if (!WHOLE || passes > 1) {
+        mine = {l.own[0][0], l.own[0][1]};
+#pragma unroll
+        for (int w = 1; w < NW; ++w) mine = {min(mine.lo, l.own[w][0]), max(mine.hi, l.own[w][1])};
+      }
+      int base = -0x40000000;
+      const int nt = (n + BN - 1) / BN;
+      for (int t = 0; t < nt; ++t) {
+        const int buf = t & 1, qt = t * BN;
+        const bool end = t + 1 == nt;
+        if (!end) load_tile(qt + BN);
+        bool in_window = true, adds = HIST, inside = true;
+        if (!WHOLE || passes > 1) {
+          const int lo = __builtin_amdgcn_readfirstlane(l.range[buf][0] - mine.hi);
+          const int hi = __builtin_amdgcn_readfirstlane(l.range[buf][1] - mine.lo);
+          if (!WHOLE) {
+            in_window = hi - lo < kWindow - 3;
+            if (in_window && (lo < base || hi >= base + kWindow)) {   // the queries' positions grow, so do the offsets
+              base = lo & ~3;
+              at0 = win + load_window<THREADS>(a.m, h, base, kWindow, win, l.row) - base;
+              __syncthreads();
+            }
+          }
+          adds = HIST && hi >= from && lo < from + a.slice;
+          inside = lo >= from && hi < from + a.slice;
+        }
+        if (wave_live && (pass == 0 || adds)) {
+          const bool far = l.far[buf] != 0;
+#pragma unroll
+          for (int sb = 0; sb < 2; ++sb) {
+            floatx16 s, dp;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const floatx4 d4 = *reinterpret_cast<const floatx4*>(&l.negD[buf][sb * 32 + 8 * g + 4 * hh]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                dp[4 * g + i] = d4[i];
+                s[4 * g + i] = 0.f;
+              }
+            }
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+              const int at_row = (sb * 32 + l32) * RS + kk * 16 + hh * 8;
+              s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&l.Q[buf][at_row]), kf[kk], s, 0, 0, 0);
+              dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&l.G[buf][at_row]), vf[kk], dp, 0, 0, 0);
+            }
+            int o[16];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const intx4 p4 = *reinterpret_cast<const intx4*>(&l.pos[buf][sb * 32 + 8 * g + 4 * hh]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int r = 4 * g + i;
+                o[r] = p4[i] - own;
+                s[r] = fmaf(s[r], a.scale, WHOLE || in_window ? __builtin_bit_cast(float, (uint32_t)at0[o[r]] << 16) : bias_at<__bf16>(a.m, h, o[r]));
+              }
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const floatx4 l4 = *reinterpret_cast<const floatx4*>(&(far ? l.lse : l.lse2)[buf][sb * 32 + 8 * g + 4 * hh]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int r = 4 * g + i;
+                s[r] = __builtin_amdgcn_exp2f(far ? (s[r] - l4[i]) * kLog2e : fmaf(s[r], kLog2e, -l4[i]));
+                dp[r] *= s[r];
+              }
+            }
+            if (pass == 0) {
+#pragma unroll
+              for (int mf = 0; mf < 2; ++mf) {
+                floatx8 fp, fd;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  fp[j] = s[8 * mf + j];
+                  fd[j] = dp[8 * mf + j];
+                }
+                const bf16x8 pb = float_to_bf16x8(fp), dsb = float_to_bf16x8(fd);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                  dva[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_frag_rowmajor<RS>(l.G[buf], d, sb * 32, mf, lane), pb, dva[d], 0, 0, 0);
+                  dka[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_frag_rowmajor<RS>(l.Q[buf], d, sb * 32, mf, lane), dsb, dka[d], 0, 0, 0);
+                }
+              }
+            }
+            if (HIST && adds && k_ok) {
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                if (inside || (unsigned)(o[r] - from) < (unsigned)a.slice)
+                  __hip_atomic_fetch_add(&hist[o[r] - from], ds_integer(dp[r], scale.factor), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            }
+          }
+        }
+        if (!end) {
+          if (t + 2 == nt) store_tile(buf ^ 1, qt + BN, std::true_type{});
+          else store_tile(buf ^ 1, qt + BN, std::false_type{});
+          __syncthreads();
+        }
+      }
+      if (pass == 0) {
+        store_rows<DH>(dka, a.scale, a.dk + k_row * a.dks + h * DH, k_ok, hh);
+        store_rows<DH>(dva, 1.0f, a.dv + k_row * a.dvs + h * DH, k_ok, hh);
+      }
+    }
+    if (HIST) write_partial<THREADS>(hist, scale, a.slice, from, a.m.offsets, a.partial + ((long)h * a.groups + group) * a.m.offsets);
+  }
+}
+
+// The sums over the workgroups, in their order: 64 offsets a workgroup, four slices of the rows beside each other.
+struct BiasSum {
+  const float* partial;
+  int groups, offsets;
+  float* sums;                    // [H][offsets]
+};
+__global__ void __launch_bounds__(256) attn_bias_sum_kernel(const BiasSum a) {
+  __shared__ double s[4][64];
+  const int h = blockIdx.y, c = threadIdx.x & 63, sl = threadIdx.x >> 6, o = blockIdx.x * 64 + c;
+  double v = 0.;
+  if (o < a.offsets) {
+    const float* p = a.partial + (long)h * a.groups * a.offsets + o;
+    constexpr int U = 8;
+    for (int g0 = sl; g0 < a.groups; g0 += 4 * U) {
+      float f[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) f[u] = g0 + 4 * u < a.groups ? p[(long)(g0 + 4 * u) * a.offsets] : 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) v += (double)f[u];
+    }
+  }
+  s[sl][c] = v;
+  __syncthreads();
+  if (sl == 0 && o < a.offsets) a.sums[(long)h * a.offsets + o] = (float)((s[0][c] + s[1][c]) + (s[2][c] + s[3][c]));
+}
+
+// The sums of the offsets into those of their buckets, with integers again, of 2^-40 of the power of two above the largest: a
+// workgroup has kTableBuckets buckets of a head in LDS and goes over all offsets.
+constexpr int kTableBuckets = 4096;
+struct BiasTable {
+  const float* sums;
+  const int32_t* buckets;
+  int nb, offsets;
+  float* d_table;
+};
+__global__ void __launch_bounds__(1024) attn_bias_table_kernel(const BiasTable a) {
+  __shared__ unsigned long long s[kTableBuckets];
+  __shared__ uint32_t s_most[16];
+  const int h = blockIdx.y, b0 = blockIdx.x * kTableBuckets, nb = min(kTableBuckets, a.nb - b0);
+  const float* sums = a.sums + (long)h * a.offsets;
+  uint32_t most = 0;
+  for (int i = threadIdx.x; i < a.offsets; i += 1024) most = max(most, __builtin_bit_cast(uint32_t, sums[i]) & 0x7fffffffu);
+  most = (uint32_t)wave_pick<true>((int)most);
+  if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = most;
+  for (int i = threadIdx.x; i < nb; i += 1024) s[i] = 0;
+  __syncthreads();
+  for (int w = 0; w < 16; ++w) most = max(most, s_most[w]);
+  const bool bad = most >= 0x7f800000u;
+  const int bits = min(40, 62 - (32 - __builtin_clz(a.offsets))), e = (int)(most >> 23) - 126;
+  if (!bad)
+    for (int i = threadIdx.x; i < a.offsets; i += 1024) {
+      const int b = a.buckets[i] - b0;
+      const float v = sums[i];
+      if ((unsigned)b < (unsigned)nb && v != 0.f) atomicAdd(&s[b], ds_integer(v, power_of_two(bits - e)));
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < nb; i += 1024)
+    a.d_table[(long)h * a.nb + b0 + i] = bad ? NAN : (float)((double)(long long)s[i] * power_of_two(e - bits));
+}
+
+// ------------------------------------------------------------------------------- fp32 backward
+// One thread per row, the other side streaming through LDS: the queries (dq, D, and what no |dS| exceeds), then the keys.
+__device__ __forceinline__ float block_most(float v, float* s) {           // largest of the 128 threads' (a NaN above all)
+  const int b = wave_pick<true>((int)(__builtin_bit_cast(uint32_t, v) & 0x7fffffffu));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = __builtin_bit_cast(float, b);
+  __syncthreads();
+  return __builtin_elementwise_maximum(s[0], s[1]);
+}
+template <int DH>
+__global__ void __launch_bounds__(kRowThreads) attn_bias_dq_rows_kernel(const BiasBwd<float> a) {
+  __shared__ float Ks[kRowTile * DH], Vs[kRowTile * DH], s_most[2];
   __shared__ int pos[kRowTile];
   const int h = blockIdx.y, r0 = blockIdx.x * kRowThreads;
   const long row0 = a.cu[blockIdx.z], C = (long)a.H * DH;
@@ -537,104 +1040,128 @@ __global__ void __launch_bounds__(kRowThreads) attn_bias_bwd_rows_kernel(const B
   const int ri = r0 + threadIdx.x;
   const bool ok = ri < n;
   const long row = row0 + (ok ? ri : 0);
-  const T *q = static_cast<const T*>(a.q) + h * DH, *k = static_cast<const T*>(a.k) + h * DH, *v = static_cast<const T*>(a.v) + h * DH,
-          *dout = static_cast<const T*>(a.dout) + h * DH;
-  float x[DH], y[DH], acc0[DH], acc1[DH];
+  float q[DH], g[DH], acc[DH], D = 0.f, l1 = 0.f;
 #pragma unroll
   for (int d = 0; d < DH; ++d) {
-    x[d] = (float)(kKeySide ? k[row * a.ks + d] : q[row * a.qs + d]);
-    y[d] = (float)(kKeySide ? v[row * a.vs + d] : dout[row * C + d]);
-    acc0[d] = acc1[d] = 0.f;
+    q[d] = a.q[row * a.qs + h * DH + d];
+    g[d] = a.dout[row * C + h * DH + d];
+    D = fmaf(g[d], a.out[row * C + h * DH + d], D);
+    l1 += fabsf(g[d]);
+    acc[d] = 0.f;
   }
-  const int p = bias_position(a.m, row, ok ? ri : 0);
-  const float my_lse = a.lse[h * a.lse_stride + row];
-  float my_d = 0.f, left = 0.f;
-  if (!kKeySide)
-    for (int d = 0; d < DH; ++d) my_d = fmaf(y[d], (float)static_cast<const T*>(a.out)[row * C + h * DH + d], my_d);
-  double factor = 0.;
-  if (kKeySide && a.sums != nullptr) {
-    const DsBound b = ds_bound<DH>(a.largest, h);
-    if (!b.bad) factor = power_of_two(a.shift - b.e);
-  }
+  const int p = bias_position(a.m, row, ok ? ri : 0) + a.m.centre;
+  const float l = a.lse[h * a.lse_stride + row];
+  float left = 0.f, most = 0.f, v_most = 0.f;
   for (int t = 0; t < n; t += kRowTile) {
     __syncthreads();
-    if (kKeySide) stage_rows<T, DH>(q, a.qs, dout, C, row0, t, n, As, Bs);
-    else stage_rows<T, DH>(k, a.ks, v, a.vs, row0, t, n, As, Bs);
-    if (threadIdx.x < kRowTile && t + threadIdx.x < n) {
-      const long r = row0 + t + threadIdx.x;
-      pos[threadIdx.x] = bias_position(a.m, r, t + threadIdx.x);
-      lses[threadIdx.x] = a.lse[h * a.lse_stride + r];
-      if (kKeySide) Ds[threadIdx.x] = a.dvec[h * a.lse_stride + r];
-    }
+    stage_rows<float, DH>(a.k + h * DH, a.ks, a.v + h * DH, a.vs, row0, t, n, Ks, Vs);
+    if (threadIdx.x < kRowTile && t + threadIdx.x < n) pos[threadIdx.x] = bias_position(a.m, row0 + t + threadIdx.x, t + threadIdx.x);
     __syncthreads();
+    for (int i = threadIdx.x; i < kRowTile * DH; i += kRowThreads) v_most = __builtin_elementwise_maximum(v_most, fabsf(Vs[i]));
     const int tn = min(kRowTile, n - t);
     for (int j = 0; j < tn; ++j) {
       float s = 0.f, dp = 0.f;
 #pragma unroll
       for (int d = 0; d < DH; ++d) {
-        s = fmaf(x[d], As[j * DH + d], s);
-        dp = fmaf(y[d], Bs[j * DH + d], dp);
+        s = fmaf(q[d], Ks[j * DH + d], s);
+        dp = fmaf(g[d], Vs[j * DH + d], dp);
       }
-      const int offset = (kKeySide ? pos[j] - p : p - pos[j]) + a.m.centre;
-      const float l = kKeySide ? lses[j] : my_lse, D = kKeySide ? Ds[j] : my_d;
-      const float pr = l == -INFINITY ? 0.f : expf(fmaf(s, a.scale, bias_at<T>(a.m, h, offset)) - l);   // (a row without a score)
+      const float pr = l == -INFINITY ? 0.f : expf(fmaf(s, a.scale, bias_at<float>(a.m, h, p - pos[j])) - l);   // (a row without a score)
       const float ds = pr * (dp - D);
       left += ds;
-      if (kKeySide && factor != 0. && ok) atomicAdd(&a.sums[(long)h * a.m.offsets + offset], ds_integer(ds, factor));
+      most = __builtin_elementwise_maximum(most, fabsf(ds));
 #pragma unroll
-      for (int d = 0; d < DH; ++d) {
-        acc0[d] = fmaf(ds, As[j * DH + d], acc0[d]);
-        if (kKeySide) acc1[d] = fmaf(pr, Bs[j * DH + d], acc1[d]);
-      }
+      for (int d = 0; d < DH; ++d) acc[d] = fmaf(ds, Ks[j * DH + d], acc[d]);
     }
   }
+  v_most = block_most(v_most, s_most);
+  most = block_most(ok ? most + fabsf(left) + l1 * v_most * 0x1p-16f : 0.f, s_most);
+  if (threadIdx.x == 0)
+    a.most[((long)h * a.B + blockIdx.z) * a.nblk + blockIdx.x] = __builtin_bit_cast(uint32_t, most) & 0x7fffffffu;
   if (!ok) return;
-  if (!kKeySide) a.dvec[h * a.lse_stride + row] = my_d + left;
+  a.dvec[h * a.lse_stride + row] = D + left;
 #pragma unroll
-  for (int d = 0; d < DH; ++d) {
-    if (kKeySide) {
-      static_cast<T*>(a.dk)[row * a.dks + h * DH + d] = (T)(acc0[d] * a.scale);
-      static_cast<T*>(a.dv)[row * a.dvs + h * DH + d] = (T)acc1[d];
-    } else {
-      static_cast<T*>(a.dq)[row * a.dqs + h * DH + d] = (T)(acc0[d] * a.scale);
-    }
-  }
+  for (int d = 0; d < DH; ++d) a.dq[row * a.dqs + h * DH + d] = acc[d] * a.scale;
 }
 
-// The sums of the offsets into those of their buckets.  A workgroup has kTableBuckets buckets of a head in LDS and goes over
-// all offsets, again with integers.
-constexpr int kTableBuckets = 4096;
-struct BiasTable {
-  const unsigned long long* sums;
-  const int32_t* buckets;
-  const uint32_t* largest;
-  int nb, offsets, shift;
-  float* d_table;
-};
-template <int DH>
-__global__ void __launch_bounds__(1024) attn_bias_table_kernel(const BiasTable a) {
-  __shared__ unsigned long long s[kTableBuckets];
-  const int h = blockIdx.y, b0 = blockIdx.x * kTableBuckets, nb = min(kTableBuckets, a.nb - b0);
-  const unsigned long long* sums = a.sums + (long)h * a.offsets;
-  if (a.buckets != nullptr) {
-    for (int i = threadIdx.x; i < nb; i += 1024) s[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.offsets; i += 1024) {
-      const int b = a.buckets[i] - b0;
-      const unsigned long long v = sums[i];
-      if ((unsigned)b < (unsigned)nb && v != 0) atomicAdd(&s[b], v);
+template <int DH, bool HIST>
+__global__ void __launch_bounds__(kRowThreads) attn_bias_dkdv_rows_kernel(const BiasBwd<float> a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned long long hist[];
+  __shared__ float Qs[kRowTile * DH], Gs[kRowTile * DH], lses[kRowTile], Ds[kRowTile];
+  __shared__ int pos[kRowTile];
+  __shared__ uint32_t s_most[kRowThreads / kWave];
+  __shared__ KeyBlocks blocks;
+  const int h = blockIdx.x % a.H, group = blockIdx.x / a.H;
+  const long C = (long)a.H * DH;
+  list_key_blocks<kRowThreads>(blocks, a.cu, a.B, kRowThreads, a.kblk);
+  DsScale scale = {0, 0., 0.f};
+  if (HIST) scale = ds_scale<kRowThreads>(a.most + (long)h * a.B * a.nblk, a.cu, a.B, a.nblk, s_most);
+  const int passes = HIST ? (a.m.offsets + a.slice - 1) / a.slice : 1;
+  for (int pass = 0; pass < passes; ++pass) {
+    const int from = pass * a.slice;
+    if (HIST)
+      for (int i = threadIdx.x; i < a.slice; i += kRowThreads) hist[i] = 0;
+    for (int round = 0;; ++round) {
+      const int item = round * a.groups + (round & 1 ? a.groups - 1 - group : group);
+      if (item >= blocks.all) break;
+      const KeyBlock kb = key_block(blocks, a.cu, a.B, kRowThreads, a.kblk, item);
+      if (kb.k0 >= kb.n) continue;
+      const int ki = kb.k0 + threadIdx.x;
+      const bool ok = ki < kb.n;
+      const long row = kb.row0 + (ok ? ki : 0);
+      float k[DH], v[DH], dk[DH], dv[DH];
+#pragma unroll
+      for (int d = 0; d < DH; ++d) {
+        k[d] = a.k[row * a.ks + h * DH + d];
+        v[d] = a.v[row * a.vs + h * DH + d];
+        dk[d] = dv[d] = 0.f;
+      }
+      const int p = bias_position(a.m, row, ok ? ki : 0) - a.m.centre;
+      for (int t = 0; t < kb.n; t += kRowTile) {
+        __syncthreads();
+        stage_rows<float, DH>(a.q + h * DH, a.qs, a.dout + h * DH, C, kb.row0, t, kb.n, Qs, Gs);
+        if (threadIdx.x < kRowTile && t + threadIdx.x < kb.n) {
+          const long r = kb.row0 + t + threadIdx.x;
+          pos[threadIdx.x] = bias_position(a.m, r, t + threadIdx.x);
+          lses[threadIdx.x] = a.lse[h * a.lse_stride + r];
+          Ds[threadIdx.x] = a.dvec[h * a.lse_stride + r];
+        }
+        __syncthreads();
+        const int tn = min(kRowTile, kb.n - t);
+        for (int j = 0; j < tn; ++j) {
+          const int o = pos[j] - p;
+          const bool adds = HIST && ok && (unsigned)(o - from) < (unsigned)a.slice;
+          if (pass > 0 && __ballot(adds) == 0) continue;
+          float s = 0.f, dp = 0.f;
+#pragma unroll
+          for (int d = 0; d < DH; ++d) {
+            s = fmaf(k[d], Qs[j * DH + d], s);
+            dp = fmaf(v[d], Gs[j * DH + d], dp);
+          }
+          const float pr = lses[j] == -INFINITY ? 0.f : expf(fmaf(s, a.scale, bias_at<float>(a.m, h, o)) - lses[j]);
+          const float ds = pr * (dp - Ds[j]);
+          if (adds) __hip_atomic_fetch_add(&hist[o - from], ds_integer(ds, scale.factor), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+          if (pass > 0) continue;
+#pragma unroll
+          for (int d = 0; d < DH; ++d) {
+            dk[d] = fmaf(ds, Qs[j * DH + d], dk[d]);
+            dv[d] = fmaf(pr, Gs[j * DH + d], dv[d]);
+          }
+        }
+      }
+      if (pass > 0 || !ok) continue;
+#pragma unroll
+      for (int d = 0; d < DH; ++d) {
+        a.dk[row * a.dks + h * DH + d] = dk[d] * a.scale;
+        a.dv[row * a.dvs + h * DH + d] = dv[d];
+      }
     }
-    __syncthreads();
-  }
-  const DsBound e = ds_bound<DH>(a.largest, h);
-  const double unit = power_of_two(e.bad ? 0 : e.e - a.shift);
-  for (int i = threadIdx.x; i < nb; i += 1024) {
-    const long long v = (long long)(a.buckets != nullptr ? s[i] : sums[b0 + i]);
-    a.d_table[(long)h * a.nb + b0 + i] = e.bad ? NAN : (float)((double)v * unit);
+    if (HIST) write_partial<kRowThreads>(hist, scale, a.slice, from, a.m.offsets, a.partial + ((long)h * a.groups + group) * a.m.offsets);
   }
 }
 
 // ------------------------------------------------------------------------------- host
+constexpr long kMostOffsets = 1L << 26;
 static int bias_checks(const char* fn, const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
                        const int32_t* cu, int B, int n_max, int H, int Dh, int dtype, float softmax_scale, const void* table,
                        const int32_t* buckets, int n_buckets, const int32_t* gather_idx, int grid_h, int grid_w, BiasMap* m) {
@@ -655,7 +1182,7 @@ static int bias_checks(const char* fn, const void* q, const void* k, const void*
   SPA_REQUIRE(aligned16(buckets), SPA_ERR_INVALID_ARG, "%s: buckets not 16-byte aligned", fn);
   SPA_REQUIRE(softmax_scale >= 0.f && std::isfinite(softmax_scale), SPA_ERR_INVALID_ARG,
               "%s: softmax_scale must be finite and >= 0 (0 = 1/sqrt(Dh))", fn);
-  SPA_REQUIRE(grid_h >= 1 && grid_w >= 1 && (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1) <= (1L << 26), SPA_ERR_INVALID_ARG,
+  SPA_REQUIRE(grid_h >= 1 && grid_w >= 1 && (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1) <= kMostOffsets, SPA_ERR_INVALID_ARG,
               "%s: grid_h, grid_w must be >= 1, with at most 2^26 offsets", fn);
   const long offsets = (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1);
   SPA_REQUIRE(n_buckets >= 1 && n_buckets <= (1 << 26), SPA_ERR_INVALID_ARG, "%s: n_buckets must lie in 1 .. 2^26", fn);
@@ -667,21 +1194,49 @@ static int bias_checks(const char* fn, const void* q, const void* k, const void*
   return SPA_OK;
 }
 
-// Bits below the bound that a sum of that many values leaves: 62 less those of their number, at most 40.
-static int ds_shift(long rows) {
-  int bits = 0;
-  while ((1L << bits) < rows) ++bits;
-  return std::min(40, 62 - bits);
-}
 // LDS of a window of that many offsets: it may start up to 7 entries into its first 16 bytes
 static size_t window_bytes(int offsets) { return ((size_t)offsets + 7 + 7) / 8 * 16; }
-#define SPA_BIAS_LAUNCH(KERNEL, GRID, LDS, ARGS)                                                                              \
+#define SPA_BIAS_LAUNCH(KERNEL, GRID, THREADS, LDS, ARGS)                                                                              \
   do {                                                                                                                        \
     const hipError_t attr = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(LDS)); \
     SPA_REQUIRE(attr == hipSuccess, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, (size_t)(LDS));                   \
-    hipLaunchKernelGGL(KERNEL, dim3(GRID), dim3(kBiasThreads), LDS, st, ARGS);                                                \
+    hipLaunchKernelGGL(KERNEL, dim3(GRID), dim3(THREADS), LDS, st, ARGS);                                                     \
   } while (0)
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// The dk / dv launch of the backward.  A workgroup of four waves, two of them a unit, where that leaves room for the whole map in
+// LDS (10 bytes an offset); else eight waves, one a unit, with as much of the histogram as fits.  As many workgroups a head as
+// are resident together, no more than there are blocks of keys, and no more than 256 MB of partial sums.
+struct BiasPlan {
+  int nw, slice, groups, kblk;
+  size_t lds;
+};
+static BiasPlan bias_plan(int H, int B, int n_max, int Dh, long offsets, int dtype) {
+  BiasPlan p = {};
+  const size_t window = window_bytes((int)(offsets <= kWholeMost ? offsets : kWindow)), most = 160 * 1024;
+  const size_t tiles4 = Dh == 32 ? sizeof(DkdvTiles<32, 4>) : sizeof(DkdvTiles<64, 4>);
+  const size_t tiles8 = Dh == 32 ? sizeof(DkdvTiles<32, 8>) : sizeof(DkdvTiles<64, 8>);
+  const auto up64 = [](long n) { return (n + 63) & ~63L; };
+  int a_unit = 2;
+  if (dtype == SPA_F32) {
+    p.nw = 4;
+    p.slice = (int)std::min<long>(up64(offsets), 4096);
+    p.lds = (size_t)p.slice * 8;
+  } else if (tiles4 + window + up64(offsets) * 8 <= most / 2) {
+    p.nw = 4;
+    p.slice = (int)up64(offsets);
+    p.lds = window + (size_t)p.slice * 8;
+  } else {
+    p.nw = offsets <= kWholeMost ? 8 : 4;                       // (eight with look-ups in memory: too few registers)
+    a_unit = 1;
+    p.slice = (int)std::min<long>(up64(offsets), (long)(most - (p.nw == 8 ? tiles8 : tiles4) - window) / 8 / 64 * 64);
+    p.lds = window + (size_t)p.slice * 8;
+  }
+  p.kblk = (n_max + 32 * p.nw - 1) / (32 * p.nw);
+  const long fit = std::max<long>(1, (256L << 20) / (4 * H * offsets));
+  p.groups = (int)std::max<long>(1, std::min<long>(std::min<long>(256 * a_unit / H, (long)B * p.kblk), fit));
+  return p;
+}
 
 }  // namespace spa
 
@@ -709,8 +1264,8 @@ extern "C" int spa_packed_attention_bias(const void* q, const void* k, const voi
     const dim3 blocks(xcd_grid(nblk, H, B));
 #define SPA_BIAS(D)                                                                                                        \
   do {                                                                                                                     \
-    if (m.offsets <= kWholeMost) SPA_BIAS_LAUNCH((attn_bias_fwd_kernel<D, true>), blocks, window_bytes(m.offsets), args);  \
-    else SPA_BIAS_LAUNCH((attn_bias_fwd_kernel<D, false>), blocks, window_bytes(kWindow), args);                           \
+    if (m.offsets <= kWholeMost) SPA_BIAS_LAUNCH((attn_bias_fwd_kernel<D, true>), blocks, kBiasThreads, window_bytes(m.offsets), args);  \
+    else SPA_BIAS_LAUNCH((attn_bias_fwd_kernel<D, false>), blocks, kBiasThreads, window_bytes(kWindow), args);                           \
   } while (0)
     if (Dh == 32) SPA_BIAS(32); else SPA_BIAS(64);
 #undef SPA_BIAS
@@ -726,11 +1281,12 @@ extern "C" int spa_packed_attention_bias(const void* q, const void* k, const voi
 }
 
 extern "C" size_t spa_attention_bias_bwd_workspace_bytes(int B, int max_seqlen, int H, int Dh, int grid_h, int grid_w, int dtype) {
-  (void)Dh; (void)dtype;
-  if (B < 1 || max_seqlen < 1 || H < 1 || grid_h < 1 || grid_w < 1) return 0;
-  const size_t offsets = (2 * (size_t)grid_h - 1) * (2 * (size_t)grid_w - 1);
-  return up256((size_t)H * B * max_seqlen * sizeof(float)) + up256((size_t)H * kBiasParts * 2 * sizeof(uint32_t)) +
-         (size_t)H * offsets * sizeof(unsigned long long);
+  if (B < 1 || max_seqlen < 1 || H < 1 || grid_h < 1 || grid_w < 1 || (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1) > kMostOffsets) return 0;
+  const long offsets = (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1);
+  const BiasPlan p = bias_plan(H, B, max_seqlen, Dh, offsets, dtype);
+  const size_t nblk = (max_seqlen + kBiasRows - 1) / kBiasRows;
+  return up256((size_t)H * B * max_seqlen * 4) + up256((size_t)H * B * nblk * 4) + up256((size_t)H * p.groups * offsets * 4) +
+         up256((size_t)H * offsets * 4);
 }
 
 extern "C" int spa_packed_attention_bias_bwd(const void* q, const void* k, const void* v, int64_t q_row_stride, int64_t k_row_stride,
@@ -759,32 +1315,63 @@ extern "C" int spa_packed_attention_bias_bwd(const void* q, const void* k, const
   SPA_REQUIRE((reinterpret_cast<uintptr_t>(workspace) & 255u) == 0, SPA_ERR_INVALID_ARG, "%s: workspace not 256-byte aligned", fn);
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)Dh);
   const long ls = (long)B * max_seqlen;
+  const BiasPlan plan = bias_plan(H, B, max_seqlen, Dh, m.offsets, dtype);
+  const int nblk = (max_seqlen + kBiasRows - 1) / kBiasRows;
+  SPA_REQUIRE(((long)H * B + 8) * nblk < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*H*blocks must be < 2^31", fn);
   char* ws = static_cast<char*>(workspace);
-  float* dvec = reinterpret_cast<float*>(ws);
-  ws += up256((size_t)H * ls * sizeof(float));
-  uint32_t* largest = reinterpret_cast<uint32_t*>(ws);
-  ws += up256((size_t)H * kBiasParts * 2 * sizeof(uint32_t));
-  unsigned long long* sums = d_table != nullptr ? reinterpret_cast<unsigned long long*>(ws) : nullptr;
+  auto take = [&](size_t bytes) {
+    char* at = ws;
+    ws += up256(bytes);
+    return at;
+  };
+  float* dvec = reinterpret_cast<float*>(take((size_t)H * ls * 4));
+  uint32_t* most = reinterpret_cast<uint32_t*>(take((size_t)H * B * nblk * 4));
+  float* partial = reinterpret_cast<float*>(take((size_t)H * plan.groups * m.offsets * 4));
+  float* sums = buckets != nullptr ? reinterpret_cast<float*>(take((size_t)H * m.offsets * 4)) : d_table;
   hipStream_t st = as_stream(stream);
-  const BiasPrep prep = {out, dout, v, (long)v_row_stride, lse, ls, cu_seqlens, B, H, largest, sums, (long)H * m.offsets};
-  const BiasBwd args = {q, k, v, out, dout, (long)q_row_stride, (long)k_row_stride, (long)v_row_stride, lse, dvec, ls, cu_seqlens, H, scale, m,
-                        dq, dk, dv, (long)dq_row_stride, (long)dk_row_stride, (long)dv_row_stride, largest, sums, ds_shift(ls)};
-  const BiasTable table_args = {sums, buckets, largest, n_buckets, m.offsets, ds_shift(ls), d_table};
-  const dim3 grid((max_seqlen + kRowThreads - 1) / kRowThreads, H, B);
-#define SPA_BIAS(T, D)                                                                                                        \
-  do {                                                                                                                        \
-    if (d_table != nullptr) hipLaunchKernelGGL((attn_bias_prep_kernel<T, D>), dim3(kBiasParts, H), dim3(256), 0, st, prep);   \
-    hipLaunchKernelGGL((attn_bias_bwd_rows_kernel<T, D, false>), grid, dim3(kRowThreads), 0, st, args);                       \
-    hipLaunchKernelGGL((attn_bias_bwd_rows_kernel<T, D, true>), grid, dim3(kRowThreads), 0, st, args);                        \
-    if (d_table != nullptr)                                                                                                   \
-      hipLaunchKernelGGL(attn_bias_table_kernel<D>, dim3((n_buckets + kTableBuckets - 1) / kTableBuckets, H), dim3(1024), 0, st, \
-                         table_args);                                                                                         \
+  const bool hist = d_table != nullptr, whole = m.offsets <= kWholeMost;
+  const size_t window = window_bytes(whole ? m.offsets : kWindow);
+#define SPA_ARGS(T)                                                                                                          \
+  {(const T*)q, (const T*)k, (const T*)v, (const T*)out, (const T*)dout, (long)q_row_stride, (long)k_row_stride, (long)v_row_stride, lse, \
+   dvec, ls, cu_seqlens, m, H, B, nblk, scale, (T*)dq, (T*)dk, (T*)dv, (long)dq_row_stride, (long)dk_row_stride, (long)dv_row_stride,     \
+   most, partial, plan.groups, plan.slice, plan.kblk}
+#define SPA_DKDV(D, NW, W)                                                                                                   \
+  do {                                                                                                                       \
+    if (hist) SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<D, NW, W, true>), H * plan.groups, 64 * NW, plan.lds, args);            \
+    else SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<D, NW, W, false>), H * plan.groups, 64 * NW, window, args);                  \
+  } while (0)
+#define SPA_BIAS16(D)                                                                                                        \
+  do {                                                                                                                       \
+    if (whole) SPA_BIAS_LAUNCH((attn_bias_dq_kernel<D, true>), xcd_grid(nblk, H, B), kBiasThreads, window, args);            \
+    else SPA_BIAS_LAUNCH((attn_bias_dq_kernel<D, false>), xcd_grid(nblk, H, B), kBiasThreads, window, args);                 \
+    if (!whole) SPA_DKDV(D, 4, false);                                                                                       \
+    else if (plan.nw == 4) SPA_DKDV(D, 4, true);                                                                             \
+    else SPA_DKDV(D, 8, true);                                                                                               \
+  } while (0)
+#define SPA_BIAS32(D)                                                                                                        \
+  do {                                                                                                                       \
+    hipLaunchKernelGGL(attn_bias_dq_rows_kernel<D>, dim3(nblk, H, B), dim3(kRowThreads), 0, st, args);                       \
+    if (hist) SPA_BIAS_LAUNCH((attn_bias_dkdv_rows_kernel<D, true>), H * plan.groups, kRowThreads, plan.lds, args);          \
+    else hipLaunchKernelGGL((attn_bias_dkdv_rows_kernel<D, false>), dim3(H * plan.groups), dim3(kRowThreads), 0, st, args);  \
   } while (0)
   if (dtype == SPA_F32) {
-    if (Dh == 32) SPA_BIAS(float, 32); else SPA_BIAS(float, 64);
+    const BiasBwd<float> args = SPA_ARGS(float);
+    if (Dh == 32) SPA_BIAS32(32); else SPA_BIAS32(64);
   } else {
-    if (Dh == 32) SPA_BIAS(__bf16, 32); else SPA_BIAS(__bf16, 64);
+    const BiasBwd<__bf16> args = SPA_ARGS(__bf16);
+    if (Dh == 32) SPA_BIAS16(32); else SPA_BIAS16(64);
   }
-#undef SPA_BIAS
+#undef SPA_ARGS
+#undef SPA_DKDV
+#undef SPA_BIAS16
+#undef SPA_BIAS32
+  if (hist) {
+    const BiasSum sum = {partial, plan.groups, m.offsets, sums};
+    hipLaunchKernelGGL(attn_bias_sum_kernel, dim3((m.offsets + 63) / 64, H), dim3(256), 0, st, sum);
+    if (buckets != nullptr) {
+      const BiasTable table_args = {sums, buckets, n_buckets, m.offsets, d_table};
+      hipLaunchKernelGGL(attn_bias_table_kernel, dim3((n_buckets + kTableBuckets - 1) / kTableBuckets, H), dim3(1024), 0, st, table_args);
+    }
+  }
   return check_launch(fn);
 }

@@ -51,31 +51,6 @@ struct TokenIO {
   long rows;               // B * N
 };
 
-// The wave's transposed accumulator tile (rows = head dim, a lane = one token) as bf16 rows: the two halves
-// of the wave exchange quads so that a lane holds 8 consecutive columns of its token, 16-byte stores.
-template <int DH>
-__device__ __forceinline__ void store_rows(const floatx16 (&acc)[DH / 32], float scale, __bf16* row, bool ok, int hh) {
-#pragma unroll
-  for (int d = 0; d < DH / 32; ++d)
-#pragma unroll
-    for (int g = 0; g < 4; g += 2) {
-      uint32_t w[2][2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const floatx4 f = {acc[d][4 * (g + u)] * scale, acc[d][4 * (g + u) + 1] * scale, acc[d][4 * (g + u) + 2] * scale,
-                           acc[d][4 * (g + u) + 3] * scale};
-        const uintx2 p = __builtin_bit_cast(uintx2, __builtin_convertvector(f, bf16x4));
-        w[u][0] = p[0];
-        w[u][1] = p[1];
-      }
-      // lanes 32.. of the first quad <-> lanes ..31 of the second
-      const auto x0 = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
-      const auto x1 = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
-      const uintx4 v = {x0[0], x1[0], x0[1], x1[1]};
-      if (ok) *reinterpret_cast<uintx4*>(row + d * 32 + 8 * g + 8 * hh) = v;
-    }
-}
-
 // Operands and results of the bf16 kernels.
 struct BwdArgs {
   const __bf16 *q, *k, *v;

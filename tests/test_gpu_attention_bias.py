@@ -310,6 +310,23 @@ def test_separate_buffers_and_wide_strides(spa):
         assert bool((t[:, :8] == 0).all()) and bool((t[:, 8 + C:] == 0).all()) and bool((t[c.T:] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("grid,Dh", [((40, 41), 32), ((60, 90), 32), ((60, 90), 64)])
+def test_maps_whose_offsets_take_more_than_one_pass(spa, grid, Dh, dtype):
+    c = Case([900, 70, 333, 128, 1], grid, 2, Dh, dtype, seed=16, buckets="exact" if Dh == 32 else "log")
+    c.check(c.run(spa))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [70, 300])
+def test_many_segments(spa, B, dtype):
+    g = torch.Generator().manual_seed(B)
+    lens = torch.randint(0, 60, (B,), generator=g).tolist()
+    lens[B // 2] = 130                                             # two blocks of keys
+    c = Case(lens, (12, 13), 2, 32, dtype, seed=17, buckets="log")
+    c.check(c.run(spa))
+
+
 def test_large_and_sparse_maps(spa):
     """Few tokens far apart on a map of many offsets, and a long sequence without a second axis."""
     for grid, lens in (((300, 300), [150, 40]), ((1, 20000), [400, 90])):
