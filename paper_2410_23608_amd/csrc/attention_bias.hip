@@ -35,15 +35,21 @@ struct BiasMap {
   Divisor gw, per_image;
 };
 
-// What says where packed row `row` sits, number j of its segment; the position index it gives.
-__device__ __forceinline__ int bias_token(const BiasMap& m, long row, int j) {
-  return m.gather_idx != nullptr ? m.gather_idx[row] & 0x7fffffff : min(j, m.tokens - 1);
-}
-__device__ __forceinline__ int bias_position(const BiasMap& m, int token) {
-  const uint32_t n = (uint32_t)token - quotient((uint32_t)token, m.per_image) * m.per_image.d, r = quotient(n, m.gw);
-  return (int)(n + r * (m.gw.d - 1));                         // r (2 gw - 1) + n - r gw
-}
-__device__ __forceinline__ int bias_position(const BiasMap& m, long row, int j) { return bias_position(m, bias_token(m, row, j)); }
+// Where the rows of the segment from packed row row0 sit: entry j of the index, in flight from load() on (nothing here may ask for
+// its value before it is wanted; without an index some word is loaded and not used), and the position index it gives.
+struct BiasTokens {
+  const int32_t* at;
+  int step;
+  __device__ __forceinline__ BiasTokens(const BiasMap& m, const int32_t* any, long row0)
+      : at(m.gather_idx != nullptr ? m.gather_idx + row0 : any), step(m.gather_idx != nullptr) {}
+  __device__ __forceinline__ int load(int j) const { return at[j * step]; }
+  __device__ __forceinline__ int position(const BiasMap& m, int loaded, int j) const {
+    const uint32_t t = step != 0 ? (uint32_t)loaded & 0x7fffffffu : (uint32_t)min(j, m.tokens - 1);
+    const uint32_t n = t - quotient(t, m.per_image) * m.per_image.d, r = quotient(n, m.gw);
+    return (int)(n + r * (m.gw.d - 1));                       // r (2 gw - 1) + n - r gw
+  }
+  __device__ __forceinline__ int position(const BiasMap& m, int j) const { return position(m, load(j), j); }
+};
 typedef int intx4 __attribute__((ext_vector_type(4)));
 template <typename T>
 __device__ __forceinline__ float bias_at(const BiasMap& m, int h, int offset) {
@@ -85,12 +91,13 @@ attn_bias_rows_kernel(const T* __restrict__ q, const T* __restrict__ k, const T*
     qf[d] = (float)q[row * qs + h * DH + d] * scale;
     o[d] = 0.f;
   }
-  const int p = bias_position(m, row, ok ? qi : 0) + m.centre;
+  const BiasTokens tokens(m, cu, row0);
+  const int p = tokens.position(m, ok ? qi : 0) + m.centre;
   float mx = -INFINITY, l = 0.f;
   for (int t = 0; t < n; t += kRowTile) {
     __syncthreads();
     stage_rows<T, DH>(k + h * DH, ks, v + h * DH, vs, row0, t, n, Ks, Vs);
-    if (threadIdx.x < kRowTile && t + threadIdx.x < n) pos[threadIdx.x] = bias_position(m, row0 + t + threadIdx.x, t + threadIdx.x);
+    if (threadIdx.x < kRowTile && t + threadIdx.x < n) pos[threadIdx.x] = tokens.position(m, t + threadIdx.x);
     __syncthreads();
     const int tn = min(kRowTile, n - t);
     for (int j = 0; j < tn; ++j) {
@@ -147,6 +154,14 @@ __device__ __forceinline__ int wave_pick(int v) {
   return pick_dpp<0xB1, MAX>(pick_dpp<0x4E, MAX>(pick_dpp<0x124, MAX>(pick_dpp<0x128, MAX>(v))));
 }
 
+// LDS by byte address: what a look-up costs in vector instructions is then the one subtraction of two positions.
+typedef __attribute__((address_space(3))) uint16_t* lds_u16_ptr;
+typedef __attribute__((address_space(3))) unsigned long long* lds_u64_ptr;
+__device__ __forceinline__ int lds_address(const void* p) { return (int)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
+__device__ __forceinline__ void lds_add(int address, unsigned long long v) {
+  __hip_atomic_fetch_add((lds_u64_ptr)(uint32_t)address, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+
 // The biases of offsets [base, base + n) of head h to win[shift ..]; returns shift.  Without a bucket map the table's row is
 // copied as it lies in memory, 16 bytes at a time (shift: where it starts in its first 16); through one, a row of up to
 // kTableLds entries is brought to LDS first, and the map comes in 16-byte pieces too where `base` allows.
@@ -175,40 +190,49 @@ __device__ __forceinline__ int load_window(const BiasMap& m, int h, int base, in
     if (tid < 8 && rest < n) win[shift + rest] = row[base + rest];
     return shift;
   }
-  const bool in_lds = m.nb <= kTableLds;
-  if (in_lds) {
+  const int quads = (base & 3) == 0 ? n / 4 : 0;
+  auto fill = [&](auto from) {                                                  // (all of a thread's look-ups in flight)
+    auto entry = [&](int b) -> uint32_t {
+      const uint32_t v = from[min((uint32_t)b, (uint32_t)m.nb - 1)];
+      return (uint32_t)b < (uint32_t)m.nb ? v : 0u;
+    };
+    constexpr int U = 4;
+    for (int i0 = tid; i0 < quads; i0 += U * THREADS) {
+      intx4 b[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) b[u] = *reinterpret_cast<const intx4*>(m.buckets + base + 4 * min(i0 + u * THREADS, quads - 1));
+      uint32_t v[U][4];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[u][i] = entry(b[u][i]);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i0 + u * THREADS < quads) *reinterpret_cast<uintx2*>(win + 4 * (i0 + u * THREADS)) = uintx2{v[u][0] | v[u][1] << 16, v[u][2] | v[u][3] << 16};
+    }
+    for (int i = 4 * quads + tid; i < n; i += THREADS) win[i] = (uint16_t)entry(m.buckets[base + i]);
+  };
+  if (m.nb <= kTableLds) {
     for (int i = tid; i < m.nb; i += THREADS) row_lds[i] = row[i];
     __syncthreads();
+    fill(row_lds);
+  } else {
+    fill(row);
   }
-  const uint16_t* from = in_lds ? row_lds : row;
-  auto entry = [&](int b) -> uint16_t { return (unsigned)b < (unsigned)m.nb ? from[b] : (uint16_t)0; };
-  const int quads = (base & 3) == 0 ? n / 4 : 0;
-  constexpr int U = 8;
-  for (int i0 = tid; i0 < quads; i0 += U * THREADS) {
-    intx4 b[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) b[u] = *reinterpret_cast<const intx4*>(m.buckets + base + 4 * min(i0 + u * THREADS, quads - 1));
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uintx2 w = {(uint32_t)entry(b[u][0]) | (uint32_t)entry(b[u][1]) << 16, (uint32_t)entry(b[u][2]) | (uint32_t)entry(b[u][3]) << 16};
-      if (i0 + u * THREADS < quads) *reinterpret_cast<uintx2*>(win + 4 * (i0 + u * THREADS)) = w;
-    }
-  }
-  for (int i = 4 * quads + tid; i < n; i += THREADS) win[i] = entry(m.buckets[base + i]);
   return 0;
 }
 
 // Positions of the streamed rows of a tile and their range, and the range of the workgroup's own rows.
 struct BiasPos {
-  __attribute__((aligned(16))) int pos[2][kBiasBN];
+  __attribute__((aligned(16))) int pos[2][kBiasBN];           // twice the position: bytes of a window
   int range[2][2];
   int own[kBiasThreads / kWave][2];
 };
 // The first wave's 64 lanes: the tile's positions, and their smallest and largest.
-__device__ __forceinline__ void put_positions(BiasPos& l, int buf, const BiasMap& m, int token, bool ranges) {
+__device__ __forceinline__ void put_positions(BiasPos& l, int buf, const BiasMap& m, const BiasTokens& tokens, int loaded, int j, bool ranges) {
   if (threadIdx.x < kBiasBN) {
-    const int p = bias_position(m, token);
-    l.pos[buf][threadIdx.x] = p;
+    const int p = tokens.position(m, loaded, j);
+    l.pos[buf][threadIdx.x] = 2 * p;
     if (ranges) {
       const int lo = wave_pick<false>(p), hi = wave_pick<true>(p);
       if (threadIdx.x == 0) {
@@ -271,26 +295,25 @@ struct BiasFwd {
   long lse_stride;
 };
 
-// Scores of the wave's 32 rows against a tile's 64 with their biases: s scale + bias.  pos: positions of the tile's rows, own:
-// that of this lane's row (with the centre), SIGN: 1 if the offset is own - pos, else pos - own.  win: where offset 0 would lie.
+// The biases (upper halves of fp32) of a lane's row against the 16 of a 32-row block that it holds scores of: LDS reads, in flight
+// from here on.  pos2: twice the positions of the block's rows, own: that of the lane's row, one of the two with the centre;
+// SIGN: 1 if the offset is own - pos, else pos - own.  win0: the LDS address that offset 0 would have.
 template <int SIGN>
-__device__ __forceinline__ void add_bias(floatx16 (&s)[2], const int* pos, int own, bool in_window, const BiasMap& m, int h,
-                                         const uint16_t* win, float scale, int hh) {
+__device__ __forceinline__ void read_bias(uint32_t (&raw)[16], const int* pos2, int own, int win0, bool in_window, const BiasMap& m, int h,
+                                          int hh) {
+  const int from = SIGN > 0 ? 2 * own + win0 : win0 - 2 * own;
 #pragma unroll
-  for (int sb = 0; sb < 2; ++sb) {
-    float b[16];
+  for (int g = 0; g < 4; ++g) {
+    const intx4 p2 = *reinterpret_cast<const intx4*>(&pos2[8 * g + 4 * hh]);
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const intx4 p = *reinterpret_cast<const intx4*>(&pos[sb * 32 + 8 * g + 4 * hh]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int o = SIGN > 0 ? own - p[e] : p[e] - own;
-        b[4 * g + e] = in_window ? __builtin_bit_cast(float, (uint32_t)win[o] << 16) : bias_at<__bf16>(m, h, o);
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[sb][r] = fmaf(s[sb][r], scale, b[r]);
+    for (int e = 0; e < 4; ++e)
+      raw[4 * g + e] = in_window ? *(lds_u16_ptr)(uint32_t)(SIGN > 0 ? from - p2[e] : from + p2[e])
+                                 : __builtin_bit_cast(uint32_t, bias_at<__bf16>(m, h, SIGN * (own - (p2[e] >> 1)))) >> 16;
   }
+}
+__device__ __forceinline__ void add_bias(floatx16& s, const uint32_t (&raw)[16], float scale) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale, __builtin_bit_cast(float, raw[r] << 16));
 }
 
 template <int DH, bool WHOLE>
@@ -311,22 +334,23 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_fwd_kernel(const BiasF
   st.last = last;
   st.source(0, a.k + h * DH, a.ks, seg.row0);
   st.source(1, a.v + h * DH, a.vs, seg.row0);
-  int token = 0;
+  const BiasTokens tokens(a.m, a.cu, seg.row0);
+  int token = 0, token_j = 0;
   auto load_tile = [&](int kt) {
     st.load(kt);
-    const int j = min(kt + lane, last);
-    if (threadIdx.x < BN) token = bias_token(a.m, seg.row0 + j, j);
+    token_j = min(kt + lane, last);
+    token = tokens.load(token_j);
   };
   auto store_tile = [&](int buf, auto clear) {
     st.template store<clear>(l.A[buf], l.B[buf]);
-    put_positions(l.p, buf, a.m, token, !WHOLE);
+    put_positions(l.p, buf, a.m, tokens, token, token_j, !WHOLE);
   };
   load_tile(0);
   bf16x8 qf[KK];
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(a.q + q_row * a.qs + h * DH + kk * 16 + hh * 8);
-  const int own = bias_position(a.m, q_row, min(qi, last)) + a.m.centre;
-  const uint16_t* at0 = win;                                  // where offset 0 would lie
+  const int own = tokens.position(a.m, min(qi, last)) + a.m.centre;
+  int win0 = lds_address(win);                                // where offset 0 would lie
   if (!WHOLE) {
     const int lo = wave_pick<false>(own), hi = wave_pick<true>(own);
     if (lane == 0) {
@@ -334,7 +358,7 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_fwd_kernel(const BiasF
       l.p.own[wv][1] = hi;
     }
   } else {
-    at0 = win + load_window(a.m, h, 0, a.m.offsets, win, l.row);
+    win0 += 2 * load_window(a.m, h, 0, a.m.offsets, win, l.row);
   }
   floatx16 o[DB];
 #pragma unroll
@@ -357,23 +381,31 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_fwd_kernel(const BiasF
       in_window = hi - lo < kWindow - 3;
       if (in_window && (lo < base || hi >= base + kWindow)) {  // the keys' positions grow, so the next offsets are lower
         base = max(hi - kWindow + 4, 0) & ~3;                 // (16-byte pieces of the map)
-        at0 = win + load_window(a.m, h, base, kWindow, win, l.row) - base;
+        win0 = lds_address(win) + 2 * (load_window(a.m, h, base, kWindow, win, l.row) - base);
         __syncthreads();
       }
     }
     if (wave_live) {
+      // LDS answers in order: the operands of the first products, then the biases, which arrive during them
+      bf16x8 kf[2][KK];
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) kf[sb][kk] = *reinterpret_cast<const bf16x8*>(&l.A[buf][(sb * 32 + l32) * RS + kk * 16 + hh * 8]);
+      __builtin_amdgcn_sched_barrier(0);
+      uint32_t raw[2][16];
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb) read_bias<1>(raw[sb], &l.p.pos[buf][sb * 32], own, win0, WHOLE || in_window, a.m, h, hh);
+      __builtin_amdgcn_sched_barrier(0);
       floatx16 s[2];
 #pragma unroll
       for (int sb = 0; sb < 2; ++sb) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[sb][r] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
-          s[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&l.A[buf][(sb * 32 + l32) * RS + kk * 16 + hh * 8]),
-                                                          qf[kk], s[sb], 0, 0, 0);
+        for (int kk = 0; kk < KK; ++kk) s[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[sb][kk], qf[kk], s[sb], 0, 0, 0);
+        add_bias(s[sb], raw[sb], a.scale);
       }
-      if (WHOLE || in_window) add_bias<1>(s, l.p.pos[buf], own, true, a.m, h, at0, a.scale, hh);
-      else add_bias<1>(s, l.p.pos[buf], own, false, a.m, h, at0, a.scale, hh);
       if (end) {
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
@@ -499,16 +531,17 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBw
   st.last = last;
   st.source(0, a.k + h * DH, a.ks, seg.row0);
   st.source(1, a.v + h * DH, a.vs, seg.row0);
-  int token = 0;
+  const BiasTokens tokens(a.m, a.cu, seg.row0);
+  int token = 0, token_j = 0;
   auto load_tile = [&](int kt) {
     st.load(kt);
-    const int j = min(kt + lane, last);
-    if (threadIdx.x < BN) token = bias_token(a.m, seg.row0 + j, j);
+    token_j = min(kt + lane, last);
+    token = tokens.load(token_j);
   };
   float v_most = 0.f;                                         // of |V|, of the rows this thread stages
   auto store_tile = [&](int buf, auto clear) {
     st.template store<clear>(l.A[buf], l.B[buf]);
-    put_positions(l.p, buf, a.m, token, !WHOLE);
+    put_positions(l.p, buf, a.m, tokens, token, token_j, !WHOLE);
 #pragma unroll
     for (int t = 0; t < decltype(st)::CPT; ++t) {
       const floatx8 f = bf16x8_to_float(st.v[1][t]);
@@ -536,8 +569,8 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBw
   const float lse = a.lse[h * a.lse_stride + q_row];
   const bool far = __ballot(fabsf(lse) >= kFarScore && lse != -INFINITY) != 0;
   const float lse2 = lse == -INFINITY || !q_ok ? INFINITY : lse * kLog2e;      // (no score, or no row: probability 0)
-  const int own = bias_position(a.m, q_row, min(qi, last)) + a.m.centre;
-  const uint16_t* at0 = win;
+  const int own = tokens.position(a.m, min(qi, last)) + a.m.centre;
+  int win0 = lds_address(win);
   if (!WHOLE) {
     const int lo = wave_pick<false>(own), hi = wave_pick<true>(own);
     if (lane == 0) {
@@ -545,7 +578,7 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBw
       l.p.own[wv][1] = hi;
     }
   } else {
-    at0 = win + load_window(a.m, h, 0, a.m.offsets, win, l.row);
+    win0 += 2 * load_window(a.m, h, 0, a.m.offsets, win, l.row);
   }
   floatx16 acc[DB], negD;
 #pragma unroll
@@ -570,53 +603,50 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBw
       in_window = hi - lo < kWindow - 3;
       if (in_window && (lo < base || hi >= base + kWindow)) {
         base = max(hi - kWindow + 4, 0) & ~3;
-        at0 = win + load_window(a.m, h, base, kWindow, win, l.row) - base;
+        win0 = lds_address(win) + 2 * (load_window(a.m, h, base, kWindow, win, l.row) - base);
         __syncthreads();
       }
     }
     if (wave_live) {
-      floatx16 s[2], dp[2];
 #pragma unroll
       for (int sb = 0; sb < 2; ++sb) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[sb][r] = 0.f;
-        dp[sb] = negD;
+        bf16x8 kf[KK], vf[KK];
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
           const int at_row = (sb * 32 + l32) * RS + kk * 16 + hh * 8;
-          s[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&l.A[buf][at_row]), qf[kk], s[sb], 0, 0, 0);
-          dp[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&l.B[buf][at_row]), dof[kk], dp[sb], 0, 0, 0);
+          kf[kk] = *reinterpret_cast<const bf16x8*>(&l.A[buf][at_row]);
+          vf[kk] = *reinterpret_cast<const bf16x8*>(&l.B[buf][at_row]);
         }
-      }
-      if (WHOLE || in_window) add_bias<1>(s, l.p.pos[buf], own, true, a.m, h, at0, a.scale, hh);
-      else add_bias<1>(s, l.p.pos[buf], own, false, a.m, h, at0, a.scale, hh);
-      if (end) {
+        uint32_t raw[16];
+        read_bias<1>(raw, &l.p.pos[buf][sb * 32], own, win0, WHOLE || in_window, a.m, h, hh);
+        floatx16 s, dp = negD;
 #pragma unroll
-        for (int sb = 0; sb < 2; ++sb)
+        for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], qf[kk], s, 0, 0, 0);
+          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[kk], dof[kk], dp, 0, 0, 0);
+        }
+        add_bias(s, raw, a.scale);
+        if (end) {
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (kt + sb * 32 + acc_row(r, hh) >= n) s[sb][r] = -INFINITY;
-      }
-      if (!far) {
+            if (kt + sb * 32 + acc_row(r, hh) >= n) s[r] = -INFINITY;
+        }
+        if (!far) {
 #pragma unroll
-        for (int sb = 0; sb < 2; ++sb)
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], kLog2e, -lse2));
+        } else {
+          const float ref = lse2 == INFINITY ? INFINITY : lse;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[sb][r] = __builtin_amdgcn_exp2f(fmaf(s[sb][r], kLog2e, -lse2));
-      } else {
-        const float ref = lse2 == INFINITY ? INFINITY : lse;
-#pragma unroll
-        for (int sb = 0; sb < 2; ++sb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[sb][r] = __builtin_amdgcn_exp2f((s[sb][r] - ref) * kLog2e);
-      }
-#pragma unroll
-      for (int sb = 0; sb < 2; ++sb)
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f((s[r] - ref) * kLog2e);
+        }
 #pragma unroll
         for (int mf = 0; mf < 2; ++mf) {
           floatx8 f;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            f[j] = s[sb][8 * mf + j] * dp[sb][8 * mf + j];
+            f[j] = s[8 * mf + j] * dp[8 * mf + j];
             left += f[j];
             most = __builtin_elementwise_maximum(most, fabsf(f[j]));
           }
@@ -625,6 +655,7 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBw
           for (int d = 0; d < DB; ++d)
             acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_frag_rowmajor<RS>(l.A[buf], d, sb * 32, mf, lane), dsb, acc[d], 0, 0, 0);
         }
+      }
     }
     if (!end) {
       store_tile(buf ^ 1, std::bool_constant<decltype(at)::value == kTileBeforeLast>{});
@@ -652,6 +683,9 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBw
     a.most[((long)h * a.B + blk.img) * a.nblk + blk.r0 / kBiasRows] = all;
   }
 }
+
+// What becomes of dS by offset: nothing, a histogram of all offsets of the map in LDS, or one slice of them after the other.
+enum HistMode { kHistNone, kHistWhole, kHistSlices };
 
 // The head's blocks of keys in the order in which the workgroups take them: up to 256 segments by length, longest first,
 // blocks that exist numbered through; more segments in index order, with blocks of the longest possible one each.
@@ -759,9 +793,10 @@ struct DkdvTiles {
   KeyBlocks blocks;
 };
 
-template <int DH, int NW, bool WHOLE, bool HIST>
+template <int DH, int NW, bool WHOLE, int HIST>
 __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<__bf16> a) {
   constexpr int RS = DH + 8, KK = DH / 16, DB = DH / 32, BN = kBiasBN, THREADS = 64 * NW, ROWS = 32 * NW;
+  constexpr bool RANGES = !WHOLE || HIST == kHistSlices;      // the offsets of a tile lie where?
   static_assert(NW >= 4, "the first four waves stage");
   extern __shared__ __attribute__((aligned(16))) unsigned long long hist[];       // [slice], then the window of biases
   __shared__ DkdvTiles<DH, NW> l;
@@ -769,20 +804,20 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, l32 = lane & 31, hh = lane >> 5;
   const bool stages = tid < kBiasThreads;
   const long C = (long)a.H * DH;
-  uint16_t* win = reinterpret_cast<uint16_t*>(hist + (HIST ? a.slice : 0));
+  uint16_t* win = reinterpret_cast<uint16_t*>(hist + (HIST != kHistNone ? a.slice : 0));
   const float* lse_h = a.lse + h * a.lse_stride;
   const float* d_h = a.dvec + h * a.lse_stride;
 
   list_key_blocks<THREADS>(l.blocks, a.cu, a.B, ROWS, a.kblk);
   DsScale scale = {0, 0., 0.f};
-  if (HIST) scale = ds_scale<THREADS>(a.most + (long)h * a.B * a.nblk, a.cu, a.B, a.nblk, l.most);
-  const uint16_t* at0 = win;
-  if (WHOLE) at0 = win + load_window<THREADS>(a.m, h, 0, a.m.offsets, win, l.row);
+  if (HIST != kHistNone) scale = ds_scale<THREADS>(a.most + (long)h * a.B * a.nblk, a.cu, a.B, a.nblk, l.most);
+  int win0 = lds_address(win);                                // where offset 0 would lie
+  if (WHOLE) win0 += 2 * load_window<THREADS>(a.m, h, 0, a.m.offsets, win, l.row);
 
-  const int passes = HIST ? (a.m.offsets + a.slice - 1) / a.slice : 1;
+  const int passes = HIST == kHistSlices ? (a.m.offsets + a.slice - 1) / a.slice : 1;
   for (int pass = 0; pass < passes; ++pass) {
-    const int from = pass * a.slice;
-    if (HIST) {
+    const int from = HIST == kHistSlices ? pass * a.slice : 0;
+    if (HIST != kHistNone) {
       for (int i = tid; i < a.slice; i += THREADS) hist[i] = 0;
       // (in front of the first add there is the barrier behind a block's first tile)
     }
@@ -799,16 +834,15 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
       st.last = last;
       st.source(0, a.q + h * DH, a.qs, kb.row0);
       st.source(1, a.dout + h * DH, C, kb.row0);
-      int token = 0;
+      const BiasTokens tokens(a.m, a.cu, kb.row0);
+      int token = 0, token_j = 0;
       float lse_t = 0.f, d_t = 0.f;
       auto load_tile = [&](int qt) {
         if (stages) st.load(qt);
-        const int j = min(qt + lane, last);
-        if (tid < BN) {
-          token = bias_token(a.m, kb.row0 + j, j);
-          lse_t = lse_h[kb.row0 + j];
-          d_t = d_h[kb.row0 + j];
-        }
+        token_j = min(qt + lane, last);
+        token = tokens.load(token_j);
+        lse_t = lse_h[kb.row0 + token_j];
+        d_t = d_h[kb.row0 + token_j];
       };
       auto store_tile = [&](int buf, int qt, auto clear) {
         if (stages) st.template store<clear>(l.Q[buf], l.G[buf]);
@@ -817,10 +851,10 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
           l.lse[buf][tid] = none ? INFINITY : lse_t;
           l.lse2[buf][tid] = none ? INFINITY : lse_t * kLog2e;
           l.negD[buf][tid] = -d_t;
-          const int p = bias_position(a.m, token) + a.m.centre;
-          l.pos[buf][tid] = p;
+          const int p = tokens.position(a.m, token, token_j) + a.m.centre;
+          l.pos[buf][tid] = 2 * p;
           const bool any = __ballot(!none && fabsf(lse_t) >= kFarScore) != 0;
-          const int lo = !WHOLE || passes > 1 ? wave_pick<false>(p) : 0, hi = !WHOLE || passes > 1 ? wave_pick<true>(p) : 0;
+          const int lo = RANGES ? wave_pick<false>(p) : 0, hi = RANGES ? wave_pick<true>(p) : 0;
           if (tid == 0) {
             l.range[buf][0] = lo;
             l.range[buf][1] = hi;
@@ -836,9 +870,9 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
         kf[kk] = *reinterpret_cast<const bf16x8*>(a.k + k_row * a.ks + col);
         vf[kk] = *reinterpret_cast<const bf16x8*>(a.v + k_row * a.vs + col);
       }
-      const int own = bias_position(a.m, k_row, min(ki, last));
+      const int own = tokens.position(a.m, min(ki, last));
       __syncthreads();                                        // every wave is past its last read of the tiles before
-      if (!WHOLE || passes > 1) {
+      if (RANGES) {
         const int lo = wave_pick<false>(own), hi = wave_pick<true>(own);
         if (lane == 0) {
           l.own[wv][0] = lo;
@@ -853,7 +887,7 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
       store_tile(0, 0, std::true_type{});
       __syncthreads();
       Range mine = {0, 0};
-      if (!WHOLE || passes > 1) {
+      if (RANGES) {
         mine = {l.own[0][0], l.own[0][1]};
 #pragma unroll
         for (int w = 1; w < NW; ++w) mine = {min(mine.lo, l.own[w][0]), max(mine.hi, l.own[w][1])};
@@ -864,25 +898,37 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
         const int buf = t & 1, qt = t * BN;
         const bool end = t + 1 == nt;
         if (!end) load_tile(qt + BN);
-        bool in_window = true, adds = HIST, inside = true;
-        if (!WHOLE || passes > 1) {
+        bool in_window = true, adds = HIST != kHistNone, inside = true;
+        if (RANGES) {
           const int lo = __builtin_amdgcn_readfirstlane(l.range[buf][0] - mine.hi);
           const int hi = __builtin_amdgcn_readfirstlane(l.range[buf][1] - mine.lo);
           if (!WHOLE) {
             in_window = hi - lo < kWindow - 3;
             if (in_window && (lo < base || hi >= base + kWindow)) {   // the queries' positions grow, so do the offsets
               base = lo & ~3;
-              at0 = win + load_window<THREADS>(a.m, h, base, kWindow, win, l.row) - base;
+              win0 = lds_address(win) + 2 * (load_window<THREADS>(a.m, h, base, kWindow, win, l.row) - base);
               __syncthreads();
             }
           }
-          adds = HIST && hi >= from && lo < from + a.slice;
-          inside = lo >= from && hi < from + a.slice;
+          if (HIST == kHistSlices) {
+            adds = hi >= from && lo < from + a.slice;
+            inside = lo >= from && hi < from + a.slice;
+          }
         }
         if (wave_live && (pass == 0 || adds)) {
-          const bool far = l.far[buf] != 0;
+          const bool far = __builtin_amdgcn_readfirstlane(l.far[buf]) != 0;
 #pragma unroll
           for (int sb = 0; sb < 2; ++sb) {
+            bf16x8 qf[KK], gf[KK];
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+              const int at_row = (sb * 32 + l32) * RS + kk * 16 + hh * 8;
+              qf[kk] = *reinterpret_cast<const bf16x8*>(&l.Q[buf][at_row]);
+              gf[kk] = *reinterpret_cast<const bf16x8*>(&l.G[buf][at_row]);
+            }
+            const int* pos2 = &l.pos[buf][sb * 32];
+            uint32_t raw[16];
+            read_bias<-1>(raw, pos2, own, win0, WHOLE || in_window, a.m, h, hh);
             floatx16 s, dp;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
@@ -895,31 +941,27 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
             }
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
-              const int at_row = (sb * 32 + l32) * RS + kk * 16 + hh * 8;
-              s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&l.Q[buf][at_row]), kf[kk], s, 0, 0, 0);
-              dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&l.G[buf][at_row]), vf[kk], dp, 0, 0, 0);
+              s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[kk], kf[kk], s, 0, 0, 0);
+              dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(gf[kk], vf[kk], dp, 0, 0, 0);
             }
-            int o[16];
+            add_bias(s, raw, a.scale);
+            if (!far) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const intx4 p4 = *reinterpret_cast<const intx4*>(&l.pos[buf][sb * 32 + 8 * g + 4 * hh]);
+              for (int g = 0; g < 4; ++g) {
+                const floatx4 l4 = *reinterpret_cast<const floatx4*>(&l.lse2[buf][sb * 32 + 8 * g + 4 * hh]);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int r = 4 * g + i;
-                o[r] = p4[i] - own;
-                s[r] = fmaf(s[r], a.scale, WHOLE || in_window ? __builtin_bit_cast(float, (uint32_t)at0[o[r]] << 16) : bias_at<__bf16>(a.m, h, o[r]));
+                for (int i = 0; i < 4; ++i) s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], kLog2e, -l4[i]));
+              }
+            } else {
+#pragma unroll
+              for (int g = 0; g < 4; ++g) {
+                const floatx4 l4 = *reinterpret_cast<const floatx4*>(&l.lse[buf][sb * 32 + 8 * g + 4 * hh]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[4 * g + i] = __builtin_amdgcn_exp2f((s[4 * g + i] - l4[i]) * kLog2e);
               }
             }
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const floatx4 l4 = *reinterpret_cast<const floatx4*>(&(far ? l.lse : l.lse2)[buf][sb * 32 + 8 * g + 4 * hh]);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int r = 4 * g + i;
-                s[r] = __builtin_amdgcn_exp2f(far ? (s[r] - l4[i]) * kLog2e : fmaf(s[r], kLog2e, -l4[i]));
-                dp[r] *= s[r];
-              }
-            }
+            for (int r = 0; r < 16; ++r) dp[r] *= s[r];
             if (pass == 0) {
 #pragma unroll
               for (int mf = 0; mf < 2; ++mf) {
@@ -937,11 +979,18 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
                 }
               }
             }
-            if (HIST && adds && k_ok) {
+            if (HIST != kHistNone && adds && k_ok) {
+              const int to = lds_address(hist) - 8 * (own + from);          // (four times twice a position: 8 bytes an offset)
 #pragma unroll
-              for (int r = 0; r < 16; ++r)
-                if (inside || (unsigned)(o[r] - from) < (unsigned)a.slice)
-                  __hip_atomic_fetch_add(&hist[o[r] - from], ds_integer(dp[r], scale.factor), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+              for (int g = 0; g < 4; ++g) {
+                const intx4 p2 = *reinterpret_cast<const intx4*>(&pos2[8 * g + 4 * hh]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const unsigned long long v = ds_integer(dp[4 * g + i], scale.factor);
+                  if (HIST == kHistWhole || inside) lds_add(p2[i] * 4 + to, v);
+                  else if ((unsigned)((p2[i] >> 1) - own - from) < (unsigned)a.slice) lds_add(p2[i] * 4 + to, v);
+                }
+              }
             }
           }
         }
@@ -956,7 +1005,7 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
         store_rows<DH>(dva, 1.0f, a.dv + k_row * a.dvs + h * DH, k_ok, hh);
       }
     }
-    if (HIST) write_partial<THREADS>(hist, scale, a.slice, from, a.m.offsets, a.partial + ((long)h * a.groups + group) * a.m.offsets);
+    if (HIST != kHistNone) write_partial<THREADS>(hist, scale, a.slice, from, a.m.offsets, a.partial + ((long)h * a.groups + group) * a.m.offsets);
   }
 }
 
@@ -1049,13 +1098,14 @@ __global__ void __launch_bounds__(kRowThreads) attn_bias_dq_rows_kernel(const Bi
     l1 += fabsf(g[d]);
     acc[d] = 0.f;
   }
-  const int p = bias_position(a.m, row, ok ? ri : 0) + a.m.centre;
+  const BiasTokens tokens(a.m, a.cu, row0);
+  const int p = tokens.position(a.m, ok ? ri : 0) + a.m.centre;
   const float l = a.lse[h * a.lse_stride + row];
   float left = 0.f, most = 0.f, v_most = 0.f;
   for (int t = 0; t < n; t += kRowTile) {
     __syncthreads();
     stage_rows<float, DH>(a.k + h * DH, a.ks, a.v + h * DH, a.vs, row0, t, n, Ks, Vs);
-    if (threadIdx.x < kRowTile && t + threadIdx.x < n) pos[threadIdx.x] = bias_position(a.m, row0 + t + threadIdx.x, t + threadIdx.x);
+    if (threadIdx.x < kRowTile && t + threadIdx.x < n) pos[threadIdx.x] = tokens.position(a.m, t + threadIdx.x);
     __syncthreads();
     for (int i = threadIdx.x; i < kRowTile * DH; i += kRowThreads) v_most = __builtin_elementwise_maximum(v_most, fabsf(Vs[i]));
     const int tn = min(kRowTile, n - t);
@@ -1116,13 +1166,14 @@ __global__ void __launch_bounds__(kRowThreads) attn_bias_dkdv_rows_kernel(const 
         v[d] = a.v[row * a.vs + h * DH + d];
         dk[d] = dv[d] = 0.f;
       }
-      const int p = bias_position(a.m, row, ok ? ki : 0) - a.m.centre;
+      const BiasTokens tokens(a.m, a.cu, kb.row0);
+      const int p = tokens.position(a.m, ok ? ki : 0) - a.m.centre;
       for (int t = 0; t < kb.n; t += kRowTile) {
         __syncthreads();
         stage_rows<float, DH>(a.q + h * DH, a.qs, a.dout + h * DH, C, kb.row0, t, kb.n, Qs, Gs);
         if (threadIdx.x < kRowTile && t + threadIdx.x < kb.n) {
           const long r = kb.row0 + t + threadIdx.x;
-          pos[threadIdx.x] = bias_position(a.m, r, t + threadIdx.x);
+          pos[threadIdx.x] = tokens.position(a.m, t + threadIdx.x);
           lses[threadIdx.x] = a.lse[h * a.lse_stride + r];
           Ds[threadIdx.x] = a.dvec[h * a.lse_stride + r];
         }
@@ -1140,7 +1191,7 @@ __global__ void __launch_bounds__(kRowThreads) attn_bias_dkdv_rows_kernel(const 
           }
           const float pr = lses[j] == -INFINITY ? 0.f : expf(fmaf(s, a.scale, bias_at<float>(a.m, h, o)) - lses[j]);
           const float ds = pr * (dp - Ds[j]);
-          if (adds) __hip_atomic_fetch_add(&hist[o - from], ds_integer(ds, scale.factor), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+          if (adds) lds_add(lds_address(hist) + 8 * (o - from), ds_integer(ds, scale.factor));
           if (pass > 0) continue;
 #pragma unroll
           for (int d = 0; d < DH; ++d) {
@@ -1211,7 +1262,7 @@ struct BiasPlan {
   int nw, slice, groups, kblk;
   size_t lds;
 };
-static BiasPlan bias_plan(int H, int B, int n_max, int Dh, long offsets, int dtype) {
+static BiasPlan bias_plan(int H, int B, int n_max, int Dh, long offsets, int dtype, bool hist) {
   BiasPlan p = {};
   const size_t window = window_bytes((int)(offsets <= kWholeMost ? offsets : kWindow)), most = 160 * 1024;
   const size_t tiles4 = Dh == 32 ? sizeof(DkdvTiles<32, 4>) : sizeof(DkdvTiles<64, 4>);
@@ -1222,7 +1273,7 @@ static BiasPlan bias_plan(int H, int B, int n_max, int Dh, long offsets, int dty
     p.nw = 4;
     p.slice = (int)std::min<long>(up64(offsets), 4096);
     p.lds = (size_t)p.slice * 8;
-  } else if (tiles4 + window + up64(offsets) * 8 <= most / 2) {
+  } else if (!hist || tiles4 + window + up64(offsets) * 8 <= most / 2) {
     p.nw = 4;
     p.slice = (int)up64(offsets);
     p.lds = window + (size_t)p.slice * 8;
@@ -1283,7 +1334,7 @@ extern "C" int spa_packed_attention_bias(const void* q, const void* k, const voi
 extern "C" size_t spa_attention_bias_bwd_workspace_bytes(int B, int max_seqlen, int H, int Dh, int grid_h, int grid_w, int dtype) {
   if (B < 1 || max_seqlen < 1 || H < 1 || grid_h < 1 || grid_w < 1 || (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1) > kMostOffsets) return 0;
   const long offsets = (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1);
-  const BiasPlan p = bias_plan(H, B, max_seqlen, Dh, offsets, dtype);
+  const BiasPlan p = bias_plan(H, B, max_seqlen, Dh, offsets, dtype, true);
   const size_t nblk = (max_seqlen + kBiasRows - 1) / kBiasRows;
   return up256((size_t)H * B * max_seqlen * 4) + up256((size_t)H * B * nblk * 4) + up256((size_t)H * p.groups * offsets * 4) +
          up256((size_t)H * offsets * 4);
@@ -1315,7 +1366,7 @@ extern "C" int spa_packed_attention_bias_bwd(const void* q, const void* k, const
   SPA_REQUIRE((reinterpret_cast<uintptr_t>(workspace) & 255u) == 0, SPA_ERR_INVALID_ARG, "%s: workspace not 256-byte aligned", fn);
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)Dh);
   const long ls = (long)B * max_seqlen;
-  const BiasPlan plan = bias_plan(H, B, max_seqlen, Dh, m.offsets, dtype);
+  const BiasPlan plan = bias_plan(H, B, max_seqlen, Dh, m.offsets, dtype, d_table != nullptr);
   const int nblk = (max_seqlen + kBiasRows - 1) / kBiasRows;
   SPA_REQUIRE(((long)H * B + 8) * nblk < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*H*blocks must be < 2^31", fn);
   char* ws = static_cast<char*>(workspace);
@@ -1335,18 +1386,19 @@ extern "C" int spa_packed_attention_bias_bwd(const void* q, const void* k, const
   {(const T*)q, (const T*)k, (const T*)v, (const T*)out, (const T*)dout, (long)q_row_stride, (long)k_row_stride, (long)v_row_stride, lse, \
    dvec, ls, cu_seqlens, m, H, B, nblk, scale, (T*)dq, (T*)dk, (T*)dv, (long)dq_row_stride, (long)dk_row_stride, (long)dv_row_stride,     \
    most, partial, plan.groups, plan.slice, plan.kblk}
-#define SPA_DKDV(D, NW, W)                                                                                                   \
+#define SPA_DKDV(D, NW, W, MODE)                                                                                             \
   do {                                                                                                                       \
-    if (hist) SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<D, NW, W, true>), H * plan.groups, 64 * NW, plan.lds, args);            \
-    else SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<D, NW, W, false>), H * plan.groups, 64 * NW, window, args);                  \
+    if (hist) SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<D, NW, W, MODE>), H * plan.groups, 64 * NW, plan.lds, args);            \
+    else SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<D, 4, W, kHistNone>), H * plan.groups, 256, window, args);                   \
   } while (0)
 #define SPA_BIAS16(D)                                                                                                        \
   do {                                                                                                                       \
     if (whole) SPA_BIAS_LAUNCH((attn_bias_dq_kernel<D, true>), xcd_grid(nblk, H, B), kBiasThreads, window, args);            \
     else SPA_BIAS_LAUNCH((attn_bias_dq_kernel<D, false>), xcd_grid(nblk, H, B), kBiasThreads, window, args);                 \
-    if (!whole) SPA_DKDV(D, 4, false);                                                                                       \
-    else if (plan.nw == 4) SPA_DKDV(D, 4, true);                                                                             \
-    else SPA_DKDV(D, 8, true);                                                                                               \
+    if (!whole) SPA_DKDV(D, 4, false, kHistSlices);                                                                          \
+    else if (plan.nw == 4) SPA_DKDV(D, 4, true, kHistWhole);                                                                 \
+    else if (plan.slice >= m.offsets) SPA_DKDV(D, 8, true, kHistWhole);                                                      \
+    else SPA_DKDV(D, 8, true, kHistSlices);                                                                                  \
   } while (0)
 #define SPA_BIAS32(D)                                                                                                        \
   do {                                                                                                                       \
