@@ -222,22 +222,24 @@ __device__ __forceinline__ int load_window(const BiasMap& m, int h, int base, in
   return 0;
 }
 
-// Positions of the streamed rows of a tile and their range, and the range of the workgroup's own rows.
+// Positions of the streamed rows of a step (SPLIT tiles) and the range of each tile's, and the range of the workgroup's own rows.
+template <int SPLIT>
 struct BiasPos {
-  __attribute__((aligned(16))) int pos[2][kBiasBN];           // twice the position: bytes of a window
-  int range[2][2];
-  int own[kBiasThreads / kWave][2];
+  __attribute__((aligned(16))) int pos[2][kBiasBN * SPLIT];   // twice the position: bytes of a window
+  int range[2][SPLIT][2];
+  int own[4 * SPLIT][2];
 };
-// The first wave's 64 lanes: the tile's positions, and their smallest and largest.
-__device__ __forceinline__ void put_positions(BiasPos& l, int buf, const BiasMap& m, const BiasTokens& tokens, int loaded, int j, bool ranges) {
-  if (threadIdx.x < kBiasBN) {
+// A wave a tile: its positions, and their smallest and largest.
+template <int SPLIT>
+__device__ __forceinline__ void put_positions(BiasPos<SPLIT>& l, int buf, const BiasMap& m, const BiasTokens& tokens, int loaded, int j, bool ranges) {
+  if (threadIdx.x < kBiasBN * SPLIT) {
     const int p = tokens.position(m, loaded, j);
     l.pos[buf][threadIdx.x] = 2 * p;
     if (ranges) {
       const int lo = wave_pick<false>(p), hi = wave_pick<true>(p);
-      if (threadIdx.x == 0) {
-        l.range[buf][0] = lo;
-        l.range[buf][1] = hi;
+      if ((threadIdx.x & 63) == 0) {
+        l.range[buf][threadIdx.x >> 6][0] = lo;
+        l.range[buf][threadIdx.x >> 6][1] = hi;
       }
     }
   }
@@ -245,19 +247,20 @@ __device__ __forceinline__ void put_positions(BiasPos& l, int buf, const BiasMap
 struct Range {
   int lo, hi;
 };
-__device__ __forceinline__ Range own_range(const BiasPos& l) {
-  Range r = {l.own[0][0], l.own[0][1]};
+template <int N>
+__device__ __forceinline__ Range whole_range(const int (&of)[N][2]) {
+  Range r = {of[0][0], of[0][1]};
 #pragma unroll
-  for (int w = 1; w < kBiasThreads / kWave; ++w) r = {min(r.lo, l.own[w][0]), max(r.hi, l.own[w][1])};
+  for (int i = 1; i < N; ++i) r = {min(r.lo, of[i][0]), max(r.hi, of[i][1])};
   return {__builtin_amdgcn_readfirstlane(r.lo), __builtin_amdgcn_readfirstlane(r.hi)};
 }
 
-template <int DH>
+template <int DH, int SPLIT>
 struct BiasTiles {
-  static constexpr int RS = DH + 8;
-  __attribute__((aligned(16))) __bf16 A[2][kBiasBN * RS];     // K (forward, dq) | Q (dk, dv)
-  __attribute__((aligned(16))) __bf16 B[2][kBiasBN * RS];     // V | dO
-  BiasPos p;
+  static constexpr int RS = DH + 8, STEP = kBiasBN * SPLIT;
+  __attribute__((aligned(16))) __bf16 A[2][STEP * RS];        // K
+  __attribute__((aligned(16))) __bf16 B[2][STEP * RS];        // V
+  BiasPos<SPLIT> p;
   uint16_t row[kTableLds];
   int s_live[sizeof(LiveTile) / sizeof(int)];
 };
@@ -268,11 +271,10 @@ struct BiasBlock {
   int img, h, r0;
   bool valid;
 };
-template <int DH>
-__device__ __forceinline__ BiasBlock bias_block(BiasTiles<DH>& l, const int32_t* cu, int H, int B, int nblk) {
+__device__ __forceinline__ BiasBlock bias_block(int* s_live, const int32_t* cu, int H, int B, int nblk) {
   const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
   if (B <= kLptMaxB) {
-    LiveTile* slot = reinterpret_cast<LiveTile*>(l.s_live);
+    LiveTile* slot = reinterpret_cast<LiveTile*>(s_live);
     const LiveTile t = live_tiles_apply(H, B) ? live_tile_block<1>(xcd, j, H, B, cu, kBiasRows, nblk, slot)
                                               : class_tile_block<1>(xcd, j, H, B, cu, kBiasRows, nblk, slot);
     return {{t.row0, t.len, t.len}, t.img, t.h, t.qb * kBiasRows, t.valid};
@@ -316,20 +318,22 @@ __device__ __forceinline__ void add_bias(floatx16& s, const uint32_t (&raw)[16],
   for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale, __builtin_bit_cast(float, raw[r] << 16));
 }
 
-template <int DH, bool WHOLE>
-__global__ void __launch_bounds__(kBiasThreads) attn_bias_fwd_kernel(const BiasFwd a) {
-  constexpr int RS = DH + 8, KK = DH / 16, DB = DH / 32, BN = kBiasBN;
+// SPLIT 2: the waves come twice, the second four take every other tile of 64 keys, and hand their sums to the first at the end.
+template <int DH, bool WHOLE, int SPLIT>
+__global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_fwd_kernel(const BiasFwd a) {
+  constexpr int RS = DH + 8, KK = DH / 16, DB = DH / 32, THREADS = kBiasThreads * SPLIT, STEP = kBiasBN * SPLIT;
   extern __shared__ __attribute__((aligned(16))) uint16_t win[];
-  __shared__ BiasTiles<DH> l;
-  const BiasBlock blk = bias_block<DH>(l, a.cu, a.H, a.B, a.nblk);
+  __shared__ BiasTiles<DH, SPLIT> l;
+  const BiasBlock blk = bias_block(l.s_live, a.cu, a.H, a.B, a.nblk);
   if (!blk.valid) return;
   const Segment seg = blk.seg;
-  const int h = blk.h, n = seg.nk, lane = threadIdx.x & 63, wv = threadIdx.x >> 6, l32 = lane & 31, hh = lane >> 5;
+  const int h = blk.h, n = seg.nk, lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5;
+  const int wv = (threadIdx.x >> 6) & 3, part = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
   const int qi = blk.r0 + wv * 32 + l32, last = n - 1;
   const bool wave_live = blk.r0 + wv * 32 < n, q_ok = qi < n;
   const long C = (long)a.H * DH, q_row = seg.row0 + min(qi, last);
 
-  PairStage<DH, kBiasThreads, BN, false, false> st(threadIdx.x);
+  PairStage<DH, THREADS, STEP, false, false> st(threadIdx.x);
   st.gi = nullptr;
   st.last = last;
   st.source(0, a.k + h * DH, a.ks, seg.row0);
@@ -338,7 +342,7 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_fwd_kernel(const BiasF
   int token = 0, token_j = 0;
   auto load_tile = [&](int kt) {
     st.load(kt);
-    token_j = min(kt + lane, last);
+    token_j = min(kt + (int)(threadIdx.x & (STEP - 1)), last);
     token = tokens.load(token_j);
   };
   auto store_tile = [&](int buf, auto clear) {
@@ -354,11 +358,11 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_fwd_kernel(const BiasF
   if (!WHOLE) {
     const int lo = wave_pick<false>(own), hi = wave_pick<true>(own);
     if (lane == 0) {
-      l.p.own[wv][0] = lo;
-      l.p.own[wv][1] = hi;
+      l.p.own[threadIdx.x >> 6][0] = lo;
+      l.p.own[threadIdx.x >> 6][1] = hi;
     }
   } else {
-    win0 += 2 * load_window(a.m, h, 0, a.m.offsets, win, l.row);
+    win0 += 2 * load_window<THREADS>(a.m, h, 0, a.m.offsets, win, l.row);
   }
   floatx16 o[DB];
 #pragma unroll
@@ -368,34 +372,37 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_fwd_kernel(const BiasF
   float m = -INFINITY, sum = 0.f;
   store_tile(0, std::true_type{});
   __syncthreads();
-  const Range mine = WHOLE ? Range{0, 0} : own_range(l.p);
+  const Range mine = WHOLE ? Range{0, 0} : whole_range(l.p.own);
   int base = -0x40000000;                                     // (no window yet)
-  const int nt = (n + BN - 1) / BN;
+  const int nt = (n + STEP - 1) / STEP;
   walk_tiles(nt, [&](int t, auto at) {
     constexpr bool end = decltype(at)::value == kTileLast;
-    const int buf = t & 1, kt = t * BN;
-    if (!end) load_tile(kt + BN);
+    const int buf = t & 1, kt = t * STEP + part * kBiasBN;      // (the wave's tile)
+    if (!end) load_tile(t * STEP + STEP);
     bool in_window = true;
     if (!WHOLE) {
-      const int lo = mine.lo - l.p.range[buf][1], hi = mine.hi - l.p.range[buf][0];
+      const Range tile = whole_range(l.p.range[buf]);
+      const int lo = mine.lo - tile.hi, hi = mine.hi - tile.lo;
       in_window = hi - lo < kWindow - 3;
       if (in_window && (lo < base || hi >= base + kWindow)) {  // the keys' positions grow, so the next offsets are lower
         base = max(hi - kWindow + 4, 0) & ~3;                 // (16-byte pieces of the map)
-        win0 = lds_address(win) + 2 * (load_window(a.m, h, base, kWindow, win, l.row) - base);
+        win0 = lds_address(win) + 2 * (load_window<THREADS>(a.m, h, base, kWindow, win, l.row) - base);
         __syncthreads();
       }
     }
-    if (wave_live) {
+    if (wave_live && (SPLIT == 1 || !end || kt < n)) {
+      const __bf16 *A = &l.A[buf][part * kBiasBN * RS], *B = &l.B[buf][part * kBiasBN * RS];
+      const int* pos = &l.p.pos[buf][part * kBiasBN];
       // LDS answers in order: the operands of the first products, then the biases, which arrive during them
       bf16x8 kf[2][KK];
 #pragma unroll
       for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) kf[sb][kk] = *reinterpret_cast<const bf16x8*>(&l.A[buf][(sb * 32 + l32) * RS + kk * 16 + hh * 8]);
+        for (int kk = 0; kk < KK; ++kk) kf[sb][kk] = *reinterpret_cast<const bf16x8*>(&A[(sb * 32 + l32) * RS + kk * 16 + hh * 8]);
       __builtin_amdgcn_sched_barrier(0);
       uint32_t raw[2][16];
 #pragma unroll
-      for (int sb = 0; sb < 2; ++sb) read_bias<1>(raw[sb], &l.p.pos[buf][sb * 32], own, win0, WHOLE || in_window, a.m, h, hh);
+      for (int sb = 0; sb < 2; ++sb) read_bias<1>(raw[sb], &pos[sb * 32], own, win0, WHOLE || in_window, a.m, h, hh);
       __builtin_amdgcn_sched_barrier(0);
       floatx16 s[2];
 #pragma unroll
@@ -454,14 +461,39 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_fwd_kernel(const BiasF
           const bf16x8 pb = float_to_bf16x8(f);
 #pragma unroll
           for (int d = 0; d < DB; ++d)
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_frag_rowmajor<RS>(l.B[buf], d, sb * 32, mf, lane), pb, o[d], 0, 0, 0);
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_frag_rowmajor<RS>(B, d, sb * 32, mf, lane), pb, o[d], 0, 0, 0);
         }
     }
     if (!end) store_tile(buf ^ 1, std::bool_constant<decltype(at)::value == kTileBeforeLast>{});
     __syncthreads();
   });
+  // (every wave is past its last read of the tiles)
+  if constexpr (SPLIT > 1) {
+    constexpr int W = DB * 16 + 2;
+    static_assert(4 * W * kWave * sizeof(float) <= sizeof(l.B), "the sums of four waves");
+    float* other = reinterpret_cast<float*>(&l.B[0][0]) + wv * W * kWave + lane;
+    if (part == 1) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) other[(d * 16 + r) * kWave] = o[d][r];
+      other[(W - 2) * kWave] = m;
+      other[(W - 1) * kWave] = sum;
+    }
+    __syncthreads();
+    if (part == 1) return;
+    const float m1 = other[(W - 2) * kWave], both = __builtin_elementwise_maximum(m, m1);
+    const float f0 = m == both ? 1.f : __builtin_amdgcn_exp2f((m - both) * kLog2e);
+    const float f1 = m1 == both ? 1.f : __builtin_amdgcn_exp2f((m1 - both) * kLog2e);
+    m = both;
+    sum = sum * f0 + other[(W - 1) * kWave] * f1;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = o[d][r] * f0 + other[(d * 16 + r) * kWave] * f1;
+  }
   const float total = sum_across_halves(sum), inv = total == 0.f ? 0.f : 1.0f / total;
-  __bf16* parked = &l.A[0][0] + wv * 32 * RS;                 // (every wave is past its last read of the tiles)
+  __bf16* parked = &l.A[0][0] + wv * 32 * RS;
   if (wave_live) {
     park_tile<DH, RS>(o, inv, parked, l32, hh);
     if (a.lse != nullptr && q_ok && hh == 0)
@@ -512,21 +544,22 @@ struct BiasBwd {
   int kblk;                       // dk / dv: blocks of 32 NW keys of the longest possible segment
 };
 
-template <int DH, bool WHOLE>
-__global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBwd<__bf16> a) {
-  constexpr int RS = DH + 8, KK = DH / 16, DB = DH / 32, BN = kBiasBN;
+template <int DH, bool WHOLE, int SPLIT>
+__global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(const BiasBwd<__bf16> a) {
+  constexpr int RS = DH + 8, KK = DH / 16, DB = DH / 32, THREADS = kBiasThreads * SPLIT, STEP = kBiasBN * SPLIT;
   extern __shared__ __attribute__((aligned(16))) uint16_t win[];
-  __shared__ BiasTiles<DH> l;
-  __shared__ float s_most[2][kBiasThreads / kWave];
-  const BiasBlock blk = bias_block<DH>(l, a.cu, a.H, a.B, a.nblk);
+  __shared__ BiasTiles<DH, SPLIT> l;
+  __shared__ float s_most[2][THREADS / kWave];
+  const BiasBlock blk = bias_block(l.s_live, a.cu, a.H, a.B, a.nblk);
   if (!blk.valid) return;
   const Segment seg = blk.seg;
-  const int h = blk.h, n = seg.nk, lane = threadIdx.x & 63, wv = threadIdx.x >> 6, l32 = lane & 31, hh = lane >> 5;
+  const int h = blk.h, n = seg.nk, lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5;
+  const int wv = (threadIdx.x >> 6) & 3, part = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
   const int qi = blk.r0 + wv * 32 + l32, last = n - 1;
   const bool wave_live = blk.r0 + wv * 32 < n, q_ok = qi < n;
   const long C = (long)a.H * DH, q_row = seg.row0 + min(qi, last);
 
-  PairStage<DH, kBiasThreads, BN, false, false> st(threadIdx.x);
+  PairStage<DH, THREADS, STEP, false, false> st(threadIdx.x);
   st.gi = nullptr;
   st.last = last;
   st.source(0, a.k + h * DH, a.ks, seg.row0);
@@ -535,7 +568,7 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBw
   int token = 0, token_j = 0;
   auto load_tile = [&](int kt) {
     st.load(kt);
-    token_j = min(kt + lane, last);
+    token_j = min(kt + (int)(threadIdx.x & (STEP - 1)), last);
     token = tokens.load(token_j);
   };
   float v_most = 0.f;                                         // of |V|, of the rows this thread stages
@@ -574,11 +607,11 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBw
   if (!WHOLE) {
     const int lo = wave_pick<false>(own), hi = wave_pick<true>(own);
     if (lane == 0) {
-      l.p.own[wv][0] = lo;
-      l.p.own[wv][1] = hi;
+      l.p.own[threadIdx.x >> 6][0] = lo;
+      l.p.own[threadIdx.x >> 6][1] = hi;
     }
   } else {
-    win0 += 2 * load_window(a.m, h, 0, a.m.offsets, win, l.row);
+    win0 += 2 * load_window<THREADS>(a.m, h, 0, a.m.offsets, win, l.row);
   }
   floatx16 acc[DB], negD;
 #pragma unroll
@@ -590,35 +623,38 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBw
   float left = 0.f, most = 0.f;
   store_tile(0, std::true_type{});
   __syncthreads();
-  const Range mine = WHOLE ? Range{0, 0} : own_range(l.p);
+  const Range mine = WHOLE ? Range{0, 0} : whole_range(l.p.own);
   int base = -0x40000000;
-  const int nt = (n + BN - 1) / BN;
+  const int nt = (n + STEP - 1) / STEP;
   walk_tiles(nt, [&](int t, auto at) {
     constexpr bool end = decltype(at)::value == kTileLast;
-    const int buf = t & 1, kt = t * BN;
-    if (!end) load_tile(kt + BN);
+    const int buf = t & 1, kt = t * STEP + part * kBiasBN;      // (the wave's tile)
+    if (!end) load_tile(t * STEP + STEP);
     bool in_window = true;
     if (!WHOLE) {
-      const int lo = mine.lo - l.p.range[buf][1], hi = mine.hi - l.p.range[buf][0];
+      const Range tile = whole_range(l.p.range[buf]);
+      const int lo = mine.lo - tile.hi, hi = mine.hi - tile.lo;
       in_window = hi - lo < kWindow - 3;
       if (in_window && (lo < base || hi >= base + kWindow)) {
         base = max(hi - kWindow + 4, 0) & ~3;
-        win0 = lds_address(win) + 2 * (load_window(a.m, h, base, kWindow, win, l.row) - base);
+        win0 = lds_address(win) + 2 * (load_window<THREADS>(a.m, h, base, kWindow, win, l.row) - base);
         __syncthreads();
       }
     }
-    if (wave_live) {
+    if (wave_live && (SPLIT == 1 || !end || kt < n)) {
+      const __bf16 *A = &l.A[buf][part * kBiasBN * RS], *B = &l.B[buf][part * kBiasBN * RS];
+      const int* pos = &l.p.pos[buf][part * kBiasBN];
 #pragma unroll
       for (int sb = 0; sb < 2; ++sb) {
         bf16x8 kf[KK], vf[KK];
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
           const int at_row = (sb * 32 + l32) * RS + kk * 16 + hh * 8;
-          kf[kk] = *reinterpret_cast<const bf16x8*>(&l.A[buf][at_row]);
-          vf[kk] = *reinterpret_cast<const bf16x8*>(&l.B[buf][at_row]);
+          kf[kk] = *reinterpret_cast<const bf16x8*>(&A[at_row]);
+          vf[kk] = *reinterpret_cast<const bf16x8*>(&B[at_row]);
         }
         uint32_t raw[16];
-        read_bias<1>(raw, &l.p.pos[buf][sb * 32], own, win0, WHOLE || in_window, a.m, h, hh);
+        read_bias<1>(raw, &pos[sb * 32], own, win0, WHOLE || in_window, a.m, h, hh);
         floatx16 s, dp = negD;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = 0.f;
@@ -653,7 +689,7 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBw
           const bf16x8 dsb = float_to_bf16x8(f);
 #pragma unroll
           for (int d = 0; d < DB; ++d)
-            acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_frag_rowmajor<RS>(l.A[buf], d, sb * 32, mf, lane), dsb, acc[d], 0, 0, 0);
+            acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_frag_rowmajor<RS>(A, d, sb * 32, mf, lane), dsb, acc[d], 0, 0, 0);
         }
       }
     }
@@ -662,24 +698,48 @@ __global__ void __launch_bounds__(kBiasThreads) attn_bias_dq_kernel(const BiasBw
       __syncthreads();
     }
   });
-  store_rows<DH>(acc, a.scale, a.dq + q_row * a.dqs + h * DH, q_ok, hh);
+  v_most = __builtin_bit_cast(float, wave_pick<true>((int)(__builtin_bit_cast(uint32_t, v_most) & 0x7fffffffu)));
+  if (lane == 0) s_most[0][threadIdx.x >> 6] = v_most;
+  __syncthreads();                                            // (and every wave is past its last read of the tiles)
+  if constexpr (SPLIT > 1) {
+    constexpr int W = DB * 16 + 2;
+    static_assert(4 * W * kWave * sizeof(float) <= sizeof(l.B), "the sums of four waves");
+    float* other = reinterpret_cast<float*>(&l.B[0][0]) + wv * W * kWave + lane;
+    if (part == 1) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) other[(d * 16 + r) * kWave] = acc[d][r];
+      other[(W - 2) * kWave] = left;
+      other[(W - 1) * kWave] = most;
+    }
+    __syncthreads();
+    if (part == 0) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[d][r] += other[(d * 16 + r) * kWave];
+      left += other[(W - 2) * kWave];
+      most = __builtin_elementwise_maximum(most, other[(W - 1) * kWave]);
+    }
+  }
   left = sum_across_halves(left);
-  if (q_ok && hh == 0) a.dvec[h * a.lse_stride + q_row] = D + left;
+  if (part == 0) {
+    store_rows<DH>(acc, a.scale, a.dq + q_row * a.dqs + h * DH, q_ok, hh);
+    if (q_ok && hh == 0) a.dvec[h * a.lse_stride + q_row] = D + left;
+  }
   // |dS| of the other launch: of this one, plus what D moves by, plus what the order of Dh products in dP can make (at most
   // Dh U sum|dO V| in either launch)
-  v_most = __builtin_bit_cast(float, wave_pick<true>((int)(__builtin_bit_cast(uint32_t, v_most) & 0x7fffffffu)));
-  if (lane == 0) s_most[0][wv] = v_most;
-  __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kBiasThreads / kWave; ++w) v_most = __builtin_elementwise_maximum(v_most, s_most[0][w]);
-  const float bound = q_ok ? most + fabsf(left) + l1 * v_most * 0x1p-16f : 0.f;
+  for (int w = 0; w < THREADS / kWave; ++w) v_most = __builtin_elementwise_maximum(v_most, s_most[0][w]);
+  const float bound = q_ok && part == 0 ? most + fabsf(left) + l1 * v_most * 0x1p-16f : 0.f;
   const int bits = wave_pick<true>((int)(__builtin_bit_cast(uint32_t, bound) & 0x7fffffffu));      // (a NaN above all)
-  if (lane == 0) s_most[1][wv] = __builtin_bit_cast(float, bits);
+  if (lane == 0) s_most[1][threadIdx.x >> 6] = __builtin_bit_cast(float, bits);
   __syncthreads();
   if (threadIdx.x == 0) {
     uint32_t all = 0;
 #pragma unroll
-    for (int w = 0; w < kBiasThreads / kWave; ++w) all = max(all, __builtin_bit_cast(uint32_t, s_most[1][w]));
+    for (int w = 0; w < 4; ++w) all = max(all, __builtin_bit_cast(uint32_t, s_most[1][w]));
     a.most[((long)h * a.B + blk.img) * a.nblk + blk.r0 / kBiasRows] = all;
   }
 }
@@ -777,7 +837,7 @@ __device__ __forceinline__ void write_partial(const unsigned long long* hist, co
   __syncthreads();
 }
 
-template <int DH, int NW>
+template <int DH, int SPLIT>
 struct DkdvTiles {
   static constexpr int RS = DH + 8;
   __attribute__((aligned(16))) __bf16 Q[2][kBiasBN * RS];
@@ -787,22 +847,24 @@ struct DkdvTiles {
   __attribute__((aligned(16))) float negD[2][kBiasBN];
   __attribute__((aligned(16))) int pos[2][kBiasBN];
   int range[2][2], far[2];
-  int own[NW][2];
-  uint32_t most[NW];
+  int own[4][2];
+  uint32_t most[4 * SPLIT];
   uint16_t row[kTableLds];
   KeyBlocks blocks;
 };
 
-template <int DH, int NW, bool WHOLE, int HIST>
-__global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<__bf16> a) {
-  constexpr int RS = DH + 8, KK = DH / 16, DB = DH / 32, BN = kBiasBN, THREADS = 64 * NW, ROWS = 32 * NW;
+// SPLIT 2: the waves come twice, the second four take the second half of every tile of 64 queries, and hand their sums to the
+// first at the end of a block.
+template <int DH, int SPLIT, bool WHOLE, int HIST>
+__global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dkdv_kernel(const BiasBwd<__bf16> a) {
+  constexpr int RS = DH + 8, KK = DH / 16, DB = DH / 32, BN = kBiasBN, THREADS = kBiasThreads * SPLIT, ROWS = kBiasRows;
   constexpr bool RANGES = !WHOLE || HIST == kHistSlices;      // the offsets of a tile lie where?
-  static_assert(NW >= 4, "the first four waves stage");
   extern __shared__ __attribute__((aligned(16))) unsigned long long hist[];       // [slice], then the window of biases
-  __shared__ DkdvTiles<DH, NW> l;
+  __shared__ DkdvTiles<DH, SPLIT> l;
   const int h = blockIdx.x % a.H, group = blockIdx.x / a.H;
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, l32 = lane & 31, hh = lane >> 5;
-  const bool stages = tid < kBiasThreads;
+  const int tid = threadIdx.x, lane = tid & 63, wv = (tid >> 6) & 3, l32 = lane & 31, hh = lane >> 5;
+  const int part = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;
+  const bool stages = part == 0;                              // (the first four waves)
   const long C = (long)a.H * DH;
   uint16_t* win = reinterpret_cast<uint16_t*>(hist + (HIST != kHistNone ? a.slice : 0));
   const float* lse_h = a.lse + h * a.lse_stride;
@@ -874,7 +936,7 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
       __syncthreads();                                        // every wave is past its last read of the tiles before
       if (RANGES) {
         const int lo = wave_pick<false>(own), hi = wave_pick<true>(own);
-        if (lane == 0) {
+        if (lane == 0 && part == 0) {
           l.own[wv][0] = lo;
           l.own[wv][1] = hi;
         }
@@ -888,9 +950,7 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
       __syncthreads();
       Range mine = {0, 0};
       if (RANGES) {
-        mine = {l.own[0][0], l.own[0][1]};
-#pragma unroll
-        for (int w = 1; w < NW; ++w) mine = {min(mine.lo, l.own[w][0]), max(mine.hi, l.own[w][1])};
+        mine = whole_range(l.own);
       }
       int base = -0x40000000;
       const int nt = (n + BN - 1) / BN;
@@ -918,7 +978,8 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
         if (wave_live && (pass == 0 || adds)) {
           const bool far = __builtin_amdgcn_readfirstlane(l.far[buf]) != 0;
 #pragma unroll
-          for (int sb = 0; sb < 2; ++sb) {
+          for (int half = 0; half < 2 / SPLIT; ++half) {
+            const int sb = SPLIT > 1 ? part : half;
             bf16x8 qf[KK], gf[KK];
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
@@ -1001,8 +1062,32 @@ __global__ void __launch_bounds__(64 * NW) attn_bias_dkdv_kernel(const BiasBwd<_
         }
       }
       if (pass == 0) {
-        store_rows<DH>(dka, a.scale, a.dk + k_row * a.dks + h * DH, k_ok, hh);
-        store_rows<DH>(dva, 1.0f, a.dv + k_row * a.dvs + h * DH, k_ok, hh);
+        if constexpr (SPLIT > 1) {
+          static_assert(4 * DB * 16 * kWave * sizeof(float) <= sizeof(l.Q) + sizeof(l.G), "one sum of four waves");
+          float* other = reinterpret_cast<float*>(&l.Q[0][0]) + wv * DB * 16 * kWave + lane;
+#pragma unroll
+          for (int which = 0; which < 2; ++which) {
+            floatx16(&sum)[DB] = which == 0 ? dka : dva;
+            __syncthreads();                                  // every wave is past its last read of the tiles, or of the sums before
+            if (part == 1) {
+#pragma unroll
+              for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) other[(d * 16 + r) * kWave] = sum[d][r];
+            }
+            __syncthreads();
+            if (part == 0) {
+#pragma unroll
+              for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum[d][r] += other[(d * 16 + r) * kWave];
+            }
+          }
+        }
+        if (part == 0) {
+          store_rows<DH>(dka, a.scale, a.dk + k_row * a.dks + h * DH, k_ok, hh);
+          store_rows<DH>(dva, 1.0f, a.dv + k_row * a.dvs + h * DH, k_ok, hh);
+        }
       }
     }
     if (HIST != kHistNone) write_partial<THREADS>(hist, scale, a.slice, from, a.m.offsets, a.partial + ((long)h * a.groups + group) * a.m.offsets);
@@ -1255,35 +1340,39 @@ static size_t window_bytes(int offsets) { return ((size_t)offsets + 7 + 7) / 8 *
   } while (0)
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// The dk / dv launch of the backward.  A workgroup of four waves, two of them a unit, where that leaves room for the whole map in
-// LDS (10 bytes an offset); else eight waves, one a unit, with as much of the histogram as fits.  As many workgroups a head as
-// are resident together, no more than there are blocks of keys, and no more than 256 MB of partial sums.
+// Forward and dq: eight waves a block (SPLIT) where a unit has one block at most and segments may have several tiles; a block is
+// then a chain of half the steps.  us forward, four | eight waves, 3 heads of 32, 56 x 56 map: one image of 1792 tokens
+// 33.6 | 26.0, 512 12.3 | 10.6; 16 images of 1792 63 | 77, of 512 13.8 | 13.9.
+static bool few_blocks(int nblk, int H, int B) { return nblk >= 4 && xcd_grid(nblk, H, B) <= 256; }
+
+// The dk / dv launch of the backward.  Two workgroups a unit where that leaves each room for the whole map in LDS (10 bytes an
+// offset); else one, with as much of the histogram as fits.  As many workgroups a head as are resident together, no more than
+// there are blocks of keys, and no more than 256 MB of partial sums.
 struct BiasPlan {
-  int nw, slice, groups, kblk;
+  int split, slice, groups, kblk;
   size_t lds;
 };
-static BiasPlan bias_plan(int H, int B, int n_max, int Dh, long offsets, int dtype, bool hist) {
+static BiasPlan bias_plan(int H, int B, int n_max, int Dh, long offsets, int dtype) {
   BiasPlan p = {};
-  const size_t window = window_bytes((int)(offsets <= kWholeMost ? offsets : kWindow)), most = 160 * 1024;
-  const size_t tiles4 = Dh == 32 ? sizeof(DkdvTiles<32, 4>) : sizeof(DkdvTiles<64, 4>);
-  const size_t tiles8 = Dh == 32 ? sizeof(DkdvTiles<32, 8>) : sizeof(DkdvTiles<64, 8>);
+  const bool whole = offsets <= kWholeMost;
+  const size_t window = window_bytes((int)(whole ? offsets : kWindow)), most = 160 * 1024;
+  const size_t tiles = Dh == 32 ? sizeof(DkdvTiles<32, 2>) : sizeof(DkdvTiles<64, 2>);
   const auto up64 = [](long n) { return (n + 63) & ~63L; };
   int a_unit = 2;
+  p.split = 1;
   if (dtype == SPA_F32) {
-    p.nw = 4;
     p.slice = (int)std::min<long>(up64(offsets), 4096);
     p.lds = (size_t)p.slice * 8;
-  } else if (!hist || tiles4 + window + up64(offsets) * 8 <= most / 2) {
-    p.nw = 4;
+  } else if (tiles + window + up64(offsets) * 8 <= most / 2) {
     p.slice = (int)up64(offsets);
     p.lds = window + (size_t)p.slice * 8;
   } else {
-    p.nw = offsets <= kWholeMost ? 8 : 4;                       // (eight with look-ups in memory: too few registers)
     a_unit = 1;
-    p.slice = (int)std::min<long>(up64(offsets), (long)(most - (p.nw == 8 ? tiles8 : tiles4) - window) / 8 / 64 * 64);
+    p.split = whole ? 2 : 1;                                    // (eight waves with look-ups in memory: too few registers)
+    p.slice = (int)std::min<long>(up64(offsets), (long)(most - tiles - window) / 8 / 64 * 64);
     p.lds = window + (size_t)p.slice * 8;
   }
-  p.kblk = (n_max + 32 * p.nw - 1) / (32 * p.nw);
+  p.kblk = (n_max + kBiasRows - 1) / kBiasRows;
   const long fit = std::max<long>(1, (256L << 20) / (4 * H * offsets));
   p.groups = (int)std::max<long>(1, std::min<long>(std::min<long>(256 * a_unit / H, (long)B * p.kblk), fit));
   return p;
@@ -1313,10 +1402,13 @@ extern "C" int spa_packed_attention_bias(const void* q, const void* k, const voi
     const BiasFwd args = {(const __bf16*)q, (const __bf16*)k, (const __bf16*)v, (long)q_row_stride, (long)k_row_stride, (long)v_row_stride,
                           cu_seqlens, m, H, B, nblk, scale, (__bf16*)out, lse, ls};
     const dim3 blocks(xcd_grid(nblk, H, B));
+    const bool split = few_blocks(nblk, H, B);
 #define SPA_BIAS(D)                                                                                                        \
   do {                                                                                                                     \
-    if (m.offsets <= kWholeMost) SPA_BIAS_LAUNCH((attn_bias_fwd_kernel<D, true>), blocks, kBiasThreads, window_bytes(m.offsets), args);  \
-    else SPA_BIAS_LAUNCH((attn_bias_fwd_kernel<D, false>), blocks, kBiasThreads, window_bytes(kWindow), args);                           \
+    const size_t window = window_bytes(m.offsets <= kWholeMost ? m.offsets : kWindow);                                     \
+    if (m.offsets > kWholeMost) SPA_BIAS_LAUNCH((attn_bias_fwd_kernel<D, false, 1>), blocks, kBiasThreads, window, args);  \
+    else if (split) SPA_BIAS_LAUNCH((attn_bias_fwd_kernel<D, true, 2>), blocks, 2 * kBiasThreads, window, args);           \
+    else SPA_BIAS_LAUNCH((attn_bias_fwd_kernel<D, true, 1>), blocks, kBiasThreads, window, args);                          \
   } while (0)
     if (Dh == 32) SPA_BIAS(32); else SPA_BIAS(64);
 #undef SPA_BIAS
@@ -1334,7 +1426,7 @@ extern "C" int spa_packed_attention_bias(const void* q, const void* k, const voi
 extern "C" size_t spa_attention_bias_bwd_workspace_bytes(int B, int max_seqlen, int H, int Dh, int grid_h, int grid_w, int dtype) {
   if (B < 1 || max_seqlen < 1 || H < 1 || grid_h < 1 || grid_w < 1 || (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1) > kMostOffsets) return 0;
   const long offsets = (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1);
-  const BiasPlan p = bias_plan(H, B, max_seqlen, Dh, offsets, dtype, true);
+  const BiasPlan p = bias_plan(H, B, max_seqlen, Dh, offsets, dtype);
   const size_t nblk = (max_seqlen + kBiasRows - 1) / kBiasRows;
   return up256((size_t)H * B * max_seqlen * 4) + up256((size_t)H * B * nblk * 4) + up256((size_t)H * p.groups * offsets * 4) +
          up256((size_t)H * offsets * 4);
@@ -1366,7 +1458,7 @@ extern "C" int spa_packed_attention_bias_bwd(const void* q, const void* k, const
   SPA_REQUIRE((reinterpret_cast<uintptr_t>(workspace) & 255u) == 0, SPA_ERR_INVALID_ARG, "%s: workspace not 256-byte aligned", fn);
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)Dh);
   const long ls = (long)B * max_seqlen;
-  const BiasPlan plan = bias_plan(H, B, max_seqlen, Dh, m.offsets, dtype, d_table != nullptr);
+  const BiasPlan plan = bias_plan(H, B, max_seqlen, Dh, m.offsets, dtype);
   const int nblk = (max_seqlen + kBiasRows - 1) / kBiasRows;
   SPA_REQUIRE(((long)H * B + 8) * nblk < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*H*blocks must be < 2^31", fn);
   char* ws = static_cast<char*>(workspace);
@@ -1386,19 +1478,22 @@ extern "C" int spa_packed_attention_bias_bwd(const void* q, const void* k, const
   {(const T*)q, (const T*)k, (const T*)v, (const T*)out, (const T*)dout, (long)q_row_stride, (long)k_row_stride, (long)v_row_stride, lse, \
    dvec, ls, cu_seqlens, m, H, B, nblk, scale, (T*)dq, (T*)dk, (T*)dv, (long)dq_row_stride, (long)dk_row_stride, (long)dv_row_stride,     \
    most, partial, plan.groups, plan.slice, plan.kblk}
-#define SPA_DKDV(D, NW, W, MODE)                                                                                             \
-  do {                                                                                                                       \
-    if (hist) SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<D, NW, W, MODE>), H * plan.groups, 64 * NW, plan.lds, args);            \
-    else SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<D, 4, W, kHistNone>), H * plan.groups, 256, window, args);                   \
-  } while (0)
+  const bool split = few_blocks(nblk, H, B);
+#define SPA_DKDV(D, SPLIT, W, MODE) \
+  SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<D, SPLIT, W, MODE>), H * plan.groups, SPLIT * kBiasThreads, hist ? plan.lds : window, args)
 #define SPA_BIAS16(D)                                                                                                        \
   do {                                                                                                                       \
-    if (whole) SPA_BIAS_LAUNCH((attn_bias_dq_kernel<D, true>), xcd_grid(nblk, H, B), kBiasThreads, window, args);            \
-    else SPA_BIAS_LAUNCH((attn_bias_dq_kernel<D, false>), xcd_grid(nblk, H, B), kBiasThreads, window, args);                 \
-    if (!whole) SPA_DKDV(D, 4, false, kHistSlices);                                                                          \
-    else if (plan.nw == 4) SPA_DKDV(D, 4, true, kHistWhole);                                                                 \
-    else if (plan.slice >= m.offsets) SPA_DKDV(D, 8, true, kHistWhole);                                                      \
-    else SPA_DKDV(D, 8, true, kHistSlices);                                                                                  \
+    const unsigned blocks = xcd_grid(nblk, H, B);                                                                            \
+    if (!whole) SPA_BIAS_LAUNCH((attn_bias_dq_kernel<D, false, 1>), blocks, kBiasThreads, window, args);                     \
+    else if (split) SPA_BIAS_LAUNCH((attn_bias_dq_kernel<D, true, 2>), blocks, 2 * kBiasThreads, window, args);              \
+    else SPA_BIAS_LAUNCH((attn_bias_dq_kernel<D, true, 1>), blocks, kBiasThreads, window, args);                             \
+    if (!whole && hist) SPA_DKDV(D, 1, false, kHistSlices);                                                                  \
+    else if (!whole) SPA_DKDV(D, 1, false, kHistNone);                                                                       \
+    else if (!hist && plan.split == 2) SPA_DKDV(D, 2, true, kHistNone);                                                      \
+    else if (!hist) SPA_DKDV(D, 1, true, kHistNone);                                                                         \
+    else if (plan.slice < m.offsets) SPA_DKDV(D, 2, true, kHistSlices);                                                      \
+    else if (plan.split == 2) SPA_DKDV(D, 2, true, kHistWhole);                                                              \
+    else SPA_DKDV(D, 1, true, kHistWhole);                                                                                   \
   } while (0)
 #define SPA_BIAS32(D)                                                                                                        \
   do {                                                                                                                       \

@@ -327,6 +327,14 @@ def test_many_segments(spa, B, dtype):
     c.check(c.run(spa))
 
 
+@pytest.mark.parametrize("Dh", [32, 64])
+@pytest.mark.parametrize("lens", [[700], [513, 64], [65, 1], [1024]])
+def test_few_long_segments(spa, lens, Dh):
+    """Few blocks of queries: the waves of a block share its keys."""
+    c = Case(lens, (33, 34), 2, Dh, "bf16", seed=18)
+    c.check(c.run(spa))
+
+
 def test_large_and_sparse_maps(spa):
     """Few tokens far apart on a map of many offsets, and a long sequence without a second axis."""
     for grid, lens in (((300, 300), [150, 40]), ((1, 20000), [400, 90])):
