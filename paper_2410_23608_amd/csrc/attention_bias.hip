@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_fwd_kernel(con
   float m = -INFINITY, sum = 0.f;
   walk_keys<T, DH, WIN, SPLIT>(
       l, win, blk.seg, h, wave_live, a.k, a.ks, a.v, a.vs, a.m, a.cu, qi, [&] { qf = O::row(a.q + q_row * a.qs + h * DH, hh); },
-      [](const auto&) {},
+      [] {}, [](const auto&) {},
       [&](const T* K, const T* V, const int* pos, int left, int own, int zero, bool in_window, auto whole) {
         floatx16 s[2];
 #pragma unroll

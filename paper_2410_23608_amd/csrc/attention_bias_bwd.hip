@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(cons
   const int part = SPLIT > 1 ? threadIdx.x >> 8 : 0, qi = blk.r0 + wv * 32 + l32;
   const bool wave_live = blk.r0 + wv * 32 < n, q_ok = qi < n;
   const long C = (long)a.H * DH, q_row = blk.seg.row0 + min(qi, n - 1);
-  typename O::Row qf, gf;
+  typename O::Row qf, gf, of;
   float D = 0.f, l1 = 0.f;                                    // <dO, out> and sum |dO| of the lane's row
   floatx16 acc[DB], negD;
 #pragma unroll
@@ -78,7 +78,10 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(cons
       [&] {
         qf = O::row(a.q + q_row * a.qs + h * DH, hh);
         gf = O::row(a.dout + q_row * C + h * DH, hh);
-        O::sums(gf, O::row(a.out + q_row * C + h * DH, hh), D, l1);
+        of = O::row(a.out + q_row * C + h * DH, hh);
+      },
+      [&] {
+        O::sums(gf, of, D, l1);
         D = sum_across_halves(D);
         l1 = sum_across_halves(l1);
 #pragma unroll
@@ -166,7 +169,7 @@ enum HistMode { kHistNone, kHistWhole, kHistSlices };
 // The head's blocks of keys in the order in which the workgroups take them: up to 256 segments by length, longest first,
 // blocks that exist numbered through; more segments in index order, with blocks of the longest possible one each.
 struct KeyBlocks {
-  int img[kLptMaxB], len[kLptMaxB], upto[kLptMaxB];           // by rank; blocks up to and including the rank's
+  int from[kLptMaxB], len[kLptMaxB], upto[kLptMaxB];          // by rank: first row, rows, blocks up to and including the rank's
   int all;
 };
 template <int THREADS>
@@ -181,8 +184,12 @@ __device__ __forceinline__ void list_key_blocks(KeyBlocks& k, const int32_t* cu,
   for (int b = threadIdx.x; b < B; b += THREADS) {
     const int mine = k.upto[b];
     int rank = 0;
-    for (int i = 0; i < B; ++i) rank += k.upto[i] > mine || (k.upto[i] == mine && i < b);
-    k.img[rank] = b;
+#pragma unroll 8
+    for (int i = 0; i < B; ++i) {
+      const int other = k.upto[i];
+      rank += (other > mine) | ((other == mine) & (i < b));
+    }
+    k.from[rank] = cu[b];
     k.len[rank] = mine;
   }
   __syncthreads();
@@ -202,23 +209,18 @@ struct KeyBlock {
   int n, k0;
 };
 __device__ __forceinline__ KeyBlock key_block(const KeyBlocks& k, const int32_t* cu, int B, int rows, int kblk, int i) {
-  int img, at;
   if (B > kLptMaxB) {
-    img = i / kblk;
-    at = i % kblk;
-  } else {
-    int lo = 0, hi = B - 1;                                   // the first rank with upto > i
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (k.upto[mid] > i) hi = mid;
-      else lo = mid + 1;
-    }
-    img = k.img[lo];
-    at = i - (lo > 0 ? k.upto[lo - 1] : 0);
+    const int img = i / kblk, from = cu[img];
+    return {from, cu[img + 1] - from, i % kblk * rows};
   }
-  img = __builtin_amdgcn_readfirstlane(img);
-  const int from = cu[img];
-  return {from, cu[img + 1] - from, __builtin_amdgcn_readfirstlane(at) * rows};
+  int lo = 0, hi = B - 1;                                     // the first rank with upto > i
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (k.upto[mid] > i) hi = mid;
+    else lo = mid + 1;
+  }
+  const int at = i - (lo > 0 ? k.upto[lo - 1] : 0);
+  return {__builtin_amdgcn_readfirstlane(k.from[lo]), __builtin_amdgcn_readfirstlane(k.len[lo]), __builtin_amdgcn_readfirstlane(at) * rows};
 }
 
 // The scale of a head's integers: 2^e is above twice what the dq launch found (its blocks that exist); `unit` NaN: some dS of
@@ -232,8 +234,9 @@ template <int THREADS>
 __device__ __forceinline__ DsScale ds_scale(const uint32_t* most_h, const int32_t* cu, int B, int nblk, uint32_t* s_most) {
   uint32_t most = 0;
   for (int i = threadIdx.x; i < B * nblk; i += THREADS) {
-    const int img = i / nblk;
-    if ((i - img * nblk) * kBiasRows < cu[img + 1] - cu[img]) most = max(most, most_h[i]);
+    const int img = i / nblk, n = cu[img + 1] - cu[img];
+    const uint32_t its = most_h[i];
+    if ((i - img * nblk) * kBiasRows < n) most = max(most, its);
   }
   most = (uint32_t)wave_pick<true>((int)most);
   if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = most;
@@ -265,7 +268,7 @@ struct KeyTiles {
   int range[2][1][2], far[2];
   int own[4][2];
   uint32_t most[4 * SPLIT];
-  T row[kTableLds];
+  typename WindowFill<T, kBiasThreads>::Raw row[kTableLds];
   KeyBlocks blocks;
 };
 
@@ -287,11 +290,13 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dkdv_kernel(co
   const float* lse_h = a.lse + h * a.lse_stride;
   const float* d_h = a.dvec + h * a.lse_stride;
 
+  WindowFill<T, THREADS> fill(a.m, h);
+  if (WIN == kWinWhole) fill.start(0, a.m.offsets);
   list_key_blocks<THREADS>(l.blocks, a.cu, a.B, ROWS, a.nblk);
   DsScale scale = {0, 0., 0.f};
   if (HIST != kHistNone) scale = ds_scale<THREADS>(a.most + (long)h * a.B * a.nblk, a.cu, a.B, a.nblk, l.most);
   int zero = 0;
-  if (WIN == kWinWhole) zero = fill_window<T, WIN, THREADS>(a.m, h, 0, win, l.row);
+  if (WIN == kWinWhole) zero = fill.finish(win, l.row);
 
   const int passes = HIST == kHistSlices ? (a.m.offsets + a.slice - 1) / a.slice : 1;
   for (int pass = 0; pass < passes; ++pass) {
@@ -360,7 +365,8 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dkdv_kernel(co
             in_window = hi - lo < kWindow - 3;
             if (in_window && (lo < base || hi >= base + kWindow)) {   // the queries' positions grow, so do the offsets
               base = lo & ~3;
-              zero = fill_window<T, WIN, THREADS>(a.m, h, base, win, l.row);
+              fill.start(base, min(kWindow, a.m.offsets - base));
+              zero = fill.finish(win, l.row);
               __syncthreads();
             }
           }

@@ -241,111 +241,104 @@ constexpr int kWholeBytes = 65536, kWindow = 8192;
 
 constexpr int kTableLds = 1024;                // a table row of up to so many entries is brought to LDS where a map picks from it
 
-// fp32 entries [base, base + n)
-template <int THREADS>
-__device__ __forceinline__ void fill_f32(const BiasMap& m, int h, int base, int n, float* win, float* row_lds) {
-  const float* row = static_cast<const float*>(m.table) + (long)h * m.nb;
-  const int tid = threadIdx.x;
-  constexpr int U = 8;
-  if (m.buckets == nullptr) {
-    for (int i0 = tid; i0 < n; i0 += U * THREADS) {
-      float v[U];
+// The entries of offsets [base, base + n) on their way to the window, 16 bytes of the map (four entries; base must be a multiple of 4 then) or, without
+// a map, of the table's row a time.  start() asks for a thread's first pieces and, of a short row that a map picks from, its part of the row;
+// nothing waits for them before finish(), which all threads call; a barrier follows before the window is read.
+template <typename T, int THREADS>
+struct WindowFill {
+  using Raw = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
+  static constexpr int VE = 16 / sizeof(T), U = 4, PART = kTableLds / THREADS;
+  const BiasMap& m;
+  const Raw* row;
+  const int tid;
+  int base, n, shift, first, pieces;         // shift: where the row starts in its first 16 bytes, first: entries in front of the next
+  intx4 v[U];
+  Raw part[PART];
+  uintx2 ends;                                // what is in front of the first whole piece and behind the last, of the thread
+  __device__ __forceinline__ WindowFill(const BiasMap& m_, int h)
+      : m(m_), row(static_cast<const Raw*>(m_.table) + (long)h * m_.nb), tid(threadIdx.x), base(0), n(0), shift(0), first(0), pieces(0) {}
+  __device__ __forceinline__ void load(int p0) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = row[base + min(i0 + u * THREADS, n - 1)];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (i0 + u * THREADS < n) win[i0 + u * THREADS] = v[u];
+    for (int u = 0; u < U; ++u) {
+      const int p = min(p0 + tid + u * THREADS, pieces - 1);
+      v[u] = m.buckets == nullptr ? *reinterpret_cast<const intx4*>(row + base + first + VE * p)
+                                  : *reinterpret_cast<const intx4*>(m.buckets + base + 4 * p);
     }
-    return;
   }
-  auto fill = [&](auto from) {
-    for (int i0 = tid; i0 < n; i0 += U * THREADS) {
-      int b[U];
-      float v[U];
+  __device__ __forceinline__ int behind() const { return first + (m.buckets == nullptr ? VE : 4) * pieces + tid; }      // the last whole piece
+  __device__ __forceinline__ void start(int base_, int n_) {
+    base = base_;
+    n = n_;
+    if (m.buckets == nullptr) {
+      shift = (int)(reinterpret_cast<uintptr_t>(row + base) & 15) / (int)sizeof(T);
+      first = (VE - shift) & (VE - 1);
+      pieces = n > first ? (n - first) / VE : 0;
+      ends[0] = row[base + min(tid, n - 1)];
+      ends[1] = row[base + min(behind(), n - 1)];
+    } else {
+      pieces = n / 4;
+      ends[1] = (uint32_t)m.buckets[base + min(behind(), n - 1)];
+      if (m.nb <= kTableLds) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) b[u] = m.buckets[base + min(i0 + u * THREADS, n - 1)];
-#pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = from[min((uint32_t)b[u], (uint32_t)m.nb - 1)];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (i0 + u * THREADS < n) win[i0 + u * THREADS] = (uint32_t)b[u] < (uint32_t)m.nb ? v[u] : 0.f;
+        for (int i = 0; i < PART; ++i) part[i] = row[min(tid + i * THREADS, m.nb - 1)];
+      }
     }
-  };
-  if (m.nb <= kTableLds) {
-    for (int i = tid; i < m.nb; i += THREADS) row_lds[i] = row[i];
-    __syncthreads();
-    fill(row_lds);
-  } else {
-    fill(row);
+    if (pieces > 0) load(0);
   }
-}
-// bf16 entries [base, base + n) to win[shift ..]; returns shift.  Without a bucket map the table's row is copied as it lies in memory, 16
-// bytes at a time (shift: where it starts in its first 16); through one, the map comes in 16-byte pieces where `base` allows.
-template <int THREADS>
-__device__ __forceinline__ int fill_bf16(const BiasMap& m, int h, int base, int n, uint16_t* win, uint16_t* row_lds) {
-  const uint16_t* row = static_cast<const uint16_t*>(m.table) + (long)h * m.nb;
-  const int tid = threadIdx.x;
-  if (m.buckets == nullptr) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(row + base);
-    const int shift = (int)(at & 15) / 2, first = (8 - shift) & 7;              // entries in front of the first whole piece
-    const int whole = n > first ? (n - first) / 8 : 0;
-    constexpr int U = 8;
-    for (int i0 = tid; i0 < whole; i0 += U * THREADS) {
-      uintx4 v[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        v[u] = *reinterpret_cast<const uintx4*>(row + base + first + 8 * min(i0 + u * THREADS, whole - 1));
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (i0 + u * THREADS < whole) *reinterpret_cast<uintx4*>(win + shift + first + 8 * (i0 + u * THREADS)) = v[u];
-    }
-    if (tid < min(first, n)) win[shift + tid] = row[base + tid];
-    const int rest = first + 8 * whole + tid;                                   // behind the last whole piece
-    if (tid < 8 && rest < n) win[shift + rest] = row[base + rest];
-    return shift;
-  }
-  const int quads = (base & 3) == 0 ? n / 4 : 0;
-  auto fill = [&](auto from) {                                                  // (all of a thread's look-ups in flight)
-    auto entry = [&](int b) -> uint32_t {
-      const uint32_t v = from[min((uint32_t)b, (uint32_t)m.nb - 1)];
-      return (uint32_t)b < (uint32_t)m.nb ? v : 0u;
+  // the LDS address that offset 0 would have
+  __device__ __forceinline__ int finish(void* window, Raw* row_lds) {
+    Raw* win = static_cast<Raw*>(window);
+    auto each = [&](auto put) {
+      for (int p0 = 0; p0 < pieces; p0 += U * THREADS) {
+        if (p0 > 0) load(p0);
+        put(p0);
+      }
     };
-    constexpr int U = 4;
-    for (int i0 = tid; i0 < quads; i0 += U * THREADS) {
-      intx4 b[U];
+    if (m.buckets == nullptr) {
+      each([&](int p0) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) b[u] = *reinterpret_cast<const intx4*>(m.buckets + base + 4 * min(i0 + u * THREADS, quads - 1));
-      uint32_t v[U][4];
+        for (int u = 0; u < U; ++u) {
+          const int p = p0 + tid + u * THREADS;
+          if (p < pieces) *reinterpret_cast<intx4*>(win + shift + first + VE * p) = v[u];
+        }
+      });
+      if (tid < min(first, n)) win[shift + tid] = (Raw)ends[0];
+      if (tid < VE && behind() < n) win[shift + behind()] = (Raw)ends[1];
+    } else {
+      auto pick = [&](const Raw* from) {                      // (all of a thread's look-ups in flight)
+        auto entry = [&](int b) -> uint32_t {
+          const uint32_t e = from[min((uint32_t)b, (uint32_t)m.nb - 1)];
+          return (uint32_t)b < (uint32_t)m.nb ? e : 0u;
+        };
+        each([&](int p0) {
+          uint32_t e[U][4];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+          for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[u][i] = entry(b[u][i]);
+            for (int i = 0; i < 4; ++i) e[u][i] = entry(v[u][i]);
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (i0 + u * THREADS < quads) *reinterpret_cast<uintx2*>(win + 4 * (i0 + u * THREADS)) = uintx2{v[u][0] | v[u][1] << 16, v[u][2] | v[u][3] << 16};
+          for (int u = 0; u < U; ++u) {
+            const int p = p0 + tid + u * THREADS;
+            if (p >= pieces) continue;
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<uintx4*>(win + 4 * p) = uintx4{e[u][0], e[u][1], e[u][2], e[u][3]};
+            else *reinterpret_cast<uintx2*>(win + 4 * p) = uintx2{e[u][0] | e[u][1] << 16, e[u][2] | e[u][3] << 16};
+          }
+        });
+        if (tid < 4 && behind() < n) win[behind()] = (Raw)entry((int)ends[1]);
+      };
+      if (m.nb <= kTableLds) {
+#pragma unroll
+        for (int i = 0; i < PART; ++i)
+          if (tid + i * THREADS < m.nb) row_lds[tid + i * THREADS] = part[i];
+        __syncthreads();
+        pick(row_lds);
+      } else {
+        pick(row);
+      }
     }
-    for (int i = 4 * quads + tid; i < n; i += THREADS) win[i] = (uint16_t)entry(m.buckets[base + i]);
-  };
-  if (m.nb <= kTableLds) {
-    for (int i = tid; i < m.nb; i += THREADS) row_lds[i] = row[i];
-    __syncthreads();
-    fill(row_lds);
-  } else {
-    fill(row);
+    return lds_address(win) + (int)sizeof(T) * (shift - base);
   }
-  return 0;
-}
-
-// The offsets from `base` on, as many as the mode holds; returns the LDS address that offset 0 would have.  All threads call it; a
-// barrier follows before the window is read.
-template <typename T, int WIN, int THREADS>
-__device__ __forceinline__ int fill_window(const BiasMap& m, int h, int base, void* win, T* row_lds) {
-  const int n = WIN == kWinWhole ? m.offsets : min(kWindow, m.offsets - base);
-  int shift = 0;
-  if constexpr (sizeof(T) == 4) fill_f32<THREADS>(m, h, base, n, static_cast<float*>(win), row_lds);
-  else shift = fill_bf16<THREADS>(m, h, base, n, static_cast<uint16_t*>(win), reinterpret_cast<uint16_t*>(row_lds));
-  return lds_address(win) + (int)sizeof(T) * (shift - base);
-}
+};
 
 // Scores of a lane's row against the 16 of a 32-row block that it holds, biases included.  pos: positions of the block's rows
 // in bytes of the window, own: position of the lane's row, one of the two with the centre; SIGN: 1 if the offset is own - pos,
@@ -427,16 +420,17 @@ struct QueryTiles {
   __attribute__((aligned(16))) T V[2][STEP * RS];
   __attribute__((aligned(16))) int pos[2][STEP];
   int range[2][SPLIT][2], own[4 * SPLIT][2];
-  T row[kTableLds];
+  typename WindowFill<T, kBiasThreads>::Raw row[kTableLds];
   int s_live[sizeof(LiveTile) / sizeof(int)];
 };
 
-// The walk of such a workgroup over the keys of its segment, SPLIT tiles of 64 a step: staging, positions, the window.  work(K, V, pos,
+// The walk of such a workgroup over the keys of its segment, SPLIT tiles of 64 a step: staging, positions, the window.  asked(): the workgroup's own loads;
+// arrived(): what is made of them in front of the first tile; work(K, V, pos,
 // rows left in the wave's tile, own position, window, in_window, whole): the wave's tile; whole: all of its 64 keys exist.
-template <typename T, int DH, int WIN, int SPLIT, class Before, class Staged, class Work>
+template <typename T, int DH, int WIN, int SPLIT, class Asked, class Arrived, class Staged, class Work>
 __device__ __forceinline__ void walk_keys(QueryTiles<T, DH, SPLIT>& l, void* win, const Segment& seg, int h, bool wave_live, const T* k, long ks, const T* v,
-                                          long vs, const BiasMap& m, const int32_t* cu, int row, Before before, Staged staged,
-                                          Work work) {
+                                          long vs, const BiasMap& m, const int32_t* cu, int row, Asked asked, Arrived arrived,
+                                          Staged staged, Work work) {
   constexpr int RS = Ops<T, DH>::RS, THREADS = kBiasThreads * SPLIT, STEP = kBiasBN * SPLIT, WB = sizeof(T);
   const int tid = threadIdx.x, n = seg.nk, last = n - 1, part = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;
   RowPair<T, DH, THREADS, STEP> st(tid, k + h * DH, ks, v + h * DH, vs, seg.row0, last);
@@ -456,12 +450,16 @@ __device__ __forceinline__ void walk_keys(QueryTiles<T, DH, SPLIT>& l, void* win
       if (WIN == kWinMoving) put_range(l.range[buf][(tid >> 6) & (SPLIT - 1)], p);
     }
   };
+  WindowFill<T, THREADS> fill(m, h);
+  if (WIN == kWinWhole) fill.start(0, m.offsets);             // (what the longer chains of loads begin with, first)
+  const int own_token = tokens.load(min(row, last));
   load(0);
-  before();
-  const int own = tokens.position(m, min(row, last)) + m.centre;
+  asked();
+  const int own = tokens.position(m, own_token, min(row, last)) + m.centre;
   int zero = 0;
-  if (WIN == kWinWhole) zero = fill_window<T, WIN, THREADS>(m, h, 0, win, l.row);
+  if (WIN == kWinWhole) zero = fill.finish(win, l.row);
   else put_range(l.own[tid >> 6], own);
+  arrived();
   store(0, std::true_type{});
   __syncthreads();
   const Range mine = WIN == kWinMoving ? whole_range(l.own) : Range{0, 0};
@@ -477,7 +475,8 @@ __device__ __forceinline__ void walk_keys(QueryTiles<T, DH, SPLIT>& l, void* win
       in_window = hi - lo < kWindow - 3;
       if (in_window && (lo < base || hi >= base + kWindow)) {  // the keys' positions grow, so the next offsets are lower
         base = max(hi - kWindow + 4, 0) & ~3;                 // (16-byte pieces of the map)
-        zero = fill_window<T, WIN, THREADS>(m, h, base, win, l.row);
+        fill.start(base, min(kWindow, m.offsets - base));
+        zero = fill.finish(win, l.row);
         __syncthreads();
       }
     }
