@@ -1,0 +1,206 @@
+"""The operators of a block together, forward and backward, as a program runs them: gate and selection, norm and pack, projections,
+attention with a position bias, projection, norm, gate and residual.
+
+Against the same block in 64 bits, by the relative error of a tensor in the Frobenius norm.  On the longest way twelve steps
+store a tensor, each rounded by at most half a step (bf16 2^-8 of a value; fp32, sums of up to 192 terms among them, 80 x 2^-24 of the
+magnitudes), and a step passes a relative error on at most doubled: 24 x 2^-8 = 0.094 in bf16, and 24 x 80 x 2^-24 = 1.2e-4 in fp32,
+four times that where a sum's magnitudes exceed its value: 4.6e-4."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+TD = {"bf16": torch.bfloat16, "f32": torch.float32}
+TOL = {"bf16": 0.094, "f32": 4.6e-4}
+EPS, BIAS, LS = 1e-6, 0.05, 0.01
+
+
+@pytest.fixture(scope="module")
+def spa():
+    from paper_2410_23608_amd import spa as mod
+    return mod
+
+
+class Block:
+    """Buffers and prepared launches (bound to the stream that is current then)."""
+
+    def __init__(self, spa, B, grid, C, H, dtype, kind, log_buckets=False, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        gh, gw = grid
+        N, td = gh * gw, TD[dtype]
+        self.B, self.grid, self.N, self.C, self.H, self.rms, cap = B, grid, N, C, H, kind == "rms", B * N
+        cuda = lambda t: t.to(td).cuda()
+        rnd = lambda *s: torch.randn(*s, generator=g)
+        self.buckets, nb = None, (2 * gh - 1) * (2 * gw - 1)
+        if log_buckets:
+            self.buckets, nb = spa.relative_position_buckets(gh, gw, 2, 3)
+            self.buckets = self.buckets.cuda()
+        self.x, self.dy = cuda(rnd(B, N, C)), cuda(rnd(B, N, C))
+        self.w = cuda(rnd(C) / math.sqrt(C))
+        self.labels = (torch.rand(B, N, generator=g) < 0.4).to(torch.uint8).cuda()
+        self.g1, self.b1, self.g2, self.b2 = cuda(1 + 0.2 * rnd(C)), cuda(0.2 * rnd(C)), cuda(1 + 0.2 * rnd(C)), cuda(0.2 * rnd(C))
+        self.scale, self.table = cuda(0.5 + 0.2 * rnd(C)), cuda(rnd(H, nb))
+        self.W1, self.c1, self.W2, self.c2 = cuda(rnd(3 * C, C) / math.sqrt(C)), cuda(0.1 * rnd(3 * C)), cuda(rnd(C, C) / math.sqrt(C)), cuda(0.1 * rnd(C))
+        new = lambda *s, t=td: torch.zeros(*s, dtype=t, device="cuda")
+        f, i = torch.float32, torch.int32
+        self.scores, mask, counts = new(B, N, t=f), new(B, N, t=torch.uint8), new(B, t=i)
+        self.cu, self.gidx, self.inv, self.total = new(B + 1, t=i), new(cap, t=i), new(cap, t=i), new(1, t=i)
+        self.packed, self.qkv, self.out, self.z, self.y = new(cap, C), new(cap, 3 * C), new(cap, C), new(cap, C), new(B, N, C)
+        st1, st2, lse = new(2, cap, t=f), new(2, cap, t=f), new(H, cap, t=f)
+        self.dz, self.dout, self.dqkv, self.dpacked, self.dx = new(cap, C), new(cap, C), new(cap, 3 * C), new(cap, C), new(B, N, C)
+        self.d_scores, self.d_table = new(B, N, t=f), new(H, nb, t=f)
+        self.dg1, self.db1, self.dg2, self.db2, self.dscale, self.dw = (new(C, t=f) for _ in range(6))
+        self.dW1, self.dc1, self.dW2, self.dc2 = new(3 * C, C, t=f), new(3 * C, t=f), new(C, C, t=f), new(C, t=f)
+        self.loss, self.dbias = new(1, t=f), new(1, t=f)
+        kd = spa.SPA_NORM_RMS if self.rms else spa.SPA_NORM_LAYER
+        code = spa.SPA_F32 if dtype == "f32" else spa.SPA_BF16
+        ws = [torch.empty(max(n, 16), dtype=torch.uint8, device="cuda") for n in (
+            spa.spa_norm_bwd_workspace_bytes(cap, C, code), spa.spa_linear_bwd_weight_workspace_bytes(cap, C, 3 * C, dtype),
+            spa.spa_attention_bias_bwd_workspace_bytes(B, N, H, C // H, gh, gw, code), spa.spa_gate_bwd_workspace_bytes(B, N, C, code))]
+        q, k, v = (self.qkv[:, j * C:(j + 1) * C] for j in range(3))
+        dq, dk, dv = (self.dqkv[:, j * C:(j + 1) * C] for j in range(3))
+        at = dict(prepare=True)
+        bias = (self.cu, self.gidx, self.table, self.buckets, grid, B, N, H, C // H)
+        self.forward = [
+            spa.spa_gate_select(self.x, self.w, BIAS, None, 0.5, self.scores, mask, counts, **at),
+            spa.spa_pack(None, mask, counts, None, 0, None, self.cu, self.gidx, self.inv, self.total, **at),
+            spa.spa_norm_packed(self.x, self.gidx, self.total, self.g1, self.b1, kd, EPS, self.packed, st1, **at),
+            spa.spa_linear_packed(self.packed, None, None, self.total, self.W1, self.c1, self.qkv, **at),
+            spa.spa_packed_attention_bias(q, k, v, *bias, self.out, lse, **at),
+            spa.spa_linear_packed(self.out, None, None, self.total, self.W2, self.c2, self.z, **at),
+            spa.spa_norm_residual_unpack(self.z, self.inv, self.x, self.g2, self.b2, self.scale, self.scores, kd, EPS, self.y, st2, **at),
+        ]
+        self.backward = [
+            spa.spa_norm_residual_unpack_bwd(self.dy, self.z, self.gidx, self.inv, self.total, self.g2, self.b2, self.scale, self.scores, kd,
+                                             st2, self.dz, self.d_scores, self.dg2, self.db2, self.dscale, ws[0], **at),
+            spa.spa_linear_packed_bwd_input(self.dz, None, self.total, self.W2, cap, None, None, self.dout, **at),
+            spa.spa_linear_packed_bwd_weight(self.dz, None, self.out, None, None, self.total, cap, self.dW2, self.dc2, ws[1], **at),
+            spa.spa_packed_attention_bias_bwd(q, k, v, self.out, self.dout, lse, *bias, dq, dk, dv, self.d_table, ws[2], **at),
+            spa.spa_linear_packed_bwd_input(self.dqkv, None, self.total, self.W1, cap, None, None, self.dpacked, **at),
+            spa.spa_linear_packed_bwd_weight(self.dqkv, None, self.packed, None, None, self.total, cap, self.dW1, self.dc1, ws[1], **at),
+            spa.spa_norm_packed_bwd(self.dpacked, self.x, self.inv, self.total, self.g1, kd, st1, self.dy, self.dx, self.dg1, self.db1, ws[0], **at),
+            spa.spa_gate_bwd_scores(self.x, self.w, BIAS, self.scores, None, self.labels, self.d_scores, self.dx, LS, self.loss, self.dx,
+                                    self.dw, self.dbias, ws[3], **at),
+        ]
+
+    def run(self):
+        for launch in self.forward + self.backward:
+            launch()
+
+    RESULTS = ("y", "dx", "dw", "dbias", "loss", "dg1", "db1", "dg2", "db2", "dscale", "d_table", "dW1", "dc1", "dW2", "dc2")
+
+    def results(self):
+        return [getattr(self, n).clone() for n in self.RESULTS]
+
+    def oracle(self):
+        """The block in 64 bits on the CPU, over the rows that were selected, with its gradients."""
+        leaf = {n: getattr(self, n).detach().cpu().double().requires_grad_()
+                for n in ("x", "w", "g1", "b1", "g2", "b2", "scale", "table", "W1", "c1", "W2", "c2")}
+        p = type("P", (), leaf)
+        bias = torch.tensor(BIAS, dtype=torch.float64, requires_grad=True)
+        B, N, C, H, (gh, gw) = self.B, self.N, self.C, self.H, self.grid
+        norm = lambda t: (lambda d: d / torch.sqrt((d * d).mean(1, keepdim=True) + EPS))(t if self.rms else t - t.mean(1, keepdim=True))
+        s = p.x.reshape(-1, C) @ p.w + bias
+        s.retain_grad()
+        cu = self.cu.cpu().tolist()
+        sel = self.gidx.cpu()[:cu[-1]].long()
+        qkv = (norm(p.x.reshape(-1, C)[sel]) * p.g1 + p.b1) @ p.W1.t() + p.c1
+        bmap = torch.arange((2 * gh - 1) * (2 * gw - 1)) if self.buckets is None else self.buckets.cpu().long()
+        outs = []
+        for b in range(B):
+            rows = slice(cu[b], cu[b + 1])
+            q, k, v = (qkv[rows, j * C:(j + 1) * C].view(-1, H, C // H).transpose(0, 1) for j in range(3))
+            n = sel[rows] % N
+            pos = n // gw * (2 * gw - 1) + n % gw
+            off = pos[:, None] - pos[None] + (gh - 1) * (2 * gw - 1) + gw - 1
+            S = q @ k.transpose(1, 2) / math.sqrt(C // H) + p.table[:, bmap[off]]
+            outs.append((torch.softmax(S, -1) @ v).transpose(0, 1).reshape(-1, C))
+        z = torch.cat(outs) @ p.W2.t() + p.c2
+        add = torch.sigmoid(s[sel])[:, None] * p.scale * (norm(z) * p.g2 + p.b2)
+        y = p.x.reshape(-1, C).index_add(0, sel, add)
+        lab = self.labels.cpu().double().view(-1)
+        loss = LS * torch.nn.functional.binary_cross_entropy_with_logits(s, lab, reduction="sum")
+        ((y * self.dy.cpu().double().view(-1, C)).sum() + loss).backward()
+        g = {n: t.grad for n, t in leaf.items()}
+        return {"y": y.detach(), "loss": loss.detach(), "dbias": bias.grad, "dx": g["x"], "dw": g["w"], "dg1": g["g1"], "db1": g["b1"],
+                "dg2": g["g2"], "db2": g["b2"], "dscale": g["scale"], "d_table": g["table"], "dW1": g["W1"], "dc1": g["c1"], "dW2": g["W2"],
+                "dc2": g["c2"]}, float(s.grad.abs().sum())
+
+
+CASES = [(2, (5, 7), 64, 2, "f32", "layer", False), (3, (9, 4), 128, 2, "f32", "rms", True), (2, (14, 14), 192, 6, "bf16", "layer", False),
+         (1, (3, 5), 64, 1, "bf16", "rms", True)]
+
+
+@pytest.mark.parametrize("B,grid,C,H,dtype,kind,log_buckets", CASES)
+def test_block_equals_formulas(spa, B, grid, C, H, dtype, kind, log_buckets):
+    blk = Block(spa, B, grid, C, H, dtype, kind, log_buckets)
+    blk.run()
+    want, ds = blk.oracle()
+    assert 0 < int(blk.total) < B * blk.N
+    for name in Block.RESULTS:
+        got, ref = getattr(blk, name).cpu().double().view(-1), want[name].reshape(-1)
+        size = ds if name == "dbias" else float(ref.norm())       # (a single sum over the tokens: by its terms)
+        off = float((got - ref).norm()) / size
+        print(name, f"{off:.2e}", flush=True)
+        assert off <= TOL[dtype], name
+    first = blk.results()                                         # and the same bits in every run
+    blk.run()
+    for name, a, b in zip(Block.RESULTS, first, blk.results()):
+        assert torch.equal(a, b), name
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_block_graph_replays_equal_eager(spa, dtype):
+    make = lambda seed: Block(spa, 3, (8, 9), 128, 4, dtype, "layer", dtype == "bf16", seed)
+    side = torch.cuda.Stream()
+    others = [make(s) for s in (1, 2)]
+    for o in others:
+        o.run()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        blk = make(1)
+        blk.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        blk.run()
+    inputs = ("x", "dy", "w", "labels", "g1", "b1", "g2", "b2", "scale", "table", "W1", "c1", "W2", "c2")
+    for rep in range(6):
+        o = others[rep % 2]
+        for n in inputs:
+            getattr(blk, n).copy_(getattr(o, n))
+        for n in ("y", "dx", "d_table", "dg1", "dqkv"):
+            getattr(blk, n).fill_(float("nan"))
+        o.run()                                                   # eager work between the replays
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, a, b in zip(Block.RESULTS, blk.results(), o.results()):
+            assert torch.equal(a, b), f"replay {rep}: {name}"
+
+
+def test_blocks_on_two_streams_at_once(spa):
+    """Blocks with buffers and workspaces of their own do not see each other."""
+    make = lambda seed: Block(spa, 4, (14, 14), 192, 6, "bf16", "layer", False, seed)
+    want = []
+    for s in (1, 2):
+        one = make(s)
+        one.run()
+        torch.cuda.synchronize()
+        want.append(one.results())
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    blocks = []
+    for s, st in zip((1, 2), streams):
+        with torch.cuda.stream(st):
+            blocks.append(make(s))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for blk, st in zip(blocks, streams):
+            with torch.cuda.stream(st):
+                blk.run()
+    torch.cuda.synchronize()
+    for blk, ref in zip(blocks, want):
+        for name, a, b in zip(Block.RESULTS, blk.results(), ref):
+            assert torch.equal(a, b), name
