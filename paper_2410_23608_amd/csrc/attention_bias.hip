@@ -50,9 +50,10 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_fwd_kernel(con
       [] {}, [](const auto&) {},
       [&](const T* K, const T* V, const int* pos, int left, int own, int zero, bool in_window, auto whole) {
         floatx16 s[2];
+        const int blocks = whole || left > 32 ? 2 : 1;        // of 32 keys that exist
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
-          bias_scores<T, DH, WIN, 1>(s[sb], O::row(&K[(sb * 32 + l32) * O::RS], hh), qf, &pos[sb * 32], own, zero, in_window, a.m, h, a.scale, hh);
+          if (whole || sb < blocks) bias_scores<T, DH, WIN, 1>(s[sb], O::row(&K[(sb * 32 + l32) * O::RS], hh), qf, &pos[sb * 32], own, zero, in_window, a.m, h, a.scale, hh);
         if (!whole) {
 #pragma unroll
           for (int sb = 0; sb < 2; ++sb)
@@ -92,7 +93,7 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_fwd_kernel(con
         for (int sb = 0; sb < 2; ++sb) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) sum += s[sb][r];
-          O::outer(o, V, sb, s[sb], lane);
+          if (whole || sb < blocks) O::outer(o, V, sb, s[sb], lane);
         }
       });
   // (every wave is past its last read of the tiles)

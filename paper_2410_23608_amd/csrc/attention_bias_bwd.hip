@@ -45,7 +45,7 @@ struct BiasBwd {
   long dqs, dks, dvs;
   uint32_t* most;                 // [H][B * nblk]: what no |dS| of a block of queries exceeds
   float* partial;                 // [H][groups][offsets] or null
-  int groups, slice;              // dk / dv: workgroups a head; offsets of a histogram
+  int key_blocks, groups, slice;  // dk / dv: blocks of keys of the longest possible segment, workgroups a head, offsets of a histogram
 };
 
 template <typename T, int DH, int WIN, int SPLIT>
@@ -91,6 +91,7 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(cons
       [&](const T* K, const T* V, const int* pos, int rows, int own, int zero, bool in_window, auto whole) {
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb) {
+          if (!whole && sb * 32 >= rows) break;
           floatx16 s, dp = negD;
           const typename O::Row kr = O::row(&K[(sb * 32 + l32) * O::RS], hh), vr = O::row(&V[(sb * 32 + l32) * O::RS], hh);
           bias_scores<T, DH, WIN, 1>(s, kr, qf, &pos[sb * 32], own, zero, in_window, a.m, h, a.scale, hh);
@@ -213,14 +214,15 @@ __device__ __forceinline__ KeyBlock key_block(const KeyBlocks& k, const int32_t*
     const int img = i / kblk, from = cu[img];
     return {from, cu[img + 1] - from, i % kblk * rows};
   }
-  int lo = 0, hi = B - 1;                                     // the first rank with upto > i
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (k.upto[mid] > i) hi = mid;
-    else lo = mid + 1;
+  int rank = 0, at = i;                                       // the first rank with upto > i
+  for (int r0 = 0; r0 < B; r0 += kWave) {
+    const int r = r0 + (threadIdx.x & (kWave - 1)), upto = r < B ? k.upto[r] : 0x7fffffff;
+    const int before = __popcll(__ballot(upto <= i));
+    if (before > 0) at = i - __builtin_amdgcn_readlane(upto, before - 1);
+    rank += before;
+    if (before < kWave) break;
   }
-  const int at = i - (lo > 0 ? k.upto[lo - 1] : 0);
-  return {__builtin_amdgcn_readfirstlane(k.from[lo]), __builtin_amdgcn_readfirstlane(k.len[lo]), __builtin_amdgcn_readfirstlane(at) * rows};
+  return {__builtin_amdgcn_readfirstlane(k.from[rank]), __builtin_amdgcn_readfirstlane(k.len[rank]), at * rows};
 }
 
 // The scale of a head's integers: 2^e is above twice what the dq launch found (its blocks that exist); `unit` NaN: some dS of
@@ -256,7 +258,7 @@ __device__ __forceinline__ void write_partial(const unsigned long long* hist, co
   __syncthreads();
 }
 
-template <typename T, int DH, int SPLIT>
+template <typename T, int DH, int RW, int SPLIT>
 struct KeyTiles {
   static constexpr int RS = Ops<T, DH>::RS;
   __attribute__((aligned(16))) T Q[2][kBiasBN * RS];
@@ -266,25 +268,25 @@ struct KeyTiles {
   __attribute__((aligned(16))) float negD[2][kBiasBN];
   __attribute__((aligned(16))) int pos[2][kBiasBN];
   int range[2][1][2], far[2];
-  int own[4][2];
-  uint32_t most[4 * SPLIT];
+  int own[RW][2];
+  uint32_t most[RW * SPLIT];
   typename WindowFill<T, kBiasThreads>::Raw row[kTableLds];
   KeyBlocks blocks;
 };
 
-// SPLIT 2: the waves come twice, the second four take the second half of every tile of 64 queries, and hand their sums to the
-// first at the end of a block.
-template <typename T, int DH, int WIN, int SPLIT, int HIST>
-__global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dkdv_kernel(const BiasBwd<T> a) {
+// RW waves own 32 keys each.  SPLIT 2: the waves come twice, the second ones take the second half of every tile of 64 queries, and hand
+// their sums to the first at the end of a block.
+template <typename T, int DH, int WIN, int RW, int SPLIT, int HIST>
+__global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(const BiasBwd<T> a) {
   using O = Ops<T, DH>;
-  constexpr int RS = O::RS, DB = DH / 32, BN = kBiasBN, THREADS = kBiasThreads * SPLIT, ROWS = kBiasRows, WB = sizeof(T);
+  constexpr int RS = O::RS, DB = DH / 32, BN = kBiasBN, THREADS = kWave * RW * SPLIT, ROWS = 32 * RW, WB = sizeof(T);
   constexpr bool RANGES = WIN == kWinMoving || HIST == kHistSlices;                // the offsets of a tile lie where?
   extern __shared__ __attribute__((aligned(16))) unsigned long long hist[];        // [slice], then the window
-  __shared__ KeyTiles<T, DH, SPLIT> l;
+  __shared__ KeyTiles<T, DH, RW, SPLIT> l;
   const int h = blockIdx.x % a.H, group = blockIdx.x / a.H;
-  const int tid = threadIdx.x, lane = tid & 63, wv = (tid >> 6) & 3, l32 = lane & 31, hh = lane >> 5;
-  const int part = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;
-  const bool stages = part == 0;                              // (the first four waves)
+  const int tid = threadIdx.x, lane = tid & 63, wv = (tid >> 6) % RW, l32 = lane & 31, hh = lane >> 5;
+  const int part = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(tid / (kWave * RW)) : 0;
+  const bool stages = tid < kBiasThreads;                     // (the first four waves)
   const long C = (long)a.H * DH;
   void* win = hist + (HIST != kHistNone ? a.slice : 0);
   const float* lse_h = a.lse + h * a.lse_stride;
@@ -292,7 +294,7 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dkdv_kernel(co
 
   WindowFill<T, THREADS> fill(a.m, h);
   if (WIN == kWinWhole) fill.start(0, a.m.offsets);
-  list_key_blocks<THREADS>(l.blocks, a.cu, a.B, ROWS, a.nblk);
+  list_key_blocks<THREADS>(l.blocks, a.cu, a.B, ROWS, a.key_blocks);
   DsScale scale = {0, 0., 0.f};
   if (HIST != kHistNone) scale = ds_scale<THREADS>(a.most + (long)h * a.B * a.nblk, a.cu, a.B, a.nblk, l.most);
   int zero = 0;
@@ -305,25 +307,47 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dkdv_kernel(co
       for (int i = tid; i < a.slice; i += THREADS) hist[i] = 0;
       // (in front of the first add there is the barrier behind a block's first tile)
     }
-    for (int round = 0;; ++round) {
-      const int item = round * a.groups + (round & 1 ? a.groups - 1 - group : group);
-      if (item >= l.blocks.all) break;
-      const KeyBlock kb = key_block(l.blocks, a.cu, a.B, ROWS, a.nblk, item);
-      if (kb.k0 >= kb.n) continue;
+    // blocks: taken there and back, so that every workgroup has long and short ones; the next one's first tile is asked for under
+    // the last of the one before
+    int round = 0;
+    auto next_block = [&]() -> KeyBlock {
+      for (;; ++round) {
+        const int item = round * a.groups + (round & 1 ? a.groups - 1 - group : group);
+        if (item >= l.blocks.all) return {0, 0, 0};
+        const KeyBlock kb = key_block(l.blocks, a.cu, a.B, ROWS, a.key_blocks, item);
+        if (kb.k0 < kb.n) {
+          ++round;
+          return kb;
+        }
+      }
+    };
+    KeyBlock kb = next_block();
+    RowPair<T, DH, kBiasThreads, BN> st(tid, a.q + h * DH, a.qs, a.dout + h * DH, C, kb.row0, kb.n - 1);
+    BiasTokens tokens(a.m, a.cu, kb.row0);
+    int token = 0, token_j = 0;
+    float lse_t = 0.f, d_t = 0.f;
+    auto load_tile = [&](const KeyBlock& of, int qt) {
+      if (stages) st.load(qt);
+      token_j = min(qt + lane, of.n - 1);
+      token = tokens.load(token_j);
+      lse_t = lse_h[of.row0 + token_j];
+      d_t = d_h[of.row0 + token_j];
+    };
+    auto advance = [&] {
+      kb = next_block();
+      if (kb.n > 0) {
+        st.from_rows(a.q + h * DH, a.qs, a.dout + h * DH, C, kb.row0, kb.n - 1);
+        tokens = BiasTokens(a.m, a.cu, kb.row0);
+        load_tile(kb, 0);
+      }
+    };
+    constexpr bool AHEAD = SPLIT == 1;
+    if (kb.n > 0) load_tile(kb, 0);
+    while (kb.n > 0) {
       const int n = kb.n, last = n - 1, ki = kb.k0 + wv * 32 + l32;
       const bool wave_live = kb.k0 + wv * 32 < n, k_ok = ki < n;
       const long k_row = kb.row0 + min(ki, last);
-      RowPair<T, DH, kBiasThreads, BN> st(tid, a.q + h * DH, a.qs, a.dout + h * DH, C, kb.row0, last);
-      const BiasTokens tokens(a.m, a.cu, kb.row0);
-      int token = 0, token_j = 0;
-      float lse_t = 0.f, d_t = 0.f;
-      auto load_tile = [&](int qt) {
-        if (stages) st.load(qt);
-        token_j = min(qt + lane, last);
-        token = tokens.load(token_j);
-        lse_t = lse_h[kb.row0 + token_j];
-        d_t = d_h[kb.row0 + token_j];
-      };
+      const BiasTokens own_tokens = tokens;
       auto store_tile = [&](int buf, int qt, auto clear) {
         if (stages) st.template store<clear>(l.Q[buf], l.G[buf]);
         if (tid < BN) {
@@ -338,9 +362,9 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dkdv_kernel(co
           if (tid == 0) l.far[buf] = any;
         }
       };
-      load_tile(0);
+      const int own_token = own_tokens.load(min(ki, last));
       const typename O::Row kf = O::row(a.k + k_row * a.ks + h * DH, hh), vf = O::row(a.v + k_row * a.vs + h * DH, hh);
-      const int own = tokens.position(a.m, min(ki, last));
+      const int own = own_tokens.position(a.m, own_token, min(ki, last));
       __syncthreads();                                        // every wave is past its last read of the tiles before
       if (RANGES && part == 0) put_range(l.own[wv], own);
       floatx16 dka[DB], dva[DB];
@@ -356,7 +380,11 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dkdv_kernel(co
       for (int t = 0; t < nt; ++t) {
         const int buf = t & 1, qt = t * BN;
         const bool end = t + 1 == nt;
-        if (!end) load_tile(qt + BN);
+        if (!end) {
+          load_tile(kb, qt + BN);
+        } else if (AHEAD) {
+          advance();
+        }
         bool in_window = true, adds = HIST != kHistNone, inside = true;
         if (RANGES) {
           const Range tile = whole_range(l.range[buf]);
@@ -380,6 +408,7 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dkdv_kernel(co
 #pragma unroll
           for (int half = 0; half < 2 / SPLIT; ++half) {
             const int sb = SPLIT > 1 ? part : half;
+            if (qt + sb * 32 >= n) break;
             const int* pos = &l.pos[buf][sb * 32];
             const typename O::Row qr = O::row(&l.Q[buf][(sb * 32 + l32) * RS], hh), gr = O::row(&l.G[buf][(sb * 32 + l32) * RS], hh);
             floatx16 s, dp;
@@ -435,24 +464,25 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dkdv_kernel(co
       }
       if (pass == 0) {
         if constexpr (SPLIT > 1) {
-          static_assert(4 * DB * 16 * kWave * sizeof(float) <= sizeof(l.Q) + sizeof(l.G), "one sum of four waves");
-          float* other = reinterpret_cast<float*>(&l.Q[0][0]) + wv * DB * 16 * kWave + lane;
+          static_assert(RW * DB * 8 * kWave * sizeof(float) <= sizeof(l.Q) + sizeof(l.G), "half a sum of the waves");
+          float* other = reinterpret_cast<float*>(&l.Q[0][0]) + wv * DB * 8 * kWave + lane;
 #pragma unroll
-          for (int which = 0; which < 2; ++which) {
-            floatx16(&sum)[DB] = which == 0 ? dka : dva;
+          for (int which = 0; which < 4; ++which) {
+            floatx16(&sum)[DB] = which < 2 ? dka : dva;
+            const int r0 = which & 1 ? 8 : 0;
             __syncthreads();                                  // every wave is past its last read of the tiles, or of the sums before
             if (part == 1) {
 #pragma unroll
               for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) other[(d * 16 + r) * kWave] = sum[d][r];
+                for (int r = 0; r < 8; ++r) other[(d * 8 + r) * kWave] = sum[d][r0 + r];
             }
             __syncthreads();
             if (part == 0) {
 #pragma unroll
               for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sum[d][r] += other[(d * 16 + r) * kWave];
+                for (int r = 0; r < 8; ++r) sum[d][r0 + r] += other[(d * 8 + r) * kWave];
             }
           }
         }
@@ -461,6 +491,7 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dkdv_kernel(co
           O::store(dva, 1.0f, a.dv + k_row * a.dvs + h * DH, k_ok, hh);
         }
       }
+      if (!AHEAD) advance();
     }
     if (HIST != kHistNone) write_partial<THREADS>(hist, scale, a.slice, from, a.m.offsets, a.partial + ((long)h * a.groups + group) * a.m.offsets);
   }
@@ -496,20 +527,39 @@ __global__ void __launch_bounds__(256) attn_bias_sum_kernel(const BiasSum a) {
 }
 
 // The sums of the offsets into those of their buckets, with integers again, of 2^-40 of the power of two above the largest: a
-// workgroup has kTableBuckets buckets of a head in LDS and goes over all offsets.
-constexpr int kTableBuckets = 2048;
+// workgroup has kTableBuckets buckets of a head in LDS and goes over all offsets.  Few workgroups on a small map: it
+// adds up their sums as well, a launch less (us backward, two launches | one: 2 images of 62 tokens, fp32, 14 x 14 map, 2
+// workgroups a head 29.4 | 28.3; 64 images, 42 workgroups a head 62 | 62).
+constexpr int kTableBuckets = 2048, kTableSums = 2048;
 struct BiasTable {
-  const float* sums;
+  const float* sums;              // [H][offsets], or the workgroups' [H][groups][offsets]
   const int32_t* buckets;
-  int nb, offsets;
+  int nb, offsets, groups;
   float* d_table;
 };
+template <bool ADDS>
 __global__ void __launch_bounds__(1024) attn_bias_table_kernel(const BiasTable a) {
-  constexpr int U = 8;
+  constexpr int U = 8, UG = 16;
   __shared__ unsigned long long s[kTableBuckets];
   __shared__ uint32_t s_most[16];
+  __shared__ float s_sums[ADDS ? kTableSums : 1];
   const int h = blockIdx.y, b0 = blockIdx.x * kTableBuckets, nb = min(kTableBuckets, a.nb - b0);
-  const float* sums = a.sums + (long)h * a.offsets;
+  const float* sums = ADDS ? s_sums : a.sums + (long)h * a.offsets;
+  if (ADDS) {
+    for (int o = threadIdx.x; o < a.offsets; o += 1024) {
+      const float* p = a.sums + (long)h * a.groups * a.offsets + o;
+      double v = 0.;
+      for (int g0 = 0; g0 < a.groups; g0 += UG) {
+        float f[UG];
+#pragma unroll
+        for (int u = 0; u < UG; ++u) f[u] = p[(long)min(g0 + u, a.groups - 1) * a.offsets];
+#pragma unroll
+        for (int u = 0; u < UG; ++u) v += g0 + u < a.groups ? (double)f[u] : 0.;
+      }
+      s_sums[o] = (float)v;
+    }
+    __syncthreads();
+  }
   uint32_t most = 0;
   for (int i0 = threadIdx.x; i0 < a.offsets; i0 += U * 1024) {
     float v[U];
@@ -551,29 +601,33 @@ static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 // and no more than 256 MB of partial sums.
 struct BiasPlan {
   bool whole;                     // the window
-  int split, slice, groups;
+  int rows, split, key_blocks, slice, groups;         // rows: waves that own keys
   size_t window, lds;
 };
+template <int DH>
+constexpr int kSplitRows = DH == 32 ? 6 : 4;
 template <typename T, int DH>
-static BiasPlan bias_plan_of(int H, int B, int nblk, long offsets) {
+static BiasPlan bias_plan_of(int H, int B, int n_max, long offsets) {
   BiasPlan p = {};
   const size_t most = 160 * 1024;
   const long all = (offsets + 63) & ~63L;
   p.whole = offsets <= kWholeBytes / (long)sizeof(T);
   p.window = window_bytes(p.whole ? (int)offsets : kWindow, sizeof(T));
-  size_t tiles = sizeof(KeyTiles<T, DH, 1>);
+  size_t tiles = sizeof(KeyTiles<T, DH, 4, 1>);
   const bool two = p.whole && tiles + p.window + all * 8 <= most / 2;
   p.split = sizeof(T) == 2 && p.whole && !two ? 2 : 1;
-  if (p.split == 2) tiles = sizeof(KeyTiles<T, DH, 2>);
+  if (p.split == 2) tiles = sizeof(KeyTiles<T, DH, kSplitRows<DH>, 2>);
   p.slice = (int)std::min<long>(all, (long)(most - tiles - p.window) / 8 / 64 * 64);
   p.lds = p.window + (size_t)p.slice * 8;
+  p.rows = p.split == 2 && p.slice == all ? kSplitRows<DH> : 4;
+  p.key_blocks = (n_max + 32 * p.rows - 1) / (32 * p.rows);
   const long fit = std::max<long>(1, (256L << 20) / (4 * H * offsets));
-  p.groups = (int)std::max<long>(1, std::min<long>(std::min<long>((two ? 512 : 256) / H, (long)B * nblk), fit));
+  p.groups = (int)std::max<long>(1, std::min<long>(std::min<long>((two ? 512 : 256) / H, (long)B * p.key_blocks), fit));
   return p;
 }
-static BiasPlan bias_plan(int H, int B, int nblk, int Dh, long offsets, int dtype) {
-  if (dtype == SPA_F32) return Dh == 32 ? bias_plan_of<float, 32>(H, B, nblk, offsets) : bias_plan_of<float, 64>(H, B, nblk, offsets);
-  return Dh == 32 ? bias_plan_of<__bf16, 32>(H, B, nblk, offsets) : bias_plan_of<__bf16, 64>(H, B, nblk, offsets);
+static BiasPlan bias_plan(int H, int B, int n_max, int Dh, long offsets, int dtype) {
+  if (dtype == SPA_F32) return Dh == 32 ? bias_plan_of<float, 32>(H, B, n_max, offsets) : bias_plan_of<float, 64>(H, B, n_max, offsets);
+  return Dh == 32 ? bias_plan_of<__bf16, 32>(H, B, n_max, offsets) : bias_plan_of<__bf16, 64>(H, B, n_max, offsets);
 }
 
 template <typename T, int D>
@@ -581,20 +635,21 @@ static int launch_bias_bwd(const char* fn, const BiasBwd<T>& args, const BiasPla
   const BiasMap& m = args.m;
   const int H = args.H, B = args.B, nblk = args.nblk;
   SPA_QUERY_LAUNCH(attn_bias_dq_kernel, T, D, args);
-#define SPA_DKDV(WIN, SPLIT, MODE)                                                                                              \
-  SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<T, D, WIN, SPLIT, MODE>), H * plan.groups, SPLIT * kBiasThreads, hist ? plan.lds : plan.window, args)
+#define SPA_DKDV(WIN, RW, SPLIT, MODE)                                                                                          \
+  SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<T, D, WIN, RW, SPLIT, MODE>), H * plan.groups, SPLIT * RW * kWave, hist ? plan.lds : plan.window, args)
   const bool slices = plan.slice < m.offsets;
   if (!plan.whole) {
-    if (!hist) SPA_DKDV(kWinMoving, 1, kHistNone);
-    else SPA_DKDV(kWinMoving, 1, kHistSlices);
+    if (!hist) SPA_DKDV(kWinMoving, 4, 1, kHistNone);
+    else SPA_DKDV(kWinMoving, 4, 1, kHistSlices);
   } else if (plan.split == 1) {
-    if (!hist) SPA_DKDV(kWinWhole, 1, kHistNone);
-    else if (!slices) SPA_DKDV(kWinWhole, 1, kHistWhole);
-    else if constexpr (sizeof(T) == 4) SPA_DKDV(kWinWhole, 1, kHistSlices);
+    if (!hist) SPA_DKDV(kWinWhole, 4, 1, kHistNone);
+    else if (!slices) SPA_DKDV(kWinWhole, 4, 1, kHistWhole);
+    else if constexpr (sizeof(T) == 4) SPA_DKDV(kWinWhole, 4, 1, kHistSlices);
   } else if constexpr (sizeof(T) == 2) {
-    if (!hist) SPA_DKDV(kWinWhole, 2, kHistNone);
-    else if (!slices) SPA_DKDV(kWinWhole, 2, kHistWhole);
-    else SPA_DKDV(kWinWhole, 2, kHistSlices);
+    if (hist && slices) SPA_DKDV(kWinWhole, 4, 2, kHistSlices);
+    else if (hist) SPA_DKDV(kWinWhole, kSplitRows<D>, 2, kHistWhole);
+    else if (slices) SPA_DKDV(kWinWhole, 4, 2, kHistNone);
+    else SPA_DKDV(kWinWhole, kSplitRows<D>, 2, kHistNone);
   }
 #undef SPA_DKDV
   return SPA_OK;
@@ -608,7 +663,7 @@ extern "C" size_t spa_attention_bias_bwd_workspace_bytes(int B, int max_seqlen, 
   if (B < 1 || max_seqlen < 1 || H < 1 || grid_h < 1 || grid_w < 1 || (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1) > kMostOffsets) return 0;
   const long offsets = (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1);
   const int nblk = (max_seqlen + kBiasRows - 1) / kBiasRows;
-  const BiasPlan p = bias_plan(H, B, nblk, Dh, offsets, dtype);
+  const BiasPlan p = bias_plan(H, B, max_seqlen, Dh, offsets, dtype);
   return up256((size_t)H * B * max_seqlen * 4) + up256((size_t)H * B * nblk * 4) + up256((size_t)H * p.groups * offsets * 4) +
          up256((size_t)H * offsets * 4);
 }
@@ -641,7 +696,7 @@ extern "C" int spa_packed_attention_bias_bwd(const void* q, const void* k, const
   const long ls = (long)B * max_seqlen;
   const int nblk = (max_seqlen + kBiasRows - 1) / kBiasRows;
   SPA_REQUIRE(((long)H * B + 8) * nblk < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*H*blocks must be < 2^31", fn);
-  const BiasPlan plan = bias_plan(H, B, nblk, Dh, m.offsets, dtype);
+  const BiasPlan plan = bias_plan(H, B, max_seqlen, Dh, m.offsets, dtype);
   char* ws = static_cast<char*>(workspace);
   auto take = [&](size_t bytes) {
     char* at = ws;
@@ -659,7 +714,7 @@ extern "C" int spa_packed_attention_bias_bwd(const void* q, const void* k, const
     const BiasBwd<T> args = {(const T*)q, (const T*)k, (const T*)v, (const T*)out, (const T*)dout, (long)q_row_stride,       \
                              (long)k_row_stride, (long)v_row_stride, lse, dvec, ls, cu_seqlens, m, H, B, nblk, scale, (T*)dq, \
                              (T*)dk, (T*)dv, (long)dq_row_stride, (long)dk_row_stride, (long)dv_row_stride, most, partial,   \
-                             plan.groups, plan.slice};                                                                       \
+                             plan.key_blocks, plan.groups, plan.slice};                                                                       \
     if (int rc = launch_bias_bwd<T, D>(fn, args, plan, hist, st)) return rc;                                                 \
   } while (0)
   if (dtype == SPA_F32) {
@@ -669,11 +724,15 @@ extern "C" int spa_packed_attention_bias_bwd(const void* q, const void* k, const
   }
 #undef SPA_BWD
   if (hist) {
-    const BiasSum sum = {partial, plan.groups, m.offsets, sums};
-    hipLaunchKernelGGL(attn_bias_sum_kernel, dim3((m.offsets + 31) / 32, H), dim3(256), 0, st, sum);
-    if (buckets != nullptr) {
-      const BiasTable table_args = {sums, buckets, n_buckets, m.offsets, d_table};
-      hipLaunchKernelGGL(attn_bias_table_kernel, dim3((n_buckets + kTableBuckets - 1) / kTableBuckets, H), dim3(1024), 0, st, table_args);
+    const bool one = buckets != nullptr && m.offsets <= kTableSums && (m.offsets + 1023) / 1024 * plan.groups <= 32;
+    const dim3 grid((n_buckets + kTableBuckets - 1) / kTableBuckets, H);
+    const BiasTable to_buckets = {one ? partial : sums, buckets, n_buckets, m.offsets, plan.groups, d_table};
+    if (one) {
+      hipLaunchKernelGGL(attn_bias_table_kernel<true>, grid, dim3(1024), 0, st, to_buckets);
+    } else {
+      const BiasSum sum = {partial, plan.groups, m.offsets, sums};
+      hipLaunchKernelGGL(attn_bias_sum_kernel, dim3((m.offsets + 31) / 32, H), dim3(256), 0, st, sum);
+      if (buckets != nullptr) hipLaunchKernelGGL(attn_bias_table_kernel<false>, grid, dim3(1024), 0, st, to_buckets);
     }
   }
   return check_launch(fn);

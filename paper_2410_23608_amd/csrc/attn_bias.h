@@ -185,7 +185,11 @@ struct RowPair {
   const char* base[2];
   uint32_t stride[2];            // bytes
   int last, from;
-  __device__ __forceinline__ RowPair(int tid_, const T* a, long as, const T* b, long bs, long row0, int last_) : tid(tid_), last(last_), from(0) {
+  __device__ __forceinline__ RowPair(int tid_, const T* a, long as, const T* b, long bs, long row0, int last_) : tid(tid_), from(0) {
+    from_rows(a, as, b, bs, row0, last_);
+  }
+  __device__ __forceinline__ void from_rows(const T* a, long as, const T* b, long bs, long row0, int last_) {
+    last = last_;
     base[0] = reinterpret_cast<const char*>(a + row0 * as + tid % CPR * VE);
     base[1] = reinterpret_cast<const char*>(b + row0 * bs + tid % CPR * VE);
     stride[0] = (uint32_t)as * (uint32_t)sizeof(T);
@@ -247,7 +251,7 @@ constexpr int kTableLds = 1024;                // a table row of up to so many e
 template <typename T, int THREADS>
 struct WindowFill {
   using Raw = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
-  static constexpr int VE = 16 / sizeof(T), U = 4, PART = kTableLds / THREADS;
+  static constexpr int VE = 16 / sizeof(T), U = 4, PART = (kTableLds + THREADS - 1) / THREADS;
   const BiasMap& m;
   const Raw* row;
   const int tid;
@@ -399,7 +403,9 @@ struct BiasBlock {
   bool valid;
 };
 __device__ __forceinline__ BiasBlock bias_block(int* s_live, const int32_t* cu, int H, int B, int nblk) {
-  const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
+  // there and back: a unit that got a long block in one turn of the XCD's 32 units gets a short one in the next
+  const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3 & ~31, width = min(32, (int)(gridDim.x >> 3) - turn);
+  const int at = blockIdx.x >> 3 & 31, j = turn + (turn & 32 ? width - 1 - at : at);
   if (B <= kLptMaxB) {
     LiveTile* slot = reinterpret_cast<LiveTile*>(s_live);
     const LiveTile t = live_tiles_apply(H, B) ? live_tile_block<1>(xcd, j, H, B, cu, kBiasRows, nblk, slot)

@@ -241,6 +241,18 @@ def test_without_the_table_gradient_the_rest_is_the_same(spa):
         assert torch.equal(a[n], b[n])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Dh", [32, 64])
+@pytest.mark.parametrize("grid,lens", [((24, 25), [300, 130]), ((56, 56), [700, 65, 193]), ((64, 64), [390, 1, 64]), ((130, 130), [1500, 65])])
+def test_every_size_of_map_with_and_without_the_table_gradient(spa, grid, lens, Dh, dtype):
+    """Maps that LDS holds beside the sums of dS by offset, or with part of them, and larger ones."""
+    c = Case(lens, grid, 2, Dh, dtype, seed=19 + Dh)
+    got, without = c.run(spa), c.run(spa, want_table=False)
+    c.check(got)
+    for n in ("dq", "dk", "dv"):
+        assert torch.equal(got[n], without[n])
+
+
 def test_results_are_the_same_in_every_run(spa):
     c = Case([700, 256, 31, 400], (30, 31), 3, 32, "bf16", seed=9, buckets="log")
     first = c.run(spa)
