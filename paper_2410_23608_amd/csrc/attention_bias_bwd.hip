@@ -307,47 +307,26 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
       for (int i = tid; i < a.slice; i += THREADS) hist[i] = 0;
       // (in front of the first add there is the barrier behind a block's first tile)
     }
-    // blocks: taken there and back, so that every workgroup has long and short ones; the next one's first tile is asked for under
-    // the last of the one before
-    int round = 0;
-    auto next_block = [&]() -> KeyBlock {
-      for (;; ++round) {
-        const int item = round * a.groups + (round & 1 ? a.groups - 1 - group : group);
-        if (item >= l.blocks.all) return {0, 0, 0};
-        const KeyBlock kb = key_block(l.blocks, a.cu, a.B, ROWS, a.key_blocks, item);
-        if (kb.k0 < kb.n) {
-          ++round;
-          return kb;
-        }
-      }
-    };
-    KeyBlock kb = next_block();
-    RowPair<T, DH, kBiasThreads, BN> st(tid, a.q + h * DH, a.qs, a.dout + h * DH, C, kb.row0, kb.n - 1);
-    BiasTokens tokens(a.m, a.cu, kb.row0);
-    int token = 0, token_j = 0;
-    float lse_t = 0.f, d_t = 0.f;
-    auto load_tile = [&](const KeyBlock& of, int qt) {
-      if (stages) st.load(qt);
-      token_j = min(qt + lane, of.n - 1);
-      token = tokens.load(token_j);
-      lse_t = lse_h[of.row0 + token_j];
-      d_t = d_h[of.row0 + token_j];
-    };
-    auto advance = [&] {
-      kb = next_block();
-      if (kb.n > 0) {
-        st.from_rows(a.q + h * DH, a.qs, a.dout + h * DH, C, kb.row0, kb.n - 1);
-        tokens = BiasTokens(a.m, a.cu, kb.row0);
-        load_tile(kb, 0);
-      }
-    };
-    constexpr bool AHEAD = SPLIT == 1;
-    if (kb.n > 0) load_tile(kb, 0);
-    while (kb.n > 0) {
+    for (int round = 0;; ++round) {
+      // there and back, so that every workgroup has long and short blocks
+      const int item = round * a.groups + (round & 1 ? a.groups - 1 - group : group);
+      if (item >= l.blocks.all) break;
+      const KeyBlock kb = key_block(l.blocks, a.cu, a.B, ROWS, a.key_blocks, item);
+      if (kb.k0 >= kb.n) continue;
       const int n = kb.n, last = n - 1, ki = kb.k0 + wv * 32 + l32;
       const bool wave_live = kb.k0 + wv * 32 < n, k_ok = ki < n;
       const long k_row = kb.row0 + min(ki, last);
-      const BiasTokens own_tokens = tokens;
+      RowPair<T, DH, kBiasThreads, BN> st(tid, a.q + h * DH, a.qs, a.dout + h * DH, C, kb.row0, last);
+      const BiasTokens tokens(a.m, a.cu, kb.row0);
+      int token = 0, token_j = 0;
+      float lse_t = 0.f, d_t = 0.f;
+      auto load_tile = [&](int qt) {
+        if (stages) st.load(qt);
+        token_j = min(qt + lane, last);
+        token = tokens.load(token_j);
+        lse_t = lse_h[kb.row0 + token_j];
+        d_t = d_h[kb.row0 + token_j];
+      };
       auto store_tile = [&](int buf, int qt, auto clear) {
         if (stages) st.template store<clear>(l.Q[buf], l.G[buf]);
         if (tid < BN) {
@@ -362,9 +341,10 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
           if (tid == 0) l.far[buf] = any;
         }
       };
-      const int own_token = own_tokens.load(min(ki, last));
+      const int own_token = tokens.load(min(ki, last));
+      load_tile(0);
       const typename O::Row kf = O::row(a.k + k_row * a.ks + h * DH, hh), vf = O::row(a.v + k_row * a.vs + h * DH, hh);
-      const int own = own_tokens.position(a.m, own_token, min(ki, last));
+      const int own = tokens.position(a.m, own_token, min(ki, last));
       __syncthreads();                                        // every wave is past its last read of the tiles before
       if (RANGES && part == 0) put_range(l.own[wv], own);
       floatx16 dka[DB], dva[DB];
@@ -380,11 +360,7 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
       for (int t = 0; t < nt; ++t) {
         const int buf = t & 1, qt = t * BN;
         const bool end = t + 1 == nt;
-        if (!end) {
-          load_tile(kb, qt + BN);
-        } else if (AHEAD) {
-          advance();
-        }
+        if (!end) load_tile(qt + BN);
         bool in_window = true, adds = HIST != kHistNone, inside = true;
         if (RANGES) {
           const Range tile = whole_range(l.range[buf]);
@@ -491,7 +467,6 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
           O::store(dva, 1.0f, a.dv + k_row * a.dvs + h * DH, k_ok, hh);
         }
       }
-      if (!AHEAD) advance();
     }
     if (HIST != kHistNone) write_partial<THREADS>(hist, scale, a.slice, from, a.m.offsets, a.partial + ((long)h * a.groups + group) * a.m.offsets);
   }

@@ -185,11 +185,7 @@ struct RowPair {
   const char* base[2];
   uint32_t stride[2];            // bytes
   int last, from;
-  __device__ __forceinline__ RowPair(int tid_, const T* a, long as, const T* b, long bs, long row0, int last_) : tid(tid_), from(0) {
-    from_rows(a, as, b, bs, row0, last_);
-  }
-  __device__ __forceinline__ void from_rows(const T* a, long as, const T* b, long bs, long row0, int last_) {
-    last = last_;
+  __device__ __forceinline__ RowPair(int tid_, const T* a, long as, const T* b, long bs, long row0, int last_) : tid(tid_), last(last_), from(0) {
     base[0] = reinterpret_cast<const char*>(a + row0 * as + tid % CPR * VE);
     base[1] = reinterpret_cast<const char*>(b + row0 * bs + tid % CPR * VE);
     stride[0] = (uint32_t)as * (uint32_t)sizeof(T);
