@@ -3,6 +3,7 @@
 //   S_ij = scale q_i k_j + table[h, buckets[offset of i from j]],   O = softmax(S) V
 // With p = row (2 gw - 1) + column the offset's index is p_i - p_j + (gh - 1)(2 gw - 1) + gw - 1: one subtraction.  A row whose
 // scores are all -inf gives 0.
+#include <algorithm>
 #include <cmath>
 
 #include "attn_bias.h"
@@ -128,6 +129,20 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_fwd_kernel(con
   if (a.lse != nullptr && q_ok && hh == 0) a.lse[h * a.lse_stride + q_row] = total == 0.f ? -INFINITY : m + logf(total);
 }
 
+// Eight waves a block as well where the LDS of larger maps leaves few waves a unit otherwise: where that is twice the waves, or more
+// waves and not too many blocks.  us four | eight waves, heads of 32: 50 x 84 map (8 | 16 waves a unit), 8 images 31.2 | 25.0, 32 images
+// 132 | 117; 56 x 56 (12 | 16), 16 images 37.2 | 30.8, 64 images 94 | 100; 28 x 28 (16 | 16), 32 images 22.0 | 23.0.
+template <typename T, int DH>
+static bool fwd_eight(int offsets, int nblk, int H, int B) {
+  if (few_blocks(nblk, H, B)) return true;
+  constexpr size_t unit = 160 * 1024;
+  constexpr int most = DH == 32 ? 16 : 12;                    // by registers
+  const size_t win = window_bytes(offsets, sizeof(T));
+  const int four = std::min<int>(most, 4 * (int)(unit / (sizeof(QueryTiles<T, DH, 1>) + win)));
+  const int eight = std::min<int>(most, 8 * (int)(unit / (sizeof(QueryTiles<T, DH, 2>) + win)));
+  return nblk >= 4 && (eight >= 2 * four || (eight > four && xcd_grid(nblk, H, B) <= 2048));
+}
+
 int bias_checks(const char* fn, const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
                        const int32_t* cu, int B, int n_max, int H, int Dh, int dtype, float softmax_scale, const void* table,
                        const int32_t* buckets, int n_buckets, const int32_t* gather_idx, int grid_h, int grid_w, BiasMap* m) {
@@ -183,7 +198,7 @@ extern "C" int spa_packed_attention_bias(const void* q, const void* k, const voi
   do {                                                                                                                        \
     const BiasFwd<T> args = {(const T*)q, (const T*)k, (const T*)v, (long)q_row_stride, (long)k_row_stride, (long)v_row_stride, \
                              cu_seqlens, m, H, B, nblk, scale, (T*)out, lse, (long)B * max_seqlen};                           \
-    SPA_QUERY_LAUNCH(attn_bias_fwd_kernel, T, D, args);                                                                       \
+    SPA_QUERY_LAUNCH(attn_bias_fwd_kernel, T, D, (fwd_eight<T, D>(m.offsets, nblk, H, B)), args);                                                                       \
   } while (0)
   if (dtype == SPA_F32) {
     if (Dh == 32) SPA_FWD(float, 32); else SPA_FWD(float, 64);

@@ -579,6 +579,8 @@ struct BiasPlan {
   int rows, split, key_blocks, slice, groups;         // rows: waves that own keys
   size_t window, lds;
 };
+// Twelve waves for 192 keys where registers allow and there may be many blocks: us backward, eight | twelve waves, 3 heads of 32, 56 x 56 map:
+// one image of 1792 tokens 87.4 | 100, 8 of 196 36.5 | 38.7, 16 of 1792 236 | 213, 64 of 0.1 - 0.6 of 3136 348 | 324.
 template <int DH>
 constexpr int kSplitRows = DH == 32 ? 6 : 4;
 template <typename T, int DH>
@@ -594,7 +596,8 @@ static BiasPlan bias_plan_of(int H, int B, int n_max, long offsets) {
   if (p.split == 2) tiles = sizeof(KeyTiles<T, DH, kSplitRows<DH>, 2>);
   p.slice = (int)std::min<long>(all, (long)(most - tiles - p.window) / 8 / 64 * 64);
   p.lds = p.window + (size_t)p.slice * 8;
-  p.rows = p.split == 2 && p.slice == all ? kSplitRows<DH> : 4;
+  const bool many = (long)H * B * ((n_max + kBiasRows - 1) / kBiasRows) >= 1024;
+  p.rows = p.split == 2 && p.slice == all && many ? kSplitRows<DH> : 4;
   p.key_blocks = (n_max + 32 * p.rows - 1) / (32 * p.rows);
   const long fit = std::max<long>(1, (256L << 20) / (4 * H * offsets));
   p.groups = (int)std::max<long>(1, std::min<long>(std::min<long>((two ? 512 : 256) / H, (long)B * p.key_blocks), fit));
@@ -609,7 +612,7 @@ template <typename T, int D>
 static int launch_bias_bwd(const char* fn, const BiasBwd<T>& args, const BiasPlan& plan, bool hist, hipStream_t st) {
   const BiasMap& m = args.m;
   const int H = args.H, B = args.B, nblk = args.nblk;
-  SPA_QUERY_LAUNCH(attn_bias_dq_kernel, T, D, args);
+  SPA_QUERY_LAUNCH(attn_bias_dq_kernel, T, D, few_blocks(nblk, H, B), args);
 #define SPA_DKDV(WIN, RW, SPLIT, MODE)                                                                                          \
   SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<T, D, WIN, RW, SPLIT, MODE>), H * plan.groups, SPLIT * RW * kWave, hist ? plan.lds : plan.window, args)
   const bool slices = plan.slice < m.offsets;
@@ -622,8 +625,9 @@ static int launch_bias_bwd(const char* fn, const BiasBwd<T>& args, const BiasPla
     else if constexpr (sizeof(T) == 4) SPA_DKDV(kWinWhole, 4, 1, kHistSlices);
   } else if constexpr (sizeof(T) == 2) {
     if (hist && slices) SPA_DKDV(kWinWhole, 4, 2, kHistSlices);
+    else if (hist && plan.rows == 4) SPA_DKDV(kWinWhole, 4, 2, kHistWhole);
+    else if (plan.rows == 4) SPA_DKDV(kWinWhole, 4, 2, kHistNone);
     else if (hist) SPA_DKDV(kWinWhole, kSplitRows<D>, 2, kHistWhole);
-    else if (slices) SPA_DKDV(kWinWhole, 4, 2, kHistNone);
     else SPA_DKDV(kWinWhole, kSplitRows<D>, 2, kHistNone);
   }
 #undef SPA_DKDV

@@ -399,7 +399,8 @@ struct BiasBlock {
   bool valid;
 };
 __device__ __forceinline__ BiasBlock bias_block(int* s_live, const int32_t* cu, int H, int B, int nblk) {
-  // there and back: a unit that got a long block in one turn of the XCD's 32 units gets a short one in the next
+  // there and back: a unit that got a long block in one turn of the XCD's 32 units gets a short one in the next (us forward,
+  // there alone | there and back: 16 images of 0.1 - 0.6 of 3136 tokens, 3 heads of 32, 38.9 | 37.2; 8 of 0.05 - 0.4 of 4200, 8 heads, 32.7 | 31.2)
   const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3 & ~31, width = min(32, (int)(gridDim.x >> 3) - turn);
   const int at = blockIdx.x >> 3 & 31, j = turn + (turn & 32 ? width - 1 - at : at);
   if (B <= kLptMaxB) {
@@ -498,8 +499,8 @@ constexpr long kMostOffsets = 1L << 26;
 // LDS of a window of that many offsets: a bf16 one may start up to 7 entries into its first 16 bytes
 inline size_t window_bytes(int offsets, int each) { return ((size_t)offsets + 7 + 7) / 8 * 8 * each; }
 // Eight waves a block (SPLIT) where a unit has one block at most and segments may have several tiles; a block is then a chain of half
-// the steps.  us forward, four | eight waves, 3 heads of 32, 56 x 56 map: one image of 1792 tokens 33.6 | 26.0, 512 12.3 | 10.6; 16 images
-// of 1792 63 | 77, of 512 13.8 | 13.9.
+// the steps.  us forward / backward, four | eight waves, 3 heads of 32, 56 x 56 map: one image of 1792 tokens 37.0 / 110 | 26.4 / 100, of 512
+// 13.4 / 44.7 | 11.2 / 42.5; 64 images of 196 19.5 / 57.5 | 26.5 / 83.0.
 inline bool few_blocks(int nblk, int H, int B) { return nblk >= 4 && xcd_grid(nblk, H, B) <= 256; }
 #define SPA_BIAS_LAUNCH(KERNEL, GRID, THREADS, LDS, ARGS)                                                                      \
   do {                                                                                                                        \
@@ -507,8 +508,8 @@ inline bool few_blocks(int nblk, int H, int B) { return nblk >= 4 && xcd_grid(nb
     SPA_REQUIRE(attr == hipSuccess, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, (size_t)(LDS));                   \
     hipLaunchKernelGGL(KERNEL, dim3(GRID), dim3(THREADS), LDS, st, ARGS);                                                     \
   } while (0)
-// KERNEL<type, head dim, window, SPLIT> of a launch whose workgroups own queries
-#define SPA_QUERY_LAUNCH(KERNEL, T, D, ARGS)                                                                                  \
+// KERNEL<type, head dim, window, SPLIT> of a launch whose workgroups own queries; EIGHT: whether a block has eight waves
+#define SPA_QUERY_LAUNCH(KERNEL, T, D, EIGHT, ARGS)                                                                           \
   do {                                                                                                                        \
     const bool whole = m.offsets <= kWholeBytes / (int)sizeof(T);                                                             \
     const size_t lds = window_bytes(whole ? m.offsets : kWindow, sizeof(T));                                                  \
@@ -517,7 +518,7 @@ inline bool few_blocks(int nblk, int H, int B) { return nblk >= 4 && xcd_grid(nb
       SPA_BIAS_LAUNCH((KERNEL<T, D, kWinMoving, 1>), blocks, kBiasThreads, lds, ARGS);                                        \
     } else {                                                                                                                  \
       if constexpr (sizeof(T) == 2)                                                                                           \
-        if (few_blocks(nblk, H, B)) {                                                                                         \
+        if (EIGHT) {                                                                                                          \
           SPA_BIAS_LAUNCH((KERNEL<T, D, kWinWhole, 2>), blocks, 2 * kBiasThreads, lds, ARGS);                                 \
           break;                                                                                                              \
         }                                                                                                                     \

@@ -340,6 +340,15 @@ def test_many_segments(spa, B, dtype):
 
 
 @pytest.mark.parametrize("Dh", [32, 64])
+def test_long_and_many_short_segments_on_a_large_map(spa, Dh):
+    c = Case([1200, 390, 700] + [20] * 52, (56, 56), 2, Dh, "bf16", seed=21)
+    got, without = c.run(spa), c.run(spa, want_table=False)
+    c.check(got)
+    for n in ("dq", "dk", "dv"):
+        assert torch.equal(got[n], without[n])
+
+
+@pytest.mark.parametrize("Dh", [32, 64])
 @pytest.mark.parametrize("lens", [[700], [513, 64], [65, 1], [1024]])
 def test_few_long_segments(spa, lens, Dh):
     """Few blocks of queries: the waves of a block share its keys."""
