@@ -249,15 +249,17 @@ __device__ __forceinline__ DsScale ds_scale(const uint32_t* most_h, const int32_
   const bool bad = most >= 0x7f800000u || e > 126;
   return {e, bad ? 0. : power_of_two(kDsBits - e), bad ? NAN : 0.f};
 }
-// A workgroup's histogram of offsets from .. from + slice of its head, as fp32; all threads call it, behind the last add.
+// A workgroup's histogram of `size` offsets of its head from `from` on, around the end, as fp32; all threads call it, behind the last add.
 template <int THREADS>
-__device__ __forceinline__ void write_partial(const unsigned long long* hist, const DsScale& s, int slice, int from, int offsets, float* out) {
+__device__ __forceinline__ void write_partial(const unsigned long long* hist, const DsScale& s, int size, int from, int offsets, float* out) {
   __syncthreads();
   const double quantum = power_of_two(s.e - kDsBits);
-  for (int i = threadIdx.x; i < min(slice, offsets - from); i += THREADS) out[from + i] = s.unit + (float)((double)(long long)hist[i] * quantum);
+  for (int i = threadIdx.x; i < size; i += THREADS)
+    out[from + i - (from + i < offsets ? 0 : offsets)] = s.unit + (float)((double)(long long)hist[i] * quantum);
   __syncthreads();
 }
 
+constexpr int kLaterBlocks = 32;
 template <typename T, int DH, int RW, int SPLIT>
 struct KeyTiles {
   static constexpr int RS = Ops<T, DH>::RS;
@@ -271,6 +273,7 @@ struct KeyTiles {
   int own[RW][2];
   uint32_t most[RW * SPLIT];
   typename WindowFill<T, kBiasThreads>::Raw row[kTableLds];
+  unsigned long long later[kLaterBlocks];
   KeyBlocks blocks;
 };
 
@@ -302,7 +305,9 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
 
   const int passes = HIST == kHistSlices ? (a.m.offsets + a.slice - 1) / a.slice : 1;
   for (int pass = 0; pass < passes; ++pass) {
-    const int from = HIST == kHistSlices ? pass * a.slice : 0;
+    // slices: the first around the middle, where most pairs are, the others go on from there and around the end
+    const int E = a.m.offsets, size = HIST == kHistSlices ? min(a.slice, E - pass * a.slice) : E;
+    const int start = (E - a.slice) / 2 + pass * a.slice, from = HIST == kHistSlices ? (start < E ? start : start - E) : 0;
     if (HIST != kHistNone) {
       for (int i = tid; i < a.slice; i += THREADS) hist[i] = 0;
       // (in front of the first add there is the barrier behind a block's first tile)
@@ -313,8 +318,23 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
       if (item >= l.blocks.all) break;
       const KeyBlock kb = key_block(l.blocks, a.cu, a.B, ROWS, a.key_blocks, item);
       if (kb.k0 >= kb.n) continue;
-      const int n = kb.n, last = n - 1, ki = kb.k0 + wv * 32 + l32;
+      const int n = kb.n, last = n - 1, ki = kb.k0 + wv * 32 + l32, nt = (n + BN - 1) / BN;
       const bool wave_live = kb.k0 + wv * 32 < n, k_ok = ki < n;
+      // which tiles the first pass left something of (one bit each; longer segments and later blocks: any)
+      const bool listed = HIST == kHistSlices && nt <= 64 && round < kLaterBlocks;
+      unsigned long long todo = ~0ull;
+      if (listed && pass > 0) {
+        todo = l.later[round];
+        todo = (unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)(todo >> 32)) << 32 |
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)todo);
+        if (todo == 0) continue;
+      }
+      auto next_tile = [&](int t) -> int {
+        if (HIST != kHistSlices || !listed || pass == 0) return t + 1;
+        const unsigned long long rest = t < 0 ? todo : todo & ~((2ull << t) - 1);
+        return rest != 0 ? __builtin_ctzll(rest) : nt;
+      };
+      unsigned long long left_over = 0;
       const long k_row = kb.row0 + min(ki, last);
       RowPair<T, DH, kBiasThreads, BN> st(tid, a.q + h * DH, a.qs, a.dout + h * DH, C, kb.row0, last);
       const BiasTokens tokens(a.m, a.cu, kb.row0);
@@ -342,7 +362,8 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
         }
       };
       const int own_token = tokens.load(min(ki, last));
-      load_tile(0);
+      int t = next_tile(-1);
+      load_tile(t * BN);
       const typename O::Row kf = O::row(a.k + k_row * a.ks + h * DH, hh), vf = O::row(a.v + k_row * a.vs + h * DH, hh);
       const int own = tokens.position(a.m, own_token, min(ki, last));
       __syncthreads();                                        // every wave is past its last read of the tiles before
@@ -352,16 +373,16 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) dka[d][r] = dva[d][r] = 0.f;
-      store_tile(0, 0, std::true_type{});
+      store_tile(0, t * BN, std::true_type{});
       __syncthreads();
       const Range mine = RANGES ? whole_range(l.own) : Range{0, 0};
       int base = -0x40000000;
-      const int nt = (n + BN - 1) / BN;
-      for (int t = 0; t < nt; ++t) {
-        const int buf = t & 1, qt = t * BN;
-        const bool end = t + 1 == nt;
-        if (!end) load_tile(qt + BN);
+      for (int step = 0; t < nt; ++step) {
+        const int buf = (HIST == kHistSlices ? step : t) & 1, qt = t * BN, next = next_tile(t);
+        const bool end = next >= nt;
+        if (!end) load_tile(next * BN);
         bool in_window = true, adds = HIST != kHistNone, inside = true;
+        int wrap = 0;                                         // of the tile's offsets, where they are inside around the end
         if (RANGES) {
           const Range tile = whole_range(l.range[buf]);
           const int lo = tile.lo - mine.hi, hi = tile.hi - mine.lo;
@@ -375,8 +396,10 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
             }
           }
           if (HIST == kHistSlices) {
-            adds = hi >= from && lo < from + a.slice;
-            inside = lo >= from && hi < from + a.slice;
+            wrap = hi + E < from + size ? E : 0;
+            inside = wrap != 0 || (lo >= from && hi < from + size);
+            adds = (hi >= from && lo < from + size) || lo + E < from + size;
+            if (!inside && t < 64) left_over |= 1ull << t;
           }
         }
         if (wave_live && (pass == 0 || adds)) {
@@ -418,7 +441,7 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
               O::outer(dka, l.Q[buf], sb, dp, lane);
             }
             if (HIST != kHistNone && adds && k_ok) {
-              const int to = lds_address(hist) - 8 * (own + from);
+              const int to = lds_address(hist) - 8 * (own + from - wrap);
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
                 const intx4 p = *reinterpret_cast<const intx4*>(&pos[8 * g + 4 * hh]);
@@ -426,18 +449,20 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
                 for (int i = 0; i < 4; ++i) {
                   const unsigned long long v = ds_integer(dp[4 * g + i], scale.factor);
                   if (HIST == kHistWhole || inside) lds_add(p[i] * (8 / WB) + to, v);
-                  else if ((unsigned)(p[i] / WB - own - from) < (unsigned)a.slice) lds_add(p[i] * (8 / WB) + to, v);
+                  else if (const int at = p[i] / WB - own - from; at + (at < 0 ? E : 0) < size) lds_add(lds_address(hist) + 8 * (at + (at < 0 ? E : 0)), v);
                 }
               }
             }
           }
         }
         if (!end) {
-          if (t + 2 == nt) store_tile(buf ^ 1, qt + BN, std::true_type{});
-          else store_tile(buf ^ 1, qt + BN, std::false_type{});
+          if (next + 1 == nt) store_tile(buf ^ 1, next * BN, std::true_type{});
+          else store_tile(buf ^ 1, next * BN, std::false_type{});
           __syncthreads();
         }
+        t = next;
       }
+      if (listed && pass == 0 && tid == 0) l.later[round] = left_over;
       if (pass == 0) {
         if constexpr (SPLIT > 1) {
           static_assert(RW * DB * 8 * kWave * sizeof(float) <= sizeof(l.Q) + sizeof(l.G), "half a sum of the waves");
@@ -468,7 +493,7 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
         }
       }
     }
-    if (HIST != kHistNone) write_partial<THREADS>(hist, scale, a.slice, from, a.m.offsets, a.partial + ((long)h * a.groups + group) * a.m.offsets);
+    if (HIST != kHistNone) write_partial<THREADS>(hist, scale, size, from, E, a.partial + ((long)h * a.groups + group) * a.m.offsets);
   }
 }
 
