@@ -405,12 +405,10 @@ __global__ void __launch_bounds__(kNormThreads) norm_residual_bwd_kernel(const N
   const int grp = threadIdx.x / G, gl = threadIdx.x % G, chunks = a.C / VE;
   const long M = a.total != nullptr ? min((long)max(*a.total, 0), a.cap) : a.cap;
   const float inv_c = 1.0f / (float)a.C;
-  // scores of the tokens that were not selected: no gradient
-  if (a.d_scores != nullptr && a.inv_pos != nullptr)
-    for (long i = (long)blockIdx.x * kNormThreads + threadIdx.x; i < a.n; i += (long)gridDim.x * kNormThreads) {
-      const int j = a.inv_pos[i];
-      if (j < 0 || j >= M) a.d_scores[i] = 0.f;
-    }
+  // scores of the tokens that were not selected: no gradient (asked for here, written behind the rows: nothing waits in between)
+  const bool zeroes = a.d_scores != nullptr && a.inv_pos != nullptr;
+  const long token = (long)blockIdx.x * kNormThreads + threadIdx.x;
+  const int its = zeroes && token < a.n ? a.inv_pos[token] : 0;
   typename Row::Raw gr[IT], br[IT], sr[IT];
   Row::load(a.gamma, gl, chunks, a.gamma != nullptr, gr);
   Row::load(a.beta, gl, chunks, a.beta != nullptr, br);
@@ -427,7 +425,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_residual_bwd_kernel(const N
   auto ask = [&](long base) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (a.gather_idx != nullptr) next[u] = a.gather_idx[max(min(base + u * kGroups + grp, M - 1), 0L)];
+      if (a.gather_idx != nullptr) next[u] = a.gather_idx[min(base + u * kGroups + grp, a.cap - 1)];      // (does not wait for M)
   };
   ask((long)blockIdx.x * kGroups * U);
   for (long base = (long)blockIdx.x * kGroups * U; base < M; base += step) {
@@ -449,7 +447,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_residual_bwd_kernel(const N
       Row::load(a.grad + i[u] * a.C, gl, chunks, ok[u], dr[u]);
       mu[u] = !RMS ? a.stats[j[u]] : 0.f;
       r[u] = a.stats[a.cap + j[u]];
-      s[u] = a.gate != nullptr ? a.gate[i[u]] : 0.f;
+      s[u] = a.gate != nullptr && ok[u] ? a.gate[i[u]] : 0.f;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -496,6 +494,13 @@ __global__ void __launch_bounds__(kNormThreads) norm_residual_bwd_kernel(const N
           if (ch < chunks) Row::store(a.out + j[u] * a.C, ch, o);
         }
       }
+    }
+  }
+  if (zeroes) {
+    int j = its;
+    for (long i = token; i < a.n; i += (long)gridDim.x * kNormThreads) {
+      if (i != token) j = a.inv_pos[i];
+      if (j < 0 || j >= M) a.d_scores[i] = 0.f;
     }
   }
   norm_fold<T, G, IT>(A, a.C, a.partial, lds);
