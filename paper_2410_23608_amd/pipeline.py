@@ -514,6 +514,122 @@ class BlockTrainPass(_Pass):
         return self.loss
 
 
+class NormBlockPass(_Pass):
+    """One SPA block of the kind that normalises its branch on both sides and knows where its tokens are:
+
+      gate_select(x) -> pack (indices only) -> norm of the selected tokens -> QKV projection -> packed attention with a bias by
+      relative position -> output projection -> y = x + Sigmoid(s) * scale * norm(projection) at the selected tokens, y = x elsewhere.
+
+    grid: the map whose tokens an image has (N = grid[0] * grid[1]); rms: norms without mean and (if the caller gives none) without
+    shift; buckets: the int32 bucket of every offset (`spa.relative_position_buckets`), None: table has an entry per offset.
+    run() takes the parameters anew every time; gamma, beta and scale may be None."""
+
+    def __init__(self, B: int, grid: Tuple[int, int], C: int, H: int, dtype: str, tau: float = 0.5, bias: float = 0.0,
+                 rms: bool = False, eps: float = 1e-6, buckets: Optional[torch.Tensor] = None):
+        N = grid[0] * grid[1]
+        self.B, self.N, self.grid, self.C, self.H, self.Dh = B, N, tuple(grid), C, H, C // H
+        self.tau, self.bias, self.eps, self.buckets = tau, bias, eps, buckets
+        self.norm = spa.SPA_NORM_RMS if rms else spa.SPA_NORM_LAYER
+        td, cap = _td(dtype), B * N
+        dv = dict(device="cuda")
+        self.scores = torch.empty(B, N, dtype=torch.float32, **dv)
+        self.mask = torch.empty(B, N, dtype=torch.uint8, **dv)
+        self.cu_seqlens = torch.zeros(B + 1, dtype=torch.int32, **dv)
+        self.gather_idx = torch.zeros(cap, dtype=torch.int32, **dv)
+        self.inv_pos = torch.zeros(cap, dtype=torch.int32, **dv)
+        self.total = torch.zeros(1, dtype=torch.int32, **dv)
+        self.normed = torch.zeros(cap, C, dtype=td, **dv)
+        self.packed_qkv = torch.zeros(cap, 3 * C, dtype=td, **dv)
+        self.attn = torch.zeros(cap, C, dtype=td, **dv)
+        self.z = torch.zeros(cap, C, dtype=td, **dv)
+        self.y = torch.empty(B, N, C, dtype=td, **dv)
+        self.stats_in = self.stats_out = self.lse = None          # kept for a backward
+
+    def stages(self, x, w, gamma_in, beta_in, W_qkv, b_qkv, table, W_o, b_o, gamma_out, beta_out, scale) -> List[Tuple[str, Callable[[], None]]]:
+        C, p = self.C, self.packed_qkv
+        return [
+            ("gate_select", spa.spa_gate_select(x, w, self.bias, None, self.tau, self.scores, self.mask, None, prepare=True)),
+            ("pack_indices", spa.spa_pack(None, self.mask, None, None, 0, None, self.cu_seqlens, self.gather_idx, self.inv_pos,
+                                          self.total, prepare=True)),
+            ("norm_packed", spa.spa_norm_packed(x, self.gather_idx, self.total, gamma_in, beta_in, self.norm, self.eps, self.normed,
+                                                self.stats_in, prepare=True)),
+            ("qkv_projection", spa.spa_linear_packed(self.normed, None, None, self.total, W_qkv, b_qkv, p, prepare=True)),
+            ("packed_attention_bias", spa.spa_packed_attention_bias(
+                p[:, :C], p[:, C:2 * C], p[:, 2 * C:], self.cu_seqlens, self.gather_idx, table, self.buckets, self.grid, self.B, self.N,
+                self.H, self.Dh, self.attn, self.lse, prepare=True)),
+            ("out_projection", spa.spa_linear_packed(self.attn, None, None, self.total, W_o, b_o, self.z, prepare=True)),
+            ("norm_residual_unpack", spa.spa_norm_residual_unpack(self.z, self.inv_pos, x, gamma_out, beta_out, scale, self.scores,
+                                                                  self.norm, self.eps, self.y, self.stats_out, prepare=True)),
+        ]
+
+    def run(self, x, w, gamma_in, beta_in, W_qkv, b_qkv, table, W_o, b_o, gamma_out, beta_out, scale):
+        self._issue(x, w, gamma_in, beta_in, W_qkv, b_qkv, table, W_o, b_o, gamma_out, beta_out, scale)
+        return self.y
+
+
+class NormBlockTrainPass(NormBlockPass):
+    """Forward + backward of a NormBlockPass block with the selection loss.  Results: dx (the residual path, the norm's and the
+    gate's gradients, all of it), dw, db, d_gamma_in, d_beta_in, dW_qkv, db_qkv, d_table, dW_o, db_o, d_gamma_out, d_beta_out,
+    d_scale (fp32), loss and y."""
+
+    def __init__(self, B: int, grid: Tuple[int, int], C: int, H: int, dtype: str, tau: float = 0.5, bias: float = 0.0,
+                 rms: bool = False, eps: float = 1e-6, buckets: Optional[torch.Tensor] = None, n_buckets: Optional[int] = None,
+                 loss_scale: Optional[float] = None):
+        super().__init__(B, grid, C, H, dtype, tau, bias, rms, eps, buckets)
+        N, td, cap = self.N, _td(dtype), B * self.N
+        if buckets is not None and n_buckets is None:
+            raise ValueError("NormBlockTrainPass: n_buckets must be given with buckets")
+        self.loss_scale = 0.01 / cap if loss_scale is None else loss_scale
+        code = spa.SPA_BF16 if dtype == "bf16" else spa.SPA_F32
+        f32 = dict(dtype=torch.float32, device="cuda")
+        entries = (2 * grid[0] - 1) * (2 * grid[1] - 1) if buckets is None else n_buckets
+        self.stats_in, self.stats_out, self.lse = torch.zeros(2, cap, **f32), torch.zeros(2, cap, **f32), torch.zeros(H, cap, **f32)
+        rows = lambda width: torch.zeros(cap, width, dtype=td, device="cuda")
+        self.dz, self.d_attn, self.d_qkv, self.d_normed = rows(C), rows(C), rows(3 * C), rows(C)
+        self.dx = torch.empty(B, N, C, dtype=td, device="cuda")
+        self.d_scores, self.d_table = torch.empty(B, N, **f32), torch.empty(H, entries, **f32)
+        self.dW_qkv, self.db_qkv = torch.empty(3 * C, C, **f32), torch.empty(3 * C, **f32)
+        self.dW_o, self.db_o = torch.empty(C, C, **f32), torch.empty(C, **f32)
+        self.d_gamma_in, self.d_beta_in, self.d_gamma_out, self.d_beta_out, self.d_scale, self.dw = (torch.empty(C, **f32) for _ in range(6))
+        self.db, self.loss = torch.empty(1, **f32), torch.empty(1, **f32)
+        u8 = lambda n: torch.empty(max(n, 256), dtype=torch.uint8, device="cuda")
+        self.ws_norm = u8(spa.spa_norm_bwd_workspace_bytes(cap, C, code))
+        self.ws_attn = u8(spa.spa_attention_bias_bwd_workspace_bytes(B, N, H, self.Dh, *self.grid, code))
+        self.ws_gate = u8(spa.spa_gate_bwd_workspace_bytes(B, N, C, code))
+        self.ws_qkv = u8(spa.spa_linear_bwd_weight_workspace_bytes(cap, C, 3 * C, dtype))
+        self.ws_o = u8(spa.spa_linear_bwd_weight_workspace_bytes(cap, C, C, dtype))
+
+    def stages(self, x, w, gamma_in, beta_in, W_qkv, b_qkv, table, W_o, b_o, gamma_out, beta_out, scale, labels, dy):
+        C, cap, p, dp, given = self.C, self.B * self.N, self.packed_qkv, self.d_qkv, lambda param, grad: None if param is None else grad
+        return super().stages(x, w, gamma_in, beta_in, W_qkv, b_qkv, table, W_o, b_o, gamma_out, beta_out, scale) + [
+            ("norm_residual_unpack_bwd", spa.spa_norm_residual_unpack_bwd(
+                dy, self.z, self.gather_idx, self.inv_pos, self.total, gamma_out, beta_out, scale, self.scores, self.norm, self.stats_out,
+                self.dz, self.d_scores, given(gamma_out, self.d_gamma_out), given(beta_out, self.d_beta_out), given(scale, self.d_scale),
+                self.ws_norm, prepare=True)),
+            ("out_projection_bwd_input", spa.spa_linear_packed_bwd_input(self.dz, None, self.total, W_o, cap, None, None, self.d_attn,
+                                                                         prepare=True)),
+            ("out_projection_bwd_weight", spa.spa_linear_packed_bwd_weight(self.dz, None, self.attn, None, None, self.total, cap,
+                                                                           self.dW_o, self.db_o, self.ws_o, prepare=True)),
+            ("packed_attention_bias_bwd", spa.spa_packed_attention_bias_bwd(
+                p[:, :C], p[:, C:2 * C], p[:, 2 * C:], self.attn, self.d_attn, self.lse, self.cu_seqlens, self.gather_idx, table,
+                self.buckets, self.grid, self.B, self.N, self.H, self.Dh, dp[:, :C], dp[:, C:2 * C], dp[:, 2 * C:], self.d_table,
+                self.ws_attn, prepare=True)),
+            ("qkv_projection_bwd_input", spa.spa_linear_packed_bwd_input(dp, None, self.total, W_qkv, cap, None, None, self.d_normed,
+                                                                         prepare=True)),
+            ("qkv_projection_bwd_weight", spa.spa_linear_packed_bwd_weight(dp, None, self.normed, None, None, self.total, cap,
+                                                                           self.dW_qkv, self.db_qkv, self.ws_qkv, prepare=True)),
+            ("norm_packed_bwd", spa.spa_norm_packed_bwd(self.d_normed, x, self.inv_pos, self.total, gamma_in, self.norm, self.stats_in, dy,
+                                                        self.dx, given(gamma_in, self.d_gamma_in), given(beta_in, self.d_beta_in),
+                                                        self.ws_norm, prepare=True)),
+            ("gate_bwd", spa.spa_gate_bwd_scores(x, w, self.bias, self.scores, None, labels, self.d_scores, self.dx, self.loss_scale,
+                                                 self.loss, self.dx, self.dw, self.db, self.ws_gate, prepare=True)),
+        ]
+
+    def run(self, x, w, gamma_in, beta_in, W_qkv, b_qkv, table, W_o, b_o, gamma_out, beta_out, scale, labels, dy):
+        self._issue(x, w, gamma_in, beta_in, W_qkv, b_qkv, table, W_o, b_o, gamma_out, beta_out, scale, labels, dy)
+        return self.loss
+
+
 class ContainerForwardPass(_Pass):
     """The forward pass with the paper's container mask (Section 3.2 "Token Packing"): the
     packed stream is cut into containers of length L and a token attends to the tokens of its
