@@ -317,7 +317,8 @@ int spa_packed_attention_running_max(const void* q, const void* k, const void* v
  * in:  q, k, v, strides, cu_seqlens, max_seqlen, softmax_scale as in spa_packed_attention, max_seqlen <= grid_h*grid_w;
  *      table [H, n_buckets] dtype; buckets [(2 grid_h - 1)(2 grid_w - 1)] int32 (16-byte aligned), or NULL: a bucket per offset (n_buckets is
  *      their number); sequences without a second axis: grid_h = 1.
- * out: out, lse as in spa_packed_attention.
+ * out: out, lse as in spa_packed_attention.  The bits are the same in every run; the order in which a row's keys are added
+ *      follows from dtype, Dh, H, B, max_seqlen and the size of the map.
  */
 int spa_packed_attention_bias(const void* q, const void* k, const void* v, int64_t q_row_stride, int64_t k_row_stride,
                               int64_t v_row_stride, const int32_t* cu_seqlens, const int32_t* gather_idx, const void* table,
@@ -680,8 +681,8 @@ size_t spa_attention_bias_bwd_workspace_bytes(int B, int max_seqlen, int H, int 
  *   d_table[h, b] = sum of dS_ij over the pairs (i, j) whose offset is in bucket b,   dS = P (dP - D)
  * D_i is sum_d dO_id O_id from the rounded out for dq; for d_table (and dk) what the row's dS then still add up to, which is the
  * error of that D, is taken off, so that d_table is good to fp32 from bf16 rows too.
- * in:  as in the forward, with its out and lse; dout [>= T, H*Dh] dtype contiguous; workspace (device, 256-byte aligned) of at least spa_attention_bias_bwd_workspace_bytes bytes, contents
- *      of no account.
+ * in:  as in the forward, with its out and lse; dout [>= T, H*Dh] dtype contiguous; workspace (device, 256-byte aligned) of at
+ *      least spa_attention_bias_bwd_workspace_bytes bytes, contents of no account.
  * out: dq, dk, dv as in spa_packed_attention_bwd (rows >= T are not written); d_table [H, n_buckets] fp32 or NULL: added in
  *      integers finer than 2^-30 of the largest dS a head can have, in any order the same.  All results run-to-run
  *      bit-stable.  A head with a gradient, value or score that is not a finite number (-inf scores aside) has NaN in its row

@@ -48,6 +48,9 @@ struct BiasBwd {
   int key_blocks, groups, slice;  // dk / dv: blocks of keys of the longest possible segment, workgroups a head, offsets of a histogram
 };
 
+// The dq launch: bound by the vector instructions like the forward (0.63 of the busy units' cycles at 16 images of 0.1 to 0.6 of 3136
+// tokens, 3 heads of 32, two waves a SIMD by registers), 51 us there; 26 at 64 images of 196, 12 heads of 64.  A block of eight waves
+// holds no more waves a unit, so only few blocks get it.
 template <typename T, int DH, int WIN, int SPLIT>
 __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(const BiasBwd<T> a) {
   using O = Ops<T, DH>;
@@ -278,7 +281,9 @@ struct KeyTiles {
 };
 
 // RW waves own 32 keys each.  SPLIT 2: the waves come twice, the second ones take the second half of every tile of 64 queries, and hand
-// their sums to the first at the end of a block.
+// their sums to the first at the end of a block.  Bound by latency and LDS together: a block's chain (look-ups, products, exponentials,
+// products, 16 atomic adds) runs on two or three waves a SIMD, LDS is busy 0.54 of the time (half of it the adds, for the offsets of
+// a wave's keys meet in banks).  us: 76 at 16 images of 0.1 to 0.6 of 3136 tokens, 3 heads of 32; 32 at 64 of 196, 12 heads of 64.
 template <typename T, int DH, int WIN, int RW, int SPLIT, int HIST>
 __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(const BiasBwd<T> a) {
   using O = Ops<T, DH>;
@@ -497,7 +502,8 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
   }
 }
 
-// The sums over the workgroups, in their order: 32 offsets a workgroup, eight slices of the rows beside each other.
+// The sums over the workgroups, in their order: 32 offsets a workgroup, eight slices of the rows beside each other, each with eight
+// loads in flight (85 workgroups x 12321 offsets x 3 heads, 12.6 MB: 6.2 us; a row at a time 8.3).
 struct BiasSum {
   const float* partial;
   int groups, offsets;
