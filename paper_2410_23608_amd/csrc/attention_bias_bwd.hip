@@ -603,7 +603,8 @@ __global__ void __launch_bounds__(1024) attn_bias_table_kernel(const BiasTable a
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // The dk / dv launch.  Two workgroups a unit where that leaves each room for the whole map in LDS; else one, of eight waves in
-// bf16, with as much of the histogram as fits.  As many workgroups a head as are resident together, no more than there are blocks of keys,
+// bf16, with as much of the histogram as fits.  Few blocks take eight waves there too (us backward, four | eight waves, heads of 32,
+// 28 x 28 map: one image of 700 tokens, 8 heads, 47.8 | 41.1, four 50.6 | 43.5).  As many workgroups a head as are resident together, no more than there are blocks of keys,
 // and no more than 256 MB of partial sums.
 struct BiasPlan {
   bool whole;                     // the window
@@ -623,12 +624,12 @@ static BiasPlan bias_plan_of(int H, int B, int n_max, long offsets) {
   p.window = window_bytes(p.whole ? (int)offsets : kWindow, sizeof(T));
   size_t tiles = sizeof(KeyTiles<T, DH, 4, 1>);
   const bool two = p.whole && tiles + p.window + all * 8 <= most / 2;
-  p.split = sizeof(T) == 2 && p.whole && !two ? 2 : 1;
+  const int nblk = (n_max + kBiasRows - 1) / kBiasRows;
+  p.split = sizeof(T) == 2 && p.whole && (!two || few_blocks(nblk, H, B)) ? 2 : 1;
   if (p.split == 2) tiles = sizeof(KeyTiles<T, DH, kSplitRows<DH>, 2>);
   p.slice = (int)std::min<long>(all, (long)(most - tiles - p.window) / 8 / 64 * 64);
   p.lds = p.window + (size_t)p.slice * 8;
-  const bool many = (long)H * B * ((n_max + kBiasRows - 1) / kBiasRows) >= 1024;
-  p.rows = p.split == 2 && p.slice == all && many ? kSplitRows<DH> : 4;
+  p.rows = p.split == 2 && p.slice == all && (long)H * B * nblk >= 1024 ? kSplitRows<DH> : 4;
   p.key_blocks = (n_max + 32 * p.rows - 1) / (32 * p.rows);
   const long fit = std::max<long>(1, (256L << 20) / (4 * H * offsets));
   p.groups = (int)std::max<long>(1, std::min<long>(std::min<long>((two ? 512 : 256) / H, (long)B * p.key_blocks), fit));
