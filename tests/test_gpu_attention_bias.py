@@ -361,3 +361,61 @@ def test_large_and_sparse_maps(spa):
     for grid, lens in (((300, 300), [150, 40]), ((1, 20000), [400, 90])):
         c = Case(lens, grid, 2, 32, "bf16", seed=13, buckets="log")
         c.check(c.run(spa))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("grid,lens", [((9, 8), [72, 30]), ((30, 31), [400, 65]), ((60, 61), [300, 129])])
+def test_a_bucket_of_its_own_for_every_offset(spa, grid, lens, dtype):
+    """A map that only renames the offsets: the results are those without a map, in the renamed places.  d_table by way of a map is rounded
+    once more, to a unit of 2^-40 of the power of two above the largest sum: 2^-40 of it at most, and its own last place."""
+    c = Case(lens, grid, 2, 32, dtype, seed=22)
+    plain = c.run(spa)
+    E = c.nb
+    name = torch.randperm(E, generator=torch.Generator().manual_seed(3))
+    table = torch.empty_like(c.table)
+    table[:, name] = c.table
+    c.table, c.buckets, c.map = table, name.int(), name
+    got = c.run(spa)
+    for n in ("out", "lse", "dq", "dk", "dv"):
+        assert torch.equal(got[n], plain[n]), n
+    a, b = got["d_table"].cpu().double()[:, name], plain["d_table"].cpu().double()
+    tol = 2.0 ** -40 * b.abs().amax(1, keepdim=True) + 2 * U * b.abs()
+    assert bool(((a - b).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("where", ["v", "dout"])
+def test_a_head_that_is_not_finite_says_so_in_fp32(spa, where):
+    c = Case([50, 80], (10, 10), 2, 32, "f32", seed=23, buckets="log")
+    clean = c.run(spa)
+    if where == "dout":
+        c.dout[60, 3] = math.inf
+    else:
+        c.qkv[60, 2 * c.C + 3] = math.nan
+    got = c.run(spa)
+    assert bool(got["d_table"][0].isnan().all()) and torch.equal(got["d_table"][1], clean["d_table"][1])
+
+
+def test_more_than_one_head_row_and_strides_of_their_own(spa):
+    """q, k, v and their gradients in buffers of different widths, what lies between the rows untouched; 70 heads."""
+    H, Dh, lens, grid = 70, 32, [40, 33, 1], (7, 9)
+    c = Case(lens, grid, H, Dh, "bf16", seed=24)
+    want = c.run(spa)
+    C, B, rows = c.C, c.B, c.rows
+    wide = [torch.full((rows, C + 8 * (i + 1)), 3.0, dtype=torch.bfloat16, device="cuda") for i in range(3)]
+    q, k, v = (w[:, 8 * i:8 * i + C] for i, w in enumerate(wide))
+    for i, t in enumerate((q, k, v)):
+        t.copy_(c.qkv[:, i * C:(i + 1) * C])
+    args = (c.cu.cuda(), c.gidx.cuda(), c.table.cuda(), None, grid, B, c.n_max, H, Dh)
+    out, lse = torch.full((rows, C), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((H, B * c.n_max), 7.0, device="cuda")
+    spa.spa_packed_attention_bias(q, k, v, *args, out, lse)
+    gw = [torch.full((rows, C + 8 * (3 - i)), 5.0, dtype=torch.bfloat16, device="cuda") for i in range(3)]
+    dq, dk, dv = (w[:, 8:8 + C] for w in gw)
+    d_table = torch.empty(H, c.nb, device="cuda")
+    ws = torch.empty(spa.spa_attention_bias_bwd_workspace_bytes(B, c.n_max, H, Dh, *grid, spa.SPA_BF16), dtype=torch.uint8, device="cuda")
+    spa.spa_packed_attention_bias_bwd(q, k, v, out, c.dout.cuda(), lse, *args, dq, dk, dv, d_table, ws)
+    for n, t in (("out", out), ("lse", lse), ("d_table", d_table)):
+        assert torch.equal(t, want[n]), n
+    for n, t in (("dq", dq), ("dk", dk), ("dv", dv)):
+        assert torch.equal(t[:c.T], want[n][:c.T]), n
+        assert bool((t[c.T:] == 5.0).all()), n
+    assert all(bool((w[:, :8] == 5.0).all()) and bool((w[:, 8 + C:] == 5.0).all()) for w in gw)
