@@ -561,7 +561,8 @@ __global__ void __launch_bounds__(16 * SL) norm_reduce_kernel(const NormReduceAr
 // The kernel shape of a row length: lanes a row and chunks a lane so that few lanes are without a chunk, up to 4 chunks a
 // lane (8 fp32) where the waves of a workgroup share a row.  U rows of a group in flight.  The backward's launch us at 12544 bf16 rows
 // of 768, in front | behind: 14.8 | 14.8; with twice the rows in flight 20.3 | 15.1 (fewer waves fit), with eight waves a
-// workgroup 18.4 | 18.0.
+// workgroup 18.4 | 18.0.  Three chunks a lane: 64 lanes for up to 192 chunks (forward behind, 100 MB of 1536 bf16 46.7 -> 39.8, backward 46.5 ->
+// 33.0 against four chunks).
 template <typename T, class F>
 static int norm_shape(const char* fn, int C, F go) {
   const int chunks = C / Vec16<T>::kElems;
@@ -572,8 +573,9 @@ static int norm_shape(const char* fn, int C, F go) {
   if (chunks <= 64) SPA_SHAPE(32, 2, 2);
   if (chunks <= 96) SPA_SHAPE(32, 3, 2);
   if (chunks <= 128) SPA_SHAPE(64, 2, 2);
+  if (chunks <= 192) SPA_SHAPE(64, 3, 1);
   if (chunks <= 256) SPA_SHAPE(64, 4, 1);
-  if (chunks <= 512) SPA_SHAPE(256, 2, 1);
+  if (chunks <= 512) SPA_SHAPE(256, 2, 2);
   if (chunks <= 1024) SPA_SHAPE(256, 4, 1);
   if constexpr (sizeof(T) == 4)
     if (chunks <= 2048) SPA_SHAPE(256, 8, 1);
@@ -594,7 +596,12 @@ static int norm_checks(const char* fn, int kind, int C, int dtype) {
 static bool norm_eps_ok(float eps) { return eps >= 0.f && std::isfinite(eps); }
 
 static unsigned norm_blocks(long rows, int per) { return (unsigned)std::min<long>((rows + per - 1) / per, 4096L); }
-static int norm_parts(long rows) { return (int)std::max<long>(1, std::min<long>((rows + 15) / 16, kNormMaxParts)); }
+// Workgroups of the backward, a partial row each: one for 16 rows, for 4 where a row takes a whole workgroup (us in front | behind, 10 MB
+// of packed rows, for 16 and for 4: 2560 bf16 27 | 27 and 22 | 20, 8192 fp32 47 | 48 and 25 | 21).
+static int norm_parts(long rows, int C, int dtype) {
+  const int each = (long)C * elem_size(dtype) > 256 * 16 ? 4 : 16;
+  return (int)std::max<long>(1, std::min<long>((rows + each - 1) / each, kNormMaxParts));
+}
 
 template <typename T>
 static int launch_norm_fwd(const char* fn, bool behind, int kind, const NormFwdArgs<T>& a, hipStream_t st) {
@@ -615,15 +622,16 @@ static int launch_norm_fwd(const char* fn, bool behind, int kind, const NormFwdA
 template <typename T>
 static int launch_norm_bwd(const char* fn, bool behind, int kind, const NormBwdArgs<T>& a, float* dgamma, float* dbeta, float* dscale,
                            hipStream_t st) {
-  const int parts = norm_parts(behind ? a.cap : a.n);
+  const int parts = norm_parts(behind ? a.cap : a.n, a.C, sizeof(T) == 4 ? SPA_F32 : SPA_BF16);
   const int rc = norm_shape<T>(fn, a.C, [&](auto g, auto it, auto u) {
     constexpr int G = decltype(g)::value, IT = decltype(it)::value, U = decltype(u)::value;
     const size_t lds = G > kWave ? 0 : (size_t)(kNormThreads / kWave) * a.C * sizeof(float);      // at most 32 KB
-#define SPA_NORM(KERNEL, RMS) hipLaunchKernelGGL((KERNEL<T, G, IT, U, RMS>), dim3(parts), dim3(kNormThreads), lds, st, a)
+#define SPA_NORM(KERNEL, ROWS, RMS) hipLaunchKernelGGL((KERNEL<T, G, IT, ROWS, RMS>), dim3(parts), dim3(kNormThreads), lds, st, a)
     if (behind) {
-      if (kind == SPA_NORM_RMS) SPA_NORM(norm_residual_bwd_kernel, true); else SPA_NORM(norm_residual_bwd_kernel, false);
+      constexpr int UB = IT >= 3 ? 1 : U;                     // (two rows of three chunks: 273 registers, one wave a SIMD; 62914 rows of 768: 42.3 us, so 32.6)
+      if (kind == SPA_NORM_RMS) SPA_NORM(norm_residual_bwd_kernel, UB, true); else SPA_NORM(norm_residual_bwd_kernel, UB, false);
     } else {
-      if (kind == SPA_NORM_RMS) SPA_NORM(norm_packed_bwd_kernel, true); else SPA_NORM(norm_packed_bwd_kernel, false);
+      if (kind == SPA_NORM_RMS) SPA_NORM(norm_packed_bwd_kernel, U, true); else SPA_NORM(norm_packed_bwd_kernel, U, false);
     }
 #undef SPA_NORM
     return SPA_OK;
@@ -679,7 +687,7 @@ extern "C" int spa_norm_residual_unpack(const void* z, const int32_t* inv_pos, c
 extern "C" size_t spa_norm_bwd_workspace_bytes(int64_t rows, int C, int dtype) {
   (void)dtype;
   if (rows < 1 || C < 1) return 0;
-  return (size_t)norm_parts((long)rows) * 2 * (size_t)C * sizeof(float);
+  return (size_t)norm_parts((long)rows, C, dtype) * 2 * (size_t)C * sizeof(float);
 }
 
 extern "C" int spa_norm_packed_bwd(const void* d_packed, const void* x, const int32_t* inv_pos, const int32_t* total, const void* gamma,

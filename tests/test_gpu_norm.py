@@ -313,3 +313,16 @@ def test_gate_backward_with_given_score_gradients(spa, shape, dtype, up):
     spa.spa_gate_bwd_scores(*args[:6], zero, None, ls, loss, dx, dw, db, ws)
     for a, b in zip((loss, dx, dw, db), plain):
         assert torch.equal(a, b)
+
+
+WIDE = [(1, 333, 640), (2, 301, 1288), (2, 90, 1536), (2, 150, 2568), (1, 500, 4096)]
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", WIDE)
+def test_wide_rows_in_front_and_behind(spa, shape, dtype, kind):
+    """Rows of one and a half to eight waves' lanes, several a workgroup, an odd number of them."""
+    c = Case(*shape, dtype, kind, 31 + shape[2], frac=0.7)
+    _check_front(c, *_front(spa, c, kind), c.sel, c.T)
+    _check_behind(c, *_behind(spa, c, kind, gate=True), c.sel, c.T, True)
