@@ -10,7 +10,7 @@
 //   dgamma = scale * A,  dbeta = scale * B,  dscale = gamma * A + beta * B
 // follow; every workgroup adds its rows and writes one partial row, a second launch adds those in a fixed order.
 // us a launch, TB/s of the bytes it cannot do without (a large copy: 4.6): 134400 bf16 rows of 256, 22 % of them packed, in front 8.9
-// (3.4) and its backward 29.5 (4.8), behind 27 (5.7); 12544 of 768, half packed, in front 7.5 (2.6) and 14.7 (3.9), behind 12.6 (3.8) and 14.8 (2.0).
+// (3.4) and its backward 29.5 (4.8), behind 27 (5.7); 12544 of 768, half packed, in front 7.5 (2.6) and 14.7 (3.9), behind 12.6 (3.8) and 11.4 (2.5).
 // Small ones are trips to memory: launch, index, rows, and for the backward the fold and the sums' launch of 4 us.
 #include <algorithm>
 #include <cmath>
@@ -560,8 +560,7 @@ __global__ void __launch_bounds__(16 * SL) norm_reduce_kernel(const NormReduceAr
 // ------------------------------------------------------------------------------- host
 // The kernel shape of a row length: lanes a row and chunks a lane so that few lanes are without a chunk, up to 4 chunks a
 // lane (8 fp32) where the waves of a workgroup share a row.  U rows of a group in flight.  The backward's launch us at 12544 bf16 rows
-// of 768, in front | behind: 14.8 | 14.8; with twice the rows in flight 20.3 | 15.1 (fewer waves fit), with eight waves a
-// workgroup 18.4 | 18.0.  Three chunks a lane: 64 lanes for up to 192 chunks (forward behind, 100 MB of 1536 bf16 46.7 -> 39.8, backward 46.5 ->
+// of 768, in front: 14.8; with twice the rows in flight 20.3 (fewer waves fit), with eight waves a workgroup 18.4.  Three chunks a lane: 64 lanes for up to 192 chunks (forward behind, 100 MB of 1536 bf16 46.7 -> 39.8, backward 46.5 ->
 // 33.0 against four chunks).
 template <typename T, class F>
 static int norm_shape(const char* fn, int C, F go) {
