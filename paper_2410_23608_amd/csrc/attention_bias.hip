@@ -57,7 +57,9 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_fwd_kernel(con
         const int blocks = whole || left > 32 ? 2 : 1;        // of 32 keys that exist
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
-          if (whole || sb < blocks) bias_scores<T, DH, WIN, 1>(s[sb], O::row(&K[(sb * 32 + l32) * O::RS], hh), qf, &pos[sb * 32], own, zero, in_window, a.m, h, a.scale, hh);
+          if (whole || sb < blocks)
+            bias_scores<T, DH, WIN, 1>(s[sb], O::row(&K[(sb * 32 + l32) * O::RS], hh), qf, &pos[sb * 32], own, zero, in_window, a.m, h,
+                                       a.scale, hh);
         if (!whole) {
 #pragma unroll
           for (int sb = 0; sb < 2; ++sb)
@@ -147,8 +149,8 @@ static bool fwd_eight(int offsets, int nblk, int H, int B) {
 }
 
 int bias_checks(const char* fn, const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
-                       const int32_t* cu, int B, int n_max, int H, int Dh, int dtype, float softmax_scale, const void* table,
-                       const int32_t* buckets, int n_buckets, const int32_t* gather_idx, int grid_h, int grid_w, BiasMap* m) {
+                const int32_t* cu, int B, int n_max, int H, int Dh, int dtype, float softmax_scale, const void* table,
+                const int32_t* buckets, int n_buckets, const int32_t* gather_idx, int grid_h, int grid_w, BiasMap* m) {
   SPA_REFUSE_IN_GROUP(fn);
   SPA_REQUIRE(q && k && v && cu && table, SPA_ERR_INVALID_ARG, "%s: null pointer", fn);
   SPA_REQUIRE(B >= 1 && n_max >= 1 && H >= 1, SPA_ERR_INVALID_ARG, "%s: B, max_seqlen, H must be >= 1", fn);
@@ -201,7 +203,7 @@ extern "C" int spa_packed_attention_bias(const void* q, const void* k, const voi
   do {                                                                                                                        \
     const BiasFwd<T> args = {(const T*)q, (const T*)k, (const T*)v, (long)q_row_stride, (long)k_row_stride, (long)v_row_stride, \
                              cu_seqlens, m, H, B, nblk, scale, (T*)out, lse, (long)B * max_seqlen};                           \
-    SPA_QUERY_LAUNCH(attn_bias_fwd_kernel, T, D, (fwd_eight<T, D>(m.offsets, nblk, H, B)), args);                                                                       \
+    SPA_QUERY_LAUNCH(attn_bias_fwd_kernel, T, D, (fwd_eight<T, D>(m.offsets, nblk, H, B)), args);                     \
   } while (0)
   if (dtype == SPA_F32) {
     if (Dh == 32) SPA_FWD(float, 32); else SPA_FWD(float, 64);

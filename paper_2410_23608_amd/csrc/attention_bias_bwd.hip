@@ -7,7 +7,7 @@
 //
 // Two launches and the sums behind them.  The dq launch walks the keys for 128 queries a workgroup, as the forward does, and leaves
 // what the second launch needs: the corrected D of every row, and for every block of queries a number that no |dS| of its
-// rows exceeds in that launch.  The dk / dv launch walks the queries for 128 keys, S and dP un-transposed (a lane is a key), so that P
+// rows exceeds in that launch.  The dk / dv launch walks the queries for 128 (or 192) keys, S and dP un-transposed (a lane is a key), so that P
 // and dS are operands in registers again.  There dS goes into a histogram over the offsets in LDS, 64-bit integers: 32 lanes
 // hold 32 keys against one query, so that the lanes of an instruction have offsets of their own.  A workgroup keeps its
 // histogram over all the blocks it takes, of one head, and writes it once, as fp32; the sum over the workgroups has a fixed order.
@@ -262,7 +262,7 @@ __device__ __forceinline__ void write_partial(const unsigned long long* hist, co
   __syncthreads();
 }
 
-constexpr int kLaterBlocks = 32;
+constexpr int kLaterBlocks = 32;                // blocks of a workgroup whose tiles the later slices need are kept
 template <typename T, int DH, int RW, int SPLIT>
 struct KeyTiles {
   static constexpr int RS = Ops<T, DH>::RS;
@@ -454,7 +454,7 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
                 for (int i = 0; i < 4; ++i) {
                   const unsigned long long v = ds_integer(dp[4 * g + i], scale.factor);
                   if (HIST == kHistWhole || inside) lds_add(p[i] * (8 / WB) + to, v);
-                  else if (const int at = p[i] / WB - own - from; at + (at < 0 ? E : 0) < size) lds_add(lds_address(hist) + 8 * (at + (at < 0 ? E : 0)), v);
+                  else if (const int off = p[i] / WB - own - from, at = off + (off < 0 ? E : 0); at < size) lds_add(lds_address(hist) + 8 * at, v);
                 }
               }
             }
@@ -604,8 +604,8 @@ static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // The dk / dv launch.  Two workgroups a unit where that leaves each room for the whole map in LDS; else one, of eight waves in
 // bf16, with as much of the histogram as fits.  Few blocks take eight waves there too (us backward, four | eight waves, heads of 32,
-// 28 x 28 map: one image of 700 tokens, 8 heads, 47.8 | 41.1, four 50.6 | 43.5).  As many workgroups a head as are resident together, no more than there are blocks of keys,
-// and no more than 256 MB of partial sums.
+// 28 x 28 map: one image of 700 tokens, 8 heads, 47.8 | 41.1, four 50.6 | 43.5).  As many workgroups a head as are resident
+// together, no more than there are blocks of keys, and no more than 256 MB of partial sums.
 struct BiasPlan {
   bool whole;                     // the window
   int rows, split, key_blocks, slice, groups;         // rows: waves that own keys

@@ -241,9 +241,11 @@ constexpr int kWholeBytes = 65536, kWindow = 8192;
 
 constexpr int kTableLds = 1024;                // a table row of up to so many entries is brought to LDS where a map picks from it
 
-// The entries of offsets [base, base + n) on their way to the window, 16 bytes of the map (four entries; base must be a multiple of 4 then) or, without
-// a map, of the table's row a time.  start() asks for a thread's first pieces and, of a short row that a map picks from, its part of the row;
-// nothing waits for them before finish(), which all threads call; a barrier follows before the window is read.
+// The entries of offsets [base, base + n) on their way to the window, 16 bytes of the map (four entries; base must be a
+// multiple of 4 then) or, without a map, of the table's row a time.  start() asks for a thread's first pieces and, of a short row
+// that a map picks from, its part of the row; nothing waits for them before finish(), which all threads call; a barrier follows
+// before the window is read.  (Asked for where the window is filled instead, behind the first rows: forward of 64 images of 196 tokens,
+// 12 heads of 64, 18.6 -> 20.2 us.)
 template <typename T, int THREADS>
 struct WindowFill {
   using Raw = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
@@ -427,12 +429,12 @@ struct QueryTiles {
   int s_live[sizeof(LiveTile) / sizeof(int)];
 };
 
-// The walk of such a workgroup over the keys of its segment, SPLIT tiles of 64 a step: staging, positions, the window.  asked(): the workgroup's own loads;
-// arrived(): what is made of them in front of the first tile; work(K, V, pos,
+// The walk of such a workgroup over the keys of its segment, SPLIT tiles of 64 a step: staging, positions, the window.
+// asked(): the workgroup's own loads; arrived(): what is made of them in front of the first tile; work(K, V, pos,
 // rows left in the wave's tile, own position, window, in_window, whole): the wave's tile; whole: all of its 64 keys exist.
 template <typename T, int DH, int WIN, int SPLIT, class Asked, class Arrived, class Staged, class Work>
-__device__ __forceinline__ void walk_keys(QueryTiles<T, DH, SPLIT>& l, void* win, const Segment& seg, int h, bool wave_live, const T* k, long ks, const T* v,
-                                          long vs, const BiasMap& m, const int32_t* cu, int row, Asked asked, Arrived arrived,
+__device__ __forceinline__ void walk_keys(QueryTiles<T, DH, SPLIT>& l, void* win, const Segment& seg, int h, bool wave_live,
+                                          const T* k, long ks, const T* v, long vs, const BiasMap& m, const int32_t* cu, int row, Asked asked, Arrived arrived,
                                           Staged staged, Work work) {
   constexpr int RS = Ops<T, DH>::RS, THREADS = kBiasThreads * SPLIT, STEP = kBiasBN * SPLIT, WB = sizeof(T);
   const int tid = threadIdx.x, n = seg.nk, last = n - 1, part = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;

@@ -560,8 +560,8 @@ __global__ void __launch_bounds__(16 * SL) norm_reduce_kernel(const NormReduceAr
 // ------------------------------------------------------------------------------- host
 // The kernel shape of a row length: lanes a row and chunks a lane so that few lanes are without a chunk, up to 4 chunks a
 // lane (8 fp32) where the waves of a workgroup share a row.  U rows of a group in flight.  The backward's launch us at 12544 bf16 rows
-// of 768, in front: 14.8; with twice the rows in flight 20.3 (fewer waves fit), with eight waves a workgroup 18.4.  Three chunks a lane: 64 lanes for up to 192 chunks (forward behind, 100 MB of 1536 bf16 46.7 -> 39.8, backward 46.5 ->
-// 33.0 against four chunks).
+// of 768, in front: 14.8; with twice the rows in flight 20.3 (fewer waves fit), with eight waves a workgroup 18.4.  Three chunks a
+// lane: 64 lanes for up to 192 chunks (forward behind, 100 MB of 1536 bf16 46.7 -> 39.8, backward 46.5 -> 33.0 against four chunks).
 template <typename T, class F>
 static int norm_shape(const char* fn, int C, F go) {
   const int chunks = C / Vec16<T>::kElems;
@@ -627,7 +627,8 @@ static int launch_norm_bwd(const char* fn, bool behind, int kind, const NormBwdA
     const size_t lds = G > kWave ? 0 : (size_t)(kNormThreads / kWave) * a.C * sizeof(float);      // at most 32 KB
 #define SPA_NORM(KERNEL, ROWS, RMS) hipLaunchKernelGGL((KERNEL<T, G, IT, ROWS, RMS>), dim3(parts), dim3(kNormThreads), lds, st, a)
     if (behind) {
-      constexpr int UB = IT >= 3 ? 1 : U;                     // (two rows of three chunks: 273 registers, one wave a SIMD; 62914 rows of 768: 42.3 us, so 32.6)
+      // (two rows of three chunks take 273 registers, one wave a SIMD: 62914 rows of 768, half of them packed, 42.3 us, so 32.6)
+      constexpr int UB = IT >= 3 ? 1 : U;
       if (kind == SPA_NORM_RMS) SPA_NORM(norm_residual_bwd_kernel, UB, true); else SPA_NORM(norm_residual_bwd_kernel, UB, false);
     } else {
       if (kind == SPA_NORM_RMS) SPA_NORM(norm_packed_bwd_kernel, U, true); else SPA_NORM(norm_packed_bwd_kernel, U, false);
