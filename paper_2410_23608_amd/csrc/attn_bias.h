@@ -10,9 +10,10 @@
 namespace spa {
 
 constexpr float kLog2e = 1.4426950408889634f;
-// Beyond this a score times log2 e is no fp32 number any more (table entries of the type's lowest value, or -inf): such rows take
-// the difference to their maximum before the factor.
-constexpr float kFarScore = 2e38f;
+// exp(s - m) as exp2(s log2 e - m2), m2 = m log2 e rounded, is off by what that rounding is: half a last place of m2, which at -1e10
+// (a mask written into the table) is 2^9, and a row whose first keys are all masked ends as infinity times 0.  Rows whose maximum (lse) is
+// this large or more take the difference before the factor, an instruction more a score; below it P is off by at most 2^-17 of itself.
+constexpr float kFarScore = 128.f;
 // A wave owns 32 rows and a workgroup 128 (eight waves: each row twice, SPLIT 2), the others stream through LDS in tiles of 64.
 constexpr int kBiasBN = 64, kBiasThreads = 256, kBiasRows = 128;
 
