@@ -5,6 +5,10 @@
 // added as integers: dS is rounded to a multiple of 2^-kDsBits of a power of two above every |dS| of the head.  Sums are then the same in
 // any order, and finer than fp32 ones.
 //
+// P = exp(S - lse) adds up to 1 as long as lse holds its own logarithm beside the maximum.  Beside a mask it does not (at -1e9 its last place
+// is 64, and a row of n such keys has log n to add): for rows of |lse| >= kFarScore the dq launch adds up exp(S - lse), at most e^17
+// either way, divides by the sum at its end and leaves the logarithm of it for the other launch's exponent.
+//
 // Two launches and the sums behind them.  The dq launch walks the keys for 128 queries a workgroup, as the forward does, and leaves
 // what the second launch needs: the corrected D of every row, and for every block of queries a number that no |dS| of its
 // rows exceeds in that launch.  The dk / dv launch walks the queries for 128 (or 192) keys, S and dP un-transposed (a lane is a key), so that P
@@ -35,7 +39,7 @@ struct BiasBwd {
   const T *q, *k, *v, *out, *dout;
   long qs, ks, vs;
   const float* lse;
-  float* dvec;
+  floatx2* dvec;                  // [H][lse_stride]: D, log2 of what exp(S - lse) of the row adds up to (far rows, else 0)
   long lse_stride;
   const int32_t* cu;
   BiasMap m;
@@ -73,9 +77,9 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(cons
     for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
   const float lse = a.lse[h * a.lse_stride + q_row];
   const bool none = lse == -INFINITY || !q_ok;                // no score, or no row: probability 0
-  const bool far = __ballot(!none && fabsf(lse) >= kFarScore) != 0;
+  const bool far_row = !none && fabsf(lse) >= kFarScore, far = __ballot(far_row) != 0;
   const float lse2 = none ? INFINITY : lse * kLog2e;
-  float left = 0.f, most = 0.f, v_most = 0.f;                 // sum and largest magnitude of the row's dS; largest |V|
+  float left = 0.f, most = 0.f, v_most = 0.f, all = 0.f;      // sum and largest magnitude of the row's dS; largest |V|; sum of P
   walk_keys<T, DH, WIN, SPLIT>(
       l, win, blk.seg, h, wave_live, a.k, a.ks, a.v, a.vs, a.m, a.cu, qi,
       [&] {
@@ -110,7 +114,10 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(cons
           } else {
             const float ref = none ? INFINITY : lse;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f((s[r] - ref) * kLog2e);
+            for (int r = 0; r < 16; ++r) {
+              s[r] = __builtin_amdgcn_exp2f((s[r] - ref) * kLog2e);
+              all += s[r];
+            }
           }
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
@@ -125,7 +132,7 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(cons
   if (lane == 0) s_most[0][threadIdx.x >> 6] = v_most;
   __syncthreads();
   if constexpr (SPLIT > 1) {
-    constexpr int W = DB * 16 + 2;
+    constexpr int W = DB * 16 + 3;
     static_assert(4 * W * kWave * sizeof(float) <= sizeof(l.K), "the sums of four waves");
     float* other = reinterpret_cast<float*>(&l.K[0][0]) + wv * W * kWave + lane;
     if (part == 1) {
@@ -133,8 +140,9 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(cons
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) other[(d * 16 + r) * kWave] = acc[d][r];
-      other[(W - 2) * kWave] = left;
-      other[(W - 1) * kWave] = most;
+      other[(W - 3) * kWave] = left;
+      other[(W - 2) * kWave] = most;
+      other[(W - 1) * kWave] = all;
     }
     __syncthreads();
     if (part == 0) {
@@ -142,14 +150,18 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(cons
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[d][r] += other[(d * 16 + r) * kWave];
-      left += other[(W - 2) * kWave];
-      most = __builtin_elementwise_maximum(most, other[(W - 1) * kWave]);
+      left += other[(W - 3) * kWave];
+      most = __builtin_elementwise_maximum(most, other[(W - 2) * kWave]);
+      all += other[(W - 1) * kWave];
     }
   }
-  left = sum_across_halves(left);
+  all = sum_across_halves(all);
+  const float inv = far_row ? 1.0f / all : 1.f;
+  left = sum_across_halves(left) * inv;
+  most *= inv;
   if (part == 0) {
-    O::store(acc, a.scale, a.dq + q_row * a.dqs + h * DH, q_ok, hh);
-    if (q_ok && hh == 0) a.dvec[h * a.lse_stride + q_row] = D + left;
+    O::store(acc, a.scale * inv, a.dq + q_row * a.dqs + h * DH, q_ok, hh);
+    if (q_ok && hh == 0) a.dvec[h * a.lse_stride + q_row] = floatx2{D + left, far_row ? log2f(all) : 0.f};
   }
   // |dS| of the other launch: of this one, plus what D moves by, plus what the order of Dh products in dP can make (at most
   // Dh U sum|dO V| in either launch)
@@ -269,7 +281,7 @@ struct KeyTiles {
   __attribute__((aligned(16))) T Q[2][kBiasBN * RS];
   __attribute__((aligned(16))) T G[2][kBiasBN * RS];          // dO
   __attribute__((aligned(16))) float lse[2][kBiasBN];         // +inf: no score, or no row (probability 0)
-  __attribute__((aligned(16))) float lse2[2][kBiasBN];        // times log2 e
+  __attribute__((aligned(16))) float lse2[2][kBiasBN];        // times log2 e; of a tile with far rows: log2 of the sums of their P
   __attribute__((aligned(16))) float negD[2][kBiasBN];
   __attribute__((aligned(16))) int pos[2][kBiasBN];
   int range[2][1][2], far[2];
@@ -298,7 +310,7 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
   const long C = (long)a.H * DH;
   void* win = hist + (HIST != kHistNone ? a.slice : 0);
   const float* lse_h = a.lse + h * a.lse_stride;
-  const float* d_h = a.dvec + h * a.lse_stride;
+  const floatx2* d_h = a.dvec + h * a.lse_stride;
 
   WindowFill<T, THREADS> fill(a.m, h);
   if (WIN == kWinWhole) fill.start(0, a.m.offsets);
@@ -344,7 +356,8 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
       RowPair<T, DH, kBiasThreads, BN> st(tid, a.q + h * DH, a.qs, a.dout + h * DH, C, kb.row0, last);
       const BiasTokens tokens(a.m, a.cu, kb.row0);
       int token = 0, token_j = 0;
-      float lse_t = 0.f, d_t = 0.f;
+      float lse_t = 0.f;
+      floatx2 d_t = {0.f, 0.f};
       auto load_tile = [&](int qt) {
         if (stages) st.load(qt);
         token_j = min(qt + lane, last);
@@ -356,12 +369,12 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
         if (stages) st.template store<clear>(l.Q[buf], l.G[buf]);
         if (tid < BN) {
           const bool none = lse_t == -INFINITY || qt + tid >= n;
+          const bool any = __ballot(!none && fabsf(lse_t) >= kFarScore) != 0;
           l.lse[buf][tid] = none ? INFINITY : lse_t;
-          l.lse2[buf][tid] = none ? INFINITY : lse_t * kLog2e;
-          l.negD[buf][tid] = -d_t;
+          l.lse2[buf][tid] = any ? d_t[1] : none ? INFINITY : lse_t * kLog2e;
+          l.negD[buf][tid] = -d_t[0];
           const int p = tokens.position(a.m, token, token_j) + a.m.centre;
           l.pos[buf][tid] = WB * p;
-          const bool any = __ballot(!none && fabsf(lse_t) >= kFarScore) != 0;
           if (RANGES) put_range(l.range[buf][0], p);
           if (tid == 0) l.far[buf] = any;
         }
@@ -435,8 +448,9 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
                 const floatx4 l4 = *reinterpret_cast<const floatx4*>(&l.lse[buf][sb * 32 + 8 * g + 4 * hh]);
+                const floatx4 a4 = *reinterpret_cast<const floatx4*>(&l.lse2[buf][sb * 32 + 8 * g + 4 * hh]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[4 * g + i] = __builtin_amdgcn_exp2f((s[4 * g + i] - l4[i]) * kLog2e);
+                for (int i = 0; i < 4; ++i) s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i] - l4[i], kLog2e, -a4[i]));
               }
             }
 #pragma unroll
@@ -675,7 +689,7 @@ extern "C" size_t spa_attention_bias_bwd_workspace_bytes(int B, int max_seqlen, 
   const long offsets = (2 * (long)grid_h - 1) * (2 * (long)grid_w - 1);
   const int nblk = (max_seqlen + kBiasRows - 1) / kBiasRows;
   const BiasPlan p = bias_plan(H, B, max_seqlen, Dh, offsets, dtype);
-  return up256((size_t)H * B * max_seqlen * 4) + up256((size_t)H * B * nblk * 4) + up256((size_t)H * p.groups * offsets * 4) +
+  return up256((size_t)H * B * max_seqlen * 8) + up256((size_t)H * B * nblk * 4) + up256((size_t)H * p.groups * offsets * 4) +
          up256((size_t)H * offsets * 4);
 }
 
@@ -714,7 +728,7 @@ extern "C" int spa_packed_attention_bias_bwd(const void* q, const void* k, const
     ws += up256(bytes);
     return at;
   };
-  float* dvec = reinterpret_cast<float*>(take((size_t)H * ls * 4));
+  floatx2* dvec = reinterpret_cast<floatx2*>(take((size_t)H * ls * 8));
   uint32_t* most = reinterpret_cast<uint32_t*>(take((size_t)H * B * nblk * 4));
   float* partial = reinterpret_cast<float*>(take((size_t)H * plan.groups * m.offsets * 4));
   float* sums = buckets != nullptr ? reinterpret_cast<float*>(take((size_t)H * m.offsets * 4)) : d_table;

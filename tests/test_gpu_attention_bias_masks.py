@@ -103,3 +103,13 @@ def test_finite_masks_forward(spa, name, dtype, value):  # noqa: F811
     lens, grid, Dh = SHAPES[name]
     c = Masked(lens, grid, Dh, dtype, value, seed=len(name))
     c.check(c.run(spa, backward=False))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", VALUES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_finite_masks_backward(spa, name, dtype, value):  # noqa: F811
+    lens, grid, Dh = SHAPES[name]
+    c = Masked(lens, grid, Dh, dtype, value, seed=len(name))
+    c.check(c.run(spa))
