@@ -140,11 +140,10 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_fwd_kernel(con
 template <typename T, int DH>
 static bool fwd_eight(int offsets, int nblk, int H, int B) {
   if (few_blocks(nblk, H, B)) return true;
-  constexpr size_t unit = 160 * 1024;
   constexpr int most = DH == 32 ? 16 : 12;                    // by registers
   const size_t win = window_bytes(offsets, sizeof(T));
-  const int four = std::min<int>(most, 4 * (int)(unit / (sizeof(QueryTiles<T, DH, 1>) + win)));
-  const int eight = std::min<int>(most, 8 * (int)(unit / (sizeof(QueryTiles<T, DH, 2>) + win)));
+  const int four = std::min<int>(most, 4 * (int)(kUnitLds / (sizeof(QueryTiles<T, DH, 1>) + win)));
+  const int eight = std::min<int>(most, 8 * (int)(kUnitLds / (sizeof(QueryTiles<T, DH, 2>) + win)));
   return nblk >= 4 && (eight >= 2 * four || (eight > four && xcd_grid(nblk, H, B) <= 2048));
 }
 

@@ -632,7 +632,7 @@ constexpr int kSplitRows = DH == 32 ? 6 : 4;
 template <typename T, int DH>
 static BiasPlan bias_plan_of(int H, int B, int n_max, long offsets) {
   BiasPlan p = {};
-  const size_t most = 160 * 1024;
+  const size_t most = kUnitLds;
   const long all = (offsets + 63) & ~63L;
   p.whole = offsets <= kWholeBytes / (long)sizeof(T);
   p.window = window_bytes(p.whole ? (int)offsets : kWindow, sizeof(T));
@@ -660,7 +660,8 @@ static int launch_bias_bwd(const char* fn, const BiasBwd<T>& args, const BiasPla
   const int H = args.H, B = args.B, nblk = args.nblk;
   SPA_QUERY_LAUNCH(attn_bias_dq_kernel, T, D, few_blocks(nblk, H, B), args);
 #define SPA_DKDV(WIN, RW, SPLIT, MODE)                                                                                          \
-  SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<T, D, WIN, RW, SPLIT, MODE>), H * plan.groups, SPLIT * RW * kWave, hist ? plan.lds : plan.window, args)
+  SPA_BIAS_LAUNCH((attn_bias_dkdv_kernel<T, D, WIN, RW, SPLIT, MODE>), (sizeof(KeyTiles<T, D, RW, SPLIT>)), H * plan.groups,      \
+                  SPLIT * RW * kWave, hist ? plan.lds : plan.window, args)
   const bool slices = plan.slice < m.offsets;
   if (!plan.whole) {
     if (!hist) SPA_DKDV(kWinMoving, 4, 1, kHistNone);

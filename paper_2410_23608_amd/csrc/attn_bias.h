@@ -505,27 +505,33 @@ inline size_t window_bytes(int offsets, int each) { return ((size_t)offsets + 7 
 // the steps.  us forward / backward, four | eight waves, 3 heads of 32, 56 x 56 map: one image of 1792 tokens 37.0 / 110 | 26.4 / 100, of 512
 // 13.4 / 44.7 | 11.2 / 42.5; 64 images of 196 19.5 / 57.5 | 26.5 / 83.0.
 inline bool few_blocks(int nblk, int H, int B) { return nblk >= 4 && xcd_grid(nblk, H, B) <= 256; }
-#define SPA_BIAS_LAUNCH(KERNEL, GRID, THREADS, LDS, ARGS)                                                                      \
+// The kernel's limit of LDS is all that its own arrays (OWN bytes) leave, one value whatever the call: threads that launch with other maps set
+// it too, and a launch must not find a smaller one.
+constexpr size_t kUnitLds = 160 * 1024;
+#define SPA_BIAS_LAUNCH(KERNEL, OWN, GRID, THREADS, LDS, ARGS)                                                                 \
   do {                                                                                                                        \
-    const hipError_t attr = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(LDS)); \
-    SPA_REQUIRE(attr == hipSuccess, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, (size_t)(LDS));                   \
+    constexpr size_t room = kUnitLds - (OWN);                                                                                 \
+    const hipError_t attr = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, (int)room);  \
+    SPA_REQUIRE(attr == hipSuccess && (LDS) <= room, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, (size_t)(LDS));  \
     hipLaunchKernelGGL(KERNEL, dim3(GRID), dim3(THREADS), LDS, st, ARGS);                                                     \
   } while (0)
 // KERNEL<type, head dim, window, SPLIT> of a launch whose workgroups own queries; EIGHT: whether a block has eight waves
+template <typename T, int DH, int SPLIT>
+constexpr size_t kQueryLds = sizeof(QueryTiles<T, DH, SPLIT>) + 256;             // (what a kernel has beside the tiles is less)
 #define SPA_QUERY_LAUNCH(KERNEL, T, D, EIGHT, ARGS)                                                                           \
   do {                                                                                                                        \
     const bool whole = m.offsets <= kWholeBytes / (int)sizeof(T);                                                             \
     const size_t lds = window_bytes(whole ? m.offsets : kWindow, sizeof(T));                                                  \
     const unsigned blocks = xcd_grid(nblk, H, B);                                                                             \
     if (!whole) {                                                                                                             \
-      SPA_BIAS_LAUNCH((KERNEL<T, D, kWinMoving, 1>), blocks, kBiasThreads, lds, ARGS);                                        \
+      SPA_BIAS_LAUNCH((KERNEL<T, D, kWinMoving, 1>), (kQueryLds<T, D, 1>), blocks, kBiasThreads, lds, ARGS);                  \
     } else {                                                                                                                  \
       if constexpr (sizeof(T) == 2)                                                                                           \
         if (EIGHT) {                                                                                                          \
-          SPA_BIAS_LAUNCH((KERNEL<T, D, kWinWhole, 2>), blocks, 2 * kBiasThreads, lds, ARGS);                                 \
+          SPA_BIAS_LAUNCH((KERNEL<T, D, kWinWhole, 2>), (kQueryLds<T, D, 2>), blocks, 2 * kBiasThreads, lds, ARGS);           \
           break;                                                                                                              \
         }                                                                                                                     \
-      SPA_BIAS_LAUNCH((KERNEL<T, D, kWinWhole, 1>), blocks, kBiasThreads, lds, ARGS);                                         \
+      SPA_BIAS_LAUNCH((KERNEL<T, D, kWinWhole, 1>), (kQueryLds<T, D, 1>), blocks, kBiasThreads, lds, ARGS);                   \
     }                                                                                                                         \
   } while (0)
 
