@@ -684,7 +684,8 @@ size_t spa_attention_bias_bwd_workspace_bytes(int B, int max_seqlen, int H, int 
  * in:  as in the forward, with its out and lse; dout [>= T, H*Dh] dtype contiguous; workspace (device, 256-byte aligned) of at
  *      least spa_attention_bias_bwd_workspace_bytes bytes, contents of no account.
  * out: dq, dk, dv as in spa_packed_attention_bwd (rows >= T are not written); d_table [H, n_buckets] fp32 or NULL: added in
- *      integers finer than 2^-30 of the largest dS a head can have, in any order the same.  All results run-to-run
+ *      integers finer than 2^-30 of the largest dS a head can have (coarser only where max_seqlen times the rows that a workgroup
+ *      goes over, B*max_seqlen at most, passes 2^32: none of their sums may overflow), in any order the same.  All results run-to-run
  *      bit-stable.  A head with a gradient, value or score that is not a finite number (-inf scores aside) has NaN in its row
  *      of d_table.
  */

@@ -2,7 +2,7 @@
 //   dtable[h, b] = sum over the pairs of bucket b of dS_ij,  dS = P (dP - D)
 // D from the rounded out is off by a share of that rounding; sum_j dS_ij = sum_j P_ij dP_ij - D_i is what it is off by, and is added to
 // the D that dK and dtable are formed with.  The order in which the many dS of an offset are added would be the launch's, so they are
-// added as integers: dS is rounded to a multiple of 2^-kDsBits of a power of two above every |dS| of the head.  Sums are then the same in
+// added as integers: dS is rounded to a multiple of 2^-40 (kDsBits) of a power of two above every |dS| of the head.  Sums are then the same in
 // any order, and finer than fp32 ones.
 //
 // P = exp(S - lse) adds up to 1 as long as lse holds its own logarithm beside the maximum.  Beside a mask it does not (at -1e9 its last place
@@ -24,9 +24,11 @@
 
 namespace spa {
 
-// Bits of an integer dS below the power of two above every |dS|: the sum of a workgroup's, one per offset and row it goes over,
-// stays inside 64 bits for up to 2^22 rows (and |dS| cannot add up to more than its rows' |dP|).
+// Bits of an integer dS below the power of two that is above twice every |dS|: one is below 2^(bits - 1), and as many as a workgroup can
+// meet at one offset (rows at the same place all meet at the middle one: its rows of keys times the longest segment) stay inside
+// 64 bits.  40 for up to 2^24 pairs, a bit less for every doubling beyond.
 constexpr int kDsBits = 40;
+inline int ds_bits(double pairs) { return std::min(kDsBits, 63 - std::ilogb(pairs)); }
 __device__ __forceinline__ double power_of_two(int e) { return __builtin_bit_cast(double, (uint64_t)(e + 1023) << 52); }
 // x factor, a power of two, rounded to an integer: the low bits of the sum with 1.5 2^52, whose own bits are taken off again
 __device__ __forceinline__ unsigned long long ds_integer(float x, double factor) {
@@ -50,6 +52,7 @@ struct BiasBwd {
   uint32_t* most;                 // [H][B * nblk]: what no |dS| of a block of queries exceeds
   float* partial;                 // [H][groups][offsets] or null
   int key_blocks, groups, slice;  // dk / dv: blocks of keys of the longest possible segment, workgroups a head, offsets of a histogram
+  int bits;                       // of an integer dS
 };
 
 // The dq launch: bound by the vector instructions like the forward (0.63 of the busy units' cycles at 16 images of 0.1 to 0.6 of 3136
@@ -243,12 +246,11 @@ __device__ __forceinline__ KeyBlock key_block(const KeyBlocks& k, const int32_t*
 // The scale of a head's integers: 2^e is above twice what the dq launch found (its blocks that exist); `unit` NaN: some dS of
 // the head is not a finite number.  All threads call it.
 struct DsScale {
-  int e;
-  double factor;
+  double quantum, factor;         // what an integer stands for, and its reciprocal (0: see unit)
   float unit;
 };
 template <int THREADS>
-__device__ __forceinline__ DsScale ds_scale(const uint32_t* most_h, const int32_t* cu, int B, int nblk, uint32_t* s_most) {
+__device__ __forceinline__ DsScale ds_scale(const uint32_t* most_h, const int32_t* cu, int B, int nblk, int bits, uint32_t* s_most) {
   uint32_t most = 0;
   for (int i = threadIdx.x; i < B * nblk; i += THREADS) {
     const int img = i / nblk, n = cu[img + 1] - cu[img];
@@ -262,15 +264,14 @@ __device__ __forceinline__ DsScale ds_scale(const uint32_t* most_h, const int32_
   for (int w = 0; w < THREADS / kWave; ++w) most = max(most, s_most[w]);
   const int e = __builtin_amdgcn_readfirstlane((int)(most >> 23) - 126 + 1);
   const bool bad = most >= 0x7f800000u || e > 126;
-  return {e, bad ? 0. : power_of_two(kDsBits - e), bad ? NAN : 0.f};
+  return {power_of_two(e - bits), bad ? 0. : power_of_two(bits - e), bad ? NAN : 0.f};
 }
 // A workgroup's histogram of `size` offsets of its head from `from` on, around the end, as fp32; all threads call it, behind the last add.
 template <int THREADS>
 __device__ __forceinline__ void write_partial(const unsigned long long* hist, const DsScale& s, int size, int from, int offsets, float* out) {
   __syncthreads();
-  const double quantum = power_of_two(s.e - kDsBits);
   for (int i = threadIdx.x; i < size; i += THREADS)
-    out[from + i - (from + i < offsets ? 0 : offsets)] = s.unit + (float)((double)(long long)hist[i] * quantum);
+    out[from + i - (from + i < offsets ? 0 : offsets)] = s.unit + (float)((double)(long long)hist[i] * s.quantum);
   __syncthreads();
 }
 
@@ -315,8 +316,8 @@ __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(cons
   WindowFill<T, THREADS> fill(a.m, h);
   if (WIN == kWinWhole) fill.start(0, a.m.offsets);
   list_key_blocks<THREADS>(l.blocks, a.cu, a.B, ROWS, a.key_blocks);
-  DsScale scale = {0, 0., 0.f};
-  if (HIST != kHistNone) scale = ds_scale<THREADS>(a.most + (long)h * a.B * a.nblk, a.cu, a.B, a.nblk, l.most);
+  DsScale scale = {0., 0., 0.f};
+  if (HIST != kHistNone) scale = ds_scale<THREADS>(a.most + (long)h * a.B * a.nblk, a.cu, a.B, a.nblk, a.bits, l.most);
   int zero = 0;
   if (WIN == kWinWhole) zero = fill.finish(win, l.row);
 
@@ -622,7 +623,7 @@ static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 // together, no more than there are blocks of keys, and no more than 256 MB of partial sums.
 struct BiasPlan {
   bool whole;                     // the window
-  int rows, split, key_blocks, slice, groups;         // rows: waves that own keys
+  int rows, split, key_blocks, slice, groups, bits;   // rows: waves that own keys
   size_t window, lds;
 };
 // Twelve waves for 192 keys where registers allow and there may be many blocks: us backward, eight | twelve waves, 3 heads of 32, 56 x 56 map:
@@ -647,6 +648,8 @@ static BiasPlan bias_plan_of(int H, int B, int n_max, long offsets) {
   p.key_blocks = (n_max + 32 * p.rows - 1) / (32 * p.rows);
   const long fit = std::max<long>(1, (256L << 20) / (4 * H * offsets));
   p.groups = (int)std::max<long>(1, std::min<long>(std::min<long>((two ? 512 : 256) / H, (long)B * p.key_blocks), fit));
+  const long turns = ((long)B * p.key_blocks + p.groups - 1) / p.groups;                 // blocks of keys of a workgroup
+  p.bits = ds_bits((double)std::min(turns * 32 * p.rows, (long)B * n_max) * n_max);
   return p;
 }
 static BiasPlan bias_plan(int H, int B, int n_max, int Dh, long offsets, int dtype) {
@@ -740,7 +743,7 @@ extern "C" int spa_packed_attention_bias_bwd(const void* q, const void* k, const
     const BiasBwd<T> args = {(const T*)q, (const T*)k, (const T*)v, (const T*)out, (const T*)dout, (long)q_row_stride,       \
                              (long)k_row_stride, (long)v_row_stride, lse, dvec, ls, cu_seqlens, m, H, B, nblk, scale, (T*)dq, \
                              (T*)dk, (T*)dv, (long)dq_row_stride, (long)dk_row_stride, (long)dv_row_stride, most, partial,   \
-                             plan.key_blocks, plan.groups, plan.slice};                                                                       \
+                             plan.key_blocks, plan.groups, plan.slice, plan.bits};                                                            \
     if (int rc = launch_bias_bwd<T, D>(fn, args, plan, hist, st)) return rc;                                                 \
   } while (0)
   if (dtype == SPA_F32) {
