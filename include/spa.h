@@ -686,8 +686,8 @@ size_t spa_attention_bias_bwd_workspace_bytes(int B, int max_seqlen, int H, int 
  * out: dq, dk, dv as in spa_packed_attention_bwd (rows >= T are not written); d_table [H, n_buckets] fp32 or NULL: added in
  *      integers finer than 2^-30 of the largest dS a head can have (coarser only where max_seqlen times the rows that a workgroup
  *      goes over, B*max_seqlen at most, passes 2^32: none of their sums may overflow), in any order the same.  All results run-to-run
- *      bit-stable.  A head with a gradient, value or score that is not a finite number (-inf scores aside) has NaN in its row
- *      of d_table.
+ *      bit-stable.  A head with a gradient, value or score that is not a finite number (-inf scores aside), or a row whose |dout| add up
+ *      to more than fp32 holds, has NaN in its row of d_table.
  */
 int spa_packed_attention_bias_bwd(const void* q, const void* k, const void* v, int64_t q_row_stride, int64_t k_row_stride,
                                   int64_t v_row_stride, const void* out, const void* dout, const float* lse,

@@ -18,6 +18,7 @@
 // Maps with more offsets than LDS has room for are taken in slices: the first pass over the blocks does everything but the offsets of
 // later slices, the others only go over the tiles that have offsets in theirs.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "attn_bias.h"
@@ -170,7 +171,9 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(cons
   // Dh U sum|dO V| in either launch)
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) v_most = __builtin_elementwise_maximum(v_most, s_most[0][w]);
-  const float bound = q_ok && part == 0 ? most + fabsf(left) + l1 * v_most * 0x1p-16f : 0.f;
+  const float more = fabsf(left) + l1 * 0x1p-16f * v_most;
+  float bound = q_ok && part == 0 ? most + more : 0.f;
+  if (bound == INFINITY && most < INFINITY && more < INFINITY) bound = FLT_MAX;               // (every |dS| is a finite number)
   const int bits = wave_pick<true>((int)(__builtin_bit_cast(uint32_t, bound) & 0x7fffffffu));      // (a NaN above all)
   if (lane == 0) s_most[1][threadIdx.x >> 6] = __builtin_bit_cast(float, bits);
   __syncthreads();
@@ -263,7 +266,7 @@ __device__ __forceinline__ DsScale ds_scale(const uint32_t* most_h, const int32_
 #pragma unroll
   for (int w = 0; w < THREADS / kWave; ++w) most = max(most, s_most[w]);
   const int e = __builtin_amdgcn_readfirstlane((int)(most >> 23) - 126 + 1);
-  const bool bad = most >= 0x7f800000u || e > 126;
+  const bool bad = most >= 0x7f800000u;
   return {power_of_two(e - bits), bad ? 0. : power_of_two(bits - e), bad ? NAN : 0.f};
 }
 // A workgroup's histogram of `size` offsets of its head from `from` on, around the end, as fp32; all threads call it, behind the last add.
