@@ -685,7 +685,6 @@ extern "C" int spa_norm_residual_unpack(const void* z, const int32_t* inv_pos, c
 }
 
 extern "C" size_t spa_norm_bwd_workspace_bytes(int64_t rows, int C, int dtype) {
-  (void)dtype;
   if (rows < 1 || C < 1) return 0;
   return (size_t)norm_parts((long)rows, C, dtype) * 2 * (size_t)C * sizeof(float);
 }
