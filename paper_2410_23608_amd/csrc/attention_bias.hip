@@ -135,8 +135,10 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_fwd_kernel(con
 }
 
 // Eight waves a block as well where the LDS of larger maps leaves few waves a unit otherwise: where that is twice the waves, or more
-// waves and not too many blocks.  us four | eight waves, heads of 32: 50 x 84 map (8 | 16 waves a unit), 8 images 31.2 | 25.0, 32 images
-// 132 | 117; 56 x 56 (12 | 16), 16 images 37.2 | 30.8, 64 images 94 | 100; 28 x 28 (16 | 16), 32 images 22.0 | 23.0.
+// waves and not too many blocks (of the longest possible segments, all that the host knows).  us four | eight waves, heads of 32: 50 x 84 map
+// (8 | 16 waves a unit), 8 images 31.5 | 25.3, 32 images 132 | 117; 56 x 56 (12 | 16), 3 heads, 16 images 37.7 | 31.3, 20 (1500 blocks)
+// 45.2 | 40.8, 24 (1800) 48.1 | 51.3, 32 55.2 | 57.3, 64 97 | 103, 8 heads, 8 (1600) 35.7 | 29.7, 12 (2400) 51.5 | 55.9; 28 x 28
+// (16 | 16), 32 images 25.1 | 28.5.
 template <typename T, int DH>
 static bool fwd_eight(int offsets, int nblk, int H, int B) {
   if (few_blocks(nblk, H, B)) return true;
@@ -144,7 +146,7 @@ static bool fwd_eight(int offsets, int nblk, int H, int B) {
   const size_t win = window_bytes(offsets, sizeof(T));
   const int four = std::min<int>(most, 4 * (int)(kUnitLds / (sizeof(QueryTiles<T, DH, 1>) + win)));
   const int eight = std::min<int>(most, 8 * (int)(kUnitLds / (sizeof(QueryTiles<T, DH, 2>) + win)));
-  return nblk >= 4 && (eight >= 2 * four || (eight > four && xcd_grid(nblk, H, B) <= 2048));
+  return nblk >= 4 && (eight >= 2 * four || (eight > four && xcd_grid(nblk, H, B) <= 1700));
 }
 
 int bias_checks(const char* fn, const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
