@@ -629,8 +629,9 @@ struct BiasPlan {
   int rows, split, key_blocks, slice, groups, bits;   // rows: waves that own keys
   size_t window, lds;
 };
-// Twelve waves for 192 keys where registers allow and there may be many blocks: us backward, eight | twelve waves, 3 heads of 32, 56 x 56 map:
-// one image of 1792 tokens 87.4 | 100, 8 of 196 36.5 | 38.7, 16 of 1792 236 | 213, 64 of 0.1 - 0.6 of 3136 348 | 324.
+// Twelve waves for 192 keys where registers allow and there may be many blocks (of the longest possible segments, all that the host
+// knows): us backward, eight | twelve waves, heads of 32, 56 x 56 map, images of 0.1 to 0.6 of 3136 tokens: 3 heads, 8 images (600 blocks)
+// 91 | 102, 14 (1050) 106 | 115, 16 (1200) 115.3 | 114.9, 20 151 | 144, 64 350 | 326; 8 heads, 5 images (1000) 72 | 80, 8 (1600) 111 | 106.
 template <int DH>
 constexpr int kSplitRows = DH == 32 ? 6 : 4;
 template <typename T, int DH>
@@ -647,7 +648,7 @@ static BiasPlan bias_plan_of(int H, int B, int n_max, long offsets) {
   if (p.split == 2) tiles = sizeof(KeyTiles<T, DH, kSplitRows<DH>, 2>);
   p.slice = (int)std::min<long>(all, (long)(most - tiles - p.window) / 8 / 64 * 64);
   p.lds = p.window + (size_t)p.slice * 8;
-  p.rows = p.split == 2 && p.slice == all && (long)H * B * nblk >= 1024 ? kSplitRows<DH> : 4;
+  p.rows = p.split == 2 && p.slice == all && (long)H * B * nblk >= 1200 ? kSplitRows<DH> : 4;
   p.key_blocks = (n_max + 32 * p.rows - 1) / (32 * p.rows);
   const long fit = std::max<long>(1, (256L << 20) / (4 * H * offsets));
   p.groups = (int)std::max<long>(1, std::min<long>(std::min<long>((two ? 512 : 256) / H, (long)B * p.key_blocks), fit));
