@@ -679,8 +679,8 @@ size_t spa_attention_bias_bwd_workspace_bytes(int B, int max_seqlen, int H, int 
 /*
  * Backward of spa_packed_attention_bias: dq, dk, dv as in spa_packed_attention_bwd, and
  *   d_table[h, b] = sum of dS_ij over the pairs (i, j) whose offset is in bucket b,   dS = P (dP - D)
- * D_i is sum_d dO_id O_id from the rounded out for dq; for d_table (and dk) what the row's dS then still add up to, which is the
- * error of that D, is taken off, so that d_table is good to fp32 from bf16 rows too.
+ * D_i is sum_d dO_id O_id from the rounded out for dq (segments of up to 32 rows: sum_j P_ij dP_ij); for d_table (and dk) what the
+ * row's dS then still add up to, which is the error of that D, is taken off, so that d_table is good to fp32 from bf16 rows too.
  * in:  as in the forward, with its out and lse; dout [>= T, H*Dh] dtype contiguous; workspace (device, 256-byte aligned) of at
  *      least spa_attention_bias_bwd_workspace_bytes bytes, contents of no account.
  * out: dq, dk, dv as in spa_packed_attention_bwd (rows >= T are not written); d_table [H, n_buckets] fp32 or NULL: added in

@@ -58,9 +58,10 @@ struct BiasBwd {
 
 // The dq launch: bound by the vector instructions like the forward (0.63 of the busy units' cycles at 16 images of 0.1 to 0.6 of 3136
 // tokens, 3 heads of 32, two waves a SIMD by registers), 51 us there; 26 at 64 images of 196, 12 heads of 64.  A block of eight waves
-// holds no more waves a unit, so only few blocks get it.
+// holds no more waves a unit, so only few blocks get it.  (Two waves a SIMD are named for heads of 32, which their registers allow in any case:
+// left to itself the compiler orders the same loop so that it takes 58 us.)
 template <typename T, int DH, int WIN, int SPLIT>
-__global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(const BiasBwd<T> a) {
+__global__ void __launch_bounds__(kBiasThreads * SPLIT, DH == 32 ? 2 : 1) attn_bias_dq_kernel(const BiasBwd<T> a) {
   using O = Ops<T, DH>;
   constexpr int DB = DH / 32, WAVES = 4 * SPLIT;
   extern __shared__ __attribute__((aligned(16))) char win[];
@@ -128,6 +129,12 @@ __global__ void __launch_bounds__(kBiasThreads * SPLIT) attn_bias_dq_kernel(cons
             dp[r] *= s[r];
             left += dp[r];
             most = __builtin_elementwise_maximum(most, fabsf(dp[r]));
+          }
+          if (!whole && n <= 32) {                            // the whole row is here: what its dS add up to off them as well
+            float off = sum_across_halves(left);
+            if (far) off = far_row ? off / sum_across_halves(all) : off;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dp[r] = fmaf(-off, s[r], dp[r]);
           }
           O::outer(acc, K, sb, dp, lane);
         }
