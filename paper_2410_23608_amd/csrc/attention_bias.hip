@@ -14,8 +14,8 @@ namespace spa {
 // query a 32 x 32 block, and the probabilities (bf16: rounded) are the second product's operand in registers; K and V stream through LDS
 // in tiles of 64.  fp32 takes the same steps on the fp32 matrix instructions.  Bound by the vector instructions: some 135 a 32 x 32
 // block, 16 of them exponentials, of which the bias is a subtraction, a shift and a multiply-add each; at 8 images of 4200 tokens, 8 heads
-// of 32, they fill 0.89 of the busy units' cycles.  us (the attention without a bias): 36 (26) at 16 images of 0.1 to 0.6 of 3136 tokens,
-// 3 heads of 32; 18.6 (14) at 64 of 196, 12 heads of 64; 40 (27) at the 8 of 4200.
+// of 32, they fill 0.89 of the busy units' cycles.  us (the attention without a bias), medians of eight selections: 33 (24) at 16 images
+// of 0.1 to 0.6 of 3136 tokens, 3 heads of 32; 18.3 (13.0) at 64 of 196, 12 heads of 64; 41 (25), 24 to 45 by the selection, at 8 of 4200.
 template <typename T>
 struct BiasFwd {
   const T *q, *k, *v;

@@ -1,10 +1,10 @@
 // Backward of the packed attention with a relative position bias (attention_bias.hip): beside dQ, dK, dV of the attention without one
 //   dtable[h, b] = sum over the pairs of bucket b of dS_ij,  dS = P (dP - D)
 // D from the rounded out is off by a share of that rounding; sum_j dS_ij = sum_j P_ij dP_ij - D_i is what it is off by, and is added to
-// the D that dK and dtable are formed with.  The order in which the many dS of an offset are added would be the launch's, so they are
-// added as integers: dS is rounded to a multiple of 2^-40 (kDsBits) of a power of two above every |dS| of the head.  Sums are then the same in
-// any order, and finer than fp32 ones.
-//
+// the D that dK and dtable are formed with.  dQ is formed while that sum is and keeps the first D, as in the attention without a bias;
+// rows of one block of 32 keys have the sum in time.  The order in which the many dS of an offset are added would be the launch's, so
+// they are added as integers: dS is rounded to a multiple of 2^-40 (kDsBits) of a power of two above every |dS| of the head.  Sums are then
+// the same in any order, and finer than fp32 ones.
 // P = exp(S - lse) adds up to 1 as long as lse holds its own logarithm beside the maximum.  Beside a mask it does not (at -1e9 its last place
 // is 64, and a row of n such keys has log n to add): for rows of |lse| >= kFarScore the dq launch adds up exp(S - lse), at most e^17
 // either way, divides by the sum at its end and leaves the logarithm of it for the other launch's exponent.
@@ -57,9 +57,9 @@ struct BiasBwd {
 };
 
 // The dq launch: bound by the vector instructions like the forward (0.63 of the busy units' cycles at 16 images of 0.1 to 0.6 of 3136
-// tokens, 3 heads of 32, two waves a SIMD by registers), 51 us there; 26 at 64 images of 196, 12 heads of 64.  A block of eight waves
-// holds no more waves a unit, so only few blocks get it.  (Two waves a SIMD are named for heads of 32, which their registers allow in any case:
-// left to itself the compiler orders the same loop so that it takes 58 us.)
+// tokens, 3 heads of 32, three waves a SIMD by registers and LDS), 49 us there; 27 at 64 images of 196, 12 heads of 64.  A block of eight
+// waves holds no more waves a unit, so only few blocks get it.  (Two waves a SIMD at least are named for heads of 32, which their registers
+// allow in any case: left to itself the compiler orders the same loop so that it takes 58 us.)
 template <typename T, int DH, int WIN, int SPLIT>
 __global__ void __launch_bounds__(kBiasThreads * SPLIT, DH == 32 ? 2 : 1) attn_bias_dq_kernel(const BiasBwd<T> a) {
   using O = Ops<T, DH>;
@@ -306,7 +306,7 @@ struct KeyTiles {
 // RW waves own 32 keys each.  SPLIT 2: the waves come twice, the second ones take the second half of every tile of 64 queries, and hand
 // their sums to the first at the end of a block.  Bound by latency and LDS together: a block's chain (look-ups, products, exponentials,
 // products, 16 atomic adds) runs on two or three waves a SIMD, LDS is busy 0.54 of the time (half of it the adds, for the offsets of
-// a wave's keys meet in banks).  us: 76 at 16 images of 0.1 to 0.6 of 3136 tokens, 3 heads of 32; 32 at 64 of 196, 12 heads of 64.
+// a wave's keys meet in banks).  us: 75 at 16 images of 0.1 to 0.6 of 3136 tokens, 3 heads of 32; 31 at 64 of 196, 12 heads of 64.
 template <typename T, int DH, int WIN, int RW, int SPLIT, int HIST>
 __global__ void __launch_bounds__(kWave * RW * SPLIT) attn_bias_dkdv_kernel(const BiasBwd<T> a) {
   using O = Ops<T, DH>;

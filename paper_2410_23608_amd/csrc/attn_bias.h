@@ -100,7 +100,8 @@ template <int DH> struct Ops<__bf16, DH> {
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.f[kk], b.f[kk], acc, 0, 0, 0);
   }
-  // acc += (rows sb 32 .. of the tile)^T p: p of a lane holds the 16 rows of acc_row of its column, rounded here
+  // acc += (rows sb 32 .. of the tile)^T p: p of a lane holds the 16 rows of acc_row of its column, P or dS, rounded here to bf16 as
+  // operands of the product have to be (half a step each, 2^-8; the sums over them stay in fp32)
   static __device__ __forceinline__ void outer(floatx16 (&acc)[DH / 32], const __bf16* tile, int sb, const floatx16& p, int lane) {
 #pragma unroll
     for (int mf = 0; mf < 2; ++mf) {
@@ -403,7 +404,8 @@ struct BiasBlock {
 };
 __device__ __forceinline__ BiasBlock bias_block(int* s_live, const int32_t* cu, int H, int B, int nblk) {
   // there and back: a unit that got a long block in one turn of the XCD's 32 units gets a short one in the next (us forward,
-  // there alone | there and back: 16 images of 0.1 - 0.6 of 3136 tokens, 3 heads of 32, 38.9 | 37.2; 8 of 0.05 - 0.4 of 4200, 8 heads, 32.7 | 31.2)
+  // four waves a block, there alone | there and back: 16 images of 0.1 - 0.6 of 3136 tokens, 3 heads of 32, 38.9 | 37.2; 8 of 0.05 - 0.4 of 4200,
+  // 8 heads, 32.7 | 31.2)
   const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3 & ~31, width = min(32, (int)(gridDim.x >> 3) - turn);
   const int at = blockIdx.x >> 3 & 31, j = turn + (turn & 32 ? width - 1 - at : at);
   if (B <= kLptMaxB) {

@@ -8,9 +8,10 @@
 // variance after the mean), G lanes a row, IT chunks of 16 bytes a lane.  Parameter gradients are sums over all rows of
 //   A = sum p dy * zh,  B = sum p dy      (in front: da for p dy), from which
 //   dgamma = scale * A,  dbeta = scale * B,  dscale = gamma * A + beta * B
-// follow; every workgroup adds its rows and writes one partial row, a second launch adds those in a fixed order.
-// us a launch, TB/s of the bytes it cannot do without (a large copy: 4.6): 134400 bf16 rows of 256, 22 % of them packed, in front 8.9
-// (3.4) and its backward 29.5 (4.8), behind 27 (5.7); 12544 of 768, half packed, in front 7.5 (2.6) and 14.7 (3.9), behind 12.6 (3.8) and 11.4 (2.5).
+// follow; every workgroup adds its rows and writes one partial row, a second launch adds those in a fixed order, all of it in fp32.
+// us a launch, TB/s of the bytes it cannot do without (a large copy: 4.6), eight batches in turn so that no rows are left in a
+// cache: 134400 bf16 rows of 256, 22 % of them packed, in front 11.0 (2.8) and its backward 33.6 (5.0), behind 34.8 (4.4); 12544 of 768, half
+// packed, in front 8.3 (2.3) and 17.0 (3.4), behind 16.6 (2.9) and 11.7 (2.5).
 // Small ones are trips to memory: launch, index, rows, and for the backward the fold and the sums' launch of 4 us.
 #include <algorithm>
 #include <cmath>
