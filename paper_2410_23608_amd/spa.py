@@ -1002,6 +1002,8 @@ def spa_packed_attention_bias_bwd(q, k, v, out, dout, lse, cu_seqlens, gather_id
                                 dout=dout, dq=dq, dk=dk, dv=dv)
     _typed(fn, torch.float32, d_table=d_table)
     _holds(fn, d_table=(d_table, table.numel()))
+    if d_table is not None and d_table.dim() > 1 and d_table.shape[-1] != table.shape[1]:
+        raise ValueError(f"{fn}: d_table must have rows of {table.shape[1]} entries as the table has, got {tuple(d_table.shape)}")
     _contig(dout, d_table, workspace)
     _keep = (q, k, v, out, dout, lse, cu_seqlens, gather_idx, table, buckets, dq, dk, dv, d_table, workspace,)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
