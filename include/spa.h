@@ -314,6 +314,8 @@ int spa_packed_attention_running_max(const void* q, const void* k, const void* v
  *   S_ij = softmax_scale <q_i, k_j> + table[h, buckets[o]],   O = softmax(S) V,   lse = log sum_j exp(S_ij)
  * A bucket outside 0 .. n_buckets-1 stands for no bias.  An entry of -inf leaves its pairs out (the rows of q, k and v have
  * to be finite there all the same); a row whose scores are all -inf gives out = 0, lse = -inf and no gradient.
+ * Finite entries are numbers like any other, whatever their size: a mask of -1e4, -1e9 or the type's lowest number weighs nothing beside a
+ * key without one, and a row whose keys all carry it is the softmax of what fp32 leaves of its scores.
  * in:  q, k, v, strides, cu_seqlens, max_seqlen, softmax_scale as in spa_packed_attention, max_seqlen <= grid_h*grid_w;
  *      table [H, n_buckets] dtype; buckets [(2 grid_h - 1)(2 grid_w - 1)] int32 (16-byte aligned), or NULL: a bucket per offset (n_buckets is
  *      their number); sequences without a second axis: grid_h = 1.
