@@ -298,6 +298,47 @@ int spa_packed_attention(const void* q, const void* k, const void* v, int64_t q_
                          int dtype, float softmax_scale, void* out, float* lse, void* stream);
 
 /*
+ * Norm of every head of q and k with the rotation by the token's place, in one pass over packed rows (what stands between the
+ * projections and the attention of a block of Section 3.2 where its positions are rotary and its heads are normed).  For packed row
+ * j < min(*total, M_cap), every head x of its row of q (H of them) and k (Hk of them), gamma and beta of the tensor shared by its heads:
+ *   u = gamma * (x - mu) r + beta;   mu, r of the head's Dh elements by kind as in spa_norm_packed, SPA_NORM_NONE: u = x
+ *   (y1, y2) = (u1 c - u2 s, u1 s + u2 c)      for pair i of its Dh / 2 pairs, (c, s) = table[p][i]
+ * The token of the row sits at n = gather_idx[j] mod (grid_t*grid_h*grid_w) of its map (gather_idx NULL: n = j mod that), in frame
+ * n / (grid_h*grid_w), row n / grid_w mod grid_h, column n mod grid_w: p is the frame for the first pairs_t pairs, the row for the next
+ * pairs_h, the column for the others.  Pair i is elements 2i and 2i + 1 (SPA_ROTARY_ADJACENT) or i and i + Dh/2 (SPA_ROTARY_HALVES).
+ * in:  q, k: packed rows, element (j, h, d) at q[j*q_row_stride + h*Dh + d], row strides < 2^31 elements; k may be NULL with Hk = 0 (q alone: queries of
+ *      spa_cross_attention); gather_idx [M_cap] int32 or NULL; total [1] int32 or NULL (M_cap rows); gamma_*, beta_* [Dh] dtype or
+ *      NULL (1 and 0; all NULL with SPA_NORM_NONE); eps finite and >= 0; table [max(grid_t, grid_h, grid_w)][Dh/2][2] fp32, 16-byte aligned:
+ *      cosine and sine by place and pair, or NULL: no rotation (the map is not looked at then); Dh in {32, 64}; H, Hk <= 256.
+ * out: q_out, k_out dtype, likewise; q_out may be q and k_out may be k (with the same row stride).  Rows from min(*total, M_cap) on are left as they are.
+ */
+#define SPA_ROTARY_ADJACENT 0
+#define SPA_ROTARY_HALVES 1
+#define SPA_NORM_NONE 2
+int spa_qk_norm_rotary(const void* q, const void* k, int64_t q_row_stride, int64_t k_row_stride, const int32_t* gather_idx,
+                       const int32_t* total, const void* gamma_q, const void* beta_q, const void* gamma_k, const void* beta_k, int kind,
+                       float eps, const float* table, int pairs_t, int pairs_h, int grid_t, int grid_h, int grid_w, int layout, int M_cap,
+                       int H, int Hk, int Dh, int dtype, void* q_out, void* k_out, int64_t q_out_row_stride, int64_t k_out_row_stride,
+                       void* stream);
+
+/*
+ * Backward of spa_qk_norm_rotary.  With du the pairs of the result's gradient turned back (the sine's sign changed), xh the normed
+ * head and g = gamma du:
+ *   dq, dk = r (g - mean(g) - xh mean(g xh))      (SPA_NORM_RMS: without mean(g); SPA_NORM_NONE: du)
+ *   dgamma = sum du xh,  dbeta = sum du           over all rows and heads of the tensor
+ * in:  dq_out, dk_out: the gradients, rows as q_out, k_out; q, k: what the forward read (SPA_NORM_NONE: not read, but given); the other
+ *      arguments as there; workspace of at least spa_qk_norm_rotary_bwd_workspace_bytes bytes (none for SPA_NORM_NONE).
+ * out: dq, dk dtype (dq may be dq_out or q, dk likewise, with the same row stride); dgamma_*, dbeta_* [Dh] fp32, each or NULL.  Deterministic.
+ */
+size_t spa_qk_norm_rotary_bwd_workspace_bytes(int M_cap, int H, int Hk, int Dh, int dtype);
+int spa_qk_norm_rotary_bwd(const void* dq_out, const void* dk_out, int64_t dq_out_row_stride, int64_t dk_out_row_stride, const void* q,
+                           const void* k, int64_t q_row_stride, int64_t k_row_stride, const int32_t* gather_idx, const int32_t* total,
+                           const void* gamma_q, const void* gamma_k, int kind, float eps, const float* table, int pairs_t, int pairs_h,
+                           int grid_t, int grid_h, int grid_w, int layout, int M_cap, int H, int Hk, int Dh, int dtype, void* dq, void* dk,
+                           int64_t dq_row_stride, int64_t dk_row_stride, float* dgamma_q, float* dbeta_q, float* dgamma_k, float* dbeta_k,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * spa_packed_attention under a second name, for callers linked against it: every form takes the exponentials against
  * the running maximum of the scores.
  */

@@ -5,6 +5,7 @@
 #include <type_traits>
 
 #include "attn_tiles.h"
+#include "divisor.h"
 #include "spa_common.h"
 
 namespace spa {
@@ -16,18 +17,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFarScore = 128.f;
 // A wave owns 32 rows and a workgroup 128 (eight waves: each row twice, SPLIT 2), the others stream through LDS in tiles of 64.
 constexpr int kBiasBN = 64, kBiasThreads = 256, kBiasRows = 128;
-
-// x / d for 0 <= x < 2^31 by one high product: with 2^s >= d > 2^(s-1), M = floor(2^(31+s) / d) + 1 < 2^32 is at most 2^s / d too
-// large in units of its last place, which times x is below 2^(31+s) / d: the quotient is exact.  (d = 1: M = 0.)
-struct Divisor {
-  uint32_t d, M, shift;
-};
-inline Divisor divisor(uint32_t d) {
-  uint32_t s = 0;
-  while ((1ull << s) < d) ++s;
-  return d == 1 ? Divisor{1, 0, 0} : Divisor{d, (uint32_t)((1ull << (31 + s)) / d + 1), s - 1};
-}
-__device__ __forceinline__ uint32_t quotient(uint32_t x, const Divisor& d) { return d.M == 0 ? x : __umulhi(x, d.M) >> d.shift; }
 
 struct BiasMap {
   const void* table;             // [H, nb]

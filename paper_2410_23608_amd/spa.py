@@ -128,6 +128,12 @@ _SIGNATURES = {
                                              _P, _P, _P, _P, c_size_t, _P]),
     "spa_gate_bwd_scores": (c_int, [_P, _P, c_float, _P, _P, _P, _P, _P, c_float, c_int, c_int, c_int, c_int, _P, _P, _P, _P, _P,
                                     c_size_t, _P]),
+    "spa_qk_norm_rotary": (c_int, [_P, _P, c_int64, c_int64, _P, _P, _P, _P, _P, _P, c_int, c_float, _P, c_int, c_int, c_int, c_int, c_int,
+                                   c_int, c_int, c_int, c_int, c_int, c_int, _P, _P, c_int64, c_int64, _P]),
+    "spa_qk_norm_rotary_bwd_workspace_bytes": (c_size_t, [c_int, c_int, c_int, c_int, c_int]),
+    "spa_qk_norm_rotary_bwd": (c_int, [_P, _P, c_int64, c_int64, _P, _P, c_int64, c_int64, _P, _P, _P, _P, c_int, c_float, _P, c_int, c_int,
+                                       c_int, c_int, c_int, c_int, c_int, c_int, c_int, c_int, c_int, _P, _P, c_int64, c_int64, _P, _P, _P,
+                                       _P, _P, c_size_t, _P]),
     "spa_padded_attention": (c_int, [_P, _P, _P, c_int64, _P, c_int, c_int, c_int, c_int, c_int, c_float, _P, _P]),
 }
 for _name, (_res, _args) in _SIGNATURES.items():
@@ -1174,6 +1180,86 @@ def spa_norm_residual_unpack_bwd(dy, z, gather_idx, inv_pos, total, gamma, beta,
                      (_ptr(dy), _ptr(z), _ptr(gather_idx), _ptr(inv_pos), _ptr(total), _ptr(gamma), _ptr(beta), _ptr(scale),
                       _ptr(gate_scores), int(kind), _ptr(stats), M, rows, C, code, _ptr(dz), _ptr(d_scores), _ptr(dgamma),
                       _ptr(dbeta), _ptr(dscale), _ptr(workspace), ws_bytes, _stream(),), _keep, prepare)
+
+
+SPA_NORM_NONE, SPA_ROTARY_ADJACENT, SPA_ROTARY_HALVES = 2, 0, 1
+
+
+def rotary_table(grid, Dh, pairs, base=10000.0):
+    """The cosines and sines of spa_qk_norm_rotary, f32 [max(grid), Dh/2, 2] on the host, formed in 64 bits: grid = (frames, rows,
+    columns), pairs = (pairs turned by the frame, by the row), the others by the column; the i-th of an axis' n pairs turns by
+    base^(-i/n) a place."""
+    grid, half = tuple(int(n) for n in grid), int(Dh) // 2
+    counts = (int(pairs[0]), int(pairs[1]), half - int(pairs[0]) - int(pairs[1]))
+    if len(grid) != 3 or min(grid) < 1 or min(counts) < 0 or not float(base) > 0.0:
+        raise ValueError("rotary_table: grid must be three sizes >= 1, pairs >= 0 with no more than Dh/2 together, base > 0")
+    freq = torch.cat([float(base) ** (-torch.arange(n, dtype=torch.float64) / max(n, 1)) for n in counts])
+    angle = torch.arange(max(grid), dtype=torch.float64)[:, None] * freq
+    return torch.stack((angle.cos(), angle.sin()), -1).float().contiguous()
+
+
+def _rotary_checks(fn, q, k, gather_idx, total, table, grid, H, Hk, Dh, params, **rows):
+    """rows: name = (tensor, heads); the row count of the call is the smallest of the given tensors'."""
+    code = _features(fn, q=q, k=k, **params, **{name: t for name, (t, _) in rows.items()})
+    rows = dict(rows, q=(q, H), k=(k, Hk))
+    if Hk == 0 and any(t is not None for t, heads in rows.values() if heads == 0):
+        raise ValueError(f"{fn}: with Hk = 0 there is no k")
+    if Hk > 0 and any(t is None for t, _ in rows.values()):
+        raise ValueError(f"{fn}: q, k and their results must be given")
+    M = min(t.shape[0] for t, _ in rows.values() if t is not None)
+    _rows(fn, H * Dh, **{name: (t, 1) for name, (t, heads) in rows.items() if heads == H and t is not None})
+    _rows(fn, Hk * Dh, **{name: (t, 1) for name, (t, heads) in rows.items() if heads == Hk and t is not None})
+    _typed(fn, torch.int32, gather_idx=gather_idx, total=total)
+    _typed(fn, torch.float32, table=table)
+    grid = tuple(int(n) for n in grid)
+    if len(grid) != 3:
+        raise ValueError(f"{fn}: grid must be (frames, rows, columns)")
+    _holds(fn, gather_idx=(gather_idx, M), total=(total, 1), table=(table, max(grid) * Dh), **{n: (t, Dh) for n, t in params.items()})
+    _contig(gather_idx, total, table, *params.values())
+    return code, M, grid
+
+
+def _stride_of(t) -> int:
+    return 0 if t is None else _row_stride(t)
+
+
+def spa_qk_norm_rotary(q, k, gather_idx, total, gamma_q, beta_q, gamma_k, beta_k, kind, eps, table, pairs, grid, H, Hk, Dh, q_out, k_out,
+                       layout=SPA_ROTARY_ADJACENT, prepare=False):
+    """q_out, k_out = the heads of the packed rows q, k normed (kind; SPA_NORM_NONE: not) and turned by the place of the row's token on
+    its map: grid = (frames, rows, columns), pairs = (pairs turned by the frame, by the row), table of `rotary_table` on the device
+    (None: not turned).  Rows may be column-slice views; k and k_out may be None with Hk = 0; q_out may be q, k_out k."""
+    fn = "spa_qk_norm_rotary"
+    params = dict(gamma_q=gamma_q, beta_q=beta_q, gamma_k=gamma_k, beta_k=beta_k)
+    code, M, grid = _rotary_checks(fn, q, k, gather_idx, total, table, grid, H, Hk, Dh, params, q_out=(q_out, H), k_out=(k_out, Hk))
+    _keep = (q, k, gather_idx, total, gamma_q, beta_q, gamma_k, beta_k, table, q_out, k_out,)
+    return _dispatch(lib.spa_qk_norm_rotary,
+                     (_ptr(q), _ptr(k), _row_stride(q), _stride_of(k), _ptr(gather_idx), _ptr(total), _ptr(gamma_q), _ptr(beta_q),
+                      _ptr(gamma_k), _ptr(beta_k), int(kind), _num(eps), _ptr(table), int(pairs[0]), int(pairs[1]), *grid, int(layout), M,
+                      H, Hk, Dh, code, _ptr(q_out), _ptr(k_out), _row_stride(q_out), _stride_of(k_out), _stream(),), _keep, prepare)
+
+
+def spa_qk_norm_rotary_bwd_workspace_bytes(M_cap, H, Hk, Dh, dtype) -> int:
+    return int(lib.spa_qk_norm_rotary_bwd_workspace_bytes(int(M_cap), int(H), int(Hk), int(Dh), int(dtype)))
+
+
+def spa_qk_norm_rotary_bwd(dq_out, dk_out, q, k, gather_idx, total, gamma_q, gamma_k, kind, eps, table, pairs, grid, H, Hk, Dh, dq, dk,
+                           dgamma_q, dbeta_q, dgamma_k, dbeta_k, workspace, layout=SPA_ROTARY_ADJACENT, prepare=False):
+    """The backward of spa_qk_norm_rotary from the gradients of its results; dgamma_*, dbeta_* [Dh] f32, each may be None; dq may be
+    dq_out or q, dk likewise."""
+    fn = "spa_qk_norm_rotary_bwd"
+    code, M, grid = _rotary_checks(fn, q, k, gather_idx, total, table, grid, H, Hk, Dh, dict(gamma_q=gamma_q, gamma_k=gamma_k),
+                                   dq_out=(dq_out, H), dk_out=(dk_out, Hk), dq=(dq, H), dk=(dk, Hk))
+    grads = dict(dgamma_q=dgamma_q, dbeta_q=dbeta_q, dgamma_k=dgamma_k, dbeta_k=dbeta_k)
+    _typed(fn, torch.float32, **grads)
+    _holds(fn, **{name: (t, Dh) for name, t in grads.items()})
+    _contig(*grads.values(), workspace)
+    _keep = (dq_out, dk_out, q, k, gather_idx, total, gamma_q, gamma_k, table, dq, dk, *grads.values(), workspace,)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return _dispatch(lib.spa_qk_norm_rotary_bwd,
+                     (_ptr(dq_out), _ptr(dk_out), _row_stride(dq_out), _stride_of(dk_out), _ptr(q), _ptr(k), _row_stride(q), _stride_of(k),
+                      _ptr(gather_idx), _ptr(total), _ptr(gamma_q), _ptr(gamma_k), int(kind), _num(eps), _ptr(table), int(pairs[0]),
+                      int(pairs[1]), *grid, int(layout), M, H, Hk, Dh, code, _ptr(dq), _ptr(dk), _row_stride(dq), _stride_of(dk),
+                      _ptr(dgamma_q), _ptr(dbeta_q), _ptr(dgamma_k), _ptr(dbeta_k), _ptr(workspace), ws_bytes, _stream(),), _keep, prepare)
 
 
 def spa_padded_attention(q, k, v, seqlens, B, n_pad, H, Dh, out, softmax_scale=0.0, prepare=False):
