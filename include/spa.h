@@ -339,6 +339,41 @@ int spa_qk_norm_rotary_bwd(const void* dq_out, const void* dk_out, int64_t dq_ou
                            void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Attention of packed rows to the keys of another sequence of another length (the tokens that a block of Section 3.2 packs attend to an encoder's states;
+ * or a few queries, or one, to the packed tokens).  For segment b, query row i in [cu_seqlens_q[b], cu_seqlens_q[b+1]) and key row j in
+ * [cu_seqlens_k[b], cu_seqlens_k[b] + n_b), n_b = the segment's rows, or min(key_lens[b], that) where key_lens is given (states in a padded batch):
+ *   O_i = softmax_j(softmax_scale <q_i, k_j>) V,   lse_i = log sum_j exp(softmax_scale <q_i, k_j>)
+ * Query head h reads key head h / (H / Hk).  A row without a key gives out = 0 and lse = -inf.  One batch of keys for all images is one segment: B = 1
+ * and cu_seqlens_q = {0, T}.
+ * in:  q, k, v: rows, element (j, h, d) at p[j*row_stride + h*Dh + d], H heads of q, Hk of k and v, H a multiple of Hk, strides < 2^31 elements;
+ *      cu_seqlens_q, cu_seqlens_k [B+1] int32; key_lens [B] int32 or NULL; max_q, max_k >= every segment's rows (B*max_q, B*max_k, max_q*H/Hk < 2^31; what
+ *      lies behind them in a longer segment is not looked at); Dh in {32, 64}; softmax_scale (host float; 0 means 1/sqrt(Dh)); workspace of at least
+ *      spa_cross_attention_workspace_bytes bytes, 256-byte aligned (NULL where that is 0: the keys are not split over workgroups).
+ * out: out [>= rows of q, H*Dh] dtype, contiguous; lse [H, B*max_q] fp32 or NULL.  Other rows are not written.  The bits are the same in every run; the
+ *      order in which a row's keys are added follows from B, H, Hk, max_q, max_k and the segment's number of keys.
+ */
+size_t spa_cross_attention_workspace_bytes(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtype);
+int spa_cross_attention(const void* q, const void* k, const void* v, int64_t q_row_stride, int64_t k_row_stride, int64_t v_row_stride,
+                        const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, const int32_t* key_lens, int B, int max_q, int max_k, int H,
+                        int Hk, int Dh, int dtype, float softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/*
+ * Backward of spa_cross_attention.  With P = exp(S - lse), dP = dout V^T, D_i = <dout_i, out_i>, dS = P (dP - D):
+ *   dq = softmax_scale dS K,   dk = softmax_scale dS^T Q,   dv = P^T dout      (dk, dv: summed over the query heads that share the key head)
+ * in:  as there; out, dout [rows of q, H*Dh] dtype, contiguous; lse as written by the forward; workspace of at least
+ *      spa_cross_attention_bwd_workspace_bytes bytes, 256-byte aligned.
+ * out: dq, dk, dv dtype, rows as q, k, v with row strides of their own; rows of a key segment behind key_lens[b] get dk = dv = 0, rows of no
+ *      segment are left as they are.  Deterministic.
+ */
+size_t spa_cross_attention_bwd_workspace_bytes(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtype);
+int spa_cross_attention_bwd(const void* q, const void* k, const void* v, int64_t q_row_stride, int64_t k_row_stride, int64_t v_row_stride,
+                            const void* out, const void* dout, const float* lse, const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k,
+                            const int32_t* key_lens, int B, int max_q, int max_k, int H, int Hk, int Dh, int dtype, float softmax_scale, void* dq,
+                            void* dk, void* dv, int64_t dq_row_stride, int64_t dk_row_stride, int64_t dv_row_stride, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
  * spa_packed_attention under a second name, for callers linked against it: every form takes the exponentials against
  * the running maximum of the scores.
  */

@@ -1,0 +1,135 @@
+// What the forward and the backward of the attention to another sequence share (cross_attention.hip, cross_attention_bwd.hip).
+//
+// The rows of a unit (segment b, key head hk) are the nq tokens of the segment times the G = H / Hk query heads that share the key
+// head: row r is token r / G, head hk G + r % G.  So keys and values are fetched once for all of them, a few tokens fill a wave's 32
+// rows, and the sums over the heads of a group are the sums over rows of the backward.
+#pragma once
+
+#include <type_traits>
+
+#include "attn_ops.h"
+#include "attn_tiles.h"
+#include "divisor.h"
+#include "spa_common.h"
+
+namespace spa {
+
+constexpr int kCrossThreads = 256;
+
+struct CrossShape {
+  const int32_t *cu_q, *cu_k, *key_lens;
+  int B, H, Hk;
+  Divisor G;                     // query heads a key head
+  int blocks;                    // workgroups along the owned rows of the longest possible segment
+  int splits;                    // and along the others
+  float scale, c;                // c = scale log2 e: exponents of 2
+  long stat_stride;              // of lse and D: entry (h, row)
+  int most_q, most_k;            // tokens and keys of the longest possible segment (longer ones are cut)
+};
+
+// A workgroup's unit: (segment, key head, block of owned rows, split of the others)
+struct CrossUnit {
+  int b, hk, block, split;
+  bool valid;
+  long q0, k0;                   // the segment's first rows
+  int nq, nk, held;              // rows (tokens times heads), keys, keys the segment has places for
+};
+__device__ __forceinline__ void cross_lengths(const CrossShape& s, int b, int q0, int k0, int& nq, int& nk, int& held) {
+  nq = min(max(s.cu_q[b + 1] - q0, 0), s.most_q) * (int)s.G.d;
+  held = min(max(s.cu_k[b + 1] - k0, 0), s.most_k);
+  nk = s.key_lens != nullptr ? min(max(s.key_lens[b], 0), held) : held;
+}
+__device__ __forceinline__ CrossUnit cross_unit(const CrossShape& s) {
+  // blocks and splits of a pair next to each other on one XCD, whose L2 then holds what they share
+  const TileId t = xcd_tile(s.blocks * s.splits, s.Hk, s.B);
+  CrossUnit u = {t.rank, t.h, t.qb / s.splits, 0, t.valid, 0, 0, 0, 0, 0};
+  u.split = t.qb - u.block * s.splits;
+  if (!t.valid) return u;
+  const int q0 = s.cu_q[u.b], k0 = s.cu_k[u.b];
+  cross_lengths(s, u.b, q0, k0, u.nq, u.nk, u.held);
+  u.q0 = q0;
+  u.k0 = k0;
+  return u;
+}
+// A split's share of n rows in steps of STEP: all of them but the last have as many
+struct Share {
+  int from, n, live;             // first row, rows, splits that have any
+};
+template <int STEP>
+__device__ __forceinline__ Share share_of(int n, int splits, int split) {
+  if (splits == 1) return {0, n, 1};
+  const int steps = (n + STEP - 1) / STEP, each = (steps + splits - 1) / splits * STEP;
+  if (n == 0) return {0, 0, 1};
+  return {split * each, min(each, n - split * each), (n + each - 1) / each};
+}
+
+// Offset of row r (token r / G, head r % G of the group) of a tensor of `stride` elements a token
+template <int DH>
+__device__ __forceinline__ long group_row(const Divisor& G, int r, long stride) {
+  const uint32_t i = quotient((uint32_t)r, G);
+  return (long)i * stride + (long)(r - (int)(i * G.d)) * DH;
+}
+
+// BT rows of two operands on their way to LDS, in 16-byte pieces.  Nothing here waits for a load or branches on one between load() and store();
+// rows past the end are loaded as the last one, and store<true>() clears operand 1's (the caller gives such rows probability 0, and 0
+// times an infinity of the last row would be NaN).  GROUPED: rows of a unit's tokens and heads (group_row), else of one head.
+template <typename T, int DH, int BT, bool GROUPED>
+struct CrossStage {
+  static constexpr int RS = Ops<T, DH>::RS, VE = 16 / sizeof(T), CPR = DH / VE, CPT = BT * CPR / kCrossThreads, RPP = kCrossThreads / CPR;
+  static_assert(BT * CPR % kCrossThreads == 0, "whole passes");
+  const T *a, *b;                // the thread's column of the first row
+  long as, bs;
+  const Divisor& G;
+  int tid, last, from;
+  uintx4 v[2][CPT];
+  __device__ __forceinline__ CrossStage(const T* a_, long as_, const T* b_, long bs_, const Divisor& G_, int last_)
+      : a(a_ + threadIdx.x % CPR * VE), b(b_ + threadIdx.x % CPR * VE), as(as_), bs(bs_), G(G_), tid(threadIdx.x), last(last_), from(0) {}
+  __device__ __forceinline__ int row(int t) const { return tid / CPR + t * RPP; }
+  __device__ __forceinline__ void load(int t0) {
+    from = t0;
+#pragma unroll
+    for (int t = 0; t < CPT; ++t) {
+      const int r = min(t0 + row(t), last);
+      v[0][t] = *reinterpret_cast<const uintx4*>(a + (GROUPED ? group_row<DH>(G, r, as) : (long)r * as));
+      v[1][t] = *reinterpret_cast<const uintx4*>(b + (GROUPED ? group_row<DH>(G, r, bs) : (long)r * bs));
+    }
+  }
+  template <bool LAST>
+  __device__ __forceinline__ void store(T* ta, T* tb) {
+#pragma unroll
+    for (int t = 0; t < CPT; ++t) {
+      if (LAST && from + row(t) > last) v[1][t] = uintx4{0, 0, 0, 0};
+      const int o = row(t) * RS + tid % CPR * VE;
+      *reinterpret_cast<uintx4*>(ta + o) = v[0][t];
+      *reinterpret_cast<uintx4*>(tb + o) = v[1][t];
+    }
+  }
+};
+
+// KW waves of the four share 32 owned rows, each takes a part of every step of the others.
+template <int KW>
+struct CrossSteps {
+  static constexpr int RW = 4 / KW, STEP = KW == 1 ? 64 : 128, TILE = STEP / KW, ROWS = 32 * RW;
+};
+
+// ---- host
+struct CrossPlan {
+  int kw, blocks, splits;
+};
+size_t cross_up(size_t n);
+// What the entry points of both directions check and have in common.
+struct CrossCall {
+  const void *q, *k, *v;
+  int64_t qs, ks, vs;
+  const int32_t *cu_q, *cu_k, *key_lens;
+  int B, max_q, max_k, H, Hk, Dh, dtype;
+  float softmax_scale;
+};
+int cross_checks(const char* fn, const CrossCall& c);
+bool cross_sizes_ok(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtype);
+// Blocks of owned rows and splits of the others for `owned` and `others` rows of the longest segment in `units` units
+CrossPlan cross_plan(long units, long owned, long others);
+CrossShape cross_shape(const CrossCall& c, const CrossPlan& p);
+inline long cross_grid(const CrossShape& s) { return ((long)s.Hk * s.B + 7) / 8 * 8 * s.blocks * s.splits; }
+
+}  // namespace spa

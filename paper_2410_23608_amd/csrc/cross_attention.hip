@@ -1,0 +1,334 @@
+// Attention of packed rows to the keys of another sequence of another length (an encoder's states, the packed tokens themselves for a few
+// queries): O = softmax(scale Q K^T) V, rows of segment b against the keys of segment b, key heads shared by G query heads; segments
+// without a key give 0.
+//
+// A wave owns 32 rows (tokens times heads of a group, cross_attention.h) and computes S^T = K Q^T, so that a lane holds 16 keys of one
+// row a 32 x 32 block, and the probabilities (bf16: rounded) are the second product's operand in registers; K and V stream through LDS.
+// The maximum and the sum run along, in fp32.  Few rows: the four waves share 32 (or 64) of them, each with its part of every step of keys;
+// few units with long keys: the keys are split over workgroups, which leave unnormalised sums, maxima and row sums in fp32 for a
+// second launch that joins them in the order of the splits.
+#include <algorithm>
+#include <cmath>
+
+#include "cross_attention.h"
+
+namespace spa {
+
+template <typename T>
+struct CrossFwd {
+  const T *q, *k, *v;
+  long qs, ks, vs;
+  CrossShape s;
+  T* out;
+  float* lse;
+  float* part;                   // [unit][split][row of the unit][DH], then [..][row][2]: maximum and sum; or null
+  long part_rows;                // rows of a unit there
+  float* part_ms;
+};
+
+template <typename T, int DH, int KW>
+struct CrossTiles {
+  static constexpr int STEP = CrossSteps<KW>::STEP, RS = Ops<T, DH>::RS;
+  __attribute__((aligned(16))) T K[2][STEP * RS];
+  __attribute__((aligned(16))) T V[2][STEP * RS];
+};
+
+template <typename T, int DH, int KW>
+__global__ void __launch_bounds__(kCrossThreads) cross_fwd_kernel(const CrossFwd<T> a) {
+  using O = Ops<T, DH>;
+  using W = CrossSteps<KW>;
+  constexpr int DB = DH / 32, NB = W::TILE / 32;
+  extern __shared__ __attribute__((aligned(16))) unsigned char cross_smem[];
+  CrossTiles<T, DH, KW>& l = *reinterpret_cast<CrossTiles<T, DH, KW>*>(cross_smem);
+  const CrossUnit u = cross_unit(a.s);
+  const int r0 = u.block * W::ROWS;
+  if (!u.valid || r0 >= u.nq) return;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rw = wave / KW, part = wave % KW, r = r0 + rw * 32 + l32;
+  const bool ok = r < u.nq, wave_live = r0 + rw * 32 < u.nq;
+  const int rc = min(r, u.nq - 1), G = (int)a.s.G.d;
+  const Share sh = share_of<W::STEP>(u.nk, a.s.splits, u.split);
+  if (sh.n <= 0 && u.split > 0) return;
+  const int n = sh.n, nt = (n + W::STEP - 1) / W::STEP;
+  const long first = u.k0 + sh.from;
+  floatx16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  float m = -INFINITY, sum = 0.f;
+  CrossStage<T, DH, W::STEP, false> st(a.k + first * a.ks + u.hk * DH, a.ks, a.v + first * a.vs + u.hk * DH, a.vs, a.s.G, n - 1);
+  if (nt > 0) st.load(0);
+  const typename O::Row qf = O::row(a.q + u.q0 * a.qs + (long)u.hk * G * DH + group_row<DH>(a.s.G, rc, a.qs), hh);
+  if (nt > 0) st.template store<true>(l.K[0], l.V[0]);
+  __syncthreads();
+  walk_tiles(nt, [&](int t, auto at) {
+    constexpr bool end = decltype(at)::value == kTileLast;
+    const int buf = t & 1, left = n - t * W::STEP - part * W::TILE;
+    if (!end) st.load(t * W::STEP + W::STEP);
+    if (wave_live && (!end || left > 0)) {
+      const T *K = &l.K[buf][part * W::TILE * O::RS], *V = &l.V[buf][part * W::TILE * O::RS];
+      floatx16 s[NB];
+      const int blocks = !end ? NB : min(NB, (left + 31) / 32);
+#pragma unroll
+      for (int sb = 0; sb < NB; ++sb)
+        if (!end || sb < blocks) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[sb][i] = 0.f;
+          O::dot(s[sb], O::row(&K[(sb * 32 + l32) * O::RS], hh), qf);
+        }
+      if (end) {
+#pragma unroll
+        for (int sb = 0; sb < NB; ++sb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (sb * 32 + acc_row(i, hh) >= left) s[sb][i] = -INFINITY;
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int sb = 0; sb < NB; ++sb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = __builtin_elementwise_maximum(mx, s[sb][i]);
+      const float m_new = __builtin_elementwise_maximum(m, max_across_halves(mx));
+      if (__ballot(m_new != m) != 0) {
+        const float f = m_new != m ? __builtin_amdgcn_exp2f((m - m_new) * a.s.c) : 1.f;
+        sum *= f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        m = m_new;
+      }
+      if (__ballot(fabsf(m) * a.s.scale >= kFarScore) == 0) {
+        const float m2 = m * a.s.c;
+#pragma unroll
+        for (int sb = 0; sb < NB; ++sb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[sb][i] = __builtin_amdgcn_exp2f(fmaf(s[sb][i], a.s.c, -m2));
+      } else {
+        const float ref = m == -INFINITY ? 0.f : m;             // (no score yet: weights of 0)
+#pragma unroll
+        for (int sb = 0; sb < NB; ++sb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[sb][i] = __builtin_amdgcn_exp2f((s[sb][i] - ref) * a.s.c);
+      }
+#pragma unroll
+      for (int sb = 0; sb < NB; ++sb) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += s[sb][i];
+        if (!end || sb < blocks) O::outer(o, V, sb, s[sb], lane);
+      }
+    }
+    if (!end) st.template store<decltype(at)::value == kTileBeforeLast>(l.K[buf ^ 1], l.V[buf ^ 1]);
+    __syncthreads();
+  });
+  // the waves that share rows: the others hand their sums to the first, which adds them in order
+  if constexpr (KW > 1) {
+    constexpr int N = DB * 16 + 2;
+    static_assert((KW - 1) * W::RW * N * kWave * sizeof(float) <= sizeof(CrossTiles<T, DH, KW>), "the sums of the other waves");
+    float* const sums = reinterpret_cast<float*>(cross_smem) + lane;
+    if (part > 0) {
+      float* mine = sums + ((part - 1) * W::RW + rw) * N * kWave;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mine[(d * 16 + i) * kWave] = o[d][i];
+      mine[(N - 2) * kWave] = m;
+      mine[(N - 1) * kWave] = sum;
+    }
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int p = 0; p < KW - 1; ++p) {
+      const float* other = sums + (p * W::RW + rw) * N * kWave;
+      const float m1 = other[(N - 2) * kWave], both = __builtin_elementwise_maximum(m, m1);
+      const float f0 = m == both ? 1.f : __builtin_amdgcn_exp2f((m - both) * a.s.c);
+      const float f1 = m1 == both ? 1.f : __builtin_amdgcn_exp2f((m1 - both) * a.s.c);
+      m = both;
+      sum = sum * f0 + other[(N - 1) * kWave] * f1;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * f0 + other[(d * 16 + i) * kWave] * f1;
+    }
+  }
+  if (!wave_live) return;
+  const float total = sum_across_halves(sum);
+  if (a.part != nullptr) {
+    const long at = (((long)u.b * a.s.Hk + u.hk) * a.s.splits + u.split) * a.part_rows + rc;
+    if (!ok) return;
+    float* row = a.part + at * DH;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<floatx4*>(row + d * 32 + 8 * g + 4 * hh) = floatx4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+    if (hh == 0) *reinterpret_cast<floatx2*>(a.part_ms + at * 2) = floatx2{m, total};
+    return;
+  }
+  const float inv = total == 0.f ? 0.f : 1.0f / total;          // (0: no key, all weights 0)
+  const long C = (long)a.s.H * DH;
+  O::store(o, inv, a.out + u.q0 * C + (long)u.hk * G * DH + group_row<DH>(a.s.G, rc, C), ok, hh);
+  if (a.lse != nullptr && ok && hh == 0) {
+    const uint32_t i = quotient((uint32_t)rc, a.s.G);
+    a.lse[(u.hk * G + (rc - (int)(i * G))) * a.s.stat_stride + u.q0 + i] = total == 0.f ? -INFINITY : m * a.s.scale + logf(total);
+  }
+}
+
+// Joins the splits of a row in their order: DH / 4 lanes a row.
+template <typename T, int DH, int STEP>
+__global__ void __launch_bounds__(kCrossThreads) cross_join_kernel(const CrossFwd<T> a) {
+  constexpr int LANES = DH / 4, ROWS = kCrossThreads / LANES, U = 8;
+  const int G = (int)a.s.G.d, c = threadIdx.x % LANES * 4;
+  const long per = (a.part_rows + ROWS - 1) / ROWS, unit = blockIdx.x / per;
+  const int r = (int)(blockIdx.x % per) * ROWS + threadIdx.x / LANES, b = (int)(unit / a.s.Hk), hk = (int)(unit % a.s.Hk);
+  const int q0 = a.s.cu_q[b];
+  int nq, nk, held;
+  cross_lengths(a.s, b, q0, a.s.cu_k[b], nq, nk, held);
+  if (r >= nq) return;
+  const int live = share_of<STEP>(nk, a.s.splits, 0).live;
+  const long at = unit * a.s.splits * a.part_rows + r;
+  float m = -INFINITY, sum = 0.f;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < live; s0 += U) {
+    floatx2 ms[U];
+    floatx4 v[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const long row = at + (long)min(s0 + i, live - 1) * a.part_rows;
+      ms[i] = *reinterpret_cast<const floatx2*>(a.part_ms + row * 2);
+      v[i] = *reinterpret_cast<const floatx4*>(a.part + row * DH + c);
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (s0 + i >= live) break;
+      const float both = __builtin_elementwise_maximum(m, ms[i][0]);
+      const float f0 = m == both ? 1.f : __builtin_amdgcn_exp2f((m - both) * a.s.c);
+      const float f1 = ms[i][0] == both ? 1.f : __builtin_amdgcn_exp2f((ms[i][0] - both) * a.s.c);
+      m = both;
+      sum = sum * f0 + ms[i][1] * f1;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = o[e] * f0 + v[i][e] * f1;
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  const long C = (long)a.s.H * DH;
+  const uint32_t i = quotient((uint32_t)r, a.s.G);
+  const int h = hk * G + r - (int)(i * G);
+  T* to = a.out + ((long)q0 + i) * C + (long)h * DH + c;
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4*>(to) = __builtin_convertvector(o * inv, bf16x4);
+  else *reinterpret_cast<floatx4*>(to) = o * inv;
+  if (a.lse != nullptr && c == 0) a.lse[h * a.s.stat_stride + q0 + i] = sum == 0.f ? -INFINITY : m * a.s.scale + logf(sum);
+}
+
+// ------------------------------------------------------------------------------- host
+size_t cross_up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+bool cross_sizes_ok(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtype) {
+  return B >= 1 && B <= 65535 && max_q >= 1 && max_k >= 1 && H >= 1 && H <= 65535 && Hk >= 1 && H % Hk == 0 && (long)B * max_q < 2147483647L &&
+         (long)B * max_k < 2147483647L && (long)max_q * (H / Hk) < 2147483647L - 256 && (Dh == 32 || Dh == 64) &&
+         (dtype == SPA_F32 || dtype == SPA_BF16);
+}
+
+// Few rows: the waves share them.  Few workgroups and long rows on the other side: these are split, into no less than four steps each, until
+// there are about three workgroups a unit.
+CrossPlan cross_plan(long units, long owned, long others) {
+  CrossPlan p = {owned <= 32 ? 4 : owned <= 64 ? 2 : 1, 1, 1};
+  const int rows = 128 / p.kw;
+  p.blocks = (int)((owned + rows - 1) / rows);
+  const long groups = units * p.blocks;
+  if (groups < 512) p.splits = (int)std::max(1L, std::min((768 + groups - 1) / groups, others / 512));
+  return p;
+}
+
+CrossShape cross_shape(const CrossCall& c, const CrossPlan& p) {
+  const float scale = c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / std::sqrt((float)c.Dh);
+  return {c.cu_q, c.cu_k, c.key_lens, c.B, c.H, c.Hk, divisor((uint32_t)(c.H / c.Hk)), p.blocks, p.splits, scale, scale * kLog2e,
+          (long)c.B * c.max_q, c.max_q, c.max_k};
+}
+
+int cross_checks(const char* fn, const CrossCall& c) {
+  SPA_REFUSE_IN_GROUP(fn);
+  SPA_REQUIRE(c.q && c.k && c.v && c.cu_q && c.cu_k, SPA_ERR_INVALID_ARG, "%s: null pointer", fn);
+  SPA_REQUIRE(c.B >= 1 && c.max_q >= 1 && c.max_k >= 1 && c.H >= 1 && c.Hk >= 1, SPA_ERR_INVALID_ARG, "%s: B, max_q, max_k, H, Hk must be >= 1", fn);
+  SPA_REQUIRE(c.H % c.Hk == 0, SPA_ERR_INVALID_ARG, "%s: H = %d is not a multiple of Hk = %d", fn, c.H, c.Hk);
+  SPA_REQUIRE(c.B <= 65535 && c.H <= 65535, SPA_ERR_INVALID_ARG, "%s: B and H must be <= 65535", fn);
+  SPA_REQUIRE((long)c.B * c.max_q < 2147483647L && (long)c.B * c.max_k < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*max_q and B*max_k must be < 2^31", fn);
+  SPA_REQUIRE((long)c.max_q * (c.H / c.Hk) < 2147483647L - 256, SPA_ERR_INVALID_ARG, "%s: max_q*H/Hk must be < 2^31", fn);
+  SPA_REQUIRE(c.dtype == SPA_F32 || c.dtype == SPA_BF16, SPA_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, c.dtype);
+  SPA_REQUIRE(c.Dh == 32 || c.Dh == 64, SPA_ERR_UNSUPPORTED, "%s: head dim %d not supported (32 or 64)", fn, c.Dh);
+  const int64_t strides[3] = {c.qs, c.ks, c.vs};
+  for (int i = 0; i < 3; ++i) {
+    SPA_REQUIRE(strides[i] >= (int64_t)(i == 0 ? c.H : c.Hk) * c.Dh, SPA_ERR_INVALID_ARG, "%s: row stride %ld < heads * Dh", fn, (long)strides[i]);
+    SPA_REQUIRE(strides[i] < (1LL << 31), SPA_ERR_INVALID_ARG, "%s: row stride %ld must be < 2^31 elements", fn, (long)strides[i]);
+    SPA_REQUIRE(strides[i] * elem_size(c.dtype) % 16 == 0, SPA_ERR_INVALID_ARG, "%s: row stride is not a multiple of 16 bytes", fn);
+  }
+  SPA_REQUIRE(aligned16(c.q) && aligned16(c.k) && aligned16(c.v), SPA_ERR_INVALID_ARG, "%s: q/k/v not 16-byte aligned", fn);
+  SPA_REQUIRE(c.softmax_scale >= 0.f && std::isfinite(c.softmax_scale), SPA_ERR_INVALID_ARG,
+              "%s: softmax_scale must be finite and >= 0 (0 = 1/sqrt(Dh))", fn);
+  return SPA_OK;
+}
+
+static CrossPlan fwd_plan(int B, int max_q, int max_k, int H, int Hk) { return cross_plan((long)B * Hk, (long)max_q * (H / Hk), max_k); }
+
+template <typename T, int DH, int KW>
+static int launch_fwd(const char* fn, const CrossFwd<T>& a, hipStream_t st) {
+  constexpr size_t lds = sizeof(CrossTiles<T, DH, KW>);
+  const auto kernel = cross_fwd_kernel<T, DH, KW>;
+  const hipError_t attr = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  SPA_REQUIRE(attr == hipSuccess, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, lds);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)cross_grid(a.s)), dim3(kCrossThreads), lds, st, a);
+  if (a.part != nullptr) {
+    constexpr int rows = kCrossThreads / (DH / 4);
+    const long blocks = (long)a.s.B * a.s.Hk * ((a.part_rows + rows - 1) / rows);
+    hipLaunchKernelGGL((cross_join_kernel<T, DH, CrossSteps<KW>::STEP>), dim3((unsigned)blocks), dim3(kCrossThreads), 0, st, a);
+  }
+  return check_launch(fn);
+}
+
+template <typename T>
+static int run_fwd(const char* fn, const CrossCall& c, const CrossPlan& p, void* out, float* lse, void* ws, hipStream_t st) {
+  CrossFwd<T> a = {(const T*)c.q, (const T*)c.k, (const T*)c.v, (long)c.qs, (long)c.ks, (long)c.vs, cross_shape(c, p), (T*)out, lse, nullptr, 0, nullptr};
+  if (p.splits > 1) {
+    a.part_rows = (long)c.max_q * (c.H / c.Hk);
+    a.part = (float*)ws;
+    a.part_ms = (float*)((char*)ws + cross_up((size_t)c.B * c.Hk * p.splits * a.part_rows * c.Dh * sizeof(float)));
+  }
+#define SPA_KW(D) \
+  return p.kw == 1 ? launch_fwd<T, D, 1>(fn, a, st) : p.kw == 2 ? launch_fwd<T, D, 2>(fn, a, st) : launch_fwd<T, D, 4>(fn, a, st)
+  if (c.Dh == 32) SPA_KW(32);
+  SPA_KW(64);
+#undef SPA_KW
+}
+
+}  // namespace spa
+
+using namespace spa;
+
+extern "C" size_t spa_cross_attention_workspace_bytes(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtype) {
+  if (!cross_sizes_ok(B, max_q, max_k, H, Hk, Dh, dtype)) return 0;
+  const CrossPlan p = fwd_plan(B, max_q, max_k, H, Hk);
+  if (p.splits == 1) return 0;
+  const size_t rows = (size_t)B * max_q * H * p.splits;
+  return cross_up(rows * Dh * sizeof(float)) + cross_up(rows * 2 * sizeof(float));
+}
+
+extern "C" int spa_cross_attention(const void* q, const void* k, const void* v, int64_t q_row_stride, int64_t k_row_stride, int64_t v_row_stride,
+                                   const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, const int32_t* key_lens, int B, int max_q,
+                                   int max_k, int H, int Hk, int Dh, int dtype, float softmax_scale, void* out, float* lse, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  const char* fn = "spa_cross_attention";
+  const CrossCall c = {q, k, v, q_row_stride, k_row_stride, v_row_stride, cu_seqlens_q, cu_seqlens_k, key_lens, B, max_q, max_k, H, Hk, Dh, dtype,
+                       softmax_scale};
+  if (int rc = cross_checks(fn, c)) return rc;
+  SPA_REQUIRE(out != nullptr, SPA_ERR_INVALID_ARG, "%s: out is null", fn);
+  SPA_REQUIRE(aligned16(out), SPA_ERR_INVALID_ARG, "%s: out not 16-byte aligned", fn);
+  const CrossPlan p = fwd_plan(B, max_q, max_k, H, Hk);
+  SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*Hk*blocks must be < 2^31", fn);
+  const size_t need = spa_cross_attention_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype);
+  SPA_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need), SPA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given",
+              fn, need, workspace_bytes);
+  SPA_REQUIRE(need == 0 || (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0, SPA_ERR_INVALID_ARG, "%s: workspace not 256-byte aligned", fn);
+  return dtype == SPA_F32 ? run_fwd<float>(fn, c, p, out, lse, workspace, as_stream(stream))
+                          : run_fwd<__bf16>(fn, c, p, out, lse, workspace, as_stream(stream));
+}

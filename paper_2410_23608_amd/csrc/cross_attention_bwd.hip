@@ -1,0 +1,427 @@
+// Backward of the attention to another sequence (cross_attention.hip): with P = exp(S - lse), dP = dO V^T, D_r = <dO_r, O_r>, dS = P (dP - D)
+//   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO        (sums over the tokens and the heads that share the key head)
+// Two launches.  The dq launch walks the keys for 32 rows a wave as the forward does and leaves D; the dk / dv launch walks the rows for 32 keys a wave, S
+// and dP un-transposed (a lane is a key), so that P and dS are operands in registers again.  D is formed from the rounded result.  Few owned
+// rows: the four waves share them.  Few units and many rows on the other side: those are split over workgroups, whose fp32 sums a further launch adds
+// in the order of the splits.  Everything is added in a fixed order.
+#include <algorithm>
+#include <cmath>
+
+#include "cross_attention.h"
+
+namespace spa {
+
+template <typename T>
+struct CrossBwd {
+  const T *q, *k, *v, *out, *dout;
+  long qs, ks, vs;
+  CrossShape s;
+  const float* lse;
+  float* D;                      // [H][stat_stride]
+  T *dq, *dk, *dv;
+  long dqs, dks, dvs;
+  float* part;                   // [unit][split][owned row][DH], of dk / dv [..][2][DH]; or null
+  long part_rows;
+};
+
+template <typename T, int DH, int KW>
+struct CrossDqTiles {
+  static constexpr int STEP = CrossSteps<KW>::STEP, RS = Ops<T, DH>::RS;
+  __attribute__((aligned(16))) T K[2][STEP * RS];
+  __attribute__((aligned(16))) T V[2][STEP * RS];
+};
+
+template <typename T, int DH, int KW>
+__global__ void __launch_bounds__(kCrossThreads, sizeof(T) == 4 ? 1 : 2) cross_dq_kernel(const CrossBwd<T> a) {
+  using O = Ops<T, DH>;
+  using W = CrossSteps<KW>;
+  constexpr int DB = DH / 32, NB = W::TILE / 32;
+  extern __shared__ __attribute__((aligned(16))) unsigned char cross_smem[];
+  CrossDqTiles<T, DH, KW>& l = *reinterpret_cast<CrossDqTiles<T, DH, KW>*>(cross_smem);
+  const CrossUnit u = cross_unit(a.s);
+  const int r0 = u.block * W::ROWS;
+  if (!u.valid || r0 >= u.nq) return;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rw = wave / KW, part = wave % KW, r = r0 + rw * 32 + l32;
+  const bool ok = r < u.nq, wave_live = r0 + rw * 32 < u.nq;
+  const int rc = min(r, u.nq - 1), G = (int)a.s.G.d;
+  const Share sh = share_of<W::STEP>(u.nk, a.s.splits, u.split);
+  if (sh.n <= 0 && u.split > 0) return;
+  const int n = sh.n, nt = (n + W::STEP - 1) / W::STEP;
+  const long first = u.k0 + sh.from, C = (long)a.s.H * DH;
+  floatx16 acc[DB], negD;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+  CrossStage<T, DH, W::STEP, false> st(a.k + first * a.ks + u.hk * DH, a.ks, a.v + first * a.vs + u.hk * DH, a.vs, a.s.G, n - 1);
+  if (nt > 0) st.load(0);
+  const uint32_t token = quotient((uint32_t)rc, a.s.G);
+  const long stat = (u.hk * G + (rc - (int)(token * G))) * a.s.stat_stride + u.q0 + token;
+  const long dense = u.q0 * C + (long)u.hk * G * DH + group_row<DH>(a.s.G, rc, C);
+  const float lse = a.lse[stat];
+  const typename O::Row qf = O::row(a.q + u.q0 * a.qs + (long)u.hk * G * DH + group_row<DH>(a.s.G, rc, a.qs), hh);
+  const typename O::Row gf = O::row(a.dout + dense, hh);
+  {
+    const typename O::Row of = O::row(a.out + dense, hh);
+    float D = 0.f, unused = 0.f;
+    O::sums(gf, of, D, unused);
+    D = sum_across_halves(D);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) negD[i] = -D;
+    if (u.split == 0 && part == 0 && ok && hh == 0) a.D[stat] = D;
+  }
+  const bool none = lse == -INFINITY || !ok, far = __ballot(!none && fabsf(lse) >= kFarScore) != 0;
+  const float ref = none ? INFINITY : lse, lse2 = ref * kLog2e;
+  if (nt > 0) st.template store<true>(l.K[0], l.V[0]);
+  __syncthreads();
+  walk_tiles(nt, [&](int t, auto at) {
+    constexpr bool end = decltype(at)::value == kTileLast;
+    const int buf = t & 1, left = n - t * W::STEP - part * W::TILE;
+    if (!end) st.load(t * W::STEP + W::STEP);
+    if (wave_live) {
+      const T *K = &l.K[buf][part * W::TILE * O::RS], *V = &l.V[buf][part * W::TILE * O::RS];
+#pragma unroll
+      for (int sb = 0; sb < NB; ++sb) {
+        if (end && sb * 32 >= left) break;
+        floatx16 s, dp = negD;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        O::dot(s, O::row(&K[(sb * 32 + l32) * O::RS], hh), qf);
+        O::dot(dp, O::row(&V[(sb * 32 + l32) * O::RS], hh), gf);
+        if (end) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (sb * 32 + acc_row(i, hh) >= left) s[i] = -INFINITY;
+        }
+        if (!far) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.s.c, -lse2));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.s.scale, -ref) * kLog2e);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dp[i] *= s[i];
+        O::outer(acc, K, sb, dp, lane);
+      }
+    }
+    if (!end) st.template store<decltype(at)::value == kTileBeforeLast>(l.K[buf ^ 1], l.V[buf ^ 1]);
+    __syncthreads();
+  });
+  if constexpr (KW > 1) {
+    constexpr int N = DB * 16;
+    static_assert((KW - 1) * W::RW * N * kWave * sizeof(float) <= sizeof(l), "the sums of the other waves");
+    float* const sums = reinterpret_cast<float*>(cross_smem) + lane;
+    if (part > 0) {
+      float* mine = sums + ((part - 1) * W::RW + rw) * N * kWave;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mine[(d * 16 + i) * kWave] = acc[d][i];
+    }
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int p = 0; p < KW - 1; ++p) {
+      const float* other = sums + (p * W::RW + rw) * N * kWave;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] += other[(d * 16 + i) * kWave];
+    }
+  }
+  if (!wave_live) return;
+  if (a.part != nullptr) {
+    if (!ok) return;
+    float* row = a.part + ((((long)u.b * a.s.Hk + u.hk) * a.s.splits + u.split) * a.part_rows + rc) * DH;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<floatx4*>(row + d * 32 + 8 * g + 4 * hh) = floatx4{acc[d][4 * g], acc[d][4 * g + 1], acc[d][4 * g + 2], acc[d][4 * g + 3]};
+    return;
+  }
+  O::store(acc, a.s.scale, a.dq + u.q0 * a.dqs + (long)u.hk * G * DH + group_row<DH>(a.s.G, rc, a.dqs), ok, hh);
+}
+
+template <typename T, int DH, int KW>
+struct CrossKeyTiles {
+  static constexpr int STEP = CrossSteps<KW>::STEP, RS = Ops<T, DH>::RS;
+  __attribute__((aligned(16))) T Q[2][STEP * RS];
+  __attribute__((aligned(16))) T G[2][STEP * RS];             // dO
+  __attribute__((aligned(16))) float lse[2][STEP];            // +inf: no key, or no row (probability 0)
+  __attribute__((aligned(16))) float lse2[2][STEP];           // times log2 e
+  __attribute__((aligned(16))) float negD[2][STEP];
+  int far[2][STEP / 64];
+};
+
+template <typename T, int DH, int KW>
+__global__ void __launch_bounds__(kCrossThreads, sizeof(T) == 4 ? 1 : 2) cross_dkdv_kernel(const CrossBwd<T> a) {
+  using O = Ops<T, DH>;
+  using W = CrossSteps<KW>;
+  constexpr int DB = DH / 32, NB = W::TILE / 32;
+  extern __shared__ __attribute__((aligned(16))) unsigned char cross_smem[];
+  CrossKeyTiles<T, DH, KW>& l = *reinterpret_cast<CrossKeyTiles<T, DH, KW>*>(cross_smem);
+  const CrossUnit u = cross_unit(a.s);
+  const int k0 = u.block * W::ROWS;
+  if (!u.valid || k0 >= u.held) return;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = wave / KW, part = wave % KW, ki = k0 + rw * 32 + l32, G = (int)a.s.G.d;
+  const bool wave_live = k0 + rw * 32 < u.nk;
+  const Share sh = share_of<W::STEP>(u.nq, a.s.splits, u.split);
+  if (sh.n <= 0 && u.split > 0) return;
+  if (a.part != nullptr && k0 >= u.nk) return;                // (rows behind the keys: the launch that adds clears them)
+  const int n = k0 < u.nk ? sh.n : 0, nt = (n + W::STEP - 1) / W::STEP;
+  const long C = (long)a.s.H * DH, head = (long)u.hk * G * DH, k_row = u.k0 + min(ki, max(u.nk - 1, 0));
+  floatx16 dka[DB], dva[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dka[d][i] = dva[d][i] = 0.f;
+  if (nt > 0) {
+    CrossStage<T, DH, W::STEP, true> st(a.q + u.q0 * a.qs + head, a.qs, a.dout + u.q0 * C + head, C, a.s.G, sh.from + n - 1);
+    float lse_t = 0.f, d_t = 0.f;
+    auto load = [&](int t0) {
+      st.load(sh.from + t0);
+      const int r = sh.from + min(t0 + (tid & (W::STEP - 1)), n - 1);
+      const uint32_t i = quotient((uint32_t)r, a.s.G);
+      const long stat = (u.hk * G + (r - (int)(i * G))) * a.s.stat_stride + u.q0 + i;
+      lse_t = a.lse[stat];
+      d_t = a.D[stat];
+    };
+    auto store = [&](int buf, int t0, auto clear) {
+      st.template store<clear>(l.Q[buf], l.G[buf]);
+      if (tid < W::STEP) {
+        const bool none = lse_t == -INFINITY || t0 + tid >= n;
+        const bool any = __ballot(!none && fabsf(lse_t) >= kFarScore) != 0;
+        l.lse[buf][tid] = none ? INFINITY : lse_t;
+        l.lse2[buf][tid] = none ? INFINITY : lse_t * kLog2e;
+        l.negD[buf][tid] = -d_t;
+        if (lane == 0) l.far[buf][tid >> 6] = any;
+      }
+    };
+    load(0);
+    const typename O::Row kf = O::row(a.k + k_row * a.ks + u.hk * DH, hh), vf = O::row(a.v + k_row * a.vs + u.hk * DH, hh);
+    store(0, 0, std::true_type{});
+    __syncthreads();
+    walk_tiles(nt, [&](int t, auto at) {
+      constexpr bool end = decltype(at)::value == kTileLast;
+      const int buf = t & 1, left = n - t * W::STEP - part * W::TILE;
+      if (!end) load(t * W::STEP + W::STEP);
+      if (wave_live) {
+#pragma unroll
+        for (int sb = 0; sb < NB; ++sb) {
+          if (end && sb * 32 >= left) break;
+          const int at0 = part * W::TILE + sb * 32;
+          floatx16 s, dp;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const floatx4 d4 = *reinterpret_cast<const floatx4*>(&l.negD[buf][at0 + 8 * g + 4 * hh]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dp[4 * g + i] = d4[i];
+          }
+          O::dot(s, O::row(&l.Q[buf][(at0 + l32) * O::RS], hh), kf);
+          O::dot(dp, O::row(&l.G[buf][(at0 + l32) * O::RS], hh), vf);
+          if (__builtin_amdgcn_readfirstlane(l.far[buf][at0 >> 6]) == 0) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const floatx4 l4 = *reinterpret_cast<const floatx4*>(&l.lse2[buf][at0 + 8 * g + 4 * hh]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], a.s.c, -l4[i]));
+            }
+          } else {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const floatx4 l4 = *reinterpret_cast<const floatx4*>(&l.lse[buf][at0 + 8 * g + 4 * hh]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], a.s.scale, -l4[i]) * kLog2e);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) dp[i] *= s[i];
+          O::outer(dva, &l.G[buf][0], at0 / 32, s, lane);
+          O::outer(dka, &l.Q[buf][0], at0 / 32, dp, lane);
+        }
+      }
+      if (!end) store(buf ^ 1, t * W::STEP + W::STEP, std::bool_constant<decltype(at)::value == kTileBeforeLast>{});
+      __syncthreads();
+    });
+  }
+  if constexpr (KW > 1) {
+    constexpr int N = 2 * DB * 16;
+    static_assert((KW - 1) * W::RW * N * kWave * sizeof(float) <= sizeof(l), "the sums of the other waves");
+    float* const sums = reinterpret_cast<float*>(cross_smem) + lane;
+    if (part > 0) {
+      float* mine = sums + ((part - 1) * W::RW + rw) * N * kWave;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          mine[(d * 16 + i) * kWave] = dka[d][i];
+          mine[((DB + d) * 16 + i) * kWave] = dva[d][i];
+        }
+    }
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int p = 0; p < KW - 1; ++p) {
+      const float* other = sums + (p * W::RW + rw) * N * kWave;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          dka[d][i] += other[(d * 16 + i) * kWave];
+          dva[d][i] += other[((DB + d) * 16 + i) * kWave];
+        }
+    }
+  }
+  if (a.part != nullptr) {
+    if (ki >= u.nk) return;
+    float* row = a.part + ((((long)u.b * a.s.Hk + u.hk) * a.s.splits + u.split) * a.part_rows + ki) * 2 * DH;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float* to = row + d * 32 + 8 * g + 4 * hh;
+        *reinterpret_cast<floatx4*>(to) = floatx4{dka[d][4 * g], dka[d][4 * g + 1], dka[d][4 * g + 2], dka[d][4 * g + 3]};
+        *reinterpret_cast<floatx4*>(to + DH) = floatx4{dva[d][4 * g], dva[d][4 * g + 1], dva[d][4 * g + 2], dva[d][4 * g + 3]};
+      }
+    return;
+  }
+  if (ki >= u.nk) {                                           // places without a key: no gradient
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dka[d][i] = dva[d][i] = 0.f;
+  }
+  const bool ok = ki < u.held;
+  const long row = u.k0 + min(ki, u.held - 1);
+  O::store(dka, a.s.scale, a.dk + row * a.dks + u.hk * DH, ok, hh);
+  O::store(dva, 1.0f, a.dv + row * a.dvs + u.hk * DH, ok, hh);
+}
+
+// Adds the splits' sums of an owned row in their order: DH / 4 lanes a row of dq (WHICH 1), twice as many a row of dk and dv (WHICH 2).
+template <typename T, int DH, int STEP, int WHICH>
+__global__ void __launch_bounds__(kCrossThreads) cross_sum_kernel(const CrossBwd<T> a) {
+  constexpr int LANES = WHICH * DH / 4, ROWS = kCrossThreads / LANES, U = 8;
+  const int G = (int)a.s.G.d, c = threadIdx.x % LANES * 4;
+  const long per = (a.part_rows + ROWS - 1) / ROWS, unit = blockIdx.x / per;
+  const int r = (int)(blockIdx.x % per) * ROWS + threadIdx.x / LANES, b = (int)(unit / a.s.Hk), hk = (int)(unit % a.s.Hk);
+  const int q0 = a.s.cu_q[b], k0 = a.s.cu_k[b];
+  int nq, nk, held;
+  cross_lengths(a.s, b, q0, k0, nq, nk, held);
+  if (r >= (WHICH == 1 ? nq : held)) return;
+  const int live = WHICH == 2 && r >= nk ? 0 : share_of<STEP>(WHICH == 1 ? nk : nq, a.s.splits, 0).live;
+  const float* p = a.part + (unit * a.s.splits * a.part_rows + r) * WHICH * DH + c;
+  floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < live; s0 += U) {
+    floatx4 v[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) v[i] = *reinterpret_cast<const floatx4*>(p + (long)min(s0 + i, live - 1) * a.part_rows * WHICH * DH);
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (s0 + i < live) sum += v[i];
+  }
+  T* to;
+  if (WHICH == 1) {
+    to = a.dq + (long)q0 * a.dqs + (long)hk * G * DH + group_row<DH>(a.s.G, r, a.dqs) + c;
+    sum *= a.s.scale;
+  } else if (c < DH) {
+    to = a.dk + ((long)k0 + r) * a.dks + hk * DH + c;
+    sum *= a.s.scale;
+  } else {
+    to = a.dv + ((long)k0 + r) * a.dvs + hk * DH + c - DH;
+  }
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x4*>(to) = __builtin_convertvector(sum, bf16x4);
+  else *reinterpret_cast<floatx4*>(to) = sum;
+}
+
+// ------------------------------------------------------------------------------- host
+static CrossPlan dq_plan(int B, int max_q, int max_k, int H, int Hk) { return cross_plan((long)B * Hk, (long)max_q * (H / Hk), max_k); }
+static CrossPlan dkdv_plan(int B, int max_q, int max_k, int H, int Hk) { return cross_plan((long)B * Hk, max_k, (long)max_q * (H / Hk)); }
+
+template <typename T, int DH, int KW, bool KEYS>
+static int launch_bwd(const char* fn, const CrossBwd<T>& a, hipStream_t st) {
+  constexpr size_t lds = KEYS ? sizeof(CrossKeyTiles<T, DH, KW>) : sizeof(CrossDqTiles<T, DH, KW>);
+  const auto kernel = KEYS ? cross_dkdv_kernel<T, DH, KW> : cross_dq_kernel<T, DH, KW>;
+  const hipError_t attr = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  SPA_REQUIRE(attr == hipSuccess, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, lds);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)cross_grid(a.s)), dim3(kCrossThreads), lds, st, a);
+  if (a.part != nullptr) {
+    constexpr int which = KEYS ? 2 : 1, rows = kCrossThreads / (which * DH / 4);
+    const long blocks = (long)a.s.B * a.s.Hk * ((a.part_rows + rows - 1) / rows);
+    hipLaunchKernelGGL((cross_sum_kernel<T, DH, CrossSteps<KW>::STEP, which>), dim3((unsigned)blocks), dim3(kCrossThreads), 0, st, a);
+  }
+  return check_launch(fn);
+}
+
+struct CrossGrads {
+  const void *out, *dout;
+  const float* lse;
+  void *dq, *dk, *dv;
+  int64_t dqs, dks, dvs;
+};
+
+template <typename T>
+static int run_bwd(const char* fn, const CrossCall& c, const CrossGrads& g, void* ws, hipStream_t st) {
+  const CrossPlan plans[2] = {dq_plan(c.B, c.max_q, c.max_k, c.H, c.Hk), dkdv_plan(c.B, c.max_q, c.max_k, c.H, c.Hk)};
+  float* D = (float*)ws;
+  float* part = (float*)((char*)ws + cross_up((size_t)c.H * c.B * c.max_q * sizeof(float)));
+  for (int keys = 0; keys < 2; ++keys) {
+    const CrossPlan& p = plans[keys];
+    CrossBwd<T> a = {(const T*)c.q, (const T*)c.k, (const T*)c.v, (const T*)g.out, (const T*)g.dout, (long)c.qs, (long)c.ks, (long)c.vs,
+                     cross_shape(c, p), g.lse, D, (T*)g.dq, (T*)g.dk, (T*)g.dv, (long)g.dqs, (long)g.dks, (long)g.dvs, nullptr, 0};
+    if (p.splits > 1) {
+      a.part = part;                                          // (dq's are added before dk's and dv's are written)
+      a.part_rows = keys ? c.max_k : (long)c.max_q * (c.H / c.Hk);
+    }
+#define SPA_KW(D_, K_) \
+  p.kw == 1 ? launch_bwd<T, D_, 1, K_>(fn, a, st) : p.kw == 2 ? launch_bwd<T, D_, 2, K_>(fn, a, st) : launch_bwd<T, D_, 4, K_>(fn, a, st)
+    const int rc = c.Dh == 32 ? (keys ? SPA_KW(32, true) : SPA_KW(32, false)) : (keys ? SPA_KW(64, true) : SPA_KW(64, false));
+#undef SPA_KW
+    if (rc != SPA_OK) return rc;
+  }
+  return SPA_OK;
+}
+
+}  // namespace spa
+
+using namespace spa;
+
+extern "C" size_t spa_cross_attention_bwd_workspace_bytes(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtype) {
+  if (!cross_sizes_ok(B, max_q, max_k, H, Hk, Dh, dtype)) return 0;
+  const CrossPlan q = dq_plan(B, max_q, max_k, H, Hk), k = dkdv_plan(B, max_q, max_k, H, Hk);
+  const size_t rows_q = q.splits > 1 ? (size_t)B * max_q * H * q.splits : 0, rows_k = k.splits > 1 ? (size_t)B * max_k * Hk * k.splits * 2 : 0;
+  return cross_up((size_t)H * B * max_q * sizeof(float)) + cross_up(std::max(rows_q, rows_k) * Dh * sizeof(float));
+}
+
+extern "C" int spa_cross_attention_bwd(const void* q, const void* k, const void* v, int64_t q_row_stride, int64_t k_row_stride,
+                                       int64_t v_row_stride, const void* out, const void* dout, const float* lse, const int32_t* cu_seqlens_q,
+                                       const int32_t* cu_seqlens_k, const int32_t* key_lens, int B, int max_q, int max_k, int H, int Hk, int Dh,
+                                       int dtype, float softmax_scale, void* dq, void* dk, void* dv, int64_t dq_row_stride,
+                                       int64_t dk_row_stride, int64_t dv_row_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "spa_cross_attention_bwd";
+  const CrossCall c = {q, k, v, q_row_stride, k_row_stride, v_row_stride, cu_seqlens_q, cu_seqlens_k, key_lens, B, max_q, max_k, H, Hk, Dh, dtype,
+                       softmax_scale};
+  if (int rc = cross_checks(fn, c)) return rc;
+  SPA_REQUIRE(out && dout && lse && dq && dk && dv, SPA_ERR_INVALID_ARG, "%s: null pointer", fn);
+  const int64_t strides[3] = {dq_row_stride, dk_row_stride, dv_row_stride};
+  for (int i = 0; i < 3; ++i) {
+    SPA_REQUIRE(strides[i] >= (int64_t)(i == 0 ? H : Hk) * Dh && strides[i] < (1LL << 31), SPA_ERR_INVALID_ARG, "%s: row stride %ld out of range", fn,
+                (long)strides[i]);
+    SPA_REQUIRE(strides[i] * elem_size(dtype) % 16 == 0, SPA_ERR_INVALID_ARG, "%s: row stride is not a multiple of 16 bytes", fn);
+  }
+  SPA_REQUIRE(aligned16(out) && aligned16(dout) && aligned16(dq) && aligned16(dk) && aligned16(dv), SPA_ERR_INVALID_ARG,
+              "%s: tensors not 16-byte aligned", fn);
+  for (const CrossPlan& p : {dq_plan(B, max_q, max_k, H, Hk), dkdv_plan(B, max_q, max_k, H, Hk)})
+    SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*Hk*blocks must be < 2^31", fn);
+  const size_t need = spa_cross_attention_bwd_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype);
+  SPA_REQUIRE(workspace != nullptr && workspace_bytes >= need, SPA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
+              workspace_bytes);
+  SPA_REQUIRE((reinterpret_cast<uintptr_t>(workspace) & 255u) == 0, SPA_ERR_INVALID_ARG, "%s: workspace not 256-byte aligned", fn);
+  const CrossGrads g = {out, dout, lse, dq, dk, dv, dq_row_stride, dk_row_stride, dv_row_stride};
+  return dtype == SPA_F32 ? run_bwd<float>(fn, c, g, workspace, as_stream(stream)) : run_bwd<__bf16>(fn, c, g, workspace, as_stream(stream));
+}

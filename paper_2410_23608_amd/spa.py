@@ -134,6 +134,12 @@ _SIGNATURES = {
     "spa_qk_norm_rotary_bwd": (c_int, [_P, _P, c_int64, c_int64, _P, _P, c_int64, c_int64, _P, _P, _P, _P, c_int, c_float, _P, c_int, c_int,
                                        c_int, c_int, c_int, c_int, c_int, c_int, c_int, c_int, c_int, _P, _P, c_int64, c_int64, _P, _P, _P,
                                        _P, _P, c_size_t, _P]),
+    "spa_cross_attention_workspace_bytes": (c_size_t, [c_int, c_int, c_int, c_int, c_int, c_int, c_int]),
+    "spa_cross_attention": (c_int, [_P, _P, _P, c_int64, c_int64, c_int64, _P, _P, _P, c_int, c_int, c_int, c_int, c_int, c_int, c_int, c_float,
+                                    _P, _P, _P, c_size_t, _P]),
+    "spa_cross_attention_bwd_workspace_bytes": (c_size_t, [c_int, c_int, c_int, c_int, c_int, c_int, c_int]),
+    "spa_cross_attention_bwd": (c_int, [_P, _P, _P, c_int64, c_int64, c_int64, _P, _P, _P, _P, _P, _P, c_int, c_int, c_int, c_int, c_int, c_int,
+                                        c_int, c_float, _P, _P, _P, c_int64, c_int64, c_int64, _P, c_size_t, _P]),
     "spa_padded_attention": (c_int, [_P, _P, _P, c_int64, _P, c_int, c_int, c_int, c_int, c_int, c_float, _P, _P]),
 }
 for _name, (_res, _args) in _SIGNATURES.items():
@@ -1260,6 +1266,59 @@ def spa_qk_norm_rotary_bwd(dq_out, dk_out, q, k, gather_idx, total, gamma_q, gam
                       _ptr(gather_idx), _ptr(total), _ptr(gamma_q), _ptr(gamma_k), int(kind), _num(eps), _ptr(table), int(pairs[0]),
                       int(pairs[1]), *grid, int(layout), M, H, Hk, Dh, code, _ptr(dq), _ptr(dk), _row_stride(dq), _stride_of(dk),
                       _ptr(dgamma_q), _ptr(dbeta_q), _ptr(dgamma_k), _ptr(dbeta_k), _ptr(workspace), ws_bytes, _stream(),), _keep, prepare)
+
+
+def _cross_checks(fn, q, k, v, cu_seqlens_q, cu_seqlens_k, key_lens, B, max_q, H, Hk, Dh, out, lse, **more):
+    """more: name = (tensor, heads)"""
+    rows = dict(q=(q, H), k=(k, Hk), v=(v, Hk), out=(out, H), **more)
+    code = _features(fn, **{name: t for name, (t, _) in rows.items()})
+    _typed(fn, torch.int32, cu_seqlens_q=cu_seqlens_q, cu_seqlens_k=cu_seqlens_k, key_lens=key_lens)
+    _typed(fn, torch.float32, lse=lse)
+    for name, (t, heads) in rows.items():
+        _rows(fn, heads * Dh, **{name: (t, 1)})
+    _holds(fn, cu_seqlens_q=(cu_seqlens_q, B + 1), cu_seqlens_k=(cu_seqlens_k, B + 1), key_lens=(key_lens, B), lse=(lse, H * B * max_q))
+    _contig(out, lse, cu_seqlens_q, cu_seqlens_k, key_lens)
+    return code
+
+
+def spa_cross_attention_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype) -> int:
+    return int(lib.spa_cross_attention_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype))
+
+
+def spa_cross_attention(q, k, v, cu_seqlens_q, cu_seqlens_k, key_lens, B, max_q, max_k, H, Hk, Dh, out, lse=None, workspace=None,
+                        softmax_scale=0.0, prepare=False):
+    """Rows of q in segment b of cu_seqlens_q attend to the rows of k, v in segment b of cu_seqlens_k, the first key_lens[b] of them where
+    that is given; query head h reads key head h // (H // Hk).  Rows may be column-slice views; out [rows, H*Dh] contiguous;
+    workspace of spa_cross_attention_workspace_bytes (None where that is 0)."""
+    fn = "spa_cross_attention"
+    code = _cross_checks(fn, q, k, v, cu_seqlens_q, cu_seqlens_k, key_lens, B, max_q, H, Hk, Dh, out, lse)
+    _contig(workspace)
+    _keep = (q, k, v, cu_seqlens_q, cu_seqlens_k, key_lens, out, lse, workspace,)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return _dispatch(lib.spa_cross_attention,
+                     (_ptr(q), _ptr(k), _ptr(v), _row_stride(q), _row_stride(k), _row_stride(v), _ptr(cu_seqlens_q), _ptr(cu_seqlens_k),
+                      _ptr(key_lens), B, max_q, max_k, H, Hk, Dh, code, _num(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes,
+                      _stream(),), _keep, prepare)
+
+
+def spa_cross_attention_bwd_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype) -> int:
+    return int(lib.spa_cross_attention_bwd_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype))
+
+
+def spa_cross_attention_bwd(q, k, v, out, dout, lse, cu_seqlens_q, cu_seqlens_k, key_lens, B, max_q, max_k, H, Hk, Dh, dq, dk, dv, workspace,
+                            softmax_scale=0.0, prepare=False):
+    """The backward of spa_cross_attention; rows of a key segment behind key_lens[b] get dk = dv = 0."""
+    fn = "spa_cross_attention_bwd"
+    code = _cross_checks(fn, q, k, v, cu_seqlens_q, cu_seqlens_k, key_lens, B, max_q, H, Hk, Dh, out, lse, dout=(dout, H), dq=(dq, H), dk=(dk, Hk),
+                         dv=(dv, Hk))
+    _contig(dout, workspace)
+    _keep = (q, k, v, out, dout, lse, cu_seqlens_q, cu_seqlens_k, key_lens, dq, dk, dv, workspace,)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return _dispatch(lib.spa_cross_attention_bwd,
+                     (_ptr(q), _ptr(k), _ptr(v), _row_stride(q), _row_stride(k), _row_stride(v), _ptr(out), _ptr(dout), _ptr(lse),
+                      _ptr(cu_seqlens_q), _ptr(cu_seqlens_k), _ptr(key_lens), B, max_q, max_k, H, Hk, Dh, code, _num(softmax_scale), _ptr(dq),
+                      _ptr(dk), _ptr(dv), _row_stride(dq), _row_stride(dk), _row_stride(dv), _ptr(workspace), ws_bytes, _stream(),), _keep,
+                     prepare)
 
 
 def spa_padded_attention(q, k, v, seqlens, B, n_pad, H, Dh, out, softmax_scale=0.0, prepare=False):
