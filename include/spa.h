@@ -654,6 +654,33 @@ int spa_linear_packed_bwd_weight(const void* dout, const int32_t* dout_idx, int6
                                  void* stream);
 
 /*
+ * The gated feed-forward block on packed rows: both projections, the activation and their product in one launch.  For j < min(*total, M_cap),
+ * row(j) = gather_idx[j] or j:
+ *   (g, u)_j = x[row(j),:] W^T + bias,   h[j,:] = act(g_j) * u_j        g: the first F of the 2F columns, u: the others
+ * act: SPA_ACT_SILU g / (1 + exp(-g)), SPA_ACT_GELU g Phi(g) with the normal distribution's Phi.  The way back onto the residual stream is spa_linear_packed_unpack
+ * (spa_linear_packed, spa_linear_packed_scatter) with x = h, W = W_down.
+ * in:  x [*, K] dtype, contiguous rows; gather_idx [M_cap] int32 or NULL; total [1] int32 or NULL; W [2F, K], bias [2F] or NULL; bf16: K and F multiples of 8.
+ * out: h [M_cap, F] dtype; pre [M_cap, 2F] dtype or NULL: (g, u), kept for the backward.  h is formed from the unrounded (g, u).  Rows from min(*total, M_cap) on
+ *      are not written.
+ */
+#define SPA_ACT_SILU 0
+#define SPA_ACT_GELU 1
+int spa_gated_linear_packed(const void* x, const int32_t* gather_idx, const int32_t* total, const void* W, const void* bias, int M_cap, int K, int F, int act,
+                            int dtype, void* h, void* pre, void* stream);
+
+/*
+ * The step of the block's backward between its two projections, in one launch: with dh_j = dy[row(j),:] W_down (W_down [N_out, F] as in the projection of h),
+ *   d_pre[j,:] = (dh_j * u_j * act'(g_j), dh_j * act(g_j))            (g, u)_j = pre[j,:]
+ * From d_pre the gradients of x, W and bias are spa_linear_packed_bwd_input and spa_linear_packed_bwd_weight with dout = d_pre; those of W_down and its
+ * bias spa_linear_packed_bwd_weight with x = h.
+ * in:  dy [*, N_out] dtype, dy_row_stride elements a row; dy_idx [M_cap] int32 (row(j) = dy_idx[j]) or NULL; total as there; pre as written by the forward;
+ *      bf16: N_out, F and dy_row_stride multiples of 8.
+ * out: d_pre [M_cap, 2F] dtype (not pre itself).  Rows from min(*total, M_cap) on are not written.
+ */
+int spa_gated_linear_packed_bwd(const void* dy, const int32_t* dy_idx, int64_t dy_row_stride, const int32_t* total, const void* W_down, const void* pre,
+                                int M_cap, int N_out, int F, int act, int dtype, void* d_pre, void* stream);
+
+/*
  * Transpose of spa_unpack: dout[j,:] = dy[gather_idx[j],:] for j < total.
  * in:  dy [B,N,C] dtype; gather_idx [B*N] int32; total [1] int32 (device).
  * out: dout [B*N, C] dtype (rows >= T untouched).

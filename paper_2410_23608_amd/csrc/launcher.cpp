@@ -77,6 +77,7 @@ const Entry kEntries[] = {
     ENTRY(spa_norm_packed), ENTRY(spa_norm_packed_bwd), ENTRY(spa_norm_residual_unpack), ENTRY(spa_norm_residual_unpack_bwd),
     ENTRY(spa_gate_bwd_scores), ENTRY(spa_packed_attention_bias), ENTRY(spa_packed_attention_bias_bwd),
     ENTRY(spa_qk_norm_rotary), ENTRY(spa_qk_norm_rotary_bwd), ENTRY(spa_cross_attention), ENTRY(spa_cross_attention_bwd),
+    ENTRY(spa_gated_linear_packed), ENTRY(spa_gated_linear_packed_bwd),
 };
 
 PyObject* g_on_error = nullptr;      // called with the return code of a failing C call; raises

@@ -140,6 +140,8 @@ _SIGNATURES = {
     "spa_cross_attention_bwd_workspace_bytes": (c_size_t, [c_int, c_int, c_int, c_int, c_int, c_int, c_int]),
     "spa_cross_attention_bwd": (c_int, [_P, _P, _P, c_int64, c_int64, c_int64, _P, _P, _P, _P, _P, _P, c_int, c_int, c_int, c_int, c_int, c_int,
                                         c_int, c_float, _P, _P, _P, c_int64, c_int64, c_int64, _P, c_size_t, _P]),
+    "spa_gated_linear_packed": (c_int, [_P, _P, _P, _P, _P, c_int, c_int, c_int, c_int, c_int, _P, _P, _P]),
+    "spa_gated_linear_packed_bwd": (c_int, [_P, _P, c_int64, _P, _P, _P, c_int, c_int, c_int, c_int, c_int, _P, _P]),
     "spa_padded_attention": (c_int, [_P, _P, _P, c_int64, _P, c_int, c_int, c_int, c_int, c_int, c_float, _P, _P]),
 }
 for _name, (_res, _args) in _SIGNATURES.items():
@@ -1319,6 +1321,45 @@ def spa_cross_attention_bwd(q, k, v, out, dout, lse, cu_seqlens_q, cu_seqlens_k,
                       _ptr(cu_seqlens_q), _ptr(cu_seqlens_k), _ptr(key_lens), B, max_q, max_k, H, Hk, Dh, code, _num(softmax_scale), _ptr(dq),
                       _ptr(dk), _ptr(dv), _row_stride(dq), _row_stride(dk), _row_stride(dv), _ptr(workspace), ws_bytes, _stream(),), _keep,
                      prepare)
+
+
+SPA_ACT_SILU, SPA_ACT_GELU = 0, 1
+
+
+def spa_gated_linear_packed(x, gather_idx, total, W, bias, act, h, pre=None, prepare=False):
+    """h[j] = act(g) * u, (g, u) = x[gather_idx[j]] W^T + bias for j < *total.  x [*, K] (any leading shape), W [2F, K], bias [2F], h [rows, F]; pre [rows, 2F]:
+    (g, u), kept for the backward; gather_idx, total, bias, pre may be None."""
+    fn = "spa_gated_linear_packed"
+    K, M, F = x.shape[-1], h.shape[0], W.shape[0] // 2
+    code = _features(fn, x=x, W=W, bias=bias, h=h, pre=pre)
+    _typed(fn, torch.int32, gather_idx=gather_idx, total=total)
+    if W.dim() != 2 or W.shape[0] % 2 != 0 or W.shape[1] != K:
+        raise ValueError(f"{fn}: W must be [2F, K = {K}], got {tuple(W.shape)}")
+    _rows(fn, F, h=(h, 1))
+    _rows(fn, 2 * F, pre=(pre, M))
+    _holds(fn, x=(x, M * K if gather_idx is None else K), gather_idx=(gather_idx, M), total=(total, 1), bias=(bias, 2 * F))
+    _keep = (x, gather_idx, total, W, bias, h, pre,)
+    _contig(*_keep)
+    return _dispatch(lib.spa_gated_linear_packed,
+                     (_ptr(x), _ptr(gather_idx), _ptr(total), _ptr(W), _ptr(bias), M, K, F, int(act), code, _ptr(h), _ptr(pre), _stream(),), _keep,
+                     prepare)
+
+
+def spa_gated_linear_packed_bwd(dy, dy_idx, total, W_down, pre, act, d_pre, prepare=False):
+    """d_pre[j] = (dh u act'(g), dh act(g)), dh = dy[dy_idx[j]] W_down, (g, u) = pre[j] for j < *total.  dy [*, N_out], may be a column-slice view;
+    W_down [N_out, F]; pre, d_pre [rows, 2F]; dy_idx, total may be None."""
+    fn = "spa_gated_linear_packed_bwd"
+    (N_out, F), M = W_down.shape, d_pre.shape[0]
+    code = _features(fn, dy=dy, W_down=W_down, pre=pre, d_pre=d_pre)
+    _typed(fn, torch.int32, dy_idx=dy_idx, total=total)
+    _rows(fn, N_out, dy=(dy, 1 if dy_idx is not None else M))
+    _rows(fn, 2 * F, pre=(pre, M), d_pre=(d_pre, 1))
+    _holds(fn, dy_idx=(dy_idx, M), total=(total, 1))
+    _keep = (dy, dy_idx, total, W_down, pre, d_pre,)
+    _contig(*_keep[1:])
+    return _dispatch(lib.spa_gated_linear_packed_bwd,
+                     (_ptr(dy), _ptr(dy_idx), _row_stride(dy), _ptr(total), _ptr(W_down), _ptr(pre), M, N_out, F, int(act), code, _ptr(d_pre),
+                      _stream(),), _keep, prepare)
 
 
 def spa_padded_attention(q, k, v, seqlens, B, n_pad, H, Dh, out, softmax_scale=0.0, prepare=False):
