@@ -175,42 +175,56 @@ __global__ void __launch_bounds__(kCrossThreads) cross_fwd_kernel(const CrossFwd
   }
 }
 
-// Joins the splits of a row in their order: DH / 4 lanes a row.
-template <typename T, int DH, int STEP>
+// Joins the splits of a row: DH / 4 lanes take a row's columns, SL of such groups every SL-th split each, and the first adds the groups'
+// sums in their order.  SL 1 for many rows.
+template <typename T, int DH, int STEP, int SL>
 __global__ void __launch_bounds__(kCrossThreads) cross_join_kernel(const CrossFwd<T> a) {
-  constexpr int LANES = DH / 4, ROWS = kCrossThreads / LANES, U = 8;
-  const int G = (int)a.s.G.d, c = threadIdx.x % LANES * 4;
+  constexpr int LANES = DH / 4, ROWS = kCrossThreads / LANES / SL, U = SL > 1 ? 4 : 8;
+  __shared__ floatx4 other_o[SL > 1 ? SL - 1 : 1][ROWS][LANES];
+  __shared__ floatx2 other_ms[SL > 1 ? SL - 1 : 1][ROWS];
+  const int G = (int)a.s.G.d, lane = threadIdx.x % LANES, c = lane * 4, in = threadIdx.x / LANES % ROWS, sl = threadIdx.x / LANES / ROWS;
   const long per = (a.part_rows + ROWS - 1) / ROWS, unit = blockIdx.x / per;
-  const int r = (int)(blockIdx.x % per) * ROWS + threadIdx.x / LANES, b = (int)(unit / a.s.Hk), hk = (int)(unit % a.s.Hk);
+  const int r = (int)(blockIdx.x % per) * ROWS + in, b = (int)(unit / a.s.Hk), hk = (int)(unit % a.s.Hk);
   const int q0 = a.s.cu_q[b];
   int nq, nk, held;
   cross_lengths(a.s, b, q0, a.s.cu_k[b], nq, nk, held);
-  if (r >= nq) return;
-  const int live = share_of<STEP>(nk, a.s.splits, 0).live;
+  const bool ok = r < nq;
+  const int live = ok ? share_of<STEP>(nk, a.s.splits, 0).live : 0;
   const long at = unit * a.s.splits * a.part_rows + r;
   float m = -INFINITY, sum = 0.f;
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < live; s0 += U) {
+  auto add = [&](float m1, float sum1, const floatx4& o1) {
+    const float both = __builtin_elementwise_maximum(m, m1);
+    const float f0 = m == both ? 1.f : __builtin_amdgcn_exp2f((m - both) * a.s.c);
+    const float f1 = m1 == both ? 1.f : __builtin_amdgcn_exp2f((m1 - both) * a.s.c);
+    m = both;
+    sum = sum * f0 + sum1 * f1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = o[e] * f0 + o1[e] * f1;
+  };
+  for (int s0 = sl; s0 < live; s0 += U * SL) {
     floatx2 ms[U];
     floatx4 v[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const long row = at + (long)min(s0 + i, live - 1) * a.part_rows;
+      const long row = at + (long)min(s0 + i * SL, live - 1) * a.part_rows;
       ms[i] = *reinterpret_cast<const floatx2*>(a.part_ms + row * 2);
       v[i] = *reinterpret_cast<const floatx4*>(a.part + row * DH + c);
     }
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (s0 + i >= live) break;
-      const float both = __builtin_elementwise_maximum(m, ms[i][0]);
-      const float f0 = m == both ? 1.f : __builtin_amdgcn_exp2f((m - both) * a.s.c);
-      const float f1 = ms[i][0] == both ? 1.f : __builtin_amdgcn_exp2f((ms[i][0] - both) * a.s.c);
-      m = both;
-      sum = sum * f0 + ms[i][1] * f1;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = o[e] * f0 + v[i][e] * f1;
-    }
+    for (int i = 0; i < U; ++i)
+      if (s0 + i * SL < live) add(ms[i][0], ms[i][1], v[i]);
   }
+  if constexpr (SL > 1) {
+    if (sl > 0) {
+      other_o[sl - 1][in][lane] = o;
+      if (lane == 0) other_ms[sl - 1][in] = floatx2{m, sum};
+    }
+    __syncthreads();
+    if (sl > 0) return;
+    for (int i = 0; i < SL - 1; ++i) add(other_ms[i][in][0], other_ms[i][in][1], other_o[i][in][lane]);
+  }
+  if (!ok) return;
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
   const long C = (long)a.s.H * DH;
   const uint32_t i = quotient((uint32_t)r, a.s.G);
@@ -279,9 +293,13 @@ static int launch_fwd(const char* fn, const CrossFwd<T>& a, hipStream_t st) {
   SPA_REQUIRE(attr == hipSuccess, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, lds);
   hipLaunchKernelGGL(kernel, dim3((unsigned)cross_grid(a.s)), dim3(kCrossThreads), lds, st, a);
   if (a.part != nullptr) {
-    constexpr int rows = kCrossThreads / (DH / 4);
-    const long blocks = (long)a.s.B * a.s.Hk * ((a.part_rows + rows - 1) / rows);
-    hipLaunchKernelGGL((cross_join_kernel<T, DH, CrossSteps<KW>::STEP>), dim3((unsigned)blocks), dim3(kCrossThreads), 0, st, a);
+    constexpr int many = kCrossThreads / (DH / 4), few = 1;
+    const long units = (long)a.s.B * a.s.Hk;
+    if (units * a.part_rows <= 4096)
+      hipLaunchKernelGGL((cross_join_kernel<T, DH, CrossSteps<KW>::STEP, many>), dim3((unsigned)(units * a.part_rows)), dim3(kCrossThreads), 0, st, a);
+    else
+      hipLaunchKernelGGL((cross_join_kernel<T, DH, CrossSteps<KW>::STEP, few>), dim3((unsigned)(units * ((a.part_rows + many - 1) / many))),
+                         dim3(kCrossThreads), 0, st, a);
   }
   return check_launch(fn);
 }

@@ -338,7 +338,8 @@ template <bool BACK>
 static int launch_gated(const char* fn, GatedArgs args, int act, hipStream_t st) {
   const int ncols = BACK ? args.F : 2 * args.F;
   const bool counted = args.total != nullptr;
-  const bool big = large_tiles(args.m_cap, counted, ncols, args.kc), ring = !big && ring_tiles(args.m_cap, counted, ncols);
+  const int cfg = options().gemm_tm;
+  const bool big = cfg != 0 ? cfg >= 6 : large_tiles(args.m_cap, counted, ncols, args.kc), ring = !big && ring_tiles(args.m_cap, counted, ncols);
   args.rule = large_rule(ncols, args.kc, false);
   const size_t smem = big ? kGatedBigLds : ring ? kGatedRingLds : kGatedSmallLds;
   const long tiles = gemm_tiles<long>(args.m_cap, ncols, big ? 192 : 128);          // (no less than with 256)
