@@ -12,6 +12,7 @@
 #include <cmath>
 #include <type_traits>
 
+#include "f32_tiles.h"
 #include "gemm_async.h"
 #include "gemm_shape.h"
 #include "spa_common.h"
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1))) g
   }
 }
 
-// ---- fp32 (tiny workload): one thread an element of h
+// ---- fp32 (tiny workload): f32_tiles.h, of W the rows of Wg and of Wu beside each other
 struct GatedF32 {
   const float* a;
   const int32_t *a_idx, *total;
@@ -295,41 +296,48 @@ struct GatedF32 {
   const float *w, *bias;
   float *h, *pre;
 };
-template <int ACT>
-__global__ void __launch_bounds__(256) gated_f32_kernel(const GatedF32 p) {
-  const int M = p.total != nullptr ? min(p.total[0], p.m_cap) : p.m_cap;
-  for (long i = (long)blockIdx.x * blockDim.x + threadIdx.x; i < (long)M * p.F; i += (long)gridDim.x * blockDim.x) {
-    const int m = (int)(i / p.F), n = (int)(i - (long)m * p.F);
-    const float* x = p.a + (p.a_idx != nullptr ? (long)p.a_idx[m] : (long)m) * p.lda;
-    const float *wg = p.w + (long)n * p.kc, *wu = p.w + (long)(p.F + n) * p.kc;
-    float g = 0.f, u = 0.f;
-    for (int k = 0; k < p.kc; ++k) {
-      g = fmaf(x[k], wg[k], g);
-      u = fmaf(x[k], wu[k], u);
+template <int ACT, bool BACK, int EDGE>
+__global__ void __launch_bounds__(kF32Threads) gated_f32_kernel(const GatedF32 p) {
+  using PA = F32Place<EDGE, true>;
+  using PB = F32Place<EDGE, !BACK>;
+  constexpr int TM = EDGE / 16, NB = BACK ? 1 : 2;
+  __shared__ F32Lds<EDGE, NB> l;
+  const int M = p.total != nullptr ? min(p.total[0], p.m_cap) : p.m_cap, n_tiles = (p.F + EDGE - 1) / EDGE;
+  const long tiles = (long)((M + EDGE - 1) / EDGE) * n_tiles;
+  for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int m0 = (int)(tile / n_tiles) * EDGE, n0 = (int)(tile % n_tiles) * EDGE;
+    const float *ap[PA::kCount], *wp[PB::kCount];
+#pragma unroll
+    for (int i = 0; i < PA::kCount; ++i) {
+      const int m = min(m0 + PA::line(i), M - 1);
+      ap[i] = p.a + (p.a_idx != nullptr ? (long)p.a_idx[m] : (long)m) * p.lda;
     }
-    if (p.bias != nullptr) {
-      g += p.bias[n];
-      u += p.bias[p.F + n];
-    }
-    p.h[i] = act_of<ACT, true>(g).value * u;
-    if (p.pre != nullptr) {
-      p.pre[(long)m * 2 * p.F + n] = g;
-      p.pre[(long)m * 2 * p.F + p.F + n] = u;
-    }
-  }
-}
-template <int ACT>
-__global__ void __launch_bounds__(256) gated_bwd_f32_kernel(const GatedF32 p) {
-  const int M = p.total != nullptr ? min(p.total[0], p.m_cap) : p.m_cap;
-  for (long i = (long)blockIdx.x * blockDim.x + threadIdx.x; i < (long)M * p.F; i += (long)gridDim.x * blockDim.x) {
-    const int m = (int)(i / p.F), n = (int)(i - (long)m * p.F);
-    const float* dy = p.a + (p.a_idx != nullptr ? (long)p.a_idx[m] : (long)m) * p.lda;
-    float dh = 0.f;
-    for (int k = 0; k < p.kc; ++k) dh = fmaf(dy[k], p.w[(long)k * p.F + n], dh);
-    const long at = (long)m * 2 * p.F + n;
-    const Act a = act_of<ACT, true>(p.pre[at]);
-    p.h[at] = dh * p.pre[at + p.F] * a.slope;
-    p.h[at + p.F] = dh * a.value;
+#pragma unroll
+    for (int i = 0; i < PB::kCount; ++i) wp[i] = p.w + (long)min(n0 + PB::line(i), p.F - 1) * (BACK ? 1 : p.kc);
+    float acc[NB][TM][TM] = {};
+    f32_tile_sums<EDGE, NB, true, !BACK>(l, p.kc, [&](int i, int k) { return ap[i][k]; },
+                                         [&](int q, int i, int k) { return BACK ? wp[i][(long)k * p.F] : wp[i][(long)q * p.F * p.kc + k]; }, acc, [](const auto&, int) {});
+    __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
+#pragma unroll
+    for (int r = 0; r < TM; ++r)
+#pragma unroll
+      for (int c = 0; c < TM; ++c) {
+        const int m = m0 + (threadIdx.x >> 4) * TM + r, n = n0 + (threadIdx.x & 15) * TM + c;
+        if (m >= M || n >= p.F) continue;
+        const long at = (long)m * 2 * p.F + n;
+        if constexpr (BACK) {
+          const Act a = act_of<ACT, true>(p.pre[at]);
+          p.h[at] = acc[0][r][c] * p.pre[at + p.F] * a.slope;
+          p.h[at + p.F] = acc[0][r][c] * a.value;
+        } else {
+          const float g = acc[0][r][c] + (p.bias != nullptr ? p.bias[n] : 0.f), u = acc[NB - 1][r][c] + (p.bias != nullptr ? p.bias[p.F + n] : 0.f);
+          p.h[(long)m * p.F + n] = act_of<ACT, true>(g).value * u;
+          if (p.pre != nullptr) {
+            p.pre[at] = g;
+            p.pre[at + p.F] = u;
+          }
+        }
+      }
   }
 }
 
@@ -349,6 +357,15 @@ static int launch_gated(const char* fn, GatedArgs args, int act, hipStream_t st)
   const hipError_t attr = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   SPA_REQUIRE(attr == hipSuccess, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, smem);
   hipLaunchKernelGGL(kernel, dim3((unsigned)(big ? std::min(tiles8, 256L) : tiles8)), dim3(big || ring ? 512 : 256), smem, st, args, act);
+  return check_launch(fn);
+}
+
+template <bool BACK>
+static int launch_gated_f32(const char* fn, const GatedF32& a, int act, hipStream_t st) {
+  const bool wide = f32_wide(a.m_cap, a.F);
+  const auto kernel = act == SPA_ACT_SILU ? (wide ? gated_f32_kernel<SPA_ACT_SILU, BACK, 64> : gated_f32_kernel<SPA_ACT_SILU, BACK, 32>)
+                                          : (wide ? gated_f32_kernel<SPA_ACT_GELU, BACK, 64> : gated_f32_kernel<SPA_ACT_GELU, BACK, 32>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(f32_tiles(a.m_cap, a.F, wide ? 64 : 32), 8192L)), dim3(kF32Threads), 0, st, a);
   return check_launch(fn);
 }
 
@@ -373,10 +390,7 @@ extern "C" int spa_gated_linear_packed(const void* x, const int32_t* gather_idx,
   hipStream_t st = as_stream(stream);
   if (dtype == SPA_F32) {
     const GatedF32 a = {(const float*)x, gather_idx, total, (long)K, M_cap, K, F, (const float*)W, (const float*)bias, (float*)h, (float*)pre};
-    const unsigned wgs = (unsigned)std::min<long>(((long)M_cap * F + 255) / 256, 8192L);
-    if (act == SPA_ACT_SILU) hipLaunchKernelGGL(gated_f32_kernel<SPA_ACT_SILU>, dim3(wgs), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(gated_f32_kernel<SPA_ACT_GELU>, dim3(wgs), dim3(256), 0, st, a);
-    return check_launch(fn);
+    return launch_gated_f32<false>(fn, a, act, st);
   }
   SPA_REQUIRE(K % 8 == 0 && F % 8 == 0, SPA_ERR_UNSUPPORTED, "%s: K and F must be multiples of 8 for bf16", fn);
   SPA_REQUIRE(aligned16(x) && aligned16(W) && aligned16(h) && aligned16(pre), SPA_ERR_INVALID_ARG, "%s: x / W / h / pre not 16-byte aligned", fn);
@@ -393,10 +407,7 @@ extern "C" int spa_gated_linear_packed_bwd(const void* dy, const int32_t* dy_idx
   hipStream_t st = as_stream(stream);
   if (dtype == SPA_F32) {
     const GatedF32 a = {(const float*)dy, dy_idx, total, (long)dy_row_stride, M_cap, N_out, F, (const float*)W_down, nullptr, (float*)d_pre, (float*)pre};
-    const unsigned wgs = (unsigned)std::min<long>(((long)M_cap * F + 255) / 256, 8192L);
-    if (act == SPA_ACT_SILU) hipLaunchKernelGGL(gated_bwd_f32_kernel<SPA_ACT_SILU>, dim3(wgs), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(gated_bwd_f32_kernel<SPA_ACT_GELU>, dim3(wgs), dim3(256), 0, st, a);
-    return check_launch(fn);
+    return launch_gated_f32<true>(fn, a, act, st);
   }
   SPA_REQUIRE(N_out % 8 == 0 && F % 8 == 0 && dy_row_stride % 8 == 0, SPA_ERR_UNSUPPORTED, "%s: N_out, F and dy_row_stride must be multiples of 8 for bf16",
               fn);

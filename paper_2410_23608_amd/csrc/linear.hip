@@ -12,19 +12,20 @@
 // (gemm_shape.h; what bounds them: gemm_rows.h).  Measured, called again and again: 12544 rows of 768 -> 2304 47 to 49 us =
 // 905 to 940 TFLOP/s (operands staged through registers: 68 us); 6272 rows of 384 -> 384: 7 us (8.7); 98 rows: 5.8 us (8.1),
 // its steps bound by latency.  The output tile leaves through LDS as whole rows.
-// fp32 path (tiny workload): one thread per output element.
+// fp32 path (tiny workload): f32_tiles.h.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
 
+#include "f32_tiles.h"
 #include "gemm_rows.h"
 #include "group.h"
 #include "spa_common.h"
 
 namespace spa {
 
-template <bool kGather, bool kScale>
-__global__ void __launch_bounds__(256)
+template <bool kGather, bool kScale, int EDGE>
+__global__ void __launch_bounds__(kF32Threads)
 linear_f32_kernel(const float* __restrict__ x, const int32_t* __restrict__ gather_idx,
                   const float* __restrict__ gate_scores, const int32_t* __restrict__ total,
                   const float* __restrict__ W, const float* __restrict__ bias, int m_cap, int K, int n_out,
@@ -35,18 +36,36 @@ linear_f32_kernel(const float* __restrict__ x, const int32_t* __restrict__ gathe
       const long r = i / n_out, at = r * out_stride + (i - r * n_out);
       if (inv_pos[r] < 0) out[at] = residual[at];
     }
-  const int M = total != nullptr ? min(total[0], m_cap) : m_cap;
-  const long work = (long)M * n_out;
-  for (long i = (long)blockIdx.x * blockDim.x + threadIdx.x; i < work; i += (long)gridDim.x * blockDim.x) {
-    const int m = (int)(i / n_out), n = (int)(i - (long)m * n_out);
-    const long src = kGather ? (long)gather_idx[m] : (long)m;
-    const float sc = kScale ? sigmoidf_dev(gate_scores[src]) : 1.f;
-    const float* xr = x + src * K;
-    const float* wr = W + (long)n * K;
-    float a = 0.f;
-    for (int kq = 0; kq < K; ++kq) a = fmaf(sc * xr[kq], wr[kq], a);
-    const long off = (long)(scatter_idx != nullptr ? scatter_idx[m] : m) * out_stride + n;
-    out[off] = a + (bias != nullptr ? bias[n] : 0.f) + (residual != nullptr ? residual[off] : 0.f);
+  using Place = F32Place<EDGE, true>;
+  constexpr int TM = EDGE / 16;
+  __shared__ F32Lds<EDGE, 1> l;
+  const int M = total != nullptr ? min(total[0], m_cap) : m_cap, n_tiles = (n_out + EDGE - 1) / EDGE;
+  const long tiles = (long)((M + EDGE - 1) / EDGE) * n_tiles;
+  for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int m0 = (int)(tile / n_tiles) * EDGE, n0 = (int)(tile % n_tiles) * EDGE;
+    const float *xp[Place::kCount], *wp[Place::kCount];
+    float sc[Place::kCount];
+#pragma unroll
+    for (int i = 0; i < Place::kCount; ++i) {
+      const int m = min(m0 + Place::line(i), M - 1), n = min(n0 + Place::line(i), n_out - 1);
+      const long src = kGather ? (long)gather_idx[m] : (long)m;
+      sc[i] = kScale ? sigmoidf_dev(gate_scores[src]) : 1.f;
+      xp[i] = x + src * K;
+      wp[i] = W + (long)n * K;
+    }
+    float acc[1][TM][TM] = {};
+    f32_tile_sums<EDGE, 1, true, true>(l, K, [&](int i, int k) { return kScale ? sc[i] * xp[i][k] : xp[i][k]; }, [&](int, int i, int k) { return wp[i][k]; },
+                                       acc, [](const auto&, int) {});
+    __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
+#pragma unroll
+    for (int r = 0; r < TM; ++r)
+#pragma unroll
+      for (int c = 0; c < TM; ++c) {
+        const int m = m0 + (threadIdx.x >> 4) * TM + r, n = n0 + (threadIdx.x & 15) * TM + c;
+        if (m >= M || n >= n_out) continue;
+        const long off = (long)(scatter_idx != nullptr ? scatter_idx[m] : m) * out_stride + n;
+        out[off] = acc[0][r][c] + (bias != nullptr ? bias[n] : 0.f) + (residual != nullptr ? residual[off] : 0.f);
+      }
   }
 }
 
@@ -103,10 +122,10 @@ static int linear_common(const char* fn, const void* x, const int32_t* gather_id
   hipStream_t st = as_stream(stream);
   const bool g = gather_idx != nullptr, sc = gate_scores != nullptr;
   if (dtype == SPA_F32) {
-    long wgs = (std::max((long)M_cap, inv_pos != nullptr ? (long)rows : 0L) * N_out + 255) / 256;
-    if (wgs > 8192) wgs = 8192;
+    const bool wide = f32_wide(M_cap, N_out);
+    const long wgs = std::min(std::max(f32_tiles(M_cap, N_out, wide ? 64 : 32), inv_pos != nullptr ? ((long)rows * N_out + 1023) / 1024 : 0L), 8192L);
 #define SPA_LIN_F32(G_, S_)                                                                                   \
-  hipLaunchKernelGGL((linear_f32_kernel<G_, S_>), dim3((unsigned)wgs), dim3(256), 0, st, (const float*)x,    \
+  hipLaunchKernelGGL((wide ? linear_f32_kernel<G_, S_, 64> : linear_f32_kernel<G_, S_, 32>), dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)x, \
                      gather_idx, gate_scores, total, (const float*)W, (const float*)bias, M_cap, K, N_out,   \
                      (float*)out, (long)out_row_stride, scatter_idx, (const float*)residual, inv_pos, (long)rows)
     if (g && sc) SPA_LIN_F32(true, true); else if (g) SPA_LIN_F32(true, false); else SPA_LIN_F32(false, false);

@@ -18,12 +18,13 @@
 // The operands come through the pipelined loop of gemm_async.h (weight_gemm_kernel); rows that have to be
 // multiplied by the gate scale and rounded on the way cannot go straight to LDS and keep the kernel that
 // stages them through registers (linear_bwd_weight_bf16_kernel).
-// fp32 (tiny workload): one thread per output element.
+// fp32 (tiny workload): f32_tiles.h.
 #include <algorithm>
 #include <cmath>
 #include <cstdlib>
 
 #include "attn_tiles.h"
+#include "f32_tiles.h"
 #include "gemm_async.h"
 #include "gemm_rows.h"
 #include "group.h"
@@ -62,7 +63,8 @@ __device__ __forceinline__ bf16x8 frag_down_columns(const __bf16* tile, int k0, 
 }
 
 // ------------------------------------------------------------------------------ input side (fp32)
-__global__ void __launch_bounds__(256)
+template <int EDGE>
+__global__ void __launch_bounds__(kF32Threads)
 linear_bwd_input_f32_kernel(const float* __restrict__ dout, const int32_t* __restrict__ dout_idx, long ldd,
                             const int32_t* __restrict__ total, const float* __restrict__ W, int m_cap, int kc, int ncols,
                             float* __restrict__ dx, long ldx, const int32_t* __restrict__ dx_idx,
@@ -73,13 +75,31 @@ linear_bwd_input_f32_kernel(const float* __restrict__ dout, const int32_t* __res
       const long r = i / ncols;
       if (inv_pos[r] < 0) dx[r * ldx + (i - r * ncols)] = 0.f;
     }
-  const int M = total != nullptr ? min(total[0], m_cap) : m_cap;
-  for (long i = first; i < (long)M * ncols; i += stride) {
-    const int m = (int)(i / ncols), c = (int)(i - (long)m * ncols);
-    const float* g = dout + (dout_idx != nullptr ? (long)dout_idx[m] : (long)m) * ldd;
-    float a = 0.f;
-    for (int n = 0; n < kc; ++n) a = fmaf(g[n], W[(long)n * ncols + c], a);
-    dx[(dx_idx != nullptr ? (long)dx_idx[m] : (long)m) * ldx + c] = a;
+  using PA = F32Place<EDGE, true>;
+  using PB = F32Place<EDGE, false>;
+  constexpr int TM = EDGE / 16;
+  __shared__ F32Lds<EDGE, 1> l;
+  const int M = total != nullptr ? min(total[0], m_cap) : m_cap, n_tiles = (ncols + EDGE - 1) / EDGE;
+  const long tiles = (long)((M + EDGE - 1) / EDGE) * n_tiles;
+  for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int m0 = (int)(tile / n_tiles) * EDGE, c0 = (int)(tile % n_tiles) * EDGE;
+    const float *gp[PA::kCount], *wp = W + min(c0 + PB::line(0), ncols - 1);
+#pragma unroll
+    for (int i = 0; i < PA::kCount; ++i) {
+      const int m = min(m0 + PA::line(i), M - 1);
+      gp[i] = dout + (dout_idx != nullptr ? (long)dout_idx[m] : (long)m) * ldd;
+    }
+    float acc[1][TM][TM] = {};
+    f32_tile_sums<EDGE, 1, true, false>(l, kc, [&](int i, int k) { return gp[i][k]; }, [&](int, int, int k) { return wp[(long)k * ncols]; }, acc,
+                                        [](const auto&, int) {});
+    __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
+#pragma unroll
+    for (int r = 0; r < TM; ++r)
+#pragma unroll
+      for (int c = 0; c < TM; ++c) {
+        const int m = m0 + (threadIdx.x >> 4) * TM + r, n = c0 + (threadIdx.x & 15) * TM + c;
+        if (m < M && n < ncols) dx[(dx_idx != nullptr ? (long)dx_idx[m] : (long)m) * ldx + n] = acc[0][r][c];
+      }
   }
 }
 
@@ -564,28 +584,49 @@ __global__ void __launch_bounds__(256) linear_bwd_weight_reduce_group_kernel(con
   weight_reduce_block(m.a[mb.s], mb.block, mb.blocks);
 }
 
-__global__ void __launch_bounds__(256)
+template <int EDGE>
+__global__ void __launch_bounds__(kF32Threads)
 linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __restrict__ dout_idx, long ldd,
                              const float* __restrict__ x, const int32_t* __restrict__ x_idx,
                              const float* __restrict__ gate_scores, const int32_t* __restrict__ total, int m_cap, int K,
                              int n_out, float* __restrict__ dW, float* __restrict__ dbias) {
-  const int M = total != nullptr ? min(total[0], m_cap) : m_cap;
-  const long nk = (long)n_out * K, work = nk + (dbias != nullptr ? n_out : 0);
-  for (long i = (long)blockIdx.x * blockDim.x + threadIdx.x; i < work; i += (long)gridDim.x * blockDim.x) {
-    const bool is_w = i < nk;
-    const int n = is_w ? (int)(i / K) : (int)(i - nk), k = is_w ? (int)(i - (long)n * K) : 0;
-    float a = 0.f;
-    for (int m = 0; m < M; ++m) {
-      const float g = dout[(dout_idx != nullptr ? (long)dout_idx[m] : (long)m) * ldd + n];
-      if (is_w) {
-        const long xr = x_idx != nullptr ? (long)x_idx[m] : (long)m;
-        const float sc = gate_scores != nullptr ? sigmoidf_dev(gate_scores[xr]) : 1.f;
-        a = fmaf(g, sc * x[xr * K + k], a);
-      } else {
-        a += g;
+  constexpr int TM = EDGE / 16;
+  __shared__ F32Lds<EDGE, 1> l;
+  const int M = total != nullptr ? min(total[0], m_cap) : m_cap, k_tiles = (K + EDGE - 1) / EDGE, n_tiles = (n_out + EDGE - 1) / EDGE;
+  for (long tile = blockIdx.x; tile < (long)n_tiles * k_tiles; tile += gridDim.x) {
+    const int n0 = (int)(tile / k_tiles) * EDGE, k0 = (int)(tile % k_tiles) * EDGE;
+    const int line = F32Place<EDGE, false>::line(0);
+    const float *gp = dout + min(n0 + line, n_out - 1), *xp = x + min(k0 + line, K - 1);
+    const bool sums = dbias != nullptr && k0 == 0 && threadIdx.x < EDGE;      // (the bias' gradient: the same rows of dout, added in order)
+    float acc[1][TM][TM] = {}, bias = 0.f;
+    f32_tile_sums<EDGE, 1, false, false>(
+        l, M, [&](int, int m) { return gp[(dout_idx != nullptr ? (long)dout_idx[m] : (long)m) * ldd]; },
+        [&](int, int, int m) {
+          const long xr = x_idx != nullptr ? (long)x_idx[m] : (long)m;
+          return gate_scores != nullptr ? sigmoidf_dev(gate_scores[xr]) * xp[xr * K] : xp[xr * K];
+        },
+        acc,
+        [&](const float (&a)[kF32Step<EDGE>][kF32Row<EDGE>], int ks) {
+          if (!sums) return;
+          int kk = 0;
+          for (; kk + 8 <= ks; kk += 8) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = a[kk + j][threadIdx.x];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) bias += v[j];
+          }
+          for (; kk < ks; ++kk) bias += a[kk][threadIdx.x];
+        });
+    __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
+    if (sums && n0 + (int)threadIdx.x < n_out) dbias[n0 + threadIdx.x] = bias;
+#pragma unroll
+    for (int r = 0; r < TM; ++r)
+#pragma unroll
+      for (int c = 0; c < TM; ++c) {
+        const int n = n0 + (threadIdx.x >> 4) * TM + r, k = k0 + (threadIdx.x & 15) * TM + c;
+        if (n < n_out && k < K) dW[(long)n * K + k] = acc[0][r][c];
       }
-    }
-    if (is_w) dW[i] = a; else dbias[n] = a;
   }
 }
 
@@ -743,11 +784,9 @@ extern "C" int spa_linear_packed_bwd_input(const void* dout, const int32_t* dout
   hipStream_t st = as_stream(stream);
   SPA_REQUIRE(!(group_open() && dtype == SPA_F32), SPA_ERR_UNSUPPORTED, "%s: fp32 calls cannot be part of a group", fn);
   if (dtype == SPA_F32) {
-    long work = (long)M_cap * K;
-    if (inv_pos != nullptr && rows * K > work) work = rows * K;
-    long wgs = (work + 255) / 256;
-    if (wgs > 8192) wgs = 8192;
-    hipLaunchKernelGGL(linear_bwd_input_f32_kernel, dim3((unsigned)wgs), dim3(256), 0, st, (const float*)dout, dout_idx,
+    const bool wide = f32_wide(M_cap, K);
+    const long wgs = std::min(std::max(f32_tiles(M_cap, K, wide ? 64 : 32), inv_pos != nullptr ? ((long)rows * K + 1023) / 1024 : 0L), 8192L);
+    hipLaunchKernelGGL((wide ? linear_bwd_input_f32_kernel<64> : linear_bwd_input_f32_kernel<32>), dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)dout, dout_idx,
                        (long)dout_row_stride, total, (const float*)W, M_cap, N_out, K, (float*)dx, (long)dx_row_stride,
                        dx_idx, inv_pos, (long)rows);
     return check_launch(fn);
@@ -793,9 +832,9 @@ extern "C" int spa_linear_packed_bwd_weight(const void* dout, const int32_t* dou
   hipStream_t st = as_stream(stream);
   SPA_REQUIRE(!(group_open() && dtype == SPA_F32), SPA_ERR_UNSUPPORTED, "%s: fp32 calls cannot be part of a group", fn);
   if (dtype == SPA_F32) {
-    long wgs = ((long)N_out * K + N_out + 255) / 256;
-    if (wgs > 8192) wgs = 8192;
-    hipLaunchKernelGGL(linear_bwd_weight_f32_kernel, dim3((unsigned)wgs), dim3(256), 0, st, (const float*)dout, dout_idx,
+    const bool wide = f32_wide(N_out, K);
+    const long wgs = std::min(f32_tiles(N_out, K, wide ? 64 : 32), 8192L);
+    hipLaunchKernelGGL((wide ? linear_bwd_weight_f32_kernel<64> : linear_bwd_weight_f32_kernel<32>), dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)dout, dout_idx,
                        (long)dout_row_stride, (const float*)x, x_idx, gate_scores, total, M_cap, K, N_out, dW, dbias);
     return check_launch(fn);
   }
