@@ -39,14 +39,44 @@ __device__ __forceinline__ void cross_lengths(const CrossShape& s, int b, int q0
   held = min(max(s.cu_k[b + 1] - k0, 0), s.most_k);
   nk = s.key_lens != nullptr ? min(max(s.key_lens[b], 0), held) : held;
 }
+// Blocks and splits of a pair (segment, key head) next to each other on one XCD, whose L2 then holds what they share, pairs dealt to the XCDs there
+// and back.  Up to kRankedB segments come by their products, most first; ranking more costs every workgroup more than it gives (us, 8 segments of 1568 to
+// 3136 tokens and 410 to 1024 keys, in index order | ranked: see the table of the kernels).
+constexpr int kRankedB = 16;
 __device__ __forceinline__ CrossUnit cross_unit(const CrossShape& s) {
-  // blocks and splits of a pair next to each other on one XCD, whose L2 then holds what they share
-  const TileId t = xcd_tile(s.blocks * s.splits, s.Hk, s.B);
-  CrossUnit u = {t.rank, t.h, t.qb / s.splits, 0, t.valid, 0, 0, 0, 0, 0};
-  u.split = t.qb - u.block * s.splits;
-  if (!t.valid) return u;
-  const int q0 = s.cu_q[u.b], k0 = s.cu_k[u.b];
-  cross_lengths(s, u.b, q0, k0, u.nq, u.nk, u.held);
+  const int per = s.blocks * s.splits, xcd = blockIdx.x & 7, j = blockIdx.x >> 3, pl = j / per, qb = j - pl * per;
+  const int pair = pl * 8 + (pl & 1 ? 7 - xcd : xcd);
+  CrossUnit u = {};
+  u.valid = pair < s.Hk * s.B;
+  if (!u.valid) return u;
+  u.b = pair / s.Hk;
+  u.hk = pair - u.b * s.Hk;
+  u.block = qb / s.splits;
+  u.split = qb - u.block * s.splits;
+  int q0, k0;
+  if (s.B > 1 && s.B <= kRankedB) {
+    const int lane = threadIdx.x & 63, b = min(lane, s.B - 1);
+    q0 = s.cu_q[b];
+    k0 = s.cu_k[b];
+    cross_lengths(s, b, q0, k0, u.nq, u.nk, u.held);
+    const float cost = (float)u.nq * (float)u.nk;
+    int rank = 0;
+    for (int o = 0; o < s.B; ++o) {
+      const float other = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, cost), o));
+      rank += (other > cost) | ((other == cost) & (o < lane));
+    }
+    const int at = __builtin_ctzll(__ballot(lane < s.B && rank == u.b));
+    u.b = at;
+    q0 = __builtin_amdgcn_readlane(q0, at);
+    k0 = __builtin_amdgcn_readlane(k0, at);
+    u.nq = __builtin_amdgcn_readlane(u.nq, at);
+    u.nk = __builtin_amdgcn_readlane(u.nk, at);
+    u.held = __builtin_amdgcn_readlane(u.held, at);
+  } else {
+    q0 = s.cu_q[u.b];
+    k0 = s.cu_k[u.b];
+    cross_lengths(s, u.b, q0, k0, u.nq, u.nk, u.held);
+  }
   u.q0 = q0;
   u.k0 = k0;
   return u;
@@ -63,16 +93,18 @@ __device__ __forceinline__ Share share_of(int n, int splits, int split) {
   return {split * each, min(each, n - split * each), (n + each - 1) / each};
 }
 
-// Offset of row r (token r / G, head r % G of the group) of a tensor of `stride` elements a token
+// Offset of row r (token r / G, head r % G of the group) of a tensor of `stride` elements a token (below 2^31)
 template <int DH>
 __device__ __forceinline__ long group_row(const Divisor& G, int r, long stride) {
   const uint32_t i = quotient((uint32_t)r, G);
-  return (long)i * stride + (long)(r - (int)(i * G.d)) * DH;
+  return (long)((uint64_t)i * (uint32_t)stride) + (r - (int)(i * G.d)) * DH;
 }
 
 // BT rows of two operands on their way to LDS, in 16-byte pieces.  Nothing here waits for a load or branches on one between load() and store();
 // rows past the end are loaded as the last one, and store<true>() clears operand 1's (the caller gives such rows probability 0, and 0
-// times an infinity of the last row would be NaN).  GROUPED: rows of a unit's tokens and heads (group_row), else of one head.
+// times an infinity of the last row would be NaN).  GROUPED: rows of a unit's tokens and heads (group_row), else of one head.  (Addresses of whole steps from the
+// first step's by a scalar's distance, without the multiplications: registers for them cost dq a wave a SIMD, 91 -> 100 us at 8 segments of 1568 to 3136 tokens
+// and 410 to 1024 keys, 12 and 4 heads of 64; forward 78 -> 77, dk / dv 141 -> 148.)
 template <typename T, int DH, int BT, bool GROUPED>
 struct CrossStage {
   static constexpr int RS = Ops<T, DH>::RS, VE = 16 / sizeof(T), CPR = DH / VE, CPT = BT * CPR / kCrossThreads, RPP = kCrossThreads / CPR;
@@ -85,13 +117,16 @@ struct CrossStage {
   __device__ __forceinline__ CrossStage(const T* a_, long as_, const T* b_, long bs_, const Divisor& G_, int last_)
       : a(a_ + threadIdx.x % CPR * VE), b(b_ + threadIdx.x % CPR * VE), as(as_), bs(bs_), G(G_), tid(threadIdx.x), last(last_), from(0) {}
   __device__ __forceinline__ int row(int t) const { return tid / CPR + t * RPP; }
+  __device__ __forceinline__ long offset(int r, long stride) const {
+    return GROUPED ? group_row<DH>(G, r, stride) : (long)((uint64_t)(uint32_t)r * (uint32_t)stride);
+  }
   __device__ __forceinline__ void load(int t0) {
     from = t0;
 #pragma unroll
     for (int t = 0; t < CPT; ++t) {
       const int r = min(t0 + row(t), last);
-      v[0][t] = *reinterpret_cast<const uintx4*>(a + (GROUPED ? group_row<DH>(G, r, as) : (long)r * as));
-      v[1][t] = *reinterpret_cast<const uintx4*>(b + (GROUPED ? group_row<DH>(G, r, bs) : (long)r * bs));
+      v[0][t] = *reinterpret_cast<const uintx4*>(a + offset(r, as));
+      v[1][t] = *reinterpret_cast<const uintx4*>(b + offset(r, bs));
     }
   }
   template <bool LAST>
@@ -128,7 +163,7 @@ struct CrossCall {
 int cross_checks(const char* fn, const CrossCall& c);
 bool cross_sizes_ok(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtype);
 // Blocks of owned rows and splits of the others for `owned` and `others` rows of the longest segment in `units` units
-CrossPlan cross_plan(long units, long owned, long others);
+CrossPlan cross_plan(long units, long owned, long others, int dtype);
 CrossShape cross_shape(const CrossCall& c, const CrossPlan& p);
 inline long cross_grid(const CrossShape& s) { return ((long)s.Hk * s.B + 7) / 8 * 8 * s.blocks * s.splits; }
 

@@ -244,14 +244,16 @@ bool cross_sizes_ok(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtyp
          (dtype == SPA_F32 || dtype == SPA_BF16);
 }
 
-// Few rows: the waves share them.  Few workgroups and long rows on the other side: these are split, into no less than four steps each, until
-// there are about three workgroups a unit.
-CrossPlan cross_plan(long units, long owned, long others) {
-  CrossPlan p = {owned <= 32 ? 4 : owned <= 64 ? 2 : 1, 1, 1};
-  const int rows = 128 / p.kw;
-  p.blocks = (int)((owned + rows - 1) / rows);
+// Few workgroups: the waves of one share its owned rows, two by two or all four, as long as one round of workgroups holds them all.  Fewer still and many rows on
+// the other side: these are split, into no less than `least` each, until there are about four workgroups a unit.
+CrossPlan cross_plan(long units, long owned, long others, int dtype) {
+  CrossPlan p = {1, 1, 1};
+  const long least = dtype == SPA_F32 ? 256 : 512;
+  auto blocks = [&](int kw) { return (owned + 128 / kw - 1) / (128 / kw); };
+  while (p.kw < 4 && (owned <= 64 / p.kw || (dtype == SPA_F32 && units * blocks(2 * p.kw) <= 512))) p.kw *= 2;
+  p.blocks = (int)blocks(p.kw);
   const long groups = units * p.blocks;
-  if (groups < 512) p.splits = (int)std::max(1L, std::min((768 + groups - 1) / groups, others / 512));
+  if (groups < 512) p.splits = (int)std::max(1L, std::min((1024 + groups - 1) / groups, others / least));
   return p;
 }
 
@@ -283,7 +285,7 @@ int cross_checks(const char* fn, const CrossCall& c) {
   return SPA_OK;
 }
 
-static CrossPlan fwd_plan(int B, int max_q, int max_k, int H, int Hk) { return cross_plan((long)B * Hk, (long)max_q * (H / Hk), max_k); }
+static CrossPlan fwd_plan(int B, int max_q, int max_k, int H, int Hk, int dtype) { return cross_plan((long)B * Hk, (long)max_q * (H / Hk), max_k, dtype); }
 
 template <typename T, int DH, int KW>
 static int launch_fwd(const char* fn, const CrossFwd<T>& a, hipStream_t st) {
@@ -325,7 +327,7 @@ using namespace spa;
 
 extern "C" size_t spa_cross_attention_workspace_bytes(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtype) {
   if (!cross_sizes_ok(B, max_q, max_k, H, Hk, Dh, dtype)) return 0;
-  const CrossPlan p = fwd_plan(B, max_q, max_k, H, Hk);
+  const CrossPlan p = fwd_plan(B, max_q, max_k, H, Hk, dtype);
   if (p.splits == 1) return 0;
   const size_t rows = (size_t)B * max_q * H * p.splits;
   return cross_up(rows * Dh * sizeof(float)) + cross_up(rows * 2 * sizeof(float));
@@ -341,7 +343,7 @@ extern "C" int spa_cross_attention(const void* q, const void* k, const void* v, 
   if (int rc = cross_checks(fn, c)) return rc;
   SPA_REQUIRE(out != nullptr, SPA_ERR_INVALID_ARG, "%s: out is null", fn);
   SPA_REQUIRE(aligned16(out), SPA_ERR_INVALID_ARG, "%s: out not 16-byte aligned", fn);
-  const CrossPlan p = fwd_plan(B, max_q, max_k, H, Hk);
+  const CrossPlan p = fwd_plan(B, max_q, max_k, H, Hk, dtype);
   SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*Hk*blocks must be < 2^31", fn);
   const size_t need = spa_cross_attention_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype);
   SPA_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need), SPA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given",

@@ -180,13 +180,14 @@ __global__ void __launch_bounds__(kCrossThreads, sizeof(T) == 4 ? 1 : 2) cross_d
 #pragma unroll
     for (int i = 0; i < 16; ++i) dka[d][i] = dva[d][i] = 0.f;
   if (nt > 0) {
-    CrossStage<T, DH, W::STEP, true> st(a.q + u.q0 * a.qs + head, a.qs, a.dout + u.q0 * C + head, C, a.s.G, sh.from + n - 1);
+    CrossStage<T, DH, W::STEP, true> st(a.q + u.q0 * a.qs + head, a.qs, a.dout + u.q0 * C + head, C, a.s.G, sh.from + n - 1);      // (rows of the unit)
     float lse_t = 0.f, d_t = 0.f;
+    const long stat0 = (long)u.hk * G * a.s.stat_stride + u.q0;
     auto load = [&](int t0) {
       st.load(sh.from + t0);
       const int r = sh.from + min(t0 + (tid & (W::STEP - 1)), n - 1);
       const uint32_t i = quotient((uint32_t)r, a.s.G);
-      const long stat = (u.hk * G + (r - (int)(i * G))) * a.s.stat_stride + u.q0 + i;
+      const long stat = stat0 + (long)((uint64_t)(uint32_t)(r - (int)(i * G)) * (uint32_t)a.s.stat_stride) + i;
       lse_t = a.lse[stat];
       d_t = a.D[stat];
     };
@@ -340,8 +341,8 @@ __global__ void __launch_bounds__(kCrossThreads) cross_sum_kernel(const CrossBwd
 }
 
 // ------------------------------------------------------------------------------- host
-static CrossPlan dq_plan(int B, int max_q, int max_k, int H, int Hk) { return cross_plan((long)B * Hk, (long)max_q * (H / Hk), max_k); }
-static CrossPlan dkdv_plan(int B, int max_q, int max_k, int H, int Hk) { return cross_plan((long)B * Hk, max_k, (long)max_q * (H / Hk)); }
+static CrossPlan dq_plan(int B, int max_q, int max_k, int H, int Hk, int dtype) { return cross_plan((long)B * Hk, (long)max_q * (H / Hk), max_k, dtype); }
+static CrossPlan dkdv_plan(int B, int max_q, int max_k, int H, int Hk, int dtype) { return cross_plan((long)B * Hk, max_k, (long)max_q * (H / Hk), dtype); }
 
 template <typename T, int DH, int KW, bool KEYS>
 static int launch_bwd(const char* fn, const CrossBwd<T>& a, hipStream_t st) {
@@ -367,7 +368,7 @@ struct CrossGrads {
 
 template <typename T>
 static int run_bwd(const char* fn, const CrossCall& c, const CrossGrads& g, void* ws, hipStream_t st) {
-  const CrossPlan plans[2] = {dq_plan(c.B, c.max_q, c.max_k, c.H, c.Hk), dkdv_plan(c.B, c.max_q, c.max_k, c.H, c.Hk)};
+  const CrossPlan plans[2] = {dq_plan(c.B, c.max_q, c.max_k, c.H, c.Hk, c.dtype), dkdv_plan(c.B, c.max_q, c.max_k, c.H, c.Hk, c.dtype)};
   float* D = (float*)ws;
   float* part = (float*)((char*)ws + cross_up((size_t)c.H * c.B * c.max_q * sizeof(float)));
   for (int keys = 0; keys < 2; ++keys) {
@@ -393,7 +394,7 @@ using namespace spa;
 
 extern "C" size_t spa_cross_attention_bwd_workspace_bytes(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtype) {
   if (!cross_sizes_ok(B, max_q, max_k, H, Hk, Dh, dtype)) return 0;
-  const CrossPlan q = dq_plan(B, max_q, max_k, H, Hk), k = dkdv_plan(B, max_q, max_k, H, Hk);
+  const CrossPlan q = dq_plan(B, max_q, max_k, H, Hk, dtype), k = dkdv_plan(B, max_q, max_k, H, Hk, dtype);
   const size_t rows_q = q.splits > 1 ? (size_t)B * max_q * H * q.splits : 0, rows_k = k.splits > 1 ? (size_t)B * max_k * Hk * k.splits * 2 : 0;
   return cross_up((size_t)H * B * max_q * sizeof(float)) + cross_up(std::max(rows_q, rows_k) * Dh * sizeof(float));
 }
@@ -416,7 +417,7 @@ extern "C" int spa_cross_attention_bwd(const void* q, const void* k, const void*
   }
   SPA_REQUIRE(aligned16(out) && aligned16(dout) && aligned16(dq) && aligned16(dk) && aligned16(dv), SPA_ERR_INVALID_ARG,
               "%s: tensors not 16-byte aligned", fn);
-  for (const CrossPlan& p : {dq_plan(B, max_q, max_k, H, Hk), dkdv_plan(B, max_q, max_k, H, Hk)})
+  for (const CrossPlan& p : {dq_plan(B, max_q, max_k, H, Hk, dtype), dkdv_plan(B, max_q, max_k, H, Hk, dtype)})
     SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*Hk*blocks must be < 2^31", fn);
   const size_t need = spa_cross_attention_bwd_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype);
   SPA_REQUIRE(workspace != nullptr && workspace_bytes >= need, SPA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
