@@ -347,7 +347,7 @@ int spa_qk_norm_rotary_bwd(const void* dq_out, const void* dk_out, int64_t dq_ou
  * and cu_seqlens_q = {0, T}.
  * in:  q, k, v: rows, element (j, h, d) at p[j*row_stride + h*Dh + d], H heads of q, Hk of k and v, H a multiple of Hk, strides < 2^31 elements;
  *      cu_seqlens_q, cu_seqlens_k [B+1] int32; key_lens [B] int32 or NULL; max_q, max_k >= every segment's rows (B*max_q, B*max_k, max_q*H/Hk < 2^31; what
- *      lies behind them in a longer segment is not looked at); Dh in {32, 64}; softmax_scale (host float; 0 means 1/sqrt(Dh)); workspace of at least
+ *      lies behind them in a longer segment, and rows of q from B*max_q on, are not looked at); Dh in {32, 64}; softmax_scale (host float; 0 means 1/sqrt(Dh)); workspace of at least
  *      spa_cross_attention_workspace_bytes bytes, 256-byte aligned (NULL where that is 0: the keys are not split over workgroups).
  * out: out [>= rows of q, H*Dh] dtype, contiguous; lse [H, B*max_q] fp32 or NULL.  Other rows are not written.  The bits are the same in every run; the
  *      order in which a row's keys are added follows from B, H, Hk, max_q, max_k and the segment's number of keys.
@@ -675,7 +675,7 @@ int spa_gated_linear_packed(const void* x, const int32_t* gather_idx, const int3
  * bias spa_linear_packed_bwd_weight with x = h.
  * in:  dy [*, N_out] dtype, dy_row_stride elements a row; dy_idx [M_cap] int32 (row(j) = dy_idx[j]) or NULL; total as there; pre as written by the forward;
  *      bf16: N_out, F and dy_row_stride multiples of 8.
- * out: d_pre [M_cap, 2F] dtype (not pre itself).  Rows from min(*total, M_cap) on are not written.
+ * out: d_pre [M_cap, 2F] dtype; it may be pre itself.  Rows from min(*total, M_cap) on are not written.
  */
 int spa_gated_linear_packed_bwd(const void* dy, const int32_t* dy_idx, int64_t dy_row_stride, const int32_t* total, const void* W_down, const void* pre,
                                 int M_cap, int N_out, int F, int act, int dtype, void* d_pre, void* stream);

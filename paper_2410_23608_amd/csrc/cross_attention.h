@@ -34,9 +34,12 @@ struct CrossUnit {
   long q0, k0;                   // the segment's first rows
   int nq, nk, held;              // rows (tokens times heads), keys, keys the segment has places for
 };
+// What of a segment is looked at: no more tokens and keys than the longest may have, no token from the B max_q-th on (lse and D have no place for
+// it), nothing of one that starts below 0.
 __device__ __forceinline__ void cross_lengths(const CrossShape& s, int b, int q0, int k0, int& nq, int& nk, int& held) {
-  nq = min(max(s.cu_q[b + 1] - q0, 0), s.most_q) * (int)s.G.d;
-  held = min(max(s.cu_k[b + 1] - k0, 0), s.most_k);
+  const int room = q0 < 0 ? 0 : (int)max(s.stat_stride - q0, 0L);
+  nq = min(min(max(s.cu_q[b + 1] - q0, 0), s.most_q), room) * (int)s.G.d;
+  held = k0 < 0 ? 0 : min(max(s.cu_k[b + 1] - k0, 0), s.most_k);
   nk = s.key_lens != nullptr ? min(max(s.key_lens[b], 0), held) : held;
 }
 // Blocks and splits of a pair (segment, key head) next to each other on one XCD, whose L2 then holds what they share, pairs dealt to the XCDs there

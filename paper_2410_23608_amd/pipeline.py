@@ -630,6 +630,185 @@ class NormBlockTrainPass(NormBlockPass):
         return self.loss
 
 
+class LayerPass(_Pass):
+    """A whole transformer layer on the selected tokens, with rotary positions, conditioned on another sequence:
+
+      gate_select(x) -> pack (indices only)
+      y1 = x + attention: norm of the selected tokens -> QKV projection -> norm of the heads of q and k and rotation by the token's
+           place -> packed attention -> output projection, onto the residual stream
+      y2 = y1 + attention to the states: norm -> query projection, key and value projection of the states -> norm of the heads -> cross
+           attention, `cross_heads` key heads -> output projection
+      y  = y2 + gated feed-forward block: norm -> both projections, activation and product -> projection back;   tokens that were
+           not selected keep x throughout
+
+    grid: (rows, columns) or (frames, rows, columns) of an image's map, pairs: pairs of a head turned by the frame and by the row
+    (default: as many by each axis that has more than one place, what is left by the columns).  states [B, L, C_states]: a padded batch,
+    key_lens [B] int32 of them count (0: the layer adds nothing to that image's tokens there).  All norms are RMS norms.  The parameters are a
+    dict with the names of PARAMS; b_in and b_out may be None."""
+
+    PARAMS = ("gamma_self", "W_qkv", "gamma_q", "gamma_k", "W_o", "gamma_cross", "W_cross_q", "W_cross_kv", "gamma_cross_q", "gamma_cross_k",
+              "W_cross_o", "gamma_ffn", "W_in", "b_in", "W_out", "b_out")
+
+    def __init__(self, B: int, grid: Tuple[int, ...], C: int, H: int, F: int, L: int, C_states: int, dtype: str, cross_heads: Optional[int] = None,
+                 tau: float = 0.5, bias: float = 0.0, eps: float = 1e-6, pairs: Optional[Tuple[int, int]] = None, base: float = 100.0,
+                 halves: bool = False, gelu: bool = False):
+        grid = (1,) * (3 - len(grid)) + tuple(grid)
+        N, Dh = grid[0] * grid[1] * grid[2], C // H
+        self.B, self.N, self.grid, self.C, self.H, self.Dh, self.F, self.L, self.C_states = B, N, grid, C, H, Dh, F, L, C_states
+        self.Hk = H if cross_heads is None else cross_heads
+        self.tau, self.bias, self.eps = tau, bias, eps
+        self.layout = spa.SPA_ROTARY_HALVES if halves else spa.SPA_ROTARY_ADJACENT
+        self.act = spa.SPA_ACT_GELU if gelu else spa.SPA_ACT_SILU
+        if pairs is None:
+            each = Dh // 2 // max(1, sum(n > 1 for n in grid))
+            pairs = (each if grid[0] > 1 else 0, each if grid[1] > 1 else 0)
+        self.pairs, self.table = tuple(pairs), spa.rotary_table(grid, Dh, pairs, base).cuda()
+        td, cap, code = _td(dtype), B * N, spa.SPA_BF16 if dtype == "bf16" else spa.SPA_F32
+        dv = dict(device="cuda")
+        i32 = lambda n: torch.zeros(n, dtype=torch.int32, **dv)
+        rows = lambda width, n=cap: torch.zeros(n, width, dtype=td, **dv)
+        self.scores, self.mask = torch.empty(B, N, dtype=torch.float32, **dv), torch.empty(B, N, dtype=torch.uint8, **dv)
+        self.cu_seqlens, self.gather_idx, self.inv_pos, self.total = i32(B + 1), i32(cap), i32(cap), i32(1)
+        self.cu_states = torch.arange(B + 1, dtype=torch.int32, **dv) * L
+        Ck = self.Hk * Dh
+        self.normed, self.qkv, self.q_rot, self.k_rot, self.attn = rows(C), rows(3 * C), rows(C), rows(C), rows(C)
+        self.normed_cross, self.cross_q, self.cross_qn, self.cross_attn = rows(C), rows(C), rows(C), rows(C)
+        self.cross_kv, self.cross_kn = rows(2 * Ck, B * L), rows(Ck, B * L)
+        self.normed_ffn, self.h = rows(C), rows(F)
+        self.y1, self.y2, self.y = (torch.empty(B, N, C, dtype=td, **dv) for _ in range(3))
+        u8 = lambda n: torch.empty(max(n, 256), dtype=torch.uint8, **dv)
+        self.ws_cross = u8(spa.spa_cross_attention_workspace_bytes(B, N, L, H, self.Hk, Dh, code))
+        self.stats_self = self.stats_cross = self.stats_ffn = self.lse = self.lse_cross = self.pre = None       # kept for a backward
+
+    def stages(self, x, w, states, key_lens, gamma_self, W_qkv, gamma_q, gamma_k, W_o, gamma_cross, W_cross_q, W_cross_kv, gamma_cross_q,
+               gamma_cross_k, W_cross_o, gamma_ffn, W_in, b_in, W_out, b_out) -> List[Tuple[str, Callable[[], None]]]:
+        C, H, Hk, Dh, t, rms = self.C, self.H, self.Hk, self.Dh, self.total, spa.SPA_NORM_RMS
+        Ck, p, kv = Hk * Dh, self.qkv, self.cross_kv
+        norm = lambda rows, gamma, out, stats: spa.spa_norm_packed(rows, self.gather_idx, t, gamma, None, rms, self.eps, out, stats, prepare=True)
+        project = lambda rows, W, out: spa.spa_linear_packed(rows, None, None, t, W, None, out, prepare=True)
+        back = lambda rows, W, b, res, y: spa.spa_linear_packed_unpack(rows, t, W, b, self.gather_idx, self.inv_pos, res, y, prepare=True)
+        heads = lambda q, total, gamma, n, out: spa.spa_qk_norm_rotary(q, None, None, total, gamma, None, None, None, rms, self.eps, None, (0, 0),
+                                                                        (1, 1, 1), n, 0, Dh, out, None, prepare=True)
+        return [
+            ("gate_select", spa.spa_gate_select(x, w, self.bias, None, self.tau, self.scores, self.mask, None, prepare=True)),
+            ("pack_indices", spa.spa_pack(None, self.mask, None, None, 0, None, self.cu_seqlens, self.gather_idx, self.inv_pos, t, prepare=True)),
+            ("norm_self", norm(x, gamma_self, self.normed, self.stats_self)),
+            ("qkv_projection", project(self.normed, W_qkv, p)),
+            ("qk_norm_rotary", spa.spa_qk_norm_rotary(
+                p[:, :C], p[:, C:2 * C], self.gather_idx, t, gamma_q, None, gamma_k, None, rms, self.eps, self.table, self.pairs, self.grid, H, H, Dh,
+                self.q_rot, self.k_rot, self.layout, prepare=True)),
+            ("packed_attention", spa.spa_packed_attention(self.q_rot, self.k_rot, p[:, 2 * C:], self.cu_seqlens, self.B, self.N, H, Dh, self.attn,
+                                                          self.lse, prepare=True)),
+            ("out_projection", back(self.attn, W_o, None, x, self.y1)),
+            ("norm_cross", norm(self.y1, gamma_cross, self.normed_cross, self.stats_cross)),
+            ("cross_q_projection", project(self.normed_cross, W_cross_q, self.cross_q)),
+            ("cross_kv_projection", spa.spa_linear_packed(states, None, None, None, W_cross_kv, None, kv, prepare=True)),
+            ("cross_q_norm", heads(self.cross_q, t, gamma_cross_q, H, self.cross_qn)),
+            ("cross_k_norm", heads(kv[:, :Ck], None, gamma_cross_k, Hk, self.cross_kn)),
+            ("cross_attention", spa.spa_cross_attention(self.cross_qn, self.cross_kn, kv[:, Ck:], self.cu_seqlens, self.cu_states, key_lens, self.B, self.N,
+                                                        self.L, H, Hk, Dh, self.cross_attn, self.lse_cross, self.ws_cross, prepare=True)),
+            ("cross_out_projection", back(self.cross_attn, W_cross_o, None, self.y1, self.y2)),
+            ("norm_ffn", norm(self.y2, gamma_ffn, self.normed_ffn, self.stats_ffn)),
+            ("gated_linear", spa.spa_gated_linear_packed(self.normed_ffn, None, t, W_in, b_in, self.act, self.h, self.pre, prepare=True)),
+            ("ffn_out_projection", back(self.h, W_out, b_out, self.y2, self.y)),
+        ]
+
+    def run(self, x, w, states, key_lens, params):
+        self._issue(x, w, states, key_lens, *(params[name] for name in self.PARAMS))
+        return self.y
+
+
+class LayerTrainPass(LayerPass):
+    """Forward + backward of a LayerPass layer with the selection loss.  Results: y, loss, dx (the residual stream's, the norm's and the
+    gate's gradients), d_states, dw, db (the gate's), and grads: a dict of the parameters' gradients (fp32; None where the parameter is)."""
+
+    def __init__(self, B: int, grid: Tuple[int, ...], C: int, H: int, F: int, L: int, C_states: int, dtype: str, cross_heads: Optional[int] = None,
+                 tau: float = 0.5, bias: float = 0.0, eps: float = 1e-6, pairs: Optional[Tuple[int, int]] = None, base: float = 100.0,
+                 halves: bool = False, gelu: bool = False, loss_scale: Optional[float] = None):
+        super().__init__(B, grid, C, H, F, L, C_states, dtype, cross_heads, tau, bias, eps, pairs, base, halves, gelu)
+        N, Dh, Hk, td, cap, Ck = self.N, self.Dh, self.Hk, _td(dtype), B * self.N, self.Hk * self.Dh
+        self.loss_scale = 0.01 / cap if loss_scale is None else loss_scale
+        code = spa.SPA_BF16 if dtype == "bf16" else spa.SPA_F32
+        f32 = dict(dtype=torch.float32, device="cuda")
+        rows = lambda width, n=cap: torch.zeros(n, width, dtype=td, device="cuda")
+        self.stats_self, self.stats_cross, self.stats_ffn = (torch.zeros(2, cap, **f32) for _ in range(3))
+        self.lse, self.lse_cross, self.pre = torch.zeros(H, cap, **f32), torch.zeros(H, cap, **f32), rows(2 * F)
+        self.d_pre, self.d_normed, self.d_attn = rows(2 * F), rows(C), rows(C)
+        self.d_qrot, self.d_krot, self.d_qkv = rows(C), rows(C), rows(3 * C)
+        self.d_cross_q, self.d_kn, self.d_kv = rows(C), rows(Ck, B * L), rows(2 * Ck, B * L)
+        self.dy2, self.dy1, self.dx = (torch.empty(B, N, C, dtype=td, device="cuda") for _ in range(3))
+        self.d_states = torch.empty(B * L, C_states, dtype=td, device="cuda")
+        self.no_d_scores = torch.zeros(B, N, **f32)            # (the scores select, nothing else)
+        e = lambda *shape: torch.empty(*shape, **f32)
+        self.grad_list = [e(C), e(3 * C, C), e(Dh), e(Dh), e(C, C), e(C), e(C, C), e(2 * Ck, C_states), e(Dh), e(Dh), e(C, C), e(C), e(2 * F, C), e(2 * F),
+                          e(C, F), e(C)]
+        self.dw, self.db, self.loss = e(C), e(1), e(1)
+        u8 = lambda n: torch.empty(max(n, 256), dtype=torch.uint8, device="cuda")
+        weight = lambda K, n_out, M=cap: spa.spa_linear_bwd_weight_workspace_bytes(M, K, n_out, dtype)
+        heads = lambda M, n, nk: spa.spa_qk_norm_rotary_bwd_workspace_bytes(M, n, nk, Dh, code)
+        # (one at a time, in order)
+        self.ws = u8(max(spa.spa_norm_bwd_workspace_bytes(cap, C, code), spa.spa_attention_bwd_workspace_bytes(B, N, H, Dh, code),
+                         spa.spa_cross_attention_bwd_workspace_bytes(B, N, L, H, Hk, Dh, code), spa.spa_gate_bwd_workspace_bytes(B, N, C, code),
+                         weight(C, 3 * C), weight(C, C), weight(C_states, 2 * Ck, B * L), weight(C, 2 * F), weight(F, C), heads(cap, H, H), heads(cap, H, 0),
+                         heads(B * L, Hk, 0)))
+
+    @property
+    def grads(self):
+        return dict(zip(self.PARAMS, self.grad_list))
+
+    def stages(self, x, w, states, key_lens, gamma_self, W_qkv, gamma_q, gamma_k, W_o, gamma_cross, W_cross_q, W_cross_kv, gamma_cross_q,
+               gamma_cross_k, W_cross_o, gamma_ffn, W_in, b_in, W_out, b_out, labels, dy):
+        C, H, Hk, Dh, t, rms, cap, ws = self.C, self.H, self.Hk, self.Dh, self.total, spa.SPA_NORM_RMS, self.B * self.N, self.ws
+        Ck, p, dp, kv, dkv, rows_k = Hk * Dh, self.qkv, self.d_qkv, self.cross_kv, self.d_kv, self.B * self.L
+        (g_self, gW_qkv, g_q, g_k, gW_o, g_cross, gW_cq, gW_ckv, g_cq, g_ck, gW_co, g_ffn, gW_in, gb_in, gW_out, gb_out) = self.grad_list
+        flat = lambda d: d.view(cap, C)
+        given = lambda param, grad: None if param is None else grad
+        into = lambda d, idx, W, out, M=cap, total=t: spa.spa_linear_packed_bwd_input(d, idx, total, W, M, None, None, out, prepare=True)
+        weight = lambda d, idx, rows, dW, db=None, M=cap, total=t: spa.spa_linear_packed_bwd_weight(d, idx, rows, None, None, total, M, dW, db, ws, prepare=True)
+        norm = lambda rows, gamma, stats, d, out, dgamma: spa.spa_norm_packed_bwd(self.d_normed, rows, self.inv_pos, t, gamma, rms, stats, d, out,
+                                                                                  given(gamma, dgamma), None, ws, prepare=True)
+        heads = lambda d, q, total, gamma, n, out, dgamma: spa.spa_qk_norm_rotary_bwd(
+            d, None, q, None, None, total, gamma, None, rms, self.eps, None, (0, 0), (1, 1, 1), n, 0, Dh, out, None, given(gamma, dgamma), None, None, None, ws,
+            prepare=True)
+        return super().stages(x, w, states, key_lens, gamma_self, W_qkv, gamma_q, gamma_k, W_o, gamma_cross, W_cross_q, W_cross_kv, gamma_cross_q,
+                              gamma_cross_k, W_cross_o, gamma_ffn, W_in, b_in, W_out, b_out) + [
+            ("gated_linear_bwd", spa.spa_gated_linear_packed_bwd(flat(dy), self.gather_idx, t, W_out, self.pre, self.act, self.d_pre, prepare=True)),
+            ("ffn_out_bwd_weight", weight(flat(dy), self.gather_idx, self.h, gW_out, given(b_out, gb_out))),
+            ("ffn_bwd_input", into(self.d_pre, None, W_in, self.d_normed)),
+            ("ffn_bwd_weight", weight(self.d_pre, None, self.normed_ffn, gW_in, given(b_in, gb_in))),
+            ("norm_ffn_bwd", norm(self.y2, gamma_ffn, self.stats_ffn, dy, self.dy2, g_ffn)),
+            ("cross_out_bwd_input", into(flat(self.dy2), self.gather_idx, W_cross_o, self.d_attn)),
+            ("cross_out_bwd_weight", weight(flat(self.dy2), self.gather_idx, self.cross_attn, gW_co)),
+            ("cross_attention_bwd", spa.spa_cross_attention_bwd(
+                self.cross_qn, self.cross_kn, kv[:, Ck:], self.cross_attn, self.d_attn, self.lse_cross, self.cu_seqlens, self.cu_states, key_lens, self.B,
+                self.N, self.L, H, Hk, Dh, self.d_cross_q, self.d_kn, dkv[:, Ck:], ws, prepare=True)),
+            ("cross_q_norm_bwd", heads(self.d_cross_q, self.cross_q, t, gamma_cross_q, H, self.d_cross_q, g_cq)),
+            ("cross_k_norm_bwd", heads(self.d_kn, kv[:, :Ck], None, gamma_cross_k, Hk, dkv[:, :Ck], g_ck)),
+            ("cross_q_bwd_input", into(self.d_cross_q, None, W_cross_q, self.d_normed)),
+            ("cross_q_bwd_weight", weight(self.d_cross_q, None, self.normed_cross, gW_cq)),
+            ("cross_kv_bwd_input", into(dkv, None, W_cross_kv, self.d_states, rows_k, None)),
+            ("cross_kv_bwd_weight", weight(dkv, None, states, gW_ckv, None, rows_k, None)),
+            ("norm_cross_bwd", norm(self.y1, gamma_cross, self.stats_cross, self.dy2, self.dy1, g_cross)),
+            ("out_bwd_input", into(flat(self.dy1), self.gather_idx, W_o, self.d_attn)),
+            ("out_bwd_weight", weight(flat(self.dy1), self.gather_idx, self.attn, gW_o)),
+            ("packed_attention_bwd", spa.spa_packed_attention_bwd(
+                self.q_rot, self.k_rot, p[:, 2 * C:], self.attn, self.d_attn, self.lse, self.cu_seqlens, self.B, self.N, H, Dh, self.d_qrot, self.d_krot,
+                dp[:, 2 * C:], ws, prepare=True)),
+            ("qk_norm_rotary_bwd", spa.spa_qk_norm_rotary_bwd(
+                self.d_qrot, self.d_krot, p[:, :C], p[:, C:2 * C], self.gather_idx, t, gamma_q, gamma_k, rms, self.eps, self.table, self.pairs, self.grid, H, H,
+                Dh, dp[:, :C], dp[:, C:2 * C], given(gamma_q, g_q), None, given(gamma_k, g_k), None, ws, self.layout, prepare=True)),
+            ("qkv_bwd_input", into(dp, None, W_qkv, self.d_normed)),
+            ("qkv_bwd_weight", weight(dp, None, self.normed, gW_qkv)),
+            ("norm_self_bwd", norm(x, gamma_self, self.stats_self, self.dy1, self.dx, g_self)),
+            ("gate_bwd", spa.spa_gate_bwd_scores(x, w, self.bias, self.scores, None, labels, self.no_d_scores, self.dx, self.loss_scale, self.loss, self.dx,
+                                                 self.dw, self.db, ws, prepare=True)),
+        ]
+
+    def run(self, x, w, states, key_lens, params, labels, dy):
+        self._issue(x, w, states, key_lens, *(params[name] for name in self.PARAMS), labels, dy)
+        return self.loss
+
+
 class ContainerForwardPass(_Pass):
     """The forward pass with the paper's container mask (Section 3.2 "Token Packing"): the
     packed stream is cut into containers of length L and a token attends to the tokens of its

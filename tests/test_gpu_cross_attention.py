@@ -267,6 +267,31 @@ def test_offsets_past_32_bits(spa):
     assert torch.equal(dkv[:75, :64], want["dkv"][:75])
 
 
+def test_rows_without_a_place_are_left(spa):
+    """Segments that are longer than max_q, max_k say, and rows from B max_q on: neither computed nor written."""
+    c = Case([6, 4], [20, 30], 2, 2, 32)
+    C, Ck, i32 = 64, 64, lambda *a: torch.tensor(a, dtype=torch.int32).cuda()
+    q, kv, dout = torch.zeros(20, C, dtype=torch.bfloat16).cuda(), c.kv.cuda(), torch.zeros(20, C, dtype=torch.bfloat16).cuda()
+    q[4:14], dout[4:14] = c.q[:10].cuda(), c.dout[:10].cuda()
+    want = c.run(spa)
+    nan = lambda *s, dt=torch.bfloat16: torch.full(s, float("nan"), dtype=dt, device="cuda")
+    out, lse, dq, dkv = nan(20, C), nan(2, 12 + 4, dt=torch.float32), nan(20, C), nan(*kv.shape)
+    cu_q, cu_k, args = i32(4, 10, 14), i32(0, 20, 50), (None, 2, 6, 30, 2, 2, 32)                # 12 rows have a place: 4 .. 11
+    spa.spa_cross_attention(q, kv[:, :Ck], kv[:, Ck:], cu_q, cu_k, *args, out, lse)
+    assert torch.equal(out[4:12], want["out"][:8]) and bool(torch.isnan(out[12:]).all()) and bool(torch.isnan(out[:4]).all())
+    ws = torch.zeros(spa.spa_cross_attention_bwd_workspace_bytes(2, 6, 30, 2, 2, 32, 1), dtype=torch.uint8, device="cuda")
+    spa.spa_cross_attention_bwd(q, kv[:, :Ck], kv[:, Ck:], out, dout, lse, cu_q, cu_k, *args, dq, dkv[:, :Ck], dkv[:, Ck:], ws)
+    assert torch.equal(dq[4:12], want["dq"][:8]) and bool(torch.isnan(dq[12:]).all())
+    assert torch.equal(dkv[:20], want["dkv"][:20])                                              # (of the first segment nothing is cut)
+    args = (None, 2, 5, 25, 2, 2, 32)                                                           # the first segment's sixth row, five keys of the second
+    out, lse = nan(20, C), nan(2, 16, dt=torch.float32)
+    spa.spa_cross_attention(c.q.cuda(), kv[:, :Ck], kv[:, Ck:], i32(0, 6, 10), cu_k, *args, out, lse)
+    assert torch.equal(out[:5], want["out"][:5]) and bool(torch.isnan(out[5]).all())
+    short = Case([6, 4], [20, 25], 2, 2, 32)
+    short.q, short.kv = c.q, torch.cat((c.kv[:45], c.kv[50:]))
+    assert torch.equal(out[6:10], short.run(spa, back=False)["out"][6:10])
+
+
 def _same(a, b):
     return all(torch.equal(torch.nan_to_num(a[n].float()), torch.nan_to_num(b[n].float())) for n in a)
 

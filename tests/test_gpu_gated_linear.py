@@ -160,6 +160,17 @@ def test_the_same_row_twice_and_a_column_slice(spa):
     assert torch.equal(d_pre, want["d_pre"])
 
 
+@BOTH
+def test_the_gradient_over_its_input(spa, dtype):
+    """d_pre may be pre itself."""
+    for M, K, F in ((300, 64, 136), (6272, 64, 1024) if dtype == "bf16" else (2100, 40, 1024)):
+        c = Case(M, K, F, 1, dtype, live=M - 7)
+        want = c.run(spa)
+        pre = want["pre"].clone()
+        spa.spa_gated_linear_packed_bwd(c.dy, c.idx, c.total, c.W_down, pre, 1, pre)
+        assert torch.equal(pre[:M - 7], want["d_pre"][:M - 7])
+
+
 def test_values_that_are_not_finite_stay_in_their_rows(spa):
     for M, K, F in ((200, 128, 72), (6272, 256, 1024)):
         c = Case(M, K, F)
