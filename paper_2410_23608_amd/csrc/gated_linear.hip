@@ -316,7 +316,8 @@ __global__ void __launch_bounds__(kF32Threads) gated_f32_kernel(const GatedF32 p
     for (int i = 0; i < PB::kCount; ++i) wp[i] = p.w + (long)min(n0 + PB::line(i), p.F - 1) * (BACK ? 1 : p.kc);
     float acc[NB][TM][TM] = {};
     f32_tile_sums<EDGE, NB, true, !BACK>(l, p.kc, [&](int i, int k) { return ap[i][k]; },
-                                         [&](int q, int i, int k) { return BACK ? wp[i][(long)k * p.F] : wp[i][(long)q * p.F * p.kc + k]; }, acc, [](const auto&, int) {});
+                                         [&](int q, int i, int k) { return BACK ? wp[i][(long)k * p.F] : wp[i][(long)q * p.F * p.kc + k]; }, F32AsIs{}, F32AsIs{},
+                                         acc, [](const auto&, int) {});
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
 #pragma unroll
     for (int r = 0; r < TM; ++r)

@@ -54,8 +54,8 @@ linear_f32_kernel(const float* __restrict__ x, const int32_t* __restrict__ gathe
       wp[i] = W + (long)n * K;
     }
     float acc[1][TM][TM] = {};
-    f32_tile_sums<EDGE, 1, true, true>(l, K, [&](int i, int k) { return kScale ? sc[i] * xp[i][k] : xp[i][k]; }, [&](int, int i, int k) { return wp[i][k]; },
-                                       acc, [](const auto&, int) {});
+    f32_tile_sums<EDGE, 1, true, true>(l, K, [&](int i, int k) { return xp[i][k]; }, [&](int, int i, int k) { return wp[i][k]; },
+                                       [&](int i, float v) { return kScale ? sc[i] * v : v; }, F32AsIs{}, acc, [](const auto&, int) {});
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
 #pragma unroll
     for (int r = 0; r < TM; ++r)

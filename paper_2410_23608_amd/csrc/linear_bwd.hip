@@ -90,8 +90,8 @@ linear_bwd_input_f32_kernel(const float* __restrict__ dout, const int32_t* __res
       gp[i] = dout + (dout_idx != nullptr ? (long)dout_idx[m] : (long)m) * ldd;
     }
     float acc[1][TM][TM] = {};
-    f32_tile_sums<EDGE, 1, true, false>(l, kc, [&](int i, int k) { return gp[i][k]; }, [&](int, int, int k) { return wp[(long)k * ncols]; }, acc,
-                                        [](const auto&, int) {});
+    f32_tile_sums<EDGE, 1, true, false>(l, kc, [&](int i, int k) { return gp[i][k]; }, [&](int, int, int k) { return wp[(long)k * ncols]; }, F32AsIs{},
+                                        F32AsIs{}, acc, [](const auto&, int) {});
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
 #pragma unroll
     for (int r = 0; r < TM; ++r)
@@ -584,7 +584,7 @@ __global__ void __launch_bounds__(256) linear_bwd_weight_reduce_group_kernel(con
   weight_reduce_block(m.a[mb.s], mb.block, mb.blocks);
 }
 
-template <int EDGE>
+template <int EDGE, bool kScale>
 __global__ void __launch_bounds__(kF32Threads)
 linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __restrict__ dout_idx, long ldd,
                              const float* __restrict__ x, const int32_t* __restrict__ x_idx,
@@ -598,14 +598,16 @@ linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __re
     const int line = F32Place<EDGE, false>::line(0);
     const float *gp = dout + min(n0 + line, n_out - 1), *xp = x + min(k0 + line, K - 1);
     const bool sums = dbias != nullptr && k0 == 0 && threadIdx.x < EDGE;      // (the bias' gradient: the same rows of dout, added in order)
-    float acc[1][TM][TM] = {}, bias = 0.f;
+    using Place = F32Place<EDGE, false>;
+    float acc[1][TM][TM] = {}, bias = 0.f, gate[Place::kCount];
+    int gr[Place::kCount], xr[Place::kCount];              // rows of the step to come
     f32_tile_sums<EDGE, 1, false, false>(
-        l, M, [&](int, int m) { return gp[(dout_idx != nullptr ? (long)dout_idx[m] : (long)m) * ldd]; },
-        [&](int, int, int m) {
-          const long xr = x_idx != nullptr ? (long)x_idx[m] : (long)m;
-          return gate_scores != nullptr ? sigmoidf_dev(gate_scores[xr]) * xp[xr * K] : xp[xr * K];
+        l, M, [&](int i, int) { return gp[(long)gr[i] * ldd]; },
+        [&](int, int i, int) {
+          if (kScale) gate[i] = gate_scores[xr[i]];
+          return xp[(long)xr[i] * K];
         },
-        acc,
+        F32AsIs{}, [&](int, int i, float v) { return kScale ? sigmoidf_dev(gate[i]) * v : v; }, acc,
         [&](const float (&a)[kF32Step<EDGE>][kF32Row<EDGE>], int ks) {
           if (!sums) return;
           int kk = 0;
@@ -617,6 +619,14 @@ linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __re
             for (int j = 0; j < 8; ++j) bias += v[j];
           }
           for (; kk < ks; ++kk) bias += a[kk][threadIdx.x];
+        },
+        [&](int m0) {
+#pragma unroll
+          for (int i = 0; i < Place::kCount; ++i) {
+            const int m = min(m0 + Place::k(i), M - 1);
+            gr[i] = dout_idx != nullptr ? dout_idx[m] : m;
+            xr[i] = x_idx != nullptr ? x_idx[m] : m;
+          }
         });
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
     if (sums && n0 + (int)threadIdx.x < n_out) dbias[n0 + threadIdx.x] = bias;
@@ -834,7 +844,9 @@ extern "C" int spa_linear_packed_bwd_weight(const void* dout, const int32_t* dou
   if (dtype == SPA_F32) {
     const bool wide = f32_wide(N_out, K);
     const long wgs = std::min(f32_tiles(N_out, K, wide ? 64 : 32), 8192L);
-    hipLaunchKernelGGL((wide ? linear_bwd_weight_f32_kernel<64> : linear_bwd_weight_f32_kernel<32>), dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)dout, dout_idx,
+    const auto kernel = gate_scores != nullptr ? (wide ? linear_bwd_weight_f32_kernel<64, true> : linear_bwd_weight_f32_kernel<32, true>)
+                                               : (wide ? linear_bwd_weight_f32_kernel<64, false> : linear_bwd_weight_f32_kernel<32, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)dout, dout_idx,
                        (long)dout_row_stride, (const float*)x, x_idx, gate_scores, total, M_cap, K, N_out, dW, dbias);
     return check_launch(fn);
   }

@@ -111,6 +111,18 @@ def test_shapes(spa, act, M, K, F):
     c.check(c.run(spa))
 
 
+@pytest.mark.parametrize("tiles", ["2", "14"])
+@pytest.mark.parametrize("M,K,F", [(40, 64, 72), (700, 200, 328), (6272, 128, 1024)])
+def test_tiles_by_option(spa, tiles, M, K, F):
+    """The option of the projections' tiles holds here too: 128 x 128, or the large ones, where the rule would not take them."""
+    c = Case(M, K, F, seed=3)
+    spa.spa_set_option("gemm_tm", tiles)
+    try:
+        c.check(c.run(spa))
+    finally:
+        spa.spa_set_option("gemm_tm")
+
+
 @BOTH
 @pytest.mark.parametrize("M,live", [(700, 700), (700, 0), (700, 1), (700, 129), (9000, 4100)])
 def test_counted_and_gathered(spa, dtype, M, live):
