@@ -334,7 +334,7 @@ extern "C" int spa_cross_attention(const void* q, const void* k, const void* v, 
   SPA_REQUIRE(out != nullptr, SPA_ERR_INVALID_ARG, "%s: out is null", fn);
   SPA_REQUIRE(aligned16(out), SPA_ERR_INVALID_ARG, "%s: out not 16-byte aligned", fn);
   const CrossPlan p = fwd_plan(B, max_q, max_k, H, Hk, dtype);
-  SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*Hk*blocks must be < 2^31", fn);
+  SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 4294967296L / kCrossThreads, SPA_ERR_INVALID_ARG, "%s: too many workgroups (B*max_q*H must be < about 2^31)", fn);
   const size_t need = spa_cross_attention_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype);
   SPA_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need), SPA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given",
               fn, need, workspace_bytes);

@@ -418,7 +418,7 @@ extern "C" int spa_cross_attention_bwd(const void* q, const void* k, const void*
   SPA_REQUIRE(aligned16(out) && aligned16(dout) && aligned16(dq) && aligned16(dk) && aligned16(dv), SPA_ERR_INVALID_ARG,
               "%s: tensors not 16-byte aligned", fn);
   for (const CrossPlan& p : {dq_plan(B, max_q, max_k, H, Hk, dtype), dkdv_plan(B, max_q, max_k, H, Hk, dtype)})
-    SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*Hk*blocks must be < 2^31", fn);
+    SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 4294967296L / kCrossThreads, SPA_ERR_INVALID_ARG, "%s: too many workgroups (B*max_q*H must be < about 2^31)", fn);
   const size_t need = spa_cross_attention_bwd_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype);
   SPA_REQUIRE(workspace != nullptr && workspace_bytes >= need, SPA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
               workspace_bytes);

@@ -31,8 +31,9 @@ struct GatedArgs {
   LargeRule rule;
 };
 
-// Phi and phi of the normal distribution.  bf16: Abramowitz and Stegun 7.1.26, erfc(x) = t (a1 + t (a2 + ... a5)) exp(-x^2), t = 1 / (1 + p x), off by at most
-// 1.5e-7, so Phi by half of that (half a bf16 step of Phi(-4)); fp32: the library's.
+// Phi and phi of the normal distribution.  bf16: erfc(x) exp(x^2) = t P(t), t = 1 / (1 + x / 2), P of degree 6 fitted so that erfc is off by at most 1.5e-7
+// absolute and 2^-12 relative for every x >= 0 (0.5e-7 and 2^-12.6 reached), Phi by half of the first: far below 0, too, the rounding of the result to
+// bf16 is what counts.  fp32: the library's.
 struct Normal {
   float cdf, density;
 };
@@ -40,11 +41,13 @@ template <bool EXACT>
 __device__ __forceinline__ Normal normal_of(float g) {
   const float e = EXACT ? expf(-0.5f * g * g) : __expf(-0.5f * g * g), density = 0.3989422804014327f * e;
   if (EXACT) return {0.5f * erfcf(-0.7071067811865476f * g), density};
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.7071067811865476f, fabsf(g), 1.f));
-  float p = fmaf(1.061405429f, t, -1.453152027f);
-  p = fmaf(p, t, 1.421413741f);
-  p = fmaf(p, t, -0.284496736f);
-  p = fmaf(p, t, 0.254829592f);
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.5f * 0.7071067811865476f, fabsf(g), 1.f));
+  float p = fmaf(0.08170961f, t, -0.32737189f);
+  p = fmaf(p, t, 0.33701283f);
+  p = fmaf(p, t, 0.08411100f);
+  p = fmaf(p, t, 0.26049545f);
+  p = fmaf(p, t, 0.28199505f);
+  p = fmaf(p, t, 0.28204799f);
   const float tail = 0.5f * p * t * e;
   return {g < 0.f ? tail : 1.f - tail, density};
 }
@@ -82,7 +85,7 @@ __device__ __forceinline__ void gated_tiles(const GatedArgs& p, int act, unsigne
                                        typename std::conditional<E == 16, DeepBlocks<BN, THREADS>, DeepPieces<BN, THREADS>>::type>::type;
   constexpr int COLS = BACK ? BN : BN / 2;                    // columns of h in a tile
   __bf16* lds = reinterpret_cast<__bf16*>(smem);
-  __shared__ float bias_s[BACK ? 1 : BN];
+  __shared__ __attribute__((aligned(16))) float bias_s[BACK ? 1 : BN];
   const int n_tiles = (p.F + COLS - 1) / COLS, live_tiles = ((M - m_first + BM - 1) / BM) * n_tiles, per_xcd = (live_tiles + 7) >> 3;
   const int xcd = block & 7;
   for (int jx = block >> 3; jx < per_xcd && xcd * per_xcd + jx < live_tiles; jx += blocks >> 3) {
@@ -352,7 +355,7 @@ static int launch_gated(const char* fn, GatedArgs args, int act, hipStream_t st)
   args.rule = large_rule(ncols, args.kc, false);
   const size_t smem = big ? kGatedBigLds : ring ? kGatedRingLds : kGatedSmallLds;
   const long tiles = gemm_tiles<long>(args.m_cap, ncols, big ? 192 : 128);          // (no less than with 256)
-  SPA_REQUIRE(tiles + 8 < 2147483647L / 2, SPA_ERR_INVALID_ARG, "%s: too many tiles", fn);
+  SPA_REQUIRE(big || tiles + 8 < 4294967296L / 512, SPA_ERR_INVALID_ARG, "%s: too many tiles (a launch has fewer than 2^32 threads)", fn);
   const long tiles8 = (tiles + 7) / 8 * 8;
   const auto kernel = big ? gated_big_kernel<BACK> : ring ? gated_ring_kernel<BACK> : gated_small_kernel<BACK>;
   const hipError_t attr = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -373,7 +376,7 @@ static int launch_gated_f32(const char* fn, const GatedF32& a, int act, hipStrea
 static int gated_checks(const char* fn, int M_cap, int K, int F, int act, int dtype) {
   SPA_REFUSE_IN_GROUP(fn);
   SPA_REQUIRE(M_cap >= 1 && K >= 1 && F >= 1, SPA_ERR_INVALID_ARG, "%s: M_cap, the contraction and F must be >= 1", fn);
-  SPA_REQUIRE(F < (1 << 30), SPA_ERR_INVALID_ARG, "%s: F must be < 2^30", fn);
+  SPA_REQUIRE(M_cap < 2147483647 - 512 && F < (1 << 30), SPA_ERR_INVALID_ARG, "%s: M_cap must be < 2^31 - 513 and F < 2^30", fn);
   SPA_REQUIRE(dtype == SPA_F32 || dtype == SPA_BF16, SPA_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
   SPA_REQUIRE(act == SPA_ACT_SILU || act == SPA_ACT_GELU, SPA_ERR_INVALID_ARG, "%s: unknown activation %d", fn, act);
   return SPA_OK;

@@ -19,7 +19,7 @@ NEED_BWD = lib.spa_cross_attention_bwd_workspace_bytes(*SIZES.values())
 
 def fwd(**k):
     a = dict(q=F, k=F, v=F, qs=128, ks=64, vs=64, cuq=F, cuk=F, lens=F, **SIZES, scale=0.0, out=F, lse=F, ws=F, bytes=NEED)
-    a.update(k)
+    a.update((n, v) for n, v in k.items() if n in a)
     return lib.spa_cross_attention(*a.values(), None)
 
 
@@ -41,6 +41,7 @@ def test_common_refusals(call):
     assert call(Hk=3) == -1 and "multiple" in msg()
     assert call(B=65536) == -1 and call(B=65535, max_q=40000) == -1 and call(B=65535, max_k=40000) == -1
     assert call(max_q=2 ** 30, H=8, Hk=2, qs=512) == -1 and "max_q" in msg()
+    assert call(B=60000, max_q=30000, max_k=30000, H=256, Hk=256, qs=8192, ks=8192, vs=8192, dqs=8192, dks=8192, dvs=8192) == -1 and "workgroups" in msg()
     assert call(dtype=5) == -2 and call(Dh=48) == -2
     assert call(qs=127) == -1 and call(qs=132) == -1 and call(ks=63) == -1 and call(vs=1 << 31) == -1
     for scale in (-1.0, float("nan"), float("inf")):

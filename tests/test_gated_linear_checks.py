@@ -14,7 +14,7 @@ def msg():
 
 def fwd(**k):
     a = dict(x=F, idx=F, total=F, W=F, bias=F, M=8, K=64, F=72, act=0, dtype=1, h=F, pre=F)
-    a.update(k)
+    a.update((n, v) for n, v in k.items() if n in a)
     return lib.spa_gated_linear_packed(*a.values(), None)
 
 
@@ -33,6 +33,7 @@ def test_refusals(call):
     for name in ("M", "K", "F"):
         assert call(**{name: 0}) == -1
     assert call(F=1 << 30) == -1
+    assert call(M=2 ** 31 - 1) == -1 and call(M=2 ** 31 - 600, K=8, F=8, stride=8) == -1 and "tiles" in msg()
     assert call(act=2) == -1 and "activation" in msg()
     assert call(dtype=3) == -2 and call(K=60) == -2 and call(F=76) == -2 and "multiples of 8" in msg()
     assert lib.spa_group_begin() == 0

@@ -151,6 +151,33 @@ def test_far_activations(spa, dtype, act, size):
     c.check(c.run(spa))
 
 
+@pytest.mark.parametrize("act", [0, 1])
+@pytest.mark.parametrize("M,F", [(200, 72), (6272, 1024)])
+def test_the_tails_are_rounded_once(spa, act, M, F):
+    """Far below 0 the activation and its slope are small, not lost: g is one element of x times 1, u = 1, dh = 1, so that h = act(g), d_g = slope, d_u = act(g).  GELU: Phi is off by 2^-12
+    relative; the slope Phi + g phi of g <= -3 is at least 2/3 |g| phi > 2 Phi, so off by 2^-12; the fast exponential by (|g| or g^2 / 2) 2^-23 <= 2^-16.  SiLU: s and its slope by 2^-16."""
+    td = torch.bfloat16
+    x, W, W_down = torch.zeros(M, 16, dtype=td, device="cuda"), torch.zeros(2 * F, 16, dtype=td, device="cuda"), torch.zeros(8, F, dtype=td, device="cuda")
+    x[:, 0] = -torch.linspace(3, 12 if act else 80, M, device="cuda").to(td)
+    x[:, 1] = 1
+    W[:F, 0] = 1
+    W[F:, 1] = 1
+    W_down[0] = 1
+    dy = torch.zeros(M, 8, dtype=td, device="cuda")
+    dy[:, 0] = 1
+    h, pre, d_pre = (torch.empty(M, n * F, dtype=td, device="cuda") for n in (1, 2, 2))
+    spa.spa_gated_linear_packed(x, None, None, W, None, act, h, pre)
+    spa.spa_gated_linear_packed_bwd(dy, None, None, W_down, pre, act, d_pre)
+    g = x[:, :1].double()
+    value, slope = act64(g, act)
+    if act:                                     # (ndtr subtracts from 1 here and is 0 at -12)
+        cdf = 0.5 * torch.special.erfc(-g / 2 ** 0.5)
+        value, slope = g * cdf, cdf + g * torch.exp(-g * g / 2) / (2 * np.pi) ** 0.5
+    assert torch.equal(pre[:, :F].double(), g.expand(M, F)) and bool((pre[:, F:] == 1).all())
+    for have, want in ((h, value), (d_pre[:, :F], slope), (d_pre[:, F:], value)):
+        assert bool(((have.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -11) * want.abs()).all())
+
+
 def test_more_live_rows_than_there_are(spa):
     c = Case(300, 64, 72)
     want = c.run(spa)
