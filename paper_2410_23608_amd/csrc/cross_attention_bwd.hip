@@ -340,6 +340,228 @@ __global__ void __launch_bounds__(kCrossThreads) cross_sum_kernel(const CrossBwd
   else *reinterpret_cast<floatx4*>(to) = sum;
 }
 
+// Few rows and keys in a unit (bf16): all of it in one workgroup, whose rows, keys and gradients are fetched once and whose scores are formed twice, in both
+// orders, out of LDS.  First the waves take 32 rows each (then the second half of the rows): K and V in LDS, Q and dO in registers, which then go to LDS in
+// their place.  Then they take 32 keys each, two or four waves to a block of keys where there are fewer blocks, whose sums the first adds in order.
+constexpr int kShortRows = 256, kShortKeys = 128;
+template <int DH>
+struct CrossShort {
+  static constexpr int RS = Ops<__bf16, DH>::RS, N = 2 * (DH / 32) * 16;                       // N: sums of a lane
+  static __host__ __device__ constexpr int tiles(int rows) { return (rows + 31) / 32; }
+  static constexpr size_t bytes(int rows, int keys) {
+    const size_t held = (size_t)2 * 32 * std::max(tiles(rows), tiles(keys)) * RS * sizeof(__bf16);
+    const int others = tiles(rows) == 1 ? 0 : tiles(rows) <= 3 ? 2 : 3;          // waves that hand over their sums: of two blocks of keys one each, of one up to three
+    const size_t sums = (size_t)others * N * kWave * sizeof(float);
+    return std::max(held, sums);
+  }
+};
+
+template <int DH>
+__global__ void __launch_bounds__(kCrossThreads) __attribute__((amdgpu_waves_per_eu(2))) cross_bwd_short_kernel(const CrossBwd<__bf16> a) {
+  using T = __bf16;
+  using O = Ops<T, DH>;
+  using S = CrossShort<DH>;
+  constexpr int DB = DH / 32, KK = DH / 16, CPR = DH / 8, RPP = kCrossThreads / CPR, CPT = kShortKeys / RPP, TILES = kShortRows / 128, KEY_TILES = kShortKeys / 32;
+  extern __shared__ __attribute__((aligned(16))) unsigned char cross_smem[];
+  __shared__ __attribute__((aligned(16))) float lse_s[kShortRows], lse2_s[kShortRows], negD_s[kShortRows];
+  __shared__ int far_s[kShortRows / 32];
+  const CrossUnit u = cross_unit(a.s);
+  if (!u.valid || (u.nq <= 0 && u.held <= 0)) return;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = (int)a.s.G.d;
+  const int nq = u.nq, nk = u.nk, row_tiles = (nq + 31) >> 5, key_tiles = (nk + 31) >> 5;
+  const long C = (long)a.s.H * DH, head = (long)u.hk * G * DH;
+  T* const first = reinterpret_cast<T*>(cross_smem);
+  T* const second = first + 32 * max(S::tiles(a.s.most_q * G), S::tiles(a.s.most_k)) * S::RS;
+  // ---- K, V on their way to LDS; every wave's rows
+  uintx4 kv[2][CPT];
+  if (nk > 0) {
+#pragma unroll
+    for (int t = 0; t < CPT; ++t) {
+      const long row = u.k0 + min(tid / CPR + t * RPP, nk - 1);
+      const int c = u.hk * DH + tid % CPR * 8;
+      kv[0][t] = *reinterpret_cast<const uintx4*>(a.k + row * a.ks + c);
+      kv[1][t] = *reinterpret_cast<const uintx4*>(a.v + row * a.vs + c);
+    }
+  }
+  typename O::Row qf[TILES], gf[TILES];
+  float lse[TILES];
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) {
+    if (wave + 4 * i >= row_tiles) continue;
+    const int rc = min((wave + 4 * i) * 32 + l32, nq - 1);
+    const uint32_t token = quotient((uint32_t)rc, a.s.G);
+    qf[i] = O::row(a.q + u.q0 * a.qs + head + group_row<DH>(a.s.G, rc, a.qs), hh);
+    gf[i] = O::row(a.dout + u.q0 * C + head + group_row<DH>(a.s.G, rc, C), hh);
+    lse[i] = a.lse[(u.hk * G + (rc - (int)(token * G))) * a.s.stat_stride + u.q0 + token];
+  }
+  if (nk > 0) {
+#pragma unroll
+    for (int t = 0; t < CPT; ++t) {
+      const int r = tid / CPR + t * RPP, o = r * S::RS + tid % CPR * 8;
+      if (r >= key_tiles * 32) break;
+      const bool ok = r < nk;
+      *reinterpret_cast<uintx4*>(first + o) = ok ? kv[0][t] : uintx4{0, 0, 0, 0};
+      *reinterpret_cast<uintx4*>(second + o) = ok ? kv[1][t] : uintx4{0, 0, 0, 0};
+    }
+  }
+  __syncthreads();
+  // ---- as rows
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) {
+    if (wave + 4 * i >= row_tiles) continue;
+    const int r = (wave + 4 * i) * 32 + l32;
+    const bool ok = r < nq, none = lse[i] == -INFINITY || !ok, far = __ballot(!none && fabsf(lse[i]) >= kFarScore) != 0;
+    const float ref = none ? INFINITY : lse[i], lse2 = ref * kLog2e;
+    floatx16 acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
+    floatx16 P[KEY_TILES], dp[KEY_TILES];
+    float D = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KEY_TILES; ++kb) {
+      if (kb >= key_tiles) break;
+      floatx16& s = P[kb];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = dp[kb][e] = 0.f;
+      O::dot(s, O::row(&first[(kb * 32 + l32) * S::RS], hh), qf[i]);
+      O::dot(dp[kb], O::row(&second[(kb * 32 + l32) * S::RS], hh), gf[i]);
+      if (kb * 32 + 32 > nk) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (kb * 32 + acc_row(e, hh) >= nk) s[e] = -INFINITY;
+      }
+      if (!far) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.s.c, -lse2));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.s.scale, -ref) * kLog2e);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) D = fmaf(s[e], dp[kb][e], D);
+    }
+    D = sum_across_halves(D);
+#pragma unroll
+    for (int kb = 0; kb < KEY_TILES; ++kb) {
+      if (kb >= key_tiles) break;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dp[kb][e] = P[kb][e] * (dp[kb][e] - D);
+      O::outer(acc, first, kb, dp[kb], lane);
+    }
+    O::store(acc, a.s.scale, a.dq + u.q0 * a.dqs + head + group_row<DH>(a.s.G, min(r, nq - 1), a.dqs), ok, hh);
+    if (hh == 0) {
+      lse_s[r] = ref;
+      lse2_s[r] = lse2;
+      negD_s[r] = -D;
+    }
+    if (lane == 0) far_s[wave + 4 * i] = far;
+  }
+  if (u.held <= 0) return;
+  // ---- as keys: parts waves a block of keys
+  const int share = key_tiles <= 1 ? 1 : key_tiles == 2 ? 2 : 4, parts = min(4 / share, max(row_tiles, 1)), kb = wave % share, part = wave / share;
+  const bool key_live = kb < key_tiles && part < parts;
+  typename O::Row kf, vf;
+  if (key_live) {
+    kf = O::row(&first[(kb * 32 + l32) * S::RS], hh);
+    vf = O::row(&second[(kb * 32 + l32) * S::RS], hh);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) {
+    if (wave + 4 * i >= row_tiles) continue;
+    const int r = (wave + 4 * i) * 32 + l32;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      *reinterpret_cast<bf16x8*>(&first[r * S::RS + kk * 16 + hh * 8]) = r < nq ? qf[i].f[kk] : zero_bf16x8();
+      *reinterpret_cast<bf16x8*>(&second[r * S::RS + kk * 16 + hh * 8]) = r < nq ? gf[i].f[kk] : zero_bf16x8();
+    }
+  }
+  __syncthreads();
+  floatx16 dka[DB], dva[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dka[d][e] = dva[d][e] = 0.f;
+  if (key_live)
+    for (int t = part; t < row_tiles; t += parts) {
+      floatx16 s, dp;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const floatx4 d4 = *reinterpret_cast<const floatx4*>(&negD_s[t * 32 + 8 * g + 4 * hh]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dp[4 * g + e] = d4[e];
+      }
+      O::dot(s, O::row(&first[(t * 32 + l32) * S::RS], hh), kf);
+      O::dot(dp, O::row(&second[(t * 32 + l32) * S::RS], hh), vf);
+      if (__builtin_amdgcn_readfirstlane(far_s[t]) == 0) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const floatx4 l4 = *reinterpret_cast<const floatx4*>(&lse2_s[t * 32 + 8 * g + 4 * hh]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + e], a.s.c, -l4[e]));
+        }
+      } else {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const floatx4 l4 = *reinterpret_cast<const floatx4*>(&lse_s[t * 32 + 8 * g + 4 * hh]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + e], a.s.scale, -l4[e]) * kLog2e);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dp[e] *= s[e];
+      O::outer(dva, second, t, s, lane);
+      O::outer(dka, first, t, dp, lane);
+    }
+  if (parts > 1) {
+    __syncthreads();
+    float* const sums = reinterpret_cast<float*>(cross_smem) + lane;
+    if (key_live && part > 0) {
+      float* mine = sums + ((part - 1) * share + kb) * S::N * kWave;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          mine[(d * 16 + e) * kWave] = dka[d][e];
+          mine[((DB + d) * 16 + e) * kWave] = dva[d][e];
+        }
+    }
+    __syncthreads();
+    if (key_live && part == 0)
+      for (int p = 0; p < parts - 1; ++p) {
+        const float* other = sums + (p * share + kb) * S::N * kWave;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            dka[d][e] += other[(d * 16 + e) * kWave];
+            dva[d][e] += other[((DB + d) * 16 + e) * kWave];
+          }
+      }
+  }
+  if (key_live && part == 0) {
+    const int ki = kb * 32 + l32;
+    if (ki >= nk) {                                             // places without a key: no gradient
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dka[d][e] = dva[d][e] = 0.f;
+    }
+    const long row = u.k0 + min(ki, u.held - 1);
+    O::store(dka, a.s.scale, a.dk + row * a.dks + u.hk * DH, ki < u.held, hh);
+    O::store(dva, 1.0f, a.dv + row * a.dvs + u.hk * DH, ki < u.held, hh);
+  }
+  for (int r = key_tiles * 32 + tid / CPR; r < u.held; r += RPP) {
+    const int c = u.hk * DH + tid % CPR * 8;
+    *reinterpret_cast<bf16x8*>(a.dk + (u.k0 + r) * a.dks + c) = zero_bf16x8();
+    *reinterpret_cast<bf16x8*>(a.dv + (u.k0 + r) * a.dvs + c) = zero_bf16x8();
+  }
+}
+
 // ------------------------------------------------------------------------------- host
 static CrossPlan dq_plan(int B, int max_q, int max_k, int H, int Hk, int dtype) { return cross_plan((long)B * Hk, (long)max_q * (H / Hk), max_k, dtype); }
 static CrossPlan dkdv_plan(int B, int max_q, int max_k, int H, int Hk, int dtype) { return cross_plan((long)B * Hk, max_k, (long)max_q * (H / Hk), dtype); }
@@ -359,6 +581,19 @@ static int launch_bwd(const char* fn, const CrossBwd<T>& a, hipStream_t st) {
   return check_launch(fn);
 }
 
+// A unit's rows and keys fit one workgroup
+static bool cross_short(int max_q, int max_k, int G, int dtype) { return dtype == SPA_BF16 && (long)max_q * G <= kShortRows && max_k <= kShortKeys; }
+
+template <int DH>
+static int launch_short(const char* fn, const CrossBwd<__bf16>& a, hipStream_t st) {
+  const size_t lds = CrossShort<DH>::bytes(a.s.most_q * (int)a.s.G.d, a.s.most_k);
+  const auto kernel = cross_bwd_short_kernel<DH>;
+  const hipError_t attr = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)CrossShort<DH>::bytes(kShortRows, kShortKeys));
+  SPA_REQUIRE(attr == hipSuccess, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, lds);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)cross_grid(a.s)), dim3(kCrossThreads), lds, st, a);
+  return check_launch(fn);
+}
+
 struct CrossGrads {
   const void *out, *dout;
   const float* lse;
@@ -368,6 +603,12 @@ struct CrossGrads {
 
 template <typename T>
 static int run_bwd(const char* fn, const CrossCall& c, const CrossGrads& g, void* ws, hipStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (cross_short(c.max_q, c.max_k, c.H / c.Hk, c.dtype)) {
+      const CrossBwd<T> a = {(const T*)c.q, (const T*)c.k, (const T*)c.v, (const T*)g.out, (const T*)g.dout, (long)c.qs, (long)c.ks, (long)c.vs,
+                             cross_shape(c, {1, 1, 1}), g.lse, nullptr, (T*)g.dq, (T*)g.dk, (T*)g.dv, (long)g.dqs, (long)g.dks, (long)g.dvs, nullptr, 0};
+      return c.Dh == 32 ? launch_short<32>(fn, a, st) : launch_short<64>(fn, a, st);
+    }
   const CrossPlan plans[2] = {dq_plan(c.B, c.max_q, c.max_k, c.H, c.Hk, c.dtype), dkdv_plan(c.B, c.max_q, c.max_k, c.H, c.Hk, c.dtype)};
   float* D = (float*)ws;
   float* part = (float*)((char*)ws + cross_up((size_t)c.H * c.B * c.max_q * sizeof(float)));
