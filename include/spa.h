@@ -361,6 +361,7 @@ int spa_cross_attention(const void* q, const void* k, const void* v, int64_t q_r
 
 /*
  * Backward of spa_cross_attention.  With P = exp(S - lse), dP = dout V^T, D_i = <dout_i, out_i>, dS = P (dP - D):
+ *   (D_i of units with few rows and keys: sum_j P_ij dP_ij, the same without the rounding of out)
  *   dq = softmax_scale dS K,   dk = softmax_scale dS^T Q,   dv = P^T dout      (dk, dv: summed over the query heads that share the key head)
  * in:  as there; out, dout [rows of q, H*Dh] dtype, contiguous; lse as written by the forward; workspace of at least
  *      spa_cross_attention_bwd_workspace_bytes bytes, 256-byte aligned.

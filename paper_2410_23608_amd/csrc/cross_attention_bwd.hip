@@ -340,14 +340,14 @@ __global__ void __launch_bounds__(kCrossThreads) cross_sum_kernel(const CrossBwd
   else *reinterpret_cast<floatx4*>(to) = sum;
 }
 
-// Few rows and keys in a unit (bf16): all of it in one workgroup, whose rows, keys and gradients are fetched once and whose scores are formed twice, in both
-// orders, out of LDS.  First the waves take 32 rows each (then the second half of the rows): K and V in LDS, Q and dO in registers, which then go to LDS in
-// their place.  Then they take 32 keys each, two or four waves to a block of keys where there are fewer blocks, whose sums the first adds in order.
+// Few rows and keys in a unit (bf16): all of it in one workgroup, whose rows, keys and gradients are fetched once and whose scores are formed again instead
+// of exchanged.  First the waves take 32 rows each (then the second half of the rows): K and V in LDS, Q and dO in registers, which then go to LDS in their
+// place, 128 rows at a time.  With those the waves take 32 keys each, two or four waves to a block of keys where there are fewer blocks, whose sums the first adds in order.
 constexpr int kShortRows = 256, kShortKeys = 128;
 template <int DH>
 struct CrossShort {
-  static constexpr int RS = Ops<__bf16, DH>::RS, N = 2 * (DH / 32) * 16;                       // N: sums of a lane
-  static __host__ __device__ constexpr int tiles(int rows) { return (rows + 31) / 32; }
+  static constexpr int RS = Ops<__bf16, DH>::RS, N = (DH / 32) * 16;                           // N: sums of a lane of one gradient
+  static __host__ __device__ constexpr int tiles(int rows) { return rows >= 128 ? 4 : (rows + 31) / 32; }
   static constexpr size_t bytes(int rows, int keys) {
     const size_t held = (size_t)2 * 32 * std::max(tiles(rows), tiles(keys)) * RS * sizeof(__bf16);
     const int others = tiles(rows) == 1 ? 0 : tiles(rows) <= 3 ? 2 : 3;          // waves that hand over their sums: of two blocks of keys one each, of one up to three
@@ -357,11 +357,11 @@ struct CrossShort {
 };
 
 template <int DH>
-__global__ void __launch_bounds__(kCrossThreads) __attribute__((amdgpu_waves_per_eu(2))) cross_bwd_short_kernel(const CrossBwd<__bf16> a) {
+__global__ void __launch_bounds__(kCrossThreads) __attribute__((amdgpu_waves_per_eu(3))) cross_bwd_short_kernel(const CrossBwd<__bf16> a) {
   using T = __bf16;
   using O = Ops<T, DH>;
   using S = CrossShort<DH>;
-  constexpr int DB = DH / 32, KK = DH / 16, CPR = DH / 8, RPP = kCrossThreads / CPR, CPT = kShortKeys / RPP, TILES = kShortRows / 128, KEY_TILES = kShortKeys / 32;
+  constexpr int DB = DH / 32, KK = DH / 16, CPR = DH / 8, RPP = kCrossThreads / CPR, CPT = kShortKeys / RPP;
   extern __shared__ __attribute__((aligned(16))) unsigned char cross_smem[];
   __shared__ __attribute__((aligned(16))) float lse_s[kShortRows], lse2_s[kShortRows], negD_s[kShortRows];
   __shared__ int far_s[kShortRows / 32];
@@ -383,16 +383,21 @@ __global__ void __launch_bounds__(kCrossThreads) __attribute__((amdgpu_waves_per
       kv[1][t] = *reinterpret_cast<const uintx4*>(a.v + row * a.vs + c);
     }
   }
-  typename O::Row qf[TILES], gf[TILES];
-  float lse[TILES];
-#pragma unroll
-  for (int i = 0; i < TILES; ++i) {
-    if (wave + 4 * i >= row_tiles) continue;
-    const int rc = min((wave + 4 * i) * 32 + l32, nq - 1);
+  typename O::Row qf, gf;
+  float lse = 0.f;
+  auto load_rows = [&](int tile) {
+    const int rc = min(tile * 32 + l32, nq - 1);
     const uint32_t token = quotient((uint32_t)rc, a.s.G);
-    qf[i] = O::row(a.q + u.q0 * a.qs + head + group_row<DH>(a.s.G, rc, a.qs), hh);
-    gf[i] = O::row(a.dout + u.q0 * C + head + group_row<DH>(a.s.G, rc, C), hh);
-    lse[i] = a.lse[(u.hk * G + (rc - (int)(token * G))) * a.s.stat_stride + u.q0 + token];
+    qf = O::row(a.q + u.q0 * a.qs + head + group_row<DH>(a.s.G, rc, a.qs), hh);
+    gf = O::row(a.dout + u.q0 * C + head + group_row<DH>(a.s.G, rc, C), hh);
+    lse = a.lse[(u.hk * G + (rc - (int)(token * G))) * a.s.stat_stride + u.q0 + token];
+  };
+  if (wave < row_tiles) load_rows(wave);
+  // (places behind the last block of keys: no gradient; while the loads are under way)
+  for (int r = key_tiles * 32 + tid / CPR; r < u.held; r += RPP) {
+    const int c = u.hk * DH + tid % CPR * 8;
+    *reinterpret_cast<bf16x8*>(a.dk + (u.k0 + r) * a.dks + c) = zero_bf16x8();
+    *reinterpret_cast<bf16x8*>(a.dv + (u.k0 + r) * a.dvs + c) = zero_bf16x8();
   }
   if (nk > 0) {
 #pragma unroll
@@ -406,27 +411,25 @@ __global__ void __launch_bounds__(kCrossThreads) __attribute__((amdgpu_waves_per
   }
   __syncthreads();
   // ---- as rows
-#pragma unroll
-  for (int i = 0; i < TILES; ++i) {
-    if (wave + 4 * i >= row_tiles) continue;
-    const int r = (wave + 4 * i) * 32 + l32;
-    const bool ok = r < nq, none = lse[i] == -INFINITY || !ok, far = __ballot(!none && fabsf(lse[i]) >= kFarScore) != 0;
-    const float ref = none ? INFINITY : lse[i], lse2 = ref * kLog2e;
+  for (int tile = wave; tile < row_tiles; tile += 4) {
+    if (tile != wave) load_rows(tile);
+    const int r = tile * 32 + l32;
+    const bool ok = r < nq, none = lse == -INFINITY || !ok, far = __ballot(!none && fabsf(lse) >= kFarScore) != 0;
+    const float ref = none ? INFINITY : lse, lse2 = ref * kLog2e;
     floatx16 acc[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
-    floatx16 P[KEY_TILES], dp[KEY_TILES];
-    float D = 0.f;
+    // (P of a block of keys, and dP - D on top of what dP starts from)
+    auto scores = [&](int kb, float start, floatx16& s, floatx16& dp) {
 #pragma unroll
-    for (int kb = 0; kb < KEY_TILES; ++kb) {
-      if (kb >= key_tiles) break;
-      floatx16& s = P[kb];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = dp[kb][e] = 0.f;
-      O::dot(s, O::row(&first[(kb * 32 + l32) * S::RS], hh), qf[i]);
-      O::dot(dp[kb], O::row(&second[(kb * 32 + l32) * S::RS], hh), gf[i]);
+      for (int e = 0; e < 16; ++e) {
+        s[e] = 0.f;
+        dp[e] = start;
+      }
+      O::dot(s, O::row(&first[(kb * 32 + l32) * S::RS], hh), qf);
+      O::dot(dp, O::row(&second[(kb * 32 + l32) * S::RS], hh), gf);
       if (kb * 32 + 32 > nk) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -439,16 +442,20 @@ __global__ void __launch_bounds__(kCrossThreads) __attribute__((amdgpu_waves_per
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.s.scale, -ref) * kLog2e);
       }
+    };
+    floatx16 s, dp;
+    float D = 0.f;
+    for (int kb = 0; kb < key_tiles; ++kb) {
+      scores(kb, 0.f, s, dp);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) D = fmaf(s[e], dp[kb][e], D);
+      for (int e = 0; e < 16; ++e) D = fmaf(s[e], dp[e], D);
     }
     D = sum_across_halves(D);
+    for (int kb = 0; kb < key_tiles; ++kb) {
+      scores(kb, -D, s, dp);
 #pragma unroll
-    for (int kb = 0; kb < KEY_TILES; ++kb) {
-      if (kb >= key_tiles) break;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) dp[kb][e] = P[kb][e] * (dp[kb][e] - D);
-      O::outer(acc, first, kb, dp[kb], lane);
+      for (int e = 0; e < 16; ++e) dp[e] *= s[e];
+      O::outer(acc, first, kb, dp, lane);
     }
     O::store(acc, a.s.scale, a.dq + u.q0 * a.dqs + head + group_row<DH>(a.s.G, min(r, nq - 1), a.dqs), ok, hh);
     if (hh == 0) {
@@ -456,7 +463,7 @@ __global__ void __launch_bounds__(kCrossThreads) __attribute__((amdgpu_waves_per
       lse2_s[r] = lse2;
       negD_s[r] = -D;
     }
-    if (lane == 0) far_s[wave + 4 * i] = far;
+    if (lane == 0) far_s[tile] = far;
   }
   if (u.held <= 0) return;
   // ---- as keys: parts waves a block of keys
@@ -467,81 +474,87 @@ __global__ void __launch_bounds__(kCrossThreads) __attribute__((amdgpu_waves_per
     kf = O::row(&first[(kb * 32 + l32) * S::RS], hh);
     vf = O::row(&second[(kb * 32 + l32) * S::RS], hh);
   }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < TILES; ++i) {
-    if (wave + 4 * i >= row_tiles) continue;
-    const int r = (wave + 4 * i) * 32 + l32;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      *reinterpret_cast<bf16x8*>(&first[r * S::RS + kk * 16 + hh * 8]) = r < nq ? qf[i].f[kk] : zero_bf16x8();
-      *reinterpret_cast<bf16x8*>(&second[r * S::RS + kk * 16 + hh * 8]) = r < nq ? gf[i].f[kk] : zero_bf16x8();
-    }
-  }
-  __syncthreads();
   floatx16 dka[DB], dva[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dka[d][e] = dva[d][e] = 0.f;
-  if (key_live)
-    for (int t = part; t < row_tiles; t += parts) {
-      floatx16 s, dp;
+  // (a wave has the rows of one tile in registers: 168 do not hold two beside the rest)
+  if (row_tiles > 4) load_rows(wave);
+  auto keys_pass = [&](int i) {
+    __syncthreads();
+    if (wave + 4 * i < row_tiles) {
+      const int r = wave * 32 + l32;
+      const bool ok = i * 128 + r < nq;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = 0.f;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const floatx4 d4 = *reinterpret_cast<const floatx4*>(&negD_s[t * 32 + 8 * g + 4 * hh]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) dp[4 * g + e] = d4[e];
+      for (int kk = 0; kk < KK; ++kk) {
+        *reinterpret_cast<bf16x8*>(&first[r * S::RS + kk * 16 + hh * 8]) = ok ? qf.f[kk] : zero_bf16x8();
+        *reinterpret_cast<bf16x8*>(&second[r * S::RS + kk * 16 + hh * 8]) = ok ? gf.f[kk] : zero_bf16x8();
       }
-      O::dot(s, O::row(&first[(t * 32 + l32) * S::RS], hh), kf);
-      O::dot(dp, O::row(&second[(t * 32 + l32) * S::RS], hh), vf);
-      if (__builtin_amdgcn_readfirstlane(far_s[t]) == 0) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const floatx4 l4 = *reinterpret_cast<const floatx4*>(&lse2_s[t * 32 + 8 * g + 4 * hh]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + e], a.s.c, -l4[e]));
-        }
-      } else {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const floatx4 l4 = *reinterpret_cast<const floatx4*>(&lse_s[t * 32 + 8 * g + 4 * hh]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + e], a.s.scale, -l4[e]) * kLog2e);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) dp[e] *= s[e];
-      O::outer(dva, second, t, s, lane);
-      O::outer(dka, first, t, dp, lane);
     }
+    __syncthreads();
+    if (key_live)
+      for (int t = 4 * i + part; t < min(4 * i + 4, row_tiles); t += parts) {
+        floatx16 s, dp;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const floatx4 d4 = *reinterpret_cast<const floatx4*>(&negD_s[t * 32 + 8 * g + 4 * hh]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dp[4 * g + e] = d4[e];
+        }
+        O::dot(s, O::row(&first[((t & 3) * 32 + l32) * S::RS], hh), kf);
+        O::dot(dp, O::row(&second[((t & 3) * 32 + l32) * S::RS], hh), vf);
+        if (__builtin_amdgcn_readfirstlane(far_s[t]) == 0) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const floatx4 l4 = *reinterpret_cast<const floatx4*>(&lse2_s[t * 32 + 8 * g + 4 * hh]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + e], a.s.c, -l4[e]));
+          }
+        } else {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const floatx4 l4 = *reinterpret_cast<const floatx4*>(&lse_s[t * 32 + 8 * g + 4 * hh]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + e], a.s.scale, -l4[e]) * kLog2e);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dp[e] *= s[e];
+        O::outer(dva, second, t & 3, s, lane);
+        O::outer(dka, first, t & 3, dp, lane);
+      }
+  };
+  keys_pass(0);
+  if (row_tiles > 4) {
+    load_rows(wave + 4);
+    keys_pass(1);
+  }
   if (parts > 1) {
-    __syncthreads();
     float* const sums = reinterpret_cast<float*>(cross_smem) + lane;
-    if (key_live && part > 0) {
-      float* mine = sums + ((part - 1) * share + kb) * S::N * kWave;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          mine[(d * 16 + e) * kWave] = dka[d][e];
-          mine[((DB + d) * 16 + e) * kWave] = dva[d][e];
-        }
-    }
-    __syncthreads();
-    if (key_live && part == 0)
-      for (int p = 0; p < parts - 1; ++p) {
-        const float* other = sums + (p * share + kb) * S::N * kWave;
+    auto join = [&](floatx16 (&x)[DB]) {
+      __syncthreads();
+      if (key_live && part > 0) {
+        float* mine = sums + ((part - 1) * share + kb) * S::N * kWave;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            dka[d][e] += other[(d * 16 + e) * kWave];
-            dva[d][e] += other[((DB + d) * 16 + e) * kWave];
-          }
+          for (int e = 0; e < 16; ++e) mine[(d * 16 + e) * kWave] = x[d][e];
       }
+      __syncthreads();
+      if (key_live && part == 0)
+        for (int p = 0; p < parts - 1; ++p) {
+          const float* other = sums + (p * share + kb) * S::N * kWave;
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[d][e] += other[(d * 16 + e) * kWave];
+        }
+    };
+    join(dka);
+    join(dva);
   }
   if (key_live && part == 0) {
     const int ki = kb * 32 + l32;
@@ -554,11 +567,6 @@ __global__ void __launch_bounds__(kCrossThreads) __attribute__((amdgpu_waves_per
     const long row = u.k0 + min(ki, u.held - 1);
     O::store(dka, a.s.scale, a.dk + row * a.dks + u.hk * DH, ki < u.held, hh);
     O::store(dva, 1.0f, a.dv + row * a.dvs + u.hk * DH, ki < u.held, hh);
-  }
-  for (int r = key_tiles * 32 + tid / CPR; r < u.held; r += RPP) {
-    const int c = u.hk * DH + tid % CPR * 8;
-    *reinterpret_cast<bf16x8*>(a.dk + (u.k0 + r) * a.dks + c) = zero_bf16x8();
-    *reinterpret_cast<bf16x8*>(a.dv + (u.k0 + r) * a.dvs + c) = zero_bf16x8();
   }
 }
 
@@ -581,8 +589,14 @@ static int launch_bwd(const char* fn, const CrossBwd<T>& a, hipStream_t st) {
   return check_launch(fn);
 }
 
-// A unit's rows and keys fit one workgroup
-static bool cross_short(int max_q, int max_k, int G, int dtype) { return dtype == SPA_BF16 && (long)max_q * G <= kShortRows && max_k <= kShortKeys; }
+// A unit's rows and keys fit one workgroup, and there are units for every compute unit, or few products in each: else dq and dk / dv are sooner formed beside
+// each other by more workgroups.  us, one workgroup a unit | two launches, heads of 64: 6 units of 196 rows and 77 keys 16.8 | 14.7, 12 of 256 and 128 19.4 | 16.3,
+// 12 of 30 and 20 6.2 | 11.3, 96 of 256 and 128 19.6 | 18.3, 192 of 196 and 77 17.1 | 18.5, 384 21.1 | 24.5, 768 26.3 | 39.3, 768 of 60 and 77 14.4 | 23.9,
+// 1536 of 256 and 128 56.2 | 78.9.
+static bool cross_short(long units, int max_q, int max_k, int G, int dtype) {
+  const long rows = (long)max_q * G;
+  return dtype == SPA_BF16 && rows <= kShortRows && max_k <= kShortKeys && (units >= 256 || rows * max_k <= 8192);
+}
 
 template <int DH>
 static int launch_short(const char* fn, const CrossBwd<__bf16>& a, hipStream_t st) {
@@ -604,7 +618,7 @@ struct CrossGrads {
 template <typename T>
 static int run_bwd(const char* fn, const CrossCall& c, const CrossGrads& g, void* ws, hipStream_t st) {
   if constexpr (sizeof(T) == 2)
-    if (cross_short(c.max_q, c.max_k, c.H / c.Hk, c.dtype)) {
+    if (cross_short((long)c.B * c.Hk, c.max_q, c.max_k, c.H / c.Hk, c.dtype)) {
       const CrossBwd<T> a = {(const T*)c.q, (const T*)c.k, (const T*)c.v, (const T*)g.out, (const T*)g.dout, (long)c.qs, (long)c.ks, (long)c.vs,
                              cross_shape(c, {1, 1, 1}), g.lse, nullptr, (T*)g.dq, (T*)g.dk, (T*)g.dv, (long)g.dqs, (long)g.dks, (long)g.dvs, nullptr, 0};
       return c.Dh == 32 ? launch_short<32>(fn, a, st) : launch_short<64>(fn, a, st);

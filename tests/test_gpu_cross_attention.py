@@ -199,6 +199,23 @@ def test_many_segments(spa, dtype):
     c.check(c.run(spa))
 
 
+@pytest.mark.parametrize("Dh,H,Hk,top", [(64, 4, 4, 256), (32, 8, 4, 128), (64, 32, 4, 30), (32, 4, 4, 97)])
+@pytest.mark.parametrize("held", [None, 128, 77])
+def test_units_of_one_workgroup(spa, Dh, H, Hk, top, held):
+    """More units than compute units, of up to 256 rows and 128 keys: every number of blocks of rows beside every number of blocks of keys."""
+    g = torch.Generator().manual_seed(top)
+    pick = lambda most, n: [0, 1, most] + torch.randint(0, most + 1, (n - 3,), generator=g).tolist()
+    c = Case(pick(top, 66), pick(held or 128, 66)[::-1], H, Hk, Dh, held=held, seed=top)
+    assert c.B * Hk >= 256 and c.max_q * (H // Hk) <= 256 and c.max_k <= 128
+    c.check(c.run(spa))
+
+
+@pytest.mark.parametrize("size", [30.0, 3000.0])
+def test_large_scores_in_one_workgroup(spa, size):
+    c = Case([60, 33, 9], [90, 64, 5], 2, 1, 64, size=size)
+    c.check(c.run(spa))
+
+
 @BOTH
 @pytest.mark.parametrize("size", [8.0, 300.0, 1e4])
 def test_large_scores(spa, dtype, size):
@@ -296,7 +313,7 @@ def _same(a, b):
     return all(torch.equal(torch.nan_to_num(a[n].float()), torch.nan_to_num(b[n].float())) for n in a)
 
 
-@pytest.mark.parametrize("q_lens,k_lens", [([300, 200], [77, 50]), ([2, 2], [3000, 700])])
+@pytest.mark.parametrize("q_lens,k_lens", [([300, 200], [77, 50]), ([2, 2], [3000, 700]), ([60, 40], [50, 77])])
 def test_replayed_and_repeated(spa, q_lens, k_lens):
     """Captured, replayed with other inputs and eager work between: bit for bit the eager results, which are the same in every run."""
     c, other = Case(q_lens, k_lens, 4, 2, seed=1), Case(q_lens, k_lens, 4, 2, seed=2)
