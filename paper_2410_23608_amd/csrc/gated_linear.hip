@@ -261,7 +261,7 @@ __device__ __forceinline__ void gated_tiles(const GatedArgs& p, int act, unsigne
 
 __device__ __forceinline__ int gated_live_rows(const GatedArgs& p) { return p.total != nullptr ? min(p.total[0], p.m_cap) : p.m_cap; }
 
-constexpr size_t kGatedSmallLds = (size_t)2 * (128 + 128) * kGaK * sizeof(__bf16), kGatedRingLds = 2 * kGatedSmallLds;
+constexpr size_t kGatedSmallLds = (size_t)2 * (128 + 128) * kGaK * sizeof(__bf16), kGatedRingLds = 2 * kGatedSmallLds, kGatedTinyLds = kGatedRingLds / 2;
 constexpr size_t kGatedBigLds = (size_t)std::max({3 * 192 + 3 * 192, 3 * 256 + 2 * 192, 2 * 256 + 2 * 256}) * kGaK * sizeof(__bf16);
 
 // 128 x 128 tiles: four waves of 64 x 64, two workgroups a unit.
@@ -275,6 +275,11 @@ template <bool BACK>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) gated_ring_kernel(const GatedArgs p, int act) {
   extern __shared__ __attribute__((aligned(16))) unsigned char gated_smem[];
   gated_tiles<Mfma32, BACK, false, 128, 128, BACK ? 2 : 4, BACK ? 4 : 2, 4, 4>(p, act, gated_smem, blockIdx.x, gridDim.x, 0, gated_live_rows(p));
+}
+// 64 x 64 tiles (32 columns of h) of few rows, as gemm_rows_tiny_kernel.
+__global__ void __launch_bounds__(128) gated_tiny_kernel(const GatedArgs p, int act) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char gated_smem[];
+  gated_tiles<Mfma32, false, false, 64, 64, 2, 1, 4, 4>(p, act, gated_smem, blockIdx.x, gridDim.x, 0, gated_live_rows(p));
 }
 // The large shapes, one resident workgroup a unit that walks the tiles of the plan for the live rows (gemm_shape.h).
 template <bool BACK>
@@ -352,15 +357,16 @@ static int launch_gated(const char* fn, GatedArgs args, int act, hipStream_t st)
   const bool counted = args.total != nullptr;
   const int cfg = options().gemm_tm;
   const bool big = cfg != 0 ? cfg >= 6 : large_tiles(args.m_cap, counted, ncols, args.kc), ring = !big && ring_tiles(args.m_cap, counted, ncols);
+  const bool tiny = !BACK && !big && cfg == 0 && tiny_tiles(args.m_cap, counted, ncols);
   args.rule = large_rule(ncols, args.kc, false);
-  const size_t smem = big ? kGatedBigLds : ring ? kGatedRingLds : kGatedSmallLds;
-  const long tiles = gemm_tiles<long>(args.m_cap, ncols, big ? 192 : 128);          // (no less than with 256)
+  const size_t smem = big ? kGatedBigLds : tiny ? kGatedTinyLds : ring ? kGatedRingLds : kGatedSmallLds;
+  const long tiles = gemm_tiles<long>(args.m_cap, ncols, big ? 192 : tiny ? 64 : 128);          // (no less than with 256)
   SPA_REQUIRE(big || tiles + 8 < 4294967296L / 512, SPA_ERR_INVALID_ARG, "%s: too many tiles (a launch has fewer than 2^32 threads)", fn);
   const long tiles8 = (tiles + 7) / 8 * 8;
-  const auto kernel = big ? gated_big_kernel<BACK> : ring ? gated_ring_kernel<BACK> : gated_small_kernel<BACK>;
+  const auto kernel = big ? gated_big_kernel<BACK> : tiny ? gated_tiny_kernel : ring ? gated_ring_kernel<BACK> : gated_small_kernel<BACK>;
   const hipError_t attr = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   SPA_REQUIRE(attr == hipSuccess, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, smem);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(big ? std::min(tiles8, 256L) : tiles8)), dim3(big || ring ? 512 : 256), smem, st, args, act);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(big ? std::min(tiles8, 256L) : tiles8)), dim3(tiny ? 128 : big || ring ? 512 : 256), smem, st, args, act);
   return check_launch(fn);
 }
 

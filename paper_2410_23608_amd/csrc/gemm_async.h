@@ -152,7 +152,7 @@ __device__ __forceinline__ void gemm_async_loop(__bf16* lds, int nk, FA&& next_a
   // then a load after each.  With two buffers and one wave a SIMD, or two of workgroups that are not in step, the loads of a
   // step go first (dealt out: 2304 -> 768, 1568 rows, 26 -> 32 us).
   constexpr int P = TM * TN, R = TM + TN, RP = (2 * R + P - 1) / P, READS = (R + RP - 1) / RP;
-  constexpr bool kLoadsFirst = THREADS == 256;
+  constexpr bool kLoadsFirst = THREADS <= 256;
   constexpr int PER_GROUP = P - READS;
   static_assert(READS < P && (kLoadsFirst || LOADS <= KK * PER_GROUP), "every read and every load has its place");
   // one ring of A and B together, or one of A and one of B behind it

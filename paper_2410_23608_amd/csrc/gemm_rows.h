@@ -175,12 +175,12 @@ __device__ __forceinline__ void gemm_unmapped_rows(const GemmArgs& p, int M, uns
   zero_unselected_rows<4, 2>(p.out, p.ldo, p.ncols, p.inv_pos, min(r0, all), min(r1, all), lane, p.residual);
 }
 __device__ __forceinline__ int gemm_live_rows(const GemmArgs& p) { return p.total != nullptr ? min(p.total[0], p.m_cap) : p.m_cap; }
-// 128 x 128 tiles, a workgroup each.  The rows no packed row maps to: shared by the waves of the workgroups without a tile, or by all
+// Tiles of EDGE x EDGE, 128 or 64, a workgroup each.  The rows no packed row maps to: shared by the waves of the workgroups without a tile, or by all
 // when those are few.
-template <bool kScale, bool kDeep, int STEPS, int THREADS>
+template <bool kScale, bool kDeep, int STEPS, int THREADS, int EDGE = 128>
 __device__ __forceinline__ void gemm_rows_small(const GemmArgs& p, unsigned char* gemm_smem, unsigned block, unsigned blocks) {
   constexpr int NW = THREADS / 64;
-  const int live = gemm_rows_tiles<Mfma32, kScale, kDeep, false, 128, 128, 2, NW / 2, STEPS, STEPS>(p, gemm_smem, block, blocks, 0, gemm_live_rows(p));
+  const int live = gemm_rows_tiles<Mfma32, kScale, kDeep, false, EDGE, EDGE, 2, NW / 2, STEPS, STEPS>(p, gemm_smem, block, blocks, 0, gemm_live_rows(p));
   if (p.inv_pos == nullptr) return;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, idle = (int)blocks - live;
   const bool by_idle = 4 * idle >= live;
@@ -191,7 +191,7 @@ __device__ __forceinline__ void gemm_rows_small(const GemmArgs& p, unsigned char
   zero_unselected_rows(p.out, p.ldo, p.ncols, p.inv_pos, r0, r1, lane, p.residual);
 }
 
-constexpr size_t kGemmSmallLds = (size_t)2 * (128 + 128) * kGaK * sizeof(__bf16), kGemmRingLds = 2 * kGemmSmallLds;
+constexpr size_t kGemmSmallLds = (size_t)2 * (128 + 128) * kGaK * sizeof(__bf16), kGemmRingLds = 2 * kGemmSmallLds, kGemmTinyLds = kGemmRingLds / 2;
 // steps of A and of B in LDS: three of 192 + 192, three of 256 and two of 192, two of 256 + 256
 constexpr size_t kGemmBigLds = (size_t)std::max({3 * 192 + 3 * 192, 3 * 256 + 2 * 192, 2 * 256 + 2 * 256}) * kGaK * sizeof(__bf16);
 
@@ -218,6 +218,15 @@ template <bool kScale, bool kDeep>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) gemm_rows_eight_kernel(const GemmArgs p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char gemm_smem[];
   gemm_rows_small<kScale, kDeep, 2, 512>(p, gemm_smem, blockIdx.x, gridDim.x);
+}
+
+// 64 x 64 tiles of few rows: two waves of 32 x 64, four steps in LDS (tiny_tiles of gemm_shape.h).  A step takes .25 us instead of .37: more units share the
+// products and the bytes from the L2.  (Eight steps in LDS, or all of a step's fragments read at once, take as long.)  The same products in the same order as
+// the 128 x 128 tiles', whose bits are these.
+template <bool kScale>
+__global__ void __launch_bounds__(128) gemm_rows_tiny_kernel(const GemmArgs p) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char gemm_smem[];
+  gemm_rows_small<kScale, false, 4, 128, 64>(p, gemm_smem, blockIdx.x, gridDim.x);
 }
 
 // Tiles of 256 x 256 (eight waves of 128 x 64), 256 x 192 (eight of 64 x 96) or 192 x 192 (eight of 48 x 96); the fewer accumulators and

@@ -95,5 +95,9 @@ inline bool ring_tiles(int m_cap, bool counted, int ncols) {
 inline bool two_rings(int m_cap, bool counted, int ncols, int kc) {
   return kc <= 320 && ring_tiles(m_cap, counted, ncols) && gemm_tiles<long>(m_cap, ncols, 128) > 256;
 }
+// 64 x 64 tiles, one a unit (forward).  us, 64 | 128: 98 rows of 1024 -> 384 7.6 | 9.1, 392 of 2304 -> 768 (84 tiles) 13.7 | 16.3, 1568 of 192 -> 576
+// (225) 4.2 | 4.8, 1568 of 768 -> 768 (300) 9.3 | 9.0, 784 of 768 -> 2304 (468) 10.3 | 9.5, 3136 of 768 -> 768 (588) 14.6 | 9.7; the gated block, 196 rows of
+// 384 -> 2 x 1024 (128) 5.6 | 6.5, 392 (224) 5.9 | 6.8, 784 (416) 7.4 | 7.2, 784 of 768 -> 2 x 2048 18.8 | 11.8.
+inline bool tiny_tiles(int m_cap, bool counted, int ncols) { return gemm_tiles<long>(counted ? m_cap - m_cap / 4 : m_cap, ncols, 64) <= 256; }
 
 }  // namespace spa

@@ -72,10 +72,11 @@ linear_f32_kernel(const float* __restrict__ x, const int32_t* __restrict__ gathe
 template <bool kScale, bool kDeep>
 static int launch_gemm_rows_tile(const char* fn, GemmArgs args, bool big, hipStream_t st) {
   args.rule = large_rule(args.ncols, args.kc, args.residual != nullptr);
+  const bool tiny = !kDeep && !big && options().gemm_tm == 0 && tiny_tiles(args.m_cap, args.total != nullptr, args.ncols);
   const bool ring = !big && ring_tiles(args.m_cap, args.total != nullptr, args.ncols);
   const bool eight = !big && two_rings(args.m_cap, args.total != nullptr, args.ncols, args.kc);
-  const size_t smem = big ? kGemmBigLds : ring && !eight ? kGemmRingLds : kGemmSmallLds;
-  const long tiles = gemm_tiles<long>(args.m_cap, args.ncols, big ? 192 : 128);     // (no less than with 256)
+  const size_t smem = big ? kGemmBigLds : tiny ? kGemmTinyLds : ring && !eight ? kGemmRingLds : kGemmSmallLds;
+  const long tiles = gemm_tiles<long>(args.m_cap, args.ncols, big ? 192 : tiny ? 64 : 128);     // (no less than with 256)
   SPA_REQUIRE(tiles + 8 < 2147483647L / 2, SPA_ERR_INVALID_ARG, "%s: too many tiles", fn);
   const long tiles8 = (tiles + 7) / 8 * 8;
   const int cfg = options().gemm_tm;
@@ -84,12 +85,13 @@ static int launch_gemm_rows_tile(const char* fn, GemmArgs args, bool big, hipStr
                      : cfg == 10 ? gemm_rows_big_kernel<kScale, kDeep, Large::k256x192>
                                  : gemm_rows_big_kernel<kScale, kDeep, Large::kByRows>;
   const auto kernel = big     ? large
+                      : tiny  ? gemm_rows_tiny_kernel<kScale>
                       : eight ? gemm_rows_eight_kernel<kScale, kDeep>
                       : ring  ? gemm_rows_ring_kernel<kScale, kDeep>
                               : gemm_rows_small_kernel<kScale, kDeep>;
   const hipError_t attr = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   SPA_REQUIRE(attr == hipSuccess, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, smem);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(big ? std::min(tiles8, 256L) : tiles8)), dim3(big || ring ? 512 : 256), smem, st, args);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(big ? std::min(tiles8, 256L) : tiles8)), dim3(tiny ? 128 : big || ring ? 512 : 256), smem, st, args);
   return check_launch(fn);
 }
 

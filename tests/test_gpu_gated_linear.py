@@ -123,6 +123,32 @@ def test_tiles_by_option(spa, tiles, M, K, F):
         spa.spa_set_option("gemm_tm")
 
 
+@pytest.mark.parametrize("M,K,F,live", [(1, 64, 72, 1), (98, 384, 1024, 98), (196, 1024, 384, 101), (300, 72, 520, 300), (900, 200, 104, 640)])
+def test_small_tiles_keep_the_bits(spa, M, K, F, live):
+    """Few rows take small tiles: the block, and the projection of its result back onto the residual stream, with the bits of the 128 x 128 tiles."""
+    c = Case(M, K, F, live=live, index=True, tokens=M + 60)
+
+    def run():
+        res = c.run(spa)
+        inv = torch.full((M + 60,), -1, dtype=torch.int32, device="cuda")
+        inv[c.idx[:live].long()] = torch.arange(live, dtype=torch.int32, device="cuda")
+        y = torch.full((1, M + 60, K), float("nan"), dtype=torch.bfloat16, device="cuda")
+        spa.spa_linear_packed_unpack(res["h"], c.total, c.W_down, None, c.idx, inv, c.x.view(1, M + 60, K), y)
+        return dict(res, y=y)
+
+    got = run()
+    c.check({n: got[n] for n in ("h", "pre", "d_pre")})
+    spa.spa_set_option("gemm_tm", "2")
+    try:
+        want = run()
+    finally:
+        spa.spa_set_option("gemm_tm")
+    for n in got:
+        rows = slice(None) if n == "y" else slice(0, live)
+        assert torch.equal(got[n][rows], want[n][rows]), n
+    assert bool(torch.isfinite(got["y"].float()).all())
+
+
 @BOTH
 @pytest.mark.parametrize("M,live", [(700, 700), (700, 0), (700, 1), (700, 129), (9000, 4100)])
 def test_counted_and_gathered(spa, dtype, M, live):
