@@ -86,14 +86,17 @@ __global__ void __launch_bounds__(kCrossThreads, sizeof(T) == 2 && KW == 1 ? 4 :
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = __builtin_elementwise_maximum(mx, s[i]);
         const float m_new = __builtin_elementwise_maximum(m, max_across_halves(mx));
-        if (__ballot(m_new != m) != 0) {
-          const float f = m_new != m ? __builtin_amdgcn_exp2f((m - m_new) * a.s.c) : 1.f;
+        // (m, what the exponents are taken from, follows a row's maximum when that is 2^8 past it, or a NaN: of 32 rows one has a new maximum in nearly
+        // every block)
+        const bool past = !((m_new - m) * a.s.c <= 8.f);
+        if (__ballot(past) != 0) {
+          const float f = past && m_new != m ? __builtin_amdgcn_exp2f((m - m_new) * a.s.c) : 1.f;
           sum *= f;
 #pragma unroll
           for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] *= f;
-          m = m_new;
+          m = past ? m_new : m;
         }
         if (__ballot(fabsf(m) * a.s.scale >= kFarScore) == 0) {
           const float m2 = m * a.s.c;
