@@ -43,8 +43,8 @@ __device__ __forceinline__ void cross_lengths(const CrossShape& s, int b, int q0
   nk = s.key_lens != nullptr ? min(max(s.key_lens[b], 0), held) : held;
 }
 // Blocks and splits of a pair (segment, key head) next to each other on one XCD, whose L2 then holds what they share, pairs dealt to the XCDs there
-// and back.  Up to kRankedB segments come by their products, most first; ranking more costs every workgroup more than it gives (us, 8 segments of 1568 to
-// 3136 tokens and 410 to 1024 keys, in index order | ranked: see the table of the kernels).
+// and back.  Up to kRankedB segments come by their products, most first; ranking more costs every workgroup more than it gives (8 segments of 1568 to
+// 3136 tokens and 410 to 1024 keys, 12 and 4 heads of 64, dk / dv in index order 171 us, ranked 158).
 constexpr int kRankedB = 16;
 __device__ __forceinline__ CrossUnit cross_unit(const CrossShape& s) {
   const int per = s.blocks * s.splits, xcd = blockIdx.x & 7, j = blockIdx.x >> 3, pl = j / per, qb = j - pl * per;

@@ -8,6 +8,10 @@
 //
 // Both are row GEMMs on the loop of gemm_async.h in the shapes of gemm_rows.h, chosen by its rules (2 F and F columns).  Forward, the rows of Wg and Wu lie
 // in turns of one matrix tile in LDS, so that a wave has a column's gate and its factor in the same register of neighbouring accumulators.
+// Rounded to bf16 are h and pre (from the same unrounded sums) and d_pre, the operands of the products that follow and what the backward keeps; act and its slope
+// are formed from pre as kept.
+// 6272 rows of 768 -> 2 x 2048 -> 768: forward 57 us (690 TFLOP/s; with 128 x 128 tiles 68), 1.8 rounds of tiles and 77 MB on their way out; backward 45 (50), 20
+// GFLOP and 102 MB of pre and d_pre behind the loop, when all units store at once.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
