@@ -312,7 +312,8 @@ template <int ACT, bool BACK, int EDGE>
 __global__ void __launch_bounds__(kF32Threads) gated_f32_kernel(const GatedF32 p) {
   using PA = F32Place<EDGE, true>;
   using PB = F32Place<EDGE, !BACK>;
-  constexpr int TM = EDGE / 16, NB = BACK ? 1 : 2;
+  using Out = F32Quarter<EDGE>;
+  constexpr int NB = BACK ? 1 : 2;
   __shared__ F32Lds<EDGE, NB> l;
   const int M = p.total != nullptr ? min(p.total[0], p.m_cap) : p.m_cap, n_tiles = (p.F + EDGE - 1) / EDGE;
   const long tiles = (long)((M + EDGE - 1) / EDGE) * n_tiles;
@@ -326,24 +327,22 @@ __global__ void __launch_bounds__(kF32Threads) gated_f32_kernel(const GatedF32 p
     }
 #pragma unroll
     for (int i = 0; i < PB::kCount; ++i) wp[i] = p.w + (long)min(n0 + PB::line(i), p.F - 1) * (BACK ? 1 : p.kc);
-    float acc[NB][TM][TM] = {};
-    f32_tile_sums<EDGE, NB, true, !BACK>(l, p.kc, [&](int i, int k) { return ap[i][k]; },
+    typename Out::Acc acc[NB] = {};
+    f32_tile_sums<EDGE, NB, true, !BACK, 2>(l, p.kc, [&](int i, int k) { return ap[i][k]; },
                                          [&](int q, int i, int k) { return BACK ? wp[i][(long)k * p.F] : wp[i][(long)q * p.F * p.kc + k]; }, F32AsIs{}, F32AsIs{},
                                          acc, [](const auto&, int) {});
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
 #pragma unroll
-    for (int r = 0; r < TM; ++r)
-#pragma unroll
-      for (int c = 0; c < TM; ++c) {
-        const int m = m0 + (threadIdx.x >> 4) * TM + r, n = n0 + (threadIdx.x & 15) * TM + c;
+    for (int e = 0; e < Out::kCount; ++e) {
+        const int m = m0 + Out::row(e), n = n0 + Out::col();
         if (m >= M || n >= p.F) continue;
         const long at = (long)m * 2 * p.F + n;
         if constexpr (BACK) {
           const Act a = act_of<ACT, true>(p.pre[at]);
-          p.h[at] = acc[0][r][c] * p.pre[at + p.F] * a.slope;
-          p.h[at + p.F] = acc[0][r][c] * a.value;
+          p.h[at] = acc[0][e] * p.pre[at + p.F] * a.slope;
+          p.h[at + p.F] = acc[0][e] * a.value;
         } else {
-          const float g = acc[0][r][c] + (p.bias != nullptr ? p.bias[n] : 0.f), u = acc[NB - 1][r][c] + (p.bias != nullptr ? p.bias[p.F + n] : 0.f);
+          const float g = acc[0][e] + (p.bias != nullptr ? p.bias[n] : 0.f), u = acc[NB - 1][e] + (p.bias != nullptr ? p.bias[p.F + n] : 0.f);
           p.h[(long)m * p.F + n] = act_of<ACT, true>(g).value * u;
           if (p.pre != nullptr) {
             p.pre[at] = g;

@@ -37,7 +37,7 @@ linear_f32_kernel(const float* __restrict__ x, const int32_t* __restrict__ gathe
       if (inv_pos[r] < 0) out[at] = residual[at];
     }
   using Place = F32Place<EDGE, true>;
-  constexpr int TM = EDGE / 16;
+  using Out = F32Quarter<EDGE>;
   __shared__ F32Lds<EDGE, 1> l;
   const int M = total != nullptr ? min(total[0], m_cap) : m_cap, n_tiles = (n_out + EDGE - 1) / EDGE;
   const long tiles = (long)((M + EDGE - 1) / EDGE) * n_tiles;
@@ -53,19 +53,24 @@ linear_f32_kernel(const float* __restrict__ x, const int32_t* __restrict__ gathe
       xp[i] = x + src * K;
       wp[i] = W + (long)n * K;
     }
-    float acc[1][TM][TM] = {};
-    f32_tile_sums<EDGE, 1, true, true>(l, K, [&](int i, int k) { return xp[i][k]; }, [&](int, int i, int k) { return wp[i][k]; },
+    typename Out::Acc acc[1] = {};
+    f32_tile_sums<EDGE, 1, true, true, 2>(l, K, [&](int i, int k) { return xp[i][k]; }, [&](int, int i, int k) { return wp[i][k]; },
                                        [&](int i, float v) { return kScale ? sc[i] * v : v; }, F32AsIs{}, acc, [](const auto&, int) {});
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
+    const int n = n0 + Out::col();
+    const float b = bias != nullptr ? bias[min(n, n_out - 1)] : 0.f;
+    long off[Out::kCount];
+    float add[Out::kCount];          // (all on their way at once)
 #pragma unroll
-    for (int r = 0; r < TM; ++r)
+    for (int e = 0; e < Out::kCount; ++e) {
+      const int m = min(m0 + Out::row(e), M - 1);
+      off[e] = (long)(scatter_idx != nullptr ? scatter_idx[m] : m) * out_stride + min(n, n_out - 1);
+    }
 #pragma unroll
-      for (int c = 0; c < TM; ++c) {
-        const int m = m0 + (threadIdx.x >> 4) * TM + r, n = n0 + (threadIdx.x & 15) * TM + c;
-        if (m >= M || n >= n_out) continue;
-        const long off = (long)(scatter_idx != nullptr ? scatter_idx[m] : m) * out_stride + n;
-        out[off] = acc[0][r][c] + (bias != nullptr ? bias[n] : 0.f) + (residual != nullptr ? residual[off] : 0.f);
-      }
+    for (int e = 0; e < Out::kCount; ++e) add[e] = residual != nullptr ? residual[off[e]] : 0.f;
+#pragma unroll
+    for (int e = 0; e < Out::kCount; ++e)
+      if (m0 + Out::row(e) < M && n < n_out) out[off[e]] = acc[0][e] + b + add[e];
   }
 }
 

@@ -77,7 +77,7 @@ linear_bwd_input_f32_kernel(const float* __restrict__ dout, const int32_t* __res
     }
   using PA = F32Place<EDGE, true>;
   using PB = F32Place<EDGE, false>;
-  constexpr int TM = EDGE / 16;
+  using Out = F32Quarter<EDGE>;
   __shared__ F32Lds<EDGE, 1> l;
   const int M = total != nullptr ? min(total[0], m_cap) : m_cap, n_tiles = (ncols + EDGE - 1) / EDGE;
   const long tiles = (long)((M + EDGE - 1) / EDGE) * n_tiles;
@@ -89,17 +89,15 @@ linear_bwd_input_f32_kernel(const float* __restrict__ dout, const int32_t* __res
       const int m = min(m0 + PA::line(i), M - 1);
       gp[i] = dout + (dout_idx != nullptr ? (long)dout_idx[m] : (long)m) * ldd;
     }
-    float acc[1][TM][TM] = {};
-    f32_tile_sums<EDGE, 1, true, false>(l, kc, [&](int i, int k) { return gp[i][k]; }, [&](int, int, int k) { return wp[(long)k * ncols]; }, F32AsIs{},
+    typename Out::Acc acc[1] = {};
+    f32_tile_sums<EDGE, 1, true, false, 2>(l, kc, [&](int i, int k) { return gp[i][k]; }, [&](int, int, int k) { return wp[(long)k * ncols]; }, F32AsIs{},
                                         F32AsIs{}, acc, [](const auto&, int) {});
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
 #pragma unroll
-    for (int r = 0; r < TM; ++r)
-#pragma unroll
-      for (int c = 0; c < TM; ++c) {
-        const int m = m0 + (threadIdx.x >> 4) * TM + r, n = c0 + (threadIdx.x & 15) * TM + c;
-        if (m < M && n < ncols) dx[(dx_idx != nullptr ? (long)dx_idx[m] : (long)m) * ldx + n] = acc[0][r][c];
-      }
+    for (int e = 0; e < Out::kCount; ++e) {
+      const int m = m0 + Out::row(e), n = c0 + Out::col();
+      if (m < M && n < ncols) dx[(dx_idx != nullptr ? (long)dx_idx[m] : (long)m) * ldx + n] = acc[0][e];
+    }
   }
 }
 
@@ -585,12 +583,12 @@ __global__ void __launch_bounds__(256) linear_bwd_weight_reduce_group_kernel(con
 }
 
 template <int EDGE, bool kScale>
-__global__ void __launch_bounds__(kF32Threads)
+__global__ void __launch_bounds__(kF32Threads, 2)
 linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __restrict__ dout_idx, long ldd,
                              const float* __restrict__ x, const int32_t* __restrict__ x_idx,
                              const float* __restrict__ gate_scores, const int32_t* __restrict__ total, int m_cap, int K,
                              int n_out, float* __restrict__ dW, float* __restrict__ dbias) {
-  constexpr int TM = EDGE / 16;
+  using Out = F32Quarter<EDGE>;
   __shared__ F32Lds<EDGE, 1> l;
   const int M = total != nullptr ? min(total[0], m_cap) : m_cap, k_tiles = (K + EDGE - 1) / EDGE, n_tiles = (n_out + EDGE - 1) / EDGE;
   for (long tile = blockIdx.x; tile < (long)n_tiles * k_tiles; tile += gridDim.x) {
@@ -599,9 +597,10 @@ linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __re
     const float *gp = dout + min(n0 + line, n_out - 1), *xp = x + min(k0 + line, K - 1);
     const bool sums = dbias != nullptr && k0 == 0 && threadIdx.x < EDGE;      // (the bias' gradient: the same rows of dout, added in order)
     using Place = F32Place<EDGE, false>;
-    float acc[1][TM][TM] = {}, bias = 0.f, gate[Place::kCount];
+    typename Out::Acc acc[1] = {};
+    float bias = 0.f, gate[Place::kCount];
     int gr[Place::kCount], xr[Place::kCount];              // rows of the step to come
-    f32_tile_sums<EDGE, 1, false, false>(
+    f32_tile_sums<EDGE, 1, false, false, kScale ? 1 : 2>(
         l, M, [&](int i, int) { return gp[(long)gr[i] * ldd]; },
         [&](int, int i, int) {
           if (kScale) gate[i] = gate_scores[xr[i]];
@@ -631,12 +630,10 @@ linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __re
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
     if (sums && n0 + (int)threadIdx.x < n_out) dbias[n0 + threadIdx.x] = bias;
 #pragma unroll
-    for (int r = 0; r < TM; ++r)
-#pragma unroll
-      for (int c = 0; c < TM; ++c) {
-        const int n = n0 + (threadIdx.x >> 4) * TM + r, k = k0 + (threadIdx.x & 15) * TM + c;
-        if (n < n_out && k < K) dW[(long)n * K + k] = acc[0][r][c];
-      }
+    for (int e = 0; e < Out::kCount; ++e) {
+      const int n = n0 + Out::row(e), k = k0 + Out::col();
+      if (n < n_out && k < K) dW[(long)n * K + k] = acc[0][e];
+    }
   }
 }
 

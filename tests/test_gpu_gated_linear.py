@@ -169,6 +169,23 @@ def test_odd_sizes_in_fp32(spa):
     c.check(c.run(spa))
 
 
+@pytest.mark.parametrize("K,F", [(7, 1030), (130, 1024), (64, 1000)])
+def test_an_fp32_element_has_its_bits_in_any_tile(spa, K, F):
+    """Every element is one chain over the contraction: the same alone, in a small tile and in a large one, whatever the tail of the contraction; and -0 stays -0."""
+    c = Case(900, K, F, 0, "f32", bias=False)
+    c.x[3] = -0.0
+    c.W[:, :] = c.W.abs()
+    big = c.run(spa)
+    for rows in (1, 40):
+        few = Case(rows, K, F, 0, "f32", bias=False)
+        few.x, few.dy, few.W, few.W_down = c.x[3:3 + rows].contiguous(), c.dy[3:3 + rows].contiguous(), c.W, c.W_down
+        got = few.run(spa)
+        for n in got:
+            assert torch.equal(got[n].view(torch.int32), big[n][3:3 + rows].view(torch.int32)), n
+    dx = lambda d, M: spa.spa_linear_packed_bwd_input(d, None, None, c.W, M, None, None, (o := torch.empty(M, K, device="cuda"))) or o
+    assert torch.equal(dx(big["d_pre"], 900)[3:43].view(torch.int32), dx(big["d_pre"][3:43].contiguous(), 40).view(torch.int32))
+
+
 @BOTH
 @ACTS
 @pytest.mark.parametrize("size", [0.01, 8.0, 100.0])
