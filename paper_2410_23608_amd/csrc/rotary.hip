@@ -407,6 +407,8 @@ static int rotary_checks(const char* fn, const RotaryCall& c) {
   }
   if (int rc = rotary_rows_ok(fn, "q", c.q, c.q_stride, c.H, c.Dh, c.dtype)) return rc;
   if (int rc = rotary_rows_ok(fn, "q's result", c.q_out, c.qo_stride, c.H, c.Dh, c.dtype)) return rc;
+  SPA_REQUIRE((c.q != c.q_out || c.q_stride == c.qo_stride) && (c.Hk == 0 || c.k != c.k_out || c.k_stride == c.ko_stride), SPA_ERR_INVALID_ARG,
+              "%s: in place the row strides must be the same", fn);
   if (c.Hk > 0) {
     if (int rc = rotary_rows_ok(fn, "k", c.k, c.k_stride, c.Hk, c.Dh, c.dtype)) return rc;
     if (int rc = rotary_rows_ok(fn, "k's result", c.k_out, c.ko_stride, c.Hk, c.Dh, c.dtype)) return rc;
@@ -522,6 +524,8 @@ extern "C" int spa_qk_norm_rotary_bwd(const void* dq_out, const void* dk_out, in
   if (int rc = rotary_rows_ok(fn, "dq_out", dq_out, dq_out_row_stride, H, Dh, dtype)) return rc;
   if (Hk > 0)
     if (int rc = rotary_rows_ok(fn, "dk_out", dk_out, dk_out_row_stride, Hk, Dh, dtype)) return rc;
+  SPA_REQUIRE((dq != dq_out || dq_row_stride == dq_out_row_stride) && (Hk == 0 || dk != dk_out || dk_row_stride == dk_out_row_stride), SPA_ERR_INVALID_ARG,
+              "%s: in place the row strides must be the same", fn);
   SPA_REQUIRE(kind != SPA_NORM_NONE || (!dgamma_q && !dbeta_q && !dgamma_k && !dbeta_k), SPA_ERR_INVALID_ARG,
               "%s: gradients of gamma and beta belong to a norm", fn);
   SPA_REQUIRE(Hk > 0 || (!dgamma_k && !dbeta_k), SPA_ERR_INVALID_ARG, "%s: without k there is no gradient of its gamma and beta", fn);

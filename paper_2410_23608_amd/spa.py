@@ -1276,8 +1276,9 @@ def _cross_checks(fn, q, k, v, cu_seqlens_q, cu_seqlens_k, key_lens, B, max_q, H
     code = _features(fn, **{name: t for name, (t, _) in rows.items()})
     _typed(fn, torch.int32, cu_seqlens_q=cu_seqlens_q, cu_seqlens_k=cu_seqlens_k, key_lens=key_lens)
     _typed(fn, torch.float32, lse=lse)
+    least = dict(v=k, dk=k, dv=k, out=q, dout=q, dq=q)
     for name, (t, heads) in rows.items():
-        _rows(fn, heads * Dh, **{name: (t, 1)})
+        _rows(fn, heads * Dh, **{name: (t, least[name].shape[0] if name in least else 1)})
     _holds(fn, cu_seqlens_q=(cu_seqlens_q, B + 1), cu_seqlens_k=(cu_seqlens_k, B + 1), key_lens=(key_lens, B), lse=(lse, H * B * max_q))
     _contig(out, lse, cu_seqlens_q, cu_seqlens_k, key_lens)
     return code

@@ -71,11 +71,11 @@ def test_the_binding_compares_types_and_sizes():
     call = lambda **k: spa.spa_cross_attention(**{**ok, **k})
     for over, match in ((dict(k=t((30, 64), f32)), "share one dtype"), (dict(q=t((9, 64))), "q must be"), (dict(v=t((30, 128))), "v must be"),
                         (dict(cu_seqlens_k=t(2, i32)), "cu_seqlens_k holds"), (dict(key_lens=t(1, i32)), "key_lens holds"), (dict(key_lens=t(2)), "key_lens must be"),
-                        (dict(lse=t((4, 15), f32)), "lse holds"), (dict(out=t((9, 256))[:, :128]), "contiguous"), (dict(), "device tensors")):
+                        (dict(lse=t((4, 15), f32)), "lse holds"), (dict(out=t((9, 256))[:, :128]), "contiguous"), (dict(out=t((8, 128))), "out must be"), (dict(v=t((29, 64))), "v must be"), (dict(), "device tensors")):
         with pytest.raises(ValueError, match=match):
             call(**over)
     more = dict(dout=t((9, 128)), dq=t((9, 128)), dk=t((30, 64)), dv=t((30, 64)))
     back = lambda **k: spa.spa_cross_attention_bwd(**{**ok, **more, **k})
-    for over, match in ((dict(dk=t((30, 128))), "dk must be"), (dict(dq=t((9, 128), f32)), "share one dtype"), (dict(), "device tensors")):
+    for over, match in ((dict(dk=t((30, 128))), "dk must be"), (dict(dv=t((29, 64))), "dv must be"), (dict(dq=t((8, 128))), "dq must be"), (dict(dout=t((8, 128))), "dout must be"), (dict(dq=t((9, 128), f32)), "share one dtype"), (dict(), "device tensors")):
         with pytest.raises(ValueError, match=match):
             back(**over)

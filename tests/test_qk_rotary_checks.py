@@ -56,6 +56,8 @@ def test_particular_refusals():
     assert fwd(qo=None) == -1 and fwd(ko=None) == -1 and bwd(dqo=None) == -1 and bwd(dko=None) == -1 and bwd(dq=None) == -1
     assert bwd(bytes=NEED - 1) == -3 and bwd(ws=None) == -3
     assert bwd(kind=2, gq=None, gk=None) == -1 and "belong" in msg()
+    assert fwd(qs=256) == -1 and "in place" in msg() and fwd(ks=128) == -1 and "in place" in msg()
+    assert bwd(qs=256) == -1 and "in place" in msg() and bwd(dkos=128) == -1 and "in place" in msg() and bwd(dqos=256) == -1 and "in place" in msg()
     assert bwd(Hk=0, bytes=NEED) == -1 and "without k" in msg()
     size = lib.spa_qk_norm_rotary_bwd_workspace_bytes
     assert size(0, 4, 2, 32, 1) == size(8, 0, 2, 32, 1) == size(8, 4, -1, 32, 1) == size(8, 4, 2, 48, 1) == size(8, 4, 2, 32, 3) == 0
