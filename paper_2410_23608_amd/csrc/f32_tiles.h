@@ -6,6 +6,7 @@
 
 #include <type_traits>
 
+#include "f32_shape.h"
 #include "spa_common.h"
 
 namespace spa {
@@ -59,15 +60,15 @@ __device__ __forceinline__ void f32_tile_sums(F32Lds<EDGE, NB>& l, int kc, FA&& 
   using PB = F32Place<EDGE, B_LINES>;
   using W = F32Quarter<EDGE>;
   constexpr int STEP = kF32Step<EDGE>, G = 4, GROUPS = STEP / (G * W::KD);
-  const int steps = (kc + STEP - 1) / STEP, la = W::line_a(), lb = W::line_b(), lk = W::k();
+  const int steps = f32_steps(kc, STEP), la = W::line_a(), lb = W::line_b(), lk = W::k();
   float ra[DEPTH][PA::kCount], rb[DEPTH][NB][PB::kCount];
   auto load = [&](float (&a)[PA::kCount], float (&b)[NB][PB::kCount], int k0) {
 #pragma unroll
-    for (int i = 0; i < PA::kCount; ++i) a[i] = fetch_a(i, min(k0 + PA::k(i), kc - 1));
+    for (int i = 0; i < PA::kCount; ++i) a[i] = fetch_a(i, f32_at(k0, PA::k(i), kc));
 #pragma unroll
     for (int q = 0; q < NB; ++q)
 #pragma unroll
-      for (int i = 0; i < PB::kCount; ++i) b[q][i] = fetch_b(q, i, min(k0 + PB::k(i), kc - 1));
+      for (int i = 0; i < PB::kCount; ++i) b[q][i] = fetch_b(q, i, f32_at(k0, PB::k(i), kc));
   };
   if (steps > 0) {
     ahead(0);
@@ -127,9 +128,5 @@ struct F32AsIs {
   __device__ __forceinline__ float operator()(int, float v) const { return v; }
   __device__ __forceinline__ float operator()(int, int, float v) const { return v; }
 };
-// The larger tiles where there are enough of them for most units.  us, 32 | 64: 1000 x 2800 -> 1000 (256 tiles of 64) backward 109 | 87, 3000 x 5760 -> 320 (235) 193 | 160,
-// weights of 1600 x 400 (175) 182 | 190.
-inline bool f32_wide(long rows, long cols) { return ((rows + 63) / 64) * ((cols + 63) / 64) >= 192; }
-inline long f32_tiles(long rows, long cols, int edge) { return ((rows + edge - 1) / edge) * ((cols + edge - 1) / edge); }
 
 }  // namespace spa

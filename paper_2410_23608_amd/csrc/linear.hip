@@ -39,15 +39,15 @@ linear_f32_kernel(const float* __restrict__ x, const int32_t* __restrict__ gathe
   using Place = F32Place<EDGE, true>;
   using Out = F32Quarter<EDGE>;
   __shared__ F32Lds<EDGE, 1> l;
-  const int M = total != nullptr ? min(total[0], m_cap) : m_cap, n_tiles = (n_out + EDGE - 1) / EDGE;
-  const long tiles = (long)((M + EDGE - 1) / EDGE) * n_tiles;
+  const int M = total != nullptr ? min(total[0], m_cap) : m_cap, n_tiles = f32_steps(n_out, EDGE);
+  const long tiles = (long)f32_steps(M, EDGE) * n_tiles;
   for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const int m0 = (int)(tile / n_tiles) * EDGE, n0 = (int)(tile % n_tiles) * EDGE;
     const float *xp[Place::kCount], *wp[Place::kCount];
     float sc[Place::kCount];
 #pragma unroll
     for (int i = 0; i < Place::kCount; ++i) {
-      const int m = min(m0 + Place::line(i), M - 1), n = min(n0 + Place::line(i), n_out - 1);
+      const int m = f32_at(m0, Place::line(i), M), n = f32_at(n0, Place::line(i), n_out);
       const long src = kGather ? (long)gather_idx[m] : (long)m;
       sc[i] = kScale ? sigmoidf_dev(gate_scores[src]) : 1.f;
       xp[i] = x + src * K;
@@ -57,20 +57,20 @@ linear_f32_kernel(const float* __restrict__ x, const int32_t* __restrict__ gathe
     f32_tile_sums<EDGE, 1, true, true, 2>(l, K, [&](int i, int k) { return xp[i][k]; }, [&](int, int i, int k) { return wp[i][k]; },
                                        [&](int i, float v) { return kScale ? sc[i] * v : v; }, F32AsIs{}, acc, [](const auto&, int) {});
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
-    const int n = n0 + Out::col();
-    const float b = bias != nullptr ? bias[min(n, n_out - 1)] : 0.f;
+    const int n = f32_at(n0, Out::col(), n_out);
+    const float b = bias != nullptr ? bias[n] : 0.f;
     long off[Out::kCount];
     float add[Out::kCount];          // (all on their way at once)
 #pragma unroll
     for (int e = 0; e < Out::kCount; ++e) {
-      const int m = min(m0 + Out::row(e), M - 1);
-      off[e] = (long)(scatter_idx != nullptr ? scatter_idx[m] : m) * out_stride + min(n, n_out - 1);
+      const int m = f32_at(m0, Out::row(e), M);
+      off[e] = (long)(scatter_idx != nullptr ? scatter_idx[m] : m) * out_stride + n;
     }
 #pragma unroll
     for (int e = 0; e < Out::kCount; ++e) add[e] = residual != nullptr ? residual[off[e]] : 0.f;
 #pragma unroll
     for (int e = 0; e < Out::kCount; ++e)
-      if (m0 + Out::row(e) < M && n < n_out) out[off[e]] = acc[0][e] + b + add[e];
+      if (f32_inside(m0, Out::row(e), M) && f32_inside(n0, Out::col(), n_out)) out[off[e]] = acc[0][e] + b + add[e];
   }
 }
 

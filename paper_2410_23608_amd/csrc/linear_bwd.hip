@@ -79,14 +79,14 @@ linear_bwd_input_f32_kernel(const float* __restrict__ dout, const int32_t* __res
   using PB = F32Place<EDGE, false>;
   using Out = F32Quarter<EDGE>;
   __shared__ F32Lds<EDGE, 1> l;
-  const int M = total != nullptr ? min(total[0], m_cap) : m_cap, n_tiles = (ncols + EDGE - 1) / EDGE;
-  const long tiles = (long)((M + EDGE - 1) / EDGE) * n_tiles;
+  const int M = total != nullptr ? min(total[0], m_cap) : m_cap, n_tiles = f32_steps(ncols, EDGE);
+  const long tiles = (long)f32_steps(M, EDGE) * n_tiles;
   for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const int m0 = (int)(tile / n_tiles) * EDGE, c0 = (int)(tile % n_tiles) * EDGE;
-    const float *gp[PA::kCount], *wp = W + min(c0 + PB::line(0), ncols - 1);
+    const float *gp[PA::kCount], *wp = W + f32_at(c0, PB::line(0), ncols);
 #pragma unroll
     for (int i = 0; i < PA::kCount; ++i) {
-      const int m = min(m0 + PA::line(i), M - 1);
+      const int m = f32_at(m0, PA::line(i), M);
       gp[i] = dout + (dout_idx != nullptr ? (long)dout_idx[m] : (long)m) * ldd;
     }
     typename Out::Acc acc[1] = {};
@@ -95,8 +95,9 @@ linear_bwd_input_f32_kernel(const float* __restrict__ dout, const int32_t* __res
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
 #pragma unroll
     for (int e = 0; e < Out::kCount; ++e) {
+      if (!f32_inside(m0, Out::row(e), M) || !f32_inside(c0, Out::col(), ncols)) continue;
       const int m = m0 + Out::row(e), n = c0 + Out::col();
-      if (m < M && n < ncols) dx[(dx_idx != nullptr ? (long)dx_idx[m] : (long)m) * ldx + n] = acc[0][e];
+      dx[(dx_idx != nullptr ? (long)dx_idx[m] : (long)m) * ldx + n] = acc[0][e];
     }
   }
 }
@@ -590,11 +591,11 @@ linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __re
                              int n_out, float* __restrict__ dW, float* __restrict__ dbias) {
   using Out = F32Quarter<EDGE>;
   __shared__ F32Lds<EDGE, 1> l;
-  const int M = total != nullptr ? min(total[0], m_cap) : m_cap, k_tiles = (K + EDGE - 1) / EDGE, n_tiles = (n_out + EDGE - 1) / EDGE;
+  const int M = total != nullptr ? min(total[0], m_cap) : m_cap, k_tiles = f32_steps(K, EDGE), n_tiles = f32_steps(n_out, EDGE);
   for (long tile = blockIdx.x; tile < (long)n_tiles * k_tiles; tile += gridDim.x) {
     const int n0 = (int)(tile / k_tiles) * EDGE, k0 = (int)(tile % k_tiles) * EDGE;
     const int line = F32Place<EDGE, false>::line(0);
-    const float *gp = dout + min(n0 + line, n_out - 1), *xp = x + min(k0 + line, K - 1);
+    const float *gp = dout + f32_at(n0, line, n_out), *xp = x + f32_at(k0, line, K);
     const bool sums = dbias != nullptr && k0 == 0 && threadIdx.x < EDGE;      // (the bias' gradient: the same rows of dout, added in order)
     using Place = F32Place<EDGE, false>;
     typename Out::Acc acc[1] = {};
@@ -622,17 +623,18 @@ linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __re
         [&](int m0) {
 #pragma unroll
           for (int i = 0; i < Place::kCount; ++i) {
-            const int m = min(m0 + Place::k(i), M - 1);
+            const int m = f32_at(m0, Place::k(i), M);
             gr[i] = dout_idx != nullptr ? dout_idx[m] : m;
             xr[i] = x_idx != nullptr ? x_idx[m] : m;
           }
         });
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
-    if (sums && n0 + (int)threadIdx.x < n_out) dbias[n0 + threadIdx.x] = bias;
+    if (sums && f32_inside(n0, threadIdx.x, n_out)) dbias[n0 + threadIdx.x] = bias;
 #pragma unroll
     for (int e = 0; e < Out::kCount; ++e) {
+      if (!f32_inside(n0, Out::row(e), n_out) || !f32_inside(k0, Out::col(), K)) continue;
       const int n = n0 + Out::row(e), k = k0 + Out::col();
-      if (n < n_out && k < K) dW[(long)n * K + k] = acc[0][e];
+      dW[(long)n * K + k] = acc[0][e];
     }
   }
 }
