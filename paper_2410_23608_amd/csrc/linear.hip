@@ -12,7 +12,7 @@
 // (gemm_shape.h; what bounds them: gemm_rows.h).  Measured, called again and again: 12544 rows of 768 -> 2304 47 to 49 us =
 // 905 to 940 TFLOP/s (operands staged through registers: 68 us); 6272 rows of 384 -> 384: 7 us (8.7); 98 rows: 5.8 us (8.1),
 // its steps bound by latency.  The output tile leaves through LDS as whole rows.
-// fp32 path (tiny workload): f32_tiles.h.
+// fp32 path (tiny workload): f32_tiles.h, or a thread an element where the contraction is short.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -23,6 +23,33 @@
 #include "spa_common.h"
 
 namespace spa {
+
+// A thread an element (f32_by_element)
+template <bool kGather, bool kScale>
+__global__ void __launch_bounds__(kF32Threads)
+linear_f32_element_kernel(const float* __restrict__ x, const int32_t* __restrict__ gather_idx,
+                          const float* __restrict__ gate_scores, const int32_t* __restrict__ total,
+                          const float* __restrict__ W, const float* __restrict__ bias, int m_cap, int K, int n_out,
+                          float* out, long out_stride, const int32_t* __restrict__ scatter_idx, const float* residual,
+                          const int32_t* __restrict__ inv_pos, long rows) {
+  const long first = (long)blockIdx.x * blockDim.x + threadIdx.x, stride = (long)gridDim.x * blockDim.x;
+  if (inv_pos != nullptr)          // the rows no packed row maps to keep the residual
+    for (long i = first; i < rows * n_out; i += stride) {
+      const long r = i / n_out, at = r * out_stride + (i - r * n_out);
+      if (inv_pos[r] < 0) out[at] = residual[at];
+    }
+  const int M = total != nullptr ? min(total[0], m_cap) : m_cap;
+  for (long i = first; i < (long)M * n_out; i += stride) {
+    const int m = (int)(i / n_out), n = (int)(i - (long)m * n_out);
+    const long src = kGather ? (long)gather_idx[m] : (long)m;
+    const float sc = kScale ? sigmoidf_dev(gate_scores[src]) : 1.f;
+    const float *xr = x + src * K, *wr = W + (long)n * K;
+    float a = 0.f;
+    for (int k = 0; k < K; ++k) a = fmaf(kScale ? sc * xr[k] : xr[k], wr[k], a);
+    const long off = (long)(scatter_idx != nullptr ? scatter_idx[m] : m) * out_stride + n;
+    out[off] = a + (bias != nullptr ? bias[n] : 0.f) + (residual != nullptr ? residual[off] : 0.f);
+  }
+}
 
 template <bool kGather, bool kScale, int EDGE>
 __global__ void __launch_bounds__(kF32Threads)
@@ -130,9 +157,13 @@ static int linear_common(const char* fn, const void* x, const int32_t* gather_id
   const bool g = gather_idx != nullptr, sc = gate_scores != nullptr;
   if (dtype == SPA_F32) {
     const bool wide = f32_wide(M_cap, N_out);
-    const long wgs = std::min(std::max(f32_tiles(M_cap, N_out, wide ? 64 : 32), inv_pos != nullptr ? ((long)rows * N_out + 1023) / 1024 : 0L), 8192L);
+    const bool by_element = f32_by_element(F32Side::kForward, M_cap, N_out, K);
+    const long most = std::max((long)M_cap, inv_pos != nullptr ? (long)rows : 0L);
+    const long wgs = std::min(by_element ? (most * N_out + kF32Threads - 1) / kF32Threads
+                                         : std::max(f32_tiles(M_cap, N_out, wide ? 64 : 32), inv_pos != nullptr ? ((long)rows * N_out + 1023) / 1024 : 0L), 8192L);
 #define SPA_LIN_F32(G_, S_)                                                                                   \
-  hipLaunchKernelGGL((wide ? linear_f32_kernel<G_, S_, 64> : linear_f32_kernel<G_, S_, 32>), dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)x, \
+  hipLaunchKernelGGL((by_element ? linear_f32_element_kernel<G_, S_> : wide ? linear_f32_kernel<G_, S_, 64> : linear_f32_kernel<G_, S_, 32>),                \
+                     dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)x,                          \
                      gather_idx, gate_scores, total, (const float*)W, (const float*)bias, M_cap, K, N_out,   \
                      (float*)out, (long)out_row_stride, scatter_idx, (const float*)residual, inv_pos, (long)rows)
     if (g && sc) SPA_LIN_F32(true, true); else if (g) SPA_LIN_F32(true, false); else SPA_LIN_F32(false, false);

@@ -18,7 +18,7 @@
 // The operands come through the pipelined loop of gemm_async.h (weight_gemm_kernel); rows that have to be
 // multiplied by the gate scale and rounded on the way cannot go straight to LDS and keep the kernel that
 // stages them through registers (linear_bwd_weight_bf16_kernel).
-// fp32 (tiny workload): f32_tiles.h.
+// fp32 (tiny workload): f32_tiles.h, or a thread an element where the contraction is short.
 #include <algorithm>
 #include <cmath>
 #include <cstdlib>
@@ -63,6 +63,28 @@ __device__ __forceinline__ bf16x8 frag_down_columns(const __bf16* tile, int k0, 
 }
 
 // ------------------------------------------------------------------------------ input side (fp32)
+// A thread an element (f32_by_element)
+__global__ void __launch_bounds__(kF32Threads)
+linear_bwd_input_f32_element_kernel(const float* __restrict__ dout, const int32_t* __restrict__ dout_idx, long ldd,
+                                    const int32_t* __restrict__ total, const float* __restrict__ W, int m_cap, int kc, int ncols,
+                                    float* __restrict__ dx, long ldx, const int32_t* __restrict__ dx_idx,
+                                    const int32_t* __restrict__ inv_pos, long rows) {
+  const long first = (long)blockIdx.x * blockDim.x + threadIdx.x, stride = (long)gridDim.x * blockDim.x;
+  if (inv_pos != nullptr)          // rows no packed row maps to
+    for (long i = first; i < rows * ncols; i += stride) {
+      const long r = i / ncols;
+      if (inv_pos[r] < 0) dx[r * ldx + (i - r * ncols)] = 0.f;
+    }
+  const int M = total != nullptr ? min(total[0], m_cap) : m_cap;
+  for (long i = first; i < (long)M * ncols; i += stride) {
+    const int m = (int)(i / ncols), c = (int)(i - (long)m * ncols);
+    const float* g = dout + (dout_idx != nullptr ? (long)dout_idx[m] : (long)m) * ldd;
+    float a = 0.f;
+    for (int n = 0; n < kc; ++n) a = fmaf(g[n], W[(long)n * ncols + c], a);
+    dx[(dx_idx != nullptr ? (long)dx_idx[m] : (long)m) * ldx + c] = a;
+  }
+}
+
 template <int EDGE>
 __global__ void __launch_bounds__(kF32Threads)
 linear_bwd_input_f32_kernel(const float* __restrict__ dout, const int32_t* __restrict__ dout_idx, long ldd,
@@ -583,6 +605,34 @@ __global__ void __launch_bounds__(256) linear_bwd_weight_reduce_group_kernel(con
   weight_reduce_block(m.a[mb.s], mb.block, mb.blocks);
 }
 
+// A thread an element (f32_by_element)
+template <bool kScale>
+__global__ void __launch_bounds__(kF32Threads)
+linear_bwd_weight_f32_element_kernel(const float* __restrict__ dout, const int32_t* __restrict__ dout_idx, long ldd,
+                                     const float* __restrict__ x, const int32_t* __restrict__ x_idx,
+                                     const float* __restrict__ gate_scores, const int32_t* __restrict__ total, int m_cap, int K,
+                                     int n_out, float* __restrict__ dW, float* __restrict__ dbias) {
+  const int M = total != nullptr ? min(total[0], m_cap) : m_cap;
+  const long nk = (long)n_out * K, work = nk + (dbias != nullptr ? n_out : 0);
+  for (long i = (long)blockIdx.x * blockDim.x + threadIdx.x; i < work; i += (long)gridDim.x * blockDim.x) {
+    const bool is_w = i < nk;
+    const int n = is_w ? (int)(i / K) : (int)(i - nk), k = is_w ? (int)(i - (long)n * K) : 0;
+    float a = 0.f;
+    for (int m = 0; m < M; ++m) {
+      const float g = dout[(dout_idx != nullptr ? (long)dout_idx[m] : (long)m) * ldd + n];
+      if (is_w) {
+        const long row = x_idx != nullptr ? (long)x_idx[m] : (long)m;
+        const float v = x[row * K + k];
+        a = fmaf(g, kScale ? sigmoidf_dev(gate_scores[row]) * v : v, a);
+      } else {
+        a += g;
+      }
+    }
+    if (is_w) dW[i] = a;
+    else dbias[n] = a;
+  }
+}
+
 template <int EDGE, bool kScale>
 __global__ void __launch_bounds__(kF32Threads, 2)
 linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __restrict__ dout_idx, long ldd,
@@ -794,9 +844,12 @@ extern "C" int spa_linear_packed_bwd_input(const void* dout, const int32_t* dout
   SPA_REQUIRE(!(group_open() && dtype == SPA_F32), SPA_ERR_UNSUPPORTED, "%s: fp32 calls cannot be part of a group", fn);
   if (dtype == SPA_F32) {
     const bool wide = f32_wide(M_cap, K);
-    const long wgs = std::min(std::max(f32_tiles(M_cap, K, wide ? 64 : 32), inv_pos != nullptr ? ((long)rows * K + 1023) / 1024 : 0L), 8192L);
-    hipLaunchKernelGGL((wide ? linear_bwd_input_f32_kernel<64> : linear_bwd_input_f32_kernel<32>), dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)dout, dout_idx,
-                       (long)dout_row_stride, total, (const float*)W, M_cap, N_out, K, (float*)dx, (long)dx_row_stride,
+    const bool by_element = f32_by_element(F32Side::kInput, M_cap, K, N_out);
+    const long most = std::max((long)M_cap, inv_pos != nullptr ? (long)rows : 0L);
+    const long wgs = std::min(by_element ? (most * K + kF32Threads - 1) / kF32Threads
+                                         : std::max(f32_tiles(M_cap, K, wide ? 64 : 32), inv_pos != nullptr ? ((long)rows * K + 1023) / 1024 : 0L), 8192L);
+    const auto kernel = by_element ? linear_bwd_input_f32_element_kernel : wide ? linear_bwd_input_f32_kernel<64> : linear_bwd_input_f32_kernel<32>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)dout, dout_idx, (long)dout_row_stride, total, (const float*)W, M_cap, N_out, K, (float*)dx, (long)dx_row_stride,
                        dx_idx, inv_pos, (long)rows);
     return check_launch(fn);
   }
@@ -842,9 +895,11 @@ extern "C" int spa_linear_packed_bwd_weight(const void* dout, const int32_t* dou
   SPA_REQUIRE(!(group_open() && dtype == SPA_F32), SPA_ERR_UNSUPPORTED, "%s: fp32 calls cannot be part of a group", fn);
   if (dtype == SPA_F32) {
     const bool wide = f32_wide(N_out, K);
-    const long wgs = std::min(f32_tiles(N_out, K, wide ? 64 : 32), 8192L);
-    const auto kernel = gate_scores != nullptr ? (wide ? linear_bwd_weight_f32_kernel<64, true> : linear_bwd_weight_f32_kernel<32, true>)
-                                               : (wide ? linear_bwd_weight_f32_kernel<64, false> : linear_bwd_weight_f32_kernel<32, false>);
+    const bool by_element = f32_by_element(F32Side::kWeight, N_out, K, M_cap);
+    const long wgs = std::min(by_element ? ((long)N_out * K + N_out + kF32Threads - 1) / kF32Threads : f32_tiles(N_out, K, wide ? 64 : 32), 8192L);
+    const auto scaled = by_element ? linear_bwd_weight_f32_element_kernel<true> : wide ? linear_bwd_weight_f32_kernel<64, true> : linear_bwd_weight_f32_kernel<32, true>;
+    const auto plain = by_element ? linear_bwd_weight_f32_element_kernel<false> : wide ? linear_bwd_weight_f32_kernel<64, false> : linear_bwd_weight_f32_kernel<32, false>;
+    const auto kernel = gate_scores != nullptr ? scaled : plain;
     hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)dout, dout_idx,
                        (long)dout_row_stride, (const float*)x, x_idx, gate_scores, total, M_cap, K, N_out, dW, dbias);
     return check_launch(fn);
