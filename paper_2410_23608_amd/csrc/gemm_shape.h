@@ -99,5 +99,12 @@ inline bool two_rings(int m_cap, bool counted, int ncols, int kc) {
 // (225) 4.2 | 4.8, 1568 of 768 -> 768 (300) 9.3 | 9.0, 784 of 768 -> 2304 (468) 10.3 | 9.5, 3136 of 768 -> 768 (588) 14.6 | 9.7; the gated block, 196 rows of
 // 384 -> 2 x 1024 (128) 5.6 | 6.5, 392 (224) 5.9 | 6.8, 784 (416) 7.4 | 7.2, 784 of 768 -> 2 x 2048 18.8 | 11.8.
 inline bool tiny_tiles(int m_cap, bool counted, int ncols) { return gemm_tiles<long>(counted ? m_cap - m_cap / 4 : m_cap, ncols, 64) <= 256; }
+// Workgroups of a launch with the small tiles.  Where it also clears or copies rows, the ones without a tile bring the waves that 128 x 128 tiles
+// have for that (eight a tile, two here), in one round (two workgroups a unit): 1000 rows of 64 -> 64 onto 2000 tokens 3.9 us, with a workgroup a tile 6.7 (128 x 128: 4.8);
+// 10000 onto 20000 (313 tiles) 5.3, with 640 workgroups 6.3 (128 x 128: 5.4).
+inline long tiny_groups(int m_cap, int ncols, bool other_rows) {
+  const auto in_eights = [&](long edge) { return (gemm_tiles<long>(m_cap, ncols, edge) + 7) / 8 * 8; };
+  return other_rows ? std::max(in_eights(64), std::min(4 * in_eights(128), 512L)) : in_eights(64);
+}
 
 }  // namespace spa

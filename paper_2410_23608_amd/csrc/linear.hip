@@ -110,7 +110,7 @@ static int launch_gemm_rows_tile(const char* fn, GemmArgs args, bool big, hipStr
   const size_t smem = big ? kGemmBigLds : tiny ? kGemmTinyLds : ring && !eight ? kGemmRingLds : kGemmSmallLds;
   const long tiles = gemm_tiles<long>(args.m_cap, args.ncols, big ? 192 : tiny ? 64 : 128);     // (no less than with 256)
   SPA_REQUIRE(tiles + 8 < 2147483647L / 2, SPA_ERR_INVALID_ARG, "%s: too many tiles", fn);
-  const long tiles8 = (tiles + 7) / 8 * 8;
+  const long tiles8 = tiny ? tiny_groups(args.m_cap, args.ncols, args.inv_pos != nullptr) : (tiles + 7) / 8 * 8;
   const int cfg = options().gemm_tm;
   const auto large = cfg == 6    ? gemm_rows_big_kernel<kScale, kDeep, Large::k192>
                      : cfg == 8  ? gemm_rows_big_kernel<kScale, kDeep, Large::k256>
