@@ -347,7 +347,7 @@ int spa_qk_norm_rotary_bwd(const void* dq_out, const void* dk_out, int64_t dq_ou
  * Query head h reads key head h / (H / Hk).  A row without a key gives out = 0 and lse = -inf.  One batch of keys for all images is one segment: B = 1
  * and cu_seqlens_q = {0, T}.
  * in:  q, k, v: rows, element (j, h, d) at p[j*row_stride + h*Dh + d], H heads of q, Hk of k and v, H a multiple of Hk, strides < 2^31 elements;
- *      cu_seqlens_q, cu_seqlens_k [B+1] int32; key_lens [B] int32 or NULL; max_q, max_k >= every segment's rows (B*max_q, B*max_k, max_q*H/Hk < 2^31; what
+ *      cu_seqlens_q, cu_seqlens_k [B+1] int32; key_lens [B] int32 or NULL; max_q, max_k >= every segment's rows (B*max_q, B*max_k < 2^31, max_k, max_q*H/Hk < 2^31 - 257; what
  *      lies behind them in a longer segment, and rows of q from B*max_q on, are not looked at); Dh in {32, 64}; softmax_scale (host float; 0 means 1/sqrt(Dh)); workspace of at least
  *      spa_cross_attention_workspace_bytes bytes, 256-byte aligned (NULL where that is 0: the keys are not split over workgroups).
  * out: out [>= rows of q, H*Dh] dtype, contiguous; lse [H, B*max_q] fp32 or NULL.  Other rows are not written.  The bits are the same in every run; the

@@ -10,6 +10,7 @@
 #include "attn_ops.h"
 #include "attn_tiles.h"
 #include "divisor.h"
+#include "share.h"
 #include "spa_common.h"
 
 namespace spa {
@@ -83,17 +84,6 @@ __device__ __forceinline__ CrossUnit cross_unit(const CrossShape& s) {
   u.q0 = q0;
   u.k0 = k0;
   return u;
-}
-// A split's share of n rows in steps of STEP: all of them but the last have as many
-struct Share {
-  int from, n, live;             // first row, rows, splits that have any
-};
-template <int STEP>
-__device__ __forceinline__ Share share_of(int n, int splits, int split) {
-  if (splits == 1) return {0, n, 1};
-  const int steps = (n + STEP - 1) / STEP, each = (steps + splits - 1) / splits * STEP;
-  if (n == 0) return {0, 0, 1};
-  return {split * each, min(each, n - split * each), (n + each - 1) / each};
 }
 
 // Offset of row r (token r / G, head r % G of the group) of a tensor of `stride` elements a token (below 2^31)

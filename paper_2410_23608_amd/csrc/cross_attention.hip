@@ -236,7 +236,7 @@ size_t cross_up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 bool cross_sizes_ok(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtype) {
   return B >= 1 && B <= 65535 && max_q >= 1 && max_k >= 1 && H >= 1 && H <= 65535 && Hk >= 1 && H % Hk == 0 && (long)B * max_q < 2147483647L &&
-         (long)B * max_k < 2147483647L && (long)max_q * (H / Hk) < 2147483647L - 256 && (Dh == 32 || Dh == 64) &&
+         (long)B * max_k < 2147483647L && max_k < 2147483647 - 256 && (long)max_q * (H / Hk) < 2147483647L - 256 && (Dh == 32 || Dh == 64) &&
          (dtype == SPA_F32 || dtype == SPA_BF16);
 }
 
@@ -266,7 +266,9 @@ int cross_checks(const char* fn, const CrossCall& c) {
   SPA_REQUIRE(c.H % c.Hk == 0, SPA_ERR_INVALID_ARG, "%s: H = %d is not a multiple of Hk = %d", fn, c.H, c.Hk);
   SPA_REQUIRE(c.B <= 65535 && c.H <= 65535, SPA_ERR_INVALID_ARG, "%s: B and H must be <= 65535", fn);
   SPA_REQUIRE((long)c.B * c.max_q < 2147483647L && (long)c.B * c.max_k < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B*max_q and B*max_k must be < 2^31", fn);
-  SPA_REQUIRE((long)c.max_q * (c.H / c.Hk) < 2147483647L - 256, SPA_ERR_INVALID_ARG, "%s: max_q*H/Hk must be < 2^31", fn);
+  // (a step's places past the last row or key are formed in an int before they are cut)
+  SPA_REQUIRE((long)c.max_q * (c.H / c.Hk) < 2147483647L - 256, SPA_ERR_INVALID_ARG, "%s: max_q*H/Hk must be < 2^31 - 257", fn);
+  SPA_REQUIRE(c.max_k < 2147483647 - 256, SPA_ERR_INVALID_ARG, "%s: max_k must be < 2^31 - 257", fn);
   SPA_REQUIRE(c.dtype == SPA_F32 || c.dtype == SPA_BF16, SPA_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, c.dtype);
   SPA_REQUIRE(c.Dh == 32 || c.Dh == 64, SPA_ERR_UNSUPPORTED, "%s: head dim %d not supported (32 or 64)", fn, c.Dh);
   const int64_t strides[3] = {c.qs, c.ks, c.vs};
