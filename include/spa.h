@@ -543,7 +543,7 @@ int spa_gathered_segment_attention_unpack(const void* q, const void* k, const vo
  * in:  x [*, K] dtype; gather_idx [>= rows] int32 or NULL; gate_scores fp32 indexed by token
  *      or NULL (needs gather_idx); total [1] int32 (device) or NULL (= M_cap rows);
  *      W [N_out, K] dtype (row n = weights of output n); bias [N_out] dtype or NULL.
- *      bf16: K, N_out and out_row_stride multiples of 8.
+ *      bf16: K, N_out and out_row_stride multiples of 8, K < 2^31 - 64.
  * out: out[j*out_row_stride + n] dtype; rows >= min(*total, M_cap) are not written.
  */
 int spa_linear_packed(const void* x, const int32_t* gather_idx, const float* gate_scores,
@@ -626,7 +626,7 @@ int spa_norm_residual_unpack(const void* z, const int32_t* inv_pos, const void* 
  *      total [1] int32 (device) or NULL (= M_cap rows); W [N_out, K] dtype; dx_idx int32
  *      (distinct rows) or NULL; inv_pos [rows] int32 or NULL: when given (needs dx_idx), every
  *      row i < rows of dx with inv_pos[i] < 0 is set to zero (the rows of unselected tokens).
- *      bf16: K, N_out and both row strides multiples of 8.
+ *      bf16: K, N_out and both row strides multiples of 8, N_out < 2^31 - 64.
  * out: dx[o(j)*dx_row_stride + k] dtype; other rows untouched unless inv_pos is given.
  */
 int spa_linear_packed_bwd_input(const void* dout, const int32_t* dout_idx, int64_t dout_row_stride,
@@ -661,7 +661,7 @@ int spa_linear_packed_bwd_weight(const void* dout, const int32_t* dout_idx, int6
  *   (g, u)_j = x[row(j),:] W^T + bias,   h[j,:] = act(g_j) * u_j        g: the first F of the 2F columns, u: the others
  * act: SPA_ACT_SILU g / (1 + exp(-g)), SPA_ACT_GELU g Phi(g) with the normal distribution's Phi.  The way back onto the residual stream is spa_linear_packed_unpack
  * (spa_linear_packed, spa_linear_packed_scatter) with x = h, W = W_down.
- * in:  x [*, K] dtype, contiguous rows; gather_idx [M_cap] int32 or NULL; total [1] int32 or NULL; W [2F, K], bias [2F] or NULL; bf16: K and F multiples of 8.
+ * in:  x [*, K] dtype, contiguous rows; gather_idx [M_cap] int32 or NULL; total [1] int32 or NULL; W [2F, K], bias [2F] or NULL; bf16: K and F multiples of 8, K < 2^31 - 64.
  * out: h [M_cap, F] dtype; pre [M_cap, 2F] dtype or NULL: (g, u), kept for the backward.  h is formed from the unrounded (g, u).  Rows from min(*total, M_cap) on
  *      are not written.
  */
@@ -676,7 +676,7 @@ int spa_gated_linear_packed(const void* x, const int32_t* gather_idx, const int3
  * From d_pre the gradients of x, W and bias are spa_linear_packed_bwd_input and spa_linear_packed_bwd_weight with dout = d_pre; those of W_down and its
  * bias spa_linear_packed_bwd_weight with x = h.
  * in:  dy [*, N_out] dtype, dy_row_stride elements a row; dy_idx [M_cap] int32 (row(j) = dy_idx[j]) or NULL; total as there; pre as written by the forward;
- *      bf16: N_out, F and dy_row_stride multiples of 8.
+ *      bf16: N_out, F and dy_row_stride multiples of 8, N_out < 2^31 - 64.
  * out: d_pre [M_cap, 2F] dtype; it may be pre itself.  Rows from min(*total, M_cap) on are not written.
  */
 int spa_gated_linear_packed_bwd(const void* dy, const int32_t* dy_idx, int64_t dy_row_stride, const int32_t* total, const void* W_down, const void* pre,

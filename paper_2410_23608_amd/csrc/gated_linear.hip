@@ -406,6 +406,7 @@ extern "C" int spa_gated_linear_packed(const void* x, const int32_t* gather_idx,
     return launch_gated_f32<false>(fn, a, act, st);
   }
   SPA_REQUIRE(K % 8 == 0 && F % 8 == 0, SPA_ERR_UNSUPPORTED, "%s: K and F must be multiples of 8 for bf16", fn);
+  SPA_REQUIRE(K <= kMostContraction, SPA_ERR_INVALID_ARG, "%s: K must be < 2^31 - 64 for bf16", fn);
   SPA_REQUIRE(aligned16(x) && aligned16(W) && aligned16(h) && aligned16(pre), SPA_ERR_INVALID_ARG, "%s: x / W / h / pre not 16-byte aligned", fn);
   GatedArgs a = {(const __bf16*)x, gather_idx, (long)K, total, M_cap, K, F, (const __bf16*)W, (const __bf16*)bias, (__bf16*)h, (__bf16*)pre, {}};
   return launch_gated<false>(fn, a, act, st);
@@ -424,6 +425,7 @@ extern "C" int spa_gated_linear_packed_bwd(const void* dy, const int32_t* dy_idx
   }
   SPA_REQUIRE(N_out % 8 == 0 && F % 8 == 0 && dy_row_stride % 8 == 0, SPA_ERR_UNSUPPORTED, "%s: N_out, F and dy_row_stride must be multiples of 8 for bf16",
               fn);
+  SPA_REQUIRE(N_out <= kMostContraction, SPA_ERR_INVALID_ARG, "%s: N_out must be < 2^31 - 64 for bf16", fn);
   SPA_REQUIRE(aligned16(dy) && aligned16(W_down) && aligned16(pre) && aligned16(d_pre), SPA_ERR_INVALID_ARG,
               "%s: dy / W_down / pre / d_pre not 16-byte aligned", fn);
   GatedArgs a = {(const __bf16*)dy, dy_idx, (long)dy_row_stride, total, M_cap, N_out, F, (const __bf16*)W_down, nullptr, (__bf16*)d_pre, (__bf16*)pre, {}};

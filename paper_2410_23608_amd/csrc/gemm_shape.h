@@ -8,6 +8,7 @@
 
 namespace spa {
 
+constexpr int kMostContraction = 2147483647 - 64;      // of the bf16 products: their steps of 64 are counted in an int
 template <class T>
 __host__ __device__ inline T gemm_tiles(T rows, T ncols, T edge) { return (rows + edge - 1) / edge * ((ncols + edge - 1) / edge); }
 __host__ __device__ inline bool medium_tiles(int rows, int ncols) {

@@ -171,6 +171,7 @@ static int linear_common(const char* fn, const void* x, const int32_t* gather_id
     return check_launch(fn);
   }
   SPA_REQUIRE(K % 8 == 0, SPA_ERR_UNSUPPORTED, "%s: K = %d must be a multiple of 8 for bf16", fn, K);
+  SPA_REQUIRE(K <= kMostContraction, SPA_ERR_INVALID_ARG, "%s: K must be < 2^31 - 64 for bf16", fn);
   SPA_REQUIRE(N_out % 8 == 0 && out_row_stride % 8 == 0, SPA_ERR_INVALID_ARG,
               "%s: N_out and out_row_stride must be multiples of 8 for bf16", fn);
   SPA_REQUIRE(aligned16(x) && aligned16(W) && aligned16(out), SPA_ERR_INVALID_ARG, "%s: x / W / out not 16-byte aligned", fn);

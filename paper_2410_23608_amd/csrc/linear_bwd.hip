@@ -855,6 +855,7 @@ extern "C" int spa_linear_packed_bwd_input(const void* dout, const int32_t* dout
   }
   SPA_REQUIRE(K % 8 == 0 && N_out % 8 == 0 && dout_row_stride % 8 == 0 && dx_row_stride % 8 == 0, SPA_ERR_UNSUPPORTED,
               "%s: K, N_out and the row strides must be multiples of 8 for bf16", fn);
+  SPA_REQUIRE(N_out <= kMostContraction, SPA_ERR_INVALID_ARG, "%s: N_out must be < 2^31 - 64 for bf16", fn);
   SPA_REQUIRE(aligned16(dout) && aligned16(W) && aligned16(dx), SPA_ERR_INVALID_ARG,
               "%s: dout / W / dx not 16-byte aligned", fn);
   GemmArgs args = {};
