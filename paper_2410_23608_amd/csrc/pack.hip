@@ -561,6 +561,37 @@ static void launch_unpack(const void* src, const int32_t* inv, const void* base,
                        static_cast<const T*>(nullptr), rows, C, rpb, static_cast<T*>(y));
 }
 
+// The index of the first lens[b] of N places of every sequence b (spa_pack_lengths): a workgroup has 1024 places of one sequence and adds up the lengths of
+// those before it.
+constexpr int kLengthsTile = 1024;
+__global__ void __launch_bounds__(kPackThreads) pack_lengths_kernel(const int32_t* __restrict__ lens, int B, int N, int tiles, int32_t* cu_seqlens,
+                                                                    int32_t* gather_idx, int32_t* inv_pos, int32_t* total) {
+  __shared__ int before_w[kPackWaves];
+  const int b = blockIdx.x / tiles, t = blockIdx.x - b * tiles, tid = threadIdx.x;
+  auto counted = [&](int i) { return min(max(lens[i], 0), N); };
+  int part = 0;
+  for (int i = tid; i < b; i += kPackThreads) part += counted(i);
+  part = wave_sum(part);
+  if (lane_id() == 0) before_w[tid / kWave] = part;
+  __syncthreads();
+  int base = 0;
+#pragma unroll
+  for (int w = 0; w < kPackWaves; ++w) base += before_w[w];
+  const int n = counted(b), end = min(N - t * kLengthsTile, kLengthsTile);
+  for (int i = tid; i < end; i += kPackThreads) {
+    const int at = t * kLengthsTile + i, place = b * N + at;
+    inv_pos[place] = at < n ? base + at : -1;
+    if (at < n) gather_idx[base + at] = place;
+  }
+  if (t == 0 && tid == 0) {
+    cu_seqlens[b] = base;
+    if (b == B - 1) {
+      cu_seqlens[B] = base + n;
+      total[0] = base + n;
+    }
+  }
+}
+
 }  // namespace spa
 
 using namespace spa;
@@ -673,6 +704,18 @@ extern "C" int spa_pack_shifted(const void* x, const uint8_t* mask, const int32_
   return pack_common(fn, x, mask, counts, gate_scores, B, grid_h * grid_w, C, dtype, container_len,
                      Shift{grid_h, grid_w, sh, sw}, sh != 0 || sw != 0, packed, cu_seqlens, gather_idx, inv_pos,
                      total, stream);
+}
+
+extern "C" int spa_pack_lengths(const int32_t* lens, int B, int N, int32_t* cu_seqlens, int32_t* gather_idx, int32_t* inv_pos, int32_t* total, void* stream) {
+  const char* fn = "spa_pack_lengths";
+  SPA_REFUSE_IN_GROUP(fn);
+  SPA_REQUIRE(lens && cu_seqlens && gather_idx && inv_pos && total, SPA_ERR_INVALID_ARG, "%s: null pointer", fn);
+  SPA_REQUIRE(B >= 1 && N >= 1 && (long)B * N < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B and N must be >= 1 and B*N < 2^31", fn);
+  const int tiles = (int)(((long)N + kLengthsTile - 1) / kLengthsTile);
+  SPA_REQUIRE((long)B * tiles < 4294967296L / kPackThreads, SPA_ERR_INVALID_ARG, "%s: too many sequences", fn);
+  hipLaunchKernelGGL(pack_lengths_kernel, dim3((unsigned)(B * tiles)), dim3(kPackThreads), 0, as_stream(stream), lens, B, N, tiles, cu_seqlens, gather_idx,
+                     inv_pos, total);
+  return check_launch(fn);
 }
 
 extern "C" int64_t spa_container_segments_capacity(int B, int64_t max_total, int container_len) {

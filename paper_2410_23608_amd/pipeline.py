@@ -643,7 +643,7 @@ class LayerPass(_Pass):
 
     grid: (rows, columns) or (frames, rows, columns) of an image's map, pairs: pairs of a head turned by the frame and by the row
     (default: as many by each axis that has more than one place, what is left by the columns).  states [B, L, C_states]: a padded batch,
-    key_lens [B] int32 of them count (0: the layer adds nothing to that image's tokens there).  All norms are RMS norms.  The parameters are a
+    key_lens [B] int32 of them count (0: the layer adds nothing to that image's tokens there), what lies behind is not looked at.  All norms are RMS norms.  The parameters are a
     dict with the names of PARAMS; b_in and b_out may be None."""
 
     PARAMS = ("gamma_self", "W_qkv", "gamma_q", "gamma_k", "W_o", "gamma_cross", "W_cross_q", "W_cross_kv", "gamma_cross_q", "gamma_cross_k",
@@ -680,8 +680,14 @@ class LayerPass(_Pass):
         self.ws_cross = u8(spa.spa_cross_attention_workspace_bytes(B, N, L, H, self.Hk, Dh, code))
         self.stats_self = self.stats_cross = self.stats_ffn = self.lse = self.lse_cross = self.pre = None       # kept for a backward
 
+    def _states_index(self, key_lens):
+        """Index and number of the rows of the states that are projected (None: all, as they lie), their segments, the keys of a segment that
+        count, and the launches that make these."""
+        return None, None, self.cu_states, key_lens, []
+
     def stages(self, x, w, states, key_lens, gamma_self, W_qkv, gamma_q, gamma_k, W_o, gamma_cross, W_cross_q, W_cross_kv, gamma_cross_q,
                gamma_cross_k, W_cross_o, gamma_ffn, W_in, b_in, W_out, b_out) -> List[Tuple[str, Callable[[], None]]]:
+        s_idx, s_total, cu_states, key_lens, index = self._states_index(key_lens)
         C, H, Hk, Dh, t, rms = self.C, self.H, self.Hk, self.Dh, self.total, spa.SPA_NORM_RMS
         Ck, p, kv = Hk * Dh, self.qkv, self.cross_kv
         norm = lambda rows, gamma, out, stats: spa.spa_norm_packed(rows, self.gather_idx, t, gamma, None, rms, self.eps, out, stats, prepare=True)
@@ -702,10 +708,11 @@ class LayerPass(_Pass):
             ("out_projection", back(self.attn, W_o, None, x, self.y1)),
             ("norm_cross", norm(self.y1, gamma_cross, self.normed_cross, self.stats_cross)),
             ("cross_q_projection", project(self.normed_cross, W_cross_q, self.cross_q)),
-            ("cross_kv_projection", spa.spa_linear_packed(states, None, None, None, W_cross_kv, None, kv, prepare=True)),
+            *index,
+            ("cross_kv_projection", spa.spa_linear_packed(states, s_idx, None, s_total, W_cross_kv, None, kv, prepare=True)),
             ("cross_q_norm", heads(self.cross_q, t, gamma_cross_q, H, self.cross_qn)),
-            ("cross_k_norm", heads(kv[:, :Ck], None, gamma_cross_k, Hk, self.cross_kn)),
-            ("cross_attention", spa.spa_cross_attention(self.cross_qn, self.cross_kn, kv[:, Ck:], self.cu_seqlens, self.cu_states, key_lens, self.B, self.N,
+            ("cross_k_norm", heads(kv[:, :Ck], s_total, gamma_cross_k, Hk, self.cross_kn)),
+            ("cross_attention", spa.spa_cross_attention(self.cross_qn, self.cross_kn, kv[:, Ck:], self.cu_seqlens, cu_states, key_lens, self.B, self.N,
                                                         self.L, H, Hk, Dh, self.cross_attn, self.lse_cross, self.ws_cross, prepare=True)),
             ("cross_out_projection", back(self.cross_attn, W_cross_o, None, self.y1, self.y2)),
             ("norm_ffn", norm(self.y2, gamma_ffn, self.normed_ffn, self.stats_ffn)),
@@ -738,6 +745,8 @@ class LayerTrainPass(LayerPass):
         self.d_cross_q, self.d_kn, self.d_kv = rows(C), rows(Ck, B * L), rows(2 * Ck, B * L)
         self.dy2, self.dy1, self.dx = (torch.empty(B, N, C, dtype=td, device="cuda") for _ in range(3))
         self.d_states = torch.empty(B * L, C_states, dtype=td, device="cuda")
+        i32 = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")
+        self.cu_packed_states, self.states_idx, self.states_inv, self.states_total = i32(B + 1), i32(B * L), i32(B * L), i32(1)
         self.no_d_scores = torch.zeros(B, N, **f32)            # (the scores select, nothing else)
         e = lambda *shape: torch.empty(*shape, **f32)
         self.grad_list = [e(C), e(3 * C, C), e(Dh), e(Dh), e(C, C), e(C), e(C, C), e(2 * Ck, C_states), e(Dh), e(Dh), e(C, C), e(C), e(2 * F, C), e(2 * F),
@@ -756,15 +765,23 @@ class LayerTrainPass(LayerPass):
     def grads(self):
         return dict(zip(self.PARAMS, self.grad_list))
 
+    def _states_index(self, key_lens):
+        # (the sums over rows of the backward would take 0 times whatever lies behind key_lens: the states that count are packed)
+        if key_lens is None:
+            return super()._states_index(key_lens)
+        return self.states_idx, self.states_total, self.cu_packed_states, None, [
+            ("pack_states", spa.spa_pack_lengths(key_lens, self.L, self.cu_packed_states, self.states_idx, self.states_inv, self.states_total, prepare=True))]
+
     def stages(self, x, w, states, key_lens, gamma_self, W_qkv, gamma_q, gamma_k, W_o, gamma_cross, W_cross_q, W_cross_kv, gamma_cross_q,
                gamma_cross_k, W_cross_o, gamma_ffn, W_in, b_in, W_out, b_out, labels, dy):
         C, H, Hk, Dh, t, rms, cap, ws = self.C, self.H, self.Hk, self.Dh, self.total, spa.SPA_NORM_RMS, self.B * self.N, self.ws
         Ck, p, dp, kv, dkv, rows_k = Hk * Dh, self.qkv, self.d_qkv, self.cross_kv, self.d_kv, self.B * self.L
+        s_idx, s_total, cu_states, s_lens, _ = self._states_index(key_lens)
         (g_self, gW_qkv, g_q, g_k, gW_o, g_cross, gW_cq, gW_ckv, g_cq, g_ck, gW_co, g_ffn, gW_in, gb_in, gW_out, gb_out) = self.grad_list
         flat = lambda d: d.view(cap, C)
         given = lambda param, grad: None if param is None else grad
-        into = lambda d, idx, W, out, M=cap, total=t: spa.spa_linear_packed_bwd_input(d, idx, total, W, M, None, None, out, prepare=True)
-        weight = lambda d, idx, rows, dW, db=None, M=cap, total=t: spa.spa_linear_packed_bwd_weight(d, idx, rows, None, None, total, M, dW, db, ws, prepare=True)
+        into = lambda d, idx, W, out: spa.spa_linear_packed_bwd_input(d, idx, t, W, cap, None, None, out, prepare=True)
+        weight = lambda d, idx, rows, dW, db=None: spa.spa_linear_packed_bwd_weight(d, idx, rows, None, None, t, cap, dW, db, ws, prepare=True)
         norm = lambda rows, gamma, stats, d, out, dgamma: spa.spa_norm_packed_bwd(self.d_normed, rows, self.inv_pos, t, gamma, rms, stats, d, out,
                                                                                   given(gamma, dgamma), None, ws, prepare=True)
         heads = lambda d, q, total, gamma, n, out, dgamma: spa.spa_qk_norm_rotary_bwd(
@@ -780,14 +797,15 @@ class LayerTrainPass(LayerPass):
             ("cross_out_bwd_input", into(flat(self.dy2), self.gather_idx, W_cross_o, self.d_attn)),
             ("cross_out_bwd_weight", weight(flat(self.dy2), self.gather_idx, self.cross_attn, gW_co)),
             ("cross_attention_bwd", spa.spa_cross_attention_bwd(
-                self.cross_qn, self.cross_kn, kv[:, Ck:], self.cross_attn, self.d_attn, self.lse_cross, self.cu_seqlens, self.cu_states, key_lens, self.B,
+                self.cross_qn, self.cross_kn, kv[:, Ck:], self.cross_attn, self.d_attn, self.lse_cross, self.cu_seqlens, cu_states, s_lens, self.B,
                 self.N, self.L, H, Hk, Dh, self.d_cross_q, self.d_kn, dkv[:, Ck:], ws, prepare=True)),
             ("cross_q_norm_bwd", heads(self.d_cross_q, self.cross_q, t, gamma_cross_q, H, self.d_cross_q, g_cq)),
-            ("cross_k_norm_bwd", heads(self.d_kn, kv[:, :Ck], None, gamma_cross_k, Hk, dkv[:, :Ck], g_ck)),
+            ("cross_k_norm_bwd", heads(self.d_kn, kv[:, :Ck], s_total, gamma_cross_k, Hk, dkv[:, :Ck], g_ck)),
             ("cross_q_bwd_input", into(self.d_cross_q, None, W_cross_q, self.d_normed)),
             ("cross_q_bwd_weight", weight(self.d_cross_q, None, self.normed_cross, gW_cq)),
-            ("cross_kv_bwd_input", into(dkv, None, W_cross_kv, self.d_states, rows_k, None)),
-            ("cross_kv_bwd_weight", weight(dkv, None, states, gW_ckv, None, rows_k, None)),
+            ("cross_kv_bwd_input", spa.spa_linear_packed_bwd_input(dkv, None, s_total, W_cross_kv, rows_k, s_idx, None if s_idx is None else self.states_inv,
+                                                                   self.d_states, prepare=True)),
+            ("cross_kv_bwd_weight", spa.spa_linear_packed_bwd_weight(dkv, None, states, s_idx, None, s_total, rows_k, gW_ckv, None, ws, prepare=True)),
             ("norm_cross_bwd", norm(self.y1, gamma_cross, self.stats_cross, self.dy2, self.dy1, g_cross)),
             ("out_bwd_input", into(flat(self.dy1), self.gather_idx, W_o, self.d_attn)),
             ("out_bwd_weight", weight(flat(self.dy1), self.gather_idx, self.attn, gW_o)),

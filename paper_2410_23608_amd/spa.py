@@ -58,6 +58,7 @@ _SIGNATURES = {
                                  _P, _P, _P]),
     "spa_container_segments_capacity": (c_int64, [c_int, c_int64, c_int]),
     "spa_container_segments": (c_int, [_P, c_int, c_int, c_int64, c_int, _P, _P, _P]),
+    "spa_pack_lengths": (c_int, [_P, c_int, c_int, _P, _P, _P, _P, _P]),
     "spa_pack_containers": (c_int, [_P, c_int, c_int, c_int, c_int, c_int, c_int, c_int, _P, _P, _P, _P, _P, _P, _P]),
     "spa_packed_attention": (c_int, [_P, _P, _P, c_int64, c_int64, c_int64, _P, c_int, c_int, c_int, c_int, c_int, c_float, _P, _P, _P]),
     "spa_packed_attention_running_max": (c_int, [_P, _P, _P, c_int64, c_int64, c_int64, _P, c_int, c_int, c_int, c_int, c_int,
@@ -553,6 +554,17 @@ def spa_container_segments(cu_seqlens, container_len, max_total, seg_cu_seqlens,
     return _dispatch(lib.spa_container_segments,
                      (_ptr(cu_seqlens), B, int(container_len), int(max_total), seg_cu_seqlens.numel() - 1,
                       _ptr(seg_cu_seqlens), _ptr(n_segments), _stream(),), _keep, prepare)
+
+
+def spa_pack_lengths(lens, N, cu_seqlens, gather_idx, inv_pos, total, prepare=False):
+    """The packing index of the first lens[b] of N places of every sequence b (spa_pack of a mask of these, indices only)."""
+    fn = "spa_pack_lengths"
+    B, N = lens.numel(), int(N)
+    _typed(fn, torch.int32, lens=lens, cu_seqlens=cu_seqlens, gather_idx=gather_idx, inv_pos=inv_pos, total=total)
+    _holds(fn, cu_seqlens=(cu_seqlens, B + 1), gather_idx=(gather_idx, B * N), inv_pos=(inv_pos, B * N), total=(total, 1))
+    _keep = (lens, cu_seqlens, gather_idx, inv_pos, total,)
+    _contig(*_keep)
+    return _dispatch(lib.spa_pack_lengths, (_ptr(lens), B, N, _ptr(cu_seqlens), _ptr(gather_idx), _ptr(inv_pos), _ptr(total), _stream(),), _keep, prepare)
 
 
 def spa_pack_containers(mask, grid_h, grid_w, shift_h, shift_w, container_len, cu_seqlens, gather_idx, inv_pos, total,
