@@ -748,6 +748,7 @@ class LayerTrainPass(LayerPass):
         i32 = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")
         self.cu_packed_states, self.states_idx, self.states_inv, self.states_total = i32(B + 1), i32(B * L), i32(B * L), i32(1)
         self.no_d_scores = torch.zeros(B, N, **f32)            # (the scores select, nothing else)
+        self._there = (True,) * len(self.PARAMS)               # the parameters of the last run that were not None
         e = lambda *shape: torch.empty(*shape, **f32)
         self.grad_list = [e(C), e(3 * C, C), e(Dh), e(Dh), e(C, C), e(C), e(C, C), e(2 * Ck, C_states), e(Dh), e(Dh), e(C, C), e(C), e(2 * F, C), e(2 * F),
                           e(C, F), e(C)]
@@ -763,7 +764,7 @@ class LayerTrainPass(LayerPass):
 
     @property
     def grads(self):
-        return dict(zip(self.PARAMS, self.grad_list))
+        return {name: g if there else None for name, g, there in zip(self.PARAMS, self.grad_list, self._there)}
 
     def _states_index(self, key_lens):
         # (the sums over rows of the backward would take 0 times whatever lies behind key_lens: the states that count are packed)
@@ -776,6 +777,8 @@ class LayerTrainPass(LayerPass):
                gamma_cross_k, W_cross_o, gamma_ffn, W_in, b_in, W_out, b_out, labels, dy):
         C, H, Hk, Dh, t, rms, cap, ws = self.C, self.H, self.Hk, self.Dh, self.total, spa.SPA_NORM_RMS, self.B * self.N, self.ws
         Ck, p, dp, kv, dkv, rows_k = Hk * Dh, self.qkv, self.d_qkv, self.cross_kv, self.d_kv, self.B * self.L
+        self._there = tuple(t is not None for t in (gamma_self, W_qkv, gamma_q, gamma_k, W_o, gamma_cross, W_cross_q, W_cross_kv, gamma_cross_q, gamma_cross_k,
+                                                    W_cross_o, gamma_ffn, W_in, b_in, W_out, b_out))
         s_idx, s_total, cu_states, s_lens, _ = self._states_index(key_lens)
         (g_self, gW_qkv, g_q, g_k, gW_o, g_cross, gW_cq, gW_ckv, g_cq, g_ck, gW_co, g_ffn, gW_in, gb_in, gW_out, gb_out) = self.grad_list
         flat = lambda d: d.view(cap, C)
@@ -823,6 +826,7 @@ class LayerTrainPass(LayerPass):
         ]
 
     def run(self, x, w, states, key_lens, params, labels, dy):
+        self._there = tuple(params[name] is not None for name in self.PARAMS)
         self._issue(x, w, states, key_lens, *(params[name] for name in self.PARAMS), labels, dy)
         return self.loss
 
