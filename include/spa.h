@@ -348,16 +348,18 @@ int spa_qk_norm_rotary_bwd(const void* dq_out, const void* dk_out, int64_t dq_ou
                            void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * Attention of packed rows to the keys of another sequence of another length (the tokens that a block of Section 3.2 packs attend to an encoder's states;
- * or a few queries, or one, to the packed tokens).  For segment b, query row i in [cu_seqlens_q[b], cu_seqlens_q[b+1]) and key row j in
+ * Attention of packed rows to the keys of another sequence of another length (the tokens that a block of Section 3.2 packs attend to an
+ * encoder's states; or a few queries, or one, to the packed tokens).  For segment b, query row i in [cu_seqlens_q[b], cu_seqlens_q[b+1]) and key row j in
  * [cu_seqlens_k[b], cu_seqlens_k[b] + n_b), n_b = the segment's rows, or min(key_lens[b], that) where key_lens is given (states in a padded batch):
  *   O_i = softmax_j(softmax_scale <q_i, k_j>) V,   lse_i = log sum_j exp(softmax_scale <q_i, k_j>)
- * Query head h reads key head h / (H / Hk).  A row without a key gives out = 0 and lse = -inf.  One batch of keys for all images is one segment: B = 1
- * and cu_seqlens_q = {0, T}.
+ * Query head h reads key head h / (H / Hk).  A row without a key, or all of whose scores are -inf, gives out = 0 and lse = -inf.  One batch of keys
+ * for all images is one segment: B = 1 and cu_seqlens_q = {0, T}.  Segments times key heads are what the chip's eight parts share: with fewer than
+ * eight of them part of it has no work.
  * in:  q, k, v: rows, element (j, h, d) at p[j*row_stride + h*Dh + d], H heads of q, Hk of k and v, H a multiple of Hk, strides < 2^31 elements;
- *      cu_seqlens_q, cu_seqlens_k [B+1] int32; key_lens [B] int32 or NULL; max_q, max_k >= every segment's rows (B*max_q, B*max_k < 2^31, max_k, max_q*H/Hk < 2^31 - 257; what
- *      lies behind them in a longer segment, and rows of q from B*max_q on, are not looked at); Dh in {32, 64}; softmax_scale (host float; 0 means 1/sqrt(Dh)); workspace of at least
- *      spa_cross_attention_workspace_bytes bytes, 256-byte aligned (NULL where that is 0: the keys are not split over workgroups).
+ *      cu_seqlens_q, cu_seqlens_k [B+1] int32; key_lens [B] int32 or NULL; max_q, max_k >= every segment's rows (B*max_q, B*max_k < 2^31,
+ *      max_k, max_q*H/Hk < 2^31 - 257; what lies behind them in a longer segment, and rows of q from B*max_q on, are not looked at);
+ *      Dh in {32, 64}; softmax_scale (host float; 0 means 1/sqrt(Dh)); workspace of at least spa_cross_attention_workspace_bytes bytes,
+ *      256-byte aligned (NULL where that is 0: the keys are not split over workgroups).
  * out: out [>= rows of q, H*Dh] dtype, contiguous; lse [H, B*max_q] fp32 or NULL.  Other rows are not written.  The bits are the same in every run; the
  *      order in which a row's keys are added follows from B, H, Hk, max_q, max_k and the segment's number of keys.
  */
@@ -667,11 +669,12 @@ int spa_linear_packed_bwd_weight(const void* dout, const int32_t* dout_idx, int6
  * The gated feed-forward block on packed rows: both projections, the activation and their product in one launch.  For j < min(*total, M_cap),
  * row(j) = gather_idx[j] or j:
  *   (g, u)_j = x[row(j),:] W^T + bias,   h[j,:] = act(g_j) * u_j        g: the first F of the 2F columns, u: the others
- * act: SPA_ACT_SILU g / (1 + exp(-g)), SPA_ACT_GELU g Phi(g) with the normal distribution's Phi.  The way back onto the residual stream is spa_linear_packed_unpack
- * (spa_linear_packed, spa_linear_packed_scatter) with x = h, W = W_down.
- * in:  x [*, K] dtype, contiguous rows; gather_idx [M_cap] int32 or NULL; total [1] int32 or NULL; W [2F, K], bias [2F] or NULL; bf16: K and F multiples of 8, K < 2^31 - 64.
- * out: h [M_cap, F] dtype; pre [M_cap, 2F] dtype or NULL: (g, u), kept for the backward.  h is formed from the unrounded (g, u).  Rows from min(*total, M_cap) on
- *      are not written.
+ * act: SPA_ACT_SILU g / (1 + exp(-g)), SPA_ACT_GELU g Phi(g) with the normal distribution's Phi.  The way back onto the residual stream is
+ * spa_linear_packed_unpack (spa_linear_packed, spa_linear_packed_scatter) with x = h, W = W_down.
+ * in:  x [*, K] dtype, contiguous rows; gather_idx [M_cap] int32 or NULL; total [1] int32 or NULL; W [2F, K], bias [2F] or NULL; bf16: K and F
+ *      multiples of 8, K < 2^31 - 64.
+ * out: h [M_cap, F] dtype; pre [M_cap, 2F] dtype or NULL: (g, u), kept for the backward, which forms act and its slope from them; h is
+ *      formed from the unrounded (g, u).  Rows from min(*total, M_cap) on are not written.
  */
 #define SPA_ACT_SILU 0
 #define SPA_ACT_GELU 1
