@@ -35,16 +35,19 @@ struct CrossUnit {
   long q0, k0;                   // the segment's first rows
   int nq, nk, held;              // rows (tokens times heads), keys, keys the segment has places for
 };
-// What of a segment is looked at: no more tokens and keys than the longest may have, no token from the B max_q-th on (lse and D have no place for
-// it), nothing of one that starts below 0.
+// What of a segment is looked at: no more tokens and keys than the longest may have, no token from the B max_q-th on (lse and D have no
+// place for it), nothing of one that starts below 0.
 __device__ __forceinline__ void cross_lengths(const CrossShape& s, int b, int q0, int k0, int& nq, int& nk, int& held) {
   const int room = q0 < 0 ? 0 : (int)max(s.stat_stride - q0, 0L);
   nq = min(min(max(s.cu_q[b + 1] - q0, 0), s.most_q), room) * (int)s.G.d;
   held = k0 < 0 ? 0 : min(max(s.cu_k[b + 1] - k0, 0), s.most_k);
   nk = s.key_lens != nullptr ? min(max(s.key_lens[b], 0), held) : held;
 }
-// Blocks and splits of a pair (segment, key head) next to each other on one XCD, whose L2 then holds what they share, pairs dealt to the XCDs there
-// and back.  Up to kRankedB segments come by their products, most first; ranking more costs every workgroup more than it gives (8 segments of 1568 to
+// Blocks and splits of a pair (segment, key head) next to each other on one XCD, whose L2 then holds what they share, pairs dealt to the
+// XCDs there and back.  So fewer than eight pairs leave XCDs without work, however many blocks each has (one image of 3136 tokens and keys,
+// 8 heads of 64 on 1 | 2 | 4 | 8 key heads: forward 205 | 121 | 75 | 51 us, backward 624 | 337 | 204 | 138), nine to fifteen give some two
+// of them.
+// Up to kRankedB segments come by their products, most first; ranking more costs every workgroup more than it gives (8 segments of 1568 to
 // 3136 tokens and 410 to 1024 keys, 12 and 4 heads of 64, dk / dv in index order 171 us, ranked 158).
 constexpr int kRankedB = 16;
 __device__ __forceinline__ CrossUnit cross_unit(const CrossShape& s) {
@@ -93,11 +96,12 @@ __device__ __forceinline__ long group_row(const Divisor& G, int r, long stride) 
   return (long)((uint64_t)i * (uint32_t)stride) + (r - (int)(i * G.d)) * DH;
 }
 
-// BT rows of two operands on their way to LDS, in 16-byte pieces.  Nothing here waits for a load or branches on one between load() and store();
-// rows past the end are loaded as the last one, and store<true>() clears operand 1's (the caller gives such rows probability 0, and 0
-// times an infinity of the last row would be NaN).  GROUPED: rows of a unit's tokens and heads (group_row), else of one head.  (Addresses of whole steps from the
-// first step's by a scalar's distance, without the multiplications: registers for them cost dq a wave a SIMD, 91 -> 100 us at 8 segments of 1568 to 3136 tokens
-// and 410 to 1024 keys, 12 and 4 heads of 64; forward 78 -> 77, dk / dv 141 -> 148.)
+// BT rows of two operands on their way to LDS, in 16-byte pieces.  Nothing here waits for a load or branches on one between load() and
+// store(); rows past the end are loaded as the last one, and store<true>() clears operand 1's (the caller gives such rows probability 0,
+// and 0 times an infinity of the last row would be NaN).  GROUPED: rows of a unit's tokens and heads (group_row), else of one head.
+// (Addresses of whole steps from the first step's by a scalar's distance, without the multiplications: registers for them cost dq a wave a
+// SIMD, 91 -> 100 us at 8 segments of 1568 to 3136 tokens and 410 to 1024 keys, 12 and 4 heads of 64; forward 78 -> 77, dk / dv 141 ->
+// 148.)
 template <typename T, int DH, int BT, bool GROUPED>
 struct CrossStage {
   static constexpr int RS = Ops<T, DH>::RS, VE = 16 / sizeof(T), CPR = DH / VE, CPT = BT * CPR / kCrossThreads, RPP = kCrossThreads / CPR;

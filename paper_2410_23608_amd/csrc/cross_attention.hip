@@ -7,9 +7,11 @@
 // The maximum and the sum run along, in fp32.  Few rows: the four waves share 32 (or 64) of them, each with its part of every step of keys;
 // few units with long keys: the keys are split over workgroups, which leave unnormalised sums, maxima and row sums in fp32 for a
 // second launch that joins them in the order of the splits.
-// Bound by the vector instructions of the softmax where there is work (of the busy cycles three quarters, the matrix pipe a third): 8 x 1568 to 3136 tokens
-// against 410 to 1024 states, 12 and 4 heads of 64, 71 us; by the keys' bytes for few rows (one token of 4 sequences of 11200 to 16000 keys, 16 and 4 heads, 14 + 4 us); by
-// chains of trips to memory for short segments (64 x 196 tokens to captions of up to 77, 13 us; one image 4.6).
+// Bound by the vector instructions of the softmax where there is work (of the busy cycles three quarters, the matrix pipe a third): 8 x
+// 1568 to 3136 tokens against 410 to 1024 states, 12 and 4 heads of 64, 71 us; by the keys' bytes for few rows (one token of 4 sequences of
+// 11200 to 16000 keys, 16 and 4 heads, 14 + 4 us); by chains of trips to memory for short segments (64 x 196 tokens to captions of up to
+// 77, 13 us; one image 4.6). fp32: 8 x 1568 to 3136 tokens, 410 to 1024 states, 428 us = 111 of 154 TFLOP/s (backward 1675, 71), to
+// captions 41 (132).
 #include <algorithm>
 #include <cmath>
 
@@ -36,8 +38,8 @@ struct CrossTiles {
   __attribute__((aligned(16))) T V[2][STEP * RS];
 };
 
-// (Maximum and exponentials block by block of 32 keys: two at a time take 147 registers at heads of 64, three waves a SIMD; 64 x 196 tokens to captions 14.1 us then,
-// 13.1 so, long keys the same.)
+// (Maximum and exponentials block by block of 32 keys: two at a time take 147 registers at heads of 64, three waves a SIMD; 64 x 196 tokens
+// to captions 14.1 us then, 13.1 so, long keys the same.)
 template <typename T, int DH, int KW>
 __global__ void __launch_bounds__(kCrossThreads, sizeof(T) == 2 && KW == 1 ? 4 : 1) cross_fwd_kernel(const CrossFwd<T> a) {
   using O = Ops<T, DH>;
@@ -89,8 +91,8 @@ __global__ void __launch_bounds__(kCrossThreads, sizeof(T) == 2 && KW == 1 ? 4 :
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = __builtin_elementwise_maximum(mx, s[i]);
         const float m_new = __builtin_elementwise_maximum(m, max_across_halves(mx));
-        // (m, what the exponents are taken from, follows a row's maximum when that is 2^8 past it, or a NaN: of 32 rows one has a new maximum in nearly
-        // every block)
+        // (m, what the exponents are taken from, follows a row's maximum when that is 2^8 past it, or a NaN: of 32 rows one has a new
+        // maximum in nearly every block)
         const bool past = !((m_new - m) * a.s.c <= 8.f);
         if (__ballot(past) != 0) {
           const float f = past && m_new != m ? __builtin_amdgcn_exp2f((m - m_new) * a.s.c) : 1.f;
@@ -240,8 +242,8 @@ bool cross_sizes_ok(int B, int max_q, int max_k, int H, int Hk, int Dh, int dtyp
          (dtype == SPA_F32 || dtype == SPA_BF16);
 }
 
-// Few workgroups: the waves of one share its owned rows, two by two or all four, as long as one round of workgroups holds them all.  Fewer still and many rows on
-// the other side: these are split, into no less than `least` each, until there are about four workgroups a unit.
+// Few workgroups: the waves of one share its owned rows, two by two or all four, as long as one round of workgroups holds them all.  Fewer
+// still and many rows on the other side: these are split, into no less than `least` each, until there are about four workgroups a unit.
 CrossPlan cross_plan(long units, long owned, long others, int dtype) {
   CrossPlan p = {1, 1, 1};
   const long least = dtype == SPA_F32 ? 256 : 512;
@@ -342,7 +344,8 @@ extern "C" int spa_cross_attention(const void* q, const void* k, const void* v, 
   SPA_REQUIRE(out != nullptr, SPA_ERR_INVALID_ARG, "%s: out is null", fn);
   SPA_REQUIRE(aligned16(out), SPA_ERR_INVALID_ARG, "%s: out not 16-byte aligned", fn);
   const CrossPlan p = fwd_plan(B, max_q, max_k, H, Hk, dtype);
-  SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 4294967296L / kCrossThreads, SPA_ERR_INVALID_ARG, "%s: too many workgroups (B*max_q*H must be < about 2^31)", fn);
+  SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 4294967296L / kCrossThreads, SPA_ERR_INVALID_ARG,
+              "%s: too many workgroups (B*max_q*H must be < about 2^31)", fn);
   const size_t need = spa_cross_attention_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype);
   SPA_REQUIRE(need == 0 || (workspace != nullptr && workspace_bytes >= need), SPA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given",
               fn, need, workspace_bytes);

@@ -1,12 +1,15 @@
-// Backward of the attention to another sequence (cross_attention.hip): with P = exp(S - lse), dP = dO V^T, D_r = <dO_r, O_r>, dS = P (dP - D)
+// Backward of the attention to another sequence (cross_attention.hip): with P = exp(S - lse), dP = dO V^T, D_r = <dO_r, O_r>, dS = P (dP -
+// D)
 //   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO        (sums over the tokens and the heads that share the key head)
-// Two launches.  The dq launch walks the keys for 32 rows a wave as the forward does and leaves D; the dk / dv launch walks the rows for 32 keys a wave, S
-// and dP un-transposed (a lane is a key), so that P and dS are operands in registers again.  D is formed from the rounded result.  Few owned
-// rows: the four waves share them.  Few units and many rows on the other side: those are split over workgroups, whose fp32 sums a further launch adds
-// in the order of the splits.  Everything is added in a fixed order.  Units of few rows and keys take one launch (cross_bwd_short_kernel).
-// Bound by the order within a wave, products, exponentials, products, at two (dk / dv) and three waves a SIMD: of the busy cycles the matrix pipe has 0.38
-// and 0.42, the vector instructions 0.43 and 0.54, LDS 0.44.  8 x 1568 to 3136 tokens, 410 to 1024 states, 12 and 4 heads of 64: dq 89 us, dk / dv 137 and
-// 10 for the splits' sums.
+// Two launches.  The dq launch walks the keys for 32 rows a wave as the forward does and leaves D; the dk / dv launch walks the rows for 32
+// keys a wave, S and dP un-transposed (a lane is a key), so that P and dS are operands in registers again.  D is formed from the rounded
+// result.  Few owned rows: the four waves share them.  Few units and many rows on the other side: those are split over workgroups, whose
+// fp32 sums a further launch adds in the order of the splits.  Everything is added in a fixed order.  Units of few rows and keys take one
+// launch (cross_bwd_short_kernel).
+// Bound by the order within a wave, products, exponentials, products, at two (dk / dv) and three waves a SIMD: of the busy cycles the
+// matrix pipe has 0.38 and 0.42, the vector instructions 0.43 and 0.54, LDS 0.44 (half of that conflicts of banks in dk / dv); S and dP are
+// formed in both launches, seven products where five would do.  8 x 1568 to 3136 tokens, 410 to 1024 states, 12 and 4 heads of 64: dq 89
+// us, dk / dv 137 and 10 for the splits' sums.
 #include <algorithm>
 #include <cmath>
 
@@ -343,10 +346,11 @@ __global__ void __launch_bounds__(kCrossThreads) cross_sum_kernel(const CrossBwd
   else *reinterpret_cast<floatx4*>(to) = sum;
 }
 
-// Few rows and keys in a unit (bf16): all of it in one workgroup, whose rows, keys and gradients are fetched once and whose scores are formed again instead
-// of exchanged.  First the waves take 32 rows each (then the second half of the rows): K and V in LDS, Q and dO in registers, which then go to LDS in their
-// place, 128 rows at a time.  64 x 196 tokens to captions of up to 77, 12 heads of 64: 23.1 us (dq and dk / dv one by one 18.0 + 16.8), 19 of them without any
-// products: the memory phases of one round of workgroups.  With those the waves take 32 keys each, two or four waves to a block of keys where there are fewer blocks, whose sums the first adds in order.
+// Few rows and keys in a unit (bf16): all of it in one workgroup, whose rows, keys and gradients are fetched once and whose scores are
+// formed again instead of exchanged.  First the waves take 32 rows each (then the second half of the rows): K and V in LDS, Q and dO in
+// registers, which then go to LDS in their place, 128 rows at a time.  64 x 196 tokens to captions of up to 77, 12 heads of 64: 23.1 us (dq
+// and dk / dv one by one 18.0 + 16.8), 19 of them without any products: the memory phases of one round of workgroups.  With those the waves
+// take 32 keys each, two or four waves to a block of keys where there are fewer blocks, whose sums the first adds in order.
 constexpr int kShortRows = 256, kShortKeys = 128;
 template <int DH>
 struct CrossShort {
@@ -354,7 +358,8 @@ struct CrossShort {
   static __host__ __device__ constexpr int tiles(int rows) { return rows >= 128 ? 4 : (rows + 31) / 32; }
   static constexpr size_t bytes(int rows, int keys) {
     const size_t held = (size_t)2 * 32 * std::max(tiles(rows), tiles(keys)) * RS * sizeof(__bf16);
-    const int others = tiles(rows) == 1 ? 0 : tiles(rows) <= 3 ? 2 : 3;          // waves that hand over their sums: of two blocks of keys one each, of one up to three
+    // waves that hand over their sums: of two blocks of keys one each, of one up to three
+    const int others = tiles(rows) == 1 ? 0 : tiles(rows) <= 3 ? 2 : 3;
     const size_t sums = (size_t)others * N * kWave * sizeof(float);
     return std::max(held, sums);
   }
@@ -593,10 +598,13 @@ static int launch_bwd(const char* fn, const CrossBwd<T>& a, hipStream_t st) {
   return check_launch(fn);
 }
 
-// A unit's rows and keys fit one workgroup, and there are units for every compute unit, or few products in each: else dq and dk / dv are sooner formed beside
-// each other by more workgroups.  us, one workgroup a unit | two launches, heads of 64: 6 units of 196 rows and 77 keys 16.8 | 14.7, 12 of 256 and 128 19.4 | 16.3,
-// 12 of 30 and 20 6.2 | 11.3, 96 of 256 and 128 19.6 | 18.3, 192 of 196 and 77 17.1 | 18.5, 384 21.1 | 24.5, 768 26.3 | 39.3, 768 of 60 and 77 14.4 | 23.9,
-// 1536 of 256 and 128 56.2 | 78.9.
+// A unit's rows and keys fit one workgroup, and there are units for every compute unit, or few products in each: else dq and dk / dv are
+// sooner formed beside each other by more workgroups.  us, one workgroup a unit | two launches, heads of 64: 6 units of 196 rows and 77
+// keys 16.8 | 14.7, 96 15.6 | 14.9, 160 to 256 17.0 to 17.5 | 17.0 to 17.4 (a tie, 192 17.3 | 17.1), 288 18.4 | 20.3, 384 21.1 | 24.5, 768
+// 26.3 | 39.3; 96 of 256 and 128 20.5 | 17.7, 192 21.3 | 20.6, 256 21.9 | 21.6, 288 22.2 | 26.0, 1536 56.2 | 78.9; 12 of 30 and 20 6.2 |
+// 11.3, 768 of 60 and 77 14.4 | 23.9.
+// Units of up to 128 rows and more than 8192 products are faster in one workgroup below 256 units, too (64 of 128 and 128 12.2 | 15.2); the
+// rule, which decides how D is formed and with it the bits, leaves them.
 static bool cross_short(long units, int max_q, int max_k, int G, int dtype) {
   const long rows = (long)max_q * G;
   return dtype == SPA_BF16 && rows <= kShortRows && max_k <= kShortKeys && (units >= 256 || rows * max_k <= 8192);
@@ -606,7 +614,8 @@ template <int DH>
 static int launch_short(const char* fn, const CrossBwd<__bf16>& a, hipStream_t st) {
   const size_t lds = CrossShort<DH>::bytes(a.s.most_q * (int)a.s.G.d, a.s.most_k);
   const auto kernel = cross_bwd_short_kernel<DH>;
-  const hipError_t attr = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)CrossShort<DH>::bytes(kShortRows, kShortKeys));
+  const hipError_t attr = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                              (int)CrossShort<DH>::bytes(kShortRows, kShortKeys));
   SPA_REQUIRE(attr == hipSuccess, SPA_ERR_HIP, "%s: cannot reserve %zu bytes of LDS", fn, lds);
   hipLaunchKernelGGL(kernel, dim3((unsigned)cross_grid(a.s)), dim3(kCrossThreads), lds, st, a);
   return check_launch(fn);
@@ -677,7 +686,8 @@ extern "C" int spa_cross_attention_bwd(const void* q, const void* k, const void*
   SPA_REQUIRE(aligned16(out) && aligned16(dout) && aligned16(dq) && aligned16(dk) && aligned16(dv), SPA_ERR_INVALID_ARG,
               "%s: tensors not 16-byte aligned", fn);
   for (const CrossPlan& p : {dq_plan(B, max_q, max_k, H, Hk, dtype), dkdv_plan(B, max_q, max_k, H, Hk, dtype)})
-    SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 4294967296L / kCrossThreads, SPA_ERR_INVALID_ARG, "%s: too many workgroups (B*max_q*H must be < about 2^31)", fn);
+    SPA_REQUIRE(((long)Hk * B + 8) * p.blocks * p.splits < 4294967296L / kCrossThreads, SPA_ERR_INVALID_ARG,
+                "%s: too many workgroups (B*max_q*H must be < about 2^31)", fn);
   const size_t need = spa_cross_attention_bwd_workspace_bytes(B, max_q, max_k, H, Hk, Dh, dtype);
   SPA_REQUIRE(workspace != nullptr && workspace_bytes >= need, SPA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
               workspace_bytes);

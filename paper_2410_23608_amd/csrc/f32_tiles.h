@@ -1,7 +1,9 @@
-// Tiles of fp32 products for the projections of small fp32 workloads (linear.hip, linear_bwd.hip, gated_linear.hip): every element is one chain of fused multiply-adds in
-// the order of the contraction, whatever the tile, so that neither its size nor the rest of the call touches an element's bits.
-// Four waves have a quarter each of EDGE x EDGE elements, in fp32 matrix instructions, whose products are that chain (checked bit for bit, with denormals, infinities and zeros of
-// either sign; 1000 rows of 1400 -> 1000 108 us in vector instructions, 53 so).  Both operands of a step of the contraction are in LDS, those of the next steps on their way in registers, eight loads of each operand a thread.
+// Tiles of fp32 products for the projections of small fp32 workloads (linear.hip, linear_bwd.hip, gated_linear.hip): every element is one
+// chain of fused multiply-adds in the order of the contraction, whatever the tile, so that neither its size nor the rest of the call
+// touches an element's bits.
+// Four waves have a quarter each of EDGE x EDGE elements, in fp32 matrix instructions, whose products are that chain (checked bit for bit,
+// with denormals, infinities and zeros of either sign; 1000 rows of 1400 -> 1000 108 us in vector instructions, 53 so).  Both operands of a
+// step of the contraction are in LDS, those of the next steps on their way in registers, eight loads of each operand a thread.
 #pragma once
 
 #include <type_traits>
@@ -29,8 +31,9 @@ struct F32Lds {
   __attribute__((aligned(16))) float b[2][NB][kF32Step<EDGE>][kF32Row<EDGE>];
 };
 
-// The quarter of a tile that a wave has, of one fp32 matrix instruction (16x16x4 or 32x32x2): element e of a lane, and which of KD neighbouring contraction elements
-// a lane hands to it.  The instruction is a chain of fused multiply-adds in the order of its contraction elements.
+// The quarter of a tile that a wave has, of one fp32 matrix instruction (16x16x4 or 32x32x2): element e of a lane, and which of KD
+// neighbouring contraction elements a lane hands to it.  The instruction is a chain of fused multiply-adds in the order of its contraction
+// elements.
 template <int EDGE>
 struct F32Quarter {
   static constexpr int Q = EDGE / 2, KD = Q == 16 ? 4 : 2, kCount = Q * Q / 64;
@@ -49,10 +52,11 @@ struct F32Quarter {
 struct F32Nothing {
   __device__ __forceinline__ void operator()(int) const {}
 };
-// acc[q] of row m and column n += sum over k in order of A(m, k) B_q(n, k).  fetch_a(i, k), fetch_b(q, i, k): the thread's i-th element of the step as it lies
-// in memory, at contraction index k < kc (clamped; what is past kc is replaced by zeros whose product is -0, which leaves any sum as it is); done_a(i, v), done_b(q, i, v): what is made
-// of it, when it is there (nothing may ask for a value before, or it waits in front of the products).  beside(a): the step's A in LDS, behind its products.  ahead(k0): called a
-// step before the fetches from k0 on, for what these need of memory themselves.  DEPTH: steps whose loads are under way.
+// acc[q] of row m and column n += sum over k in order of A(m, k) B_q(n, k).  fetch_a(i, k), fetch_b(q, i, k): the thread's i-th element of
+// the step as it lies in memory, at contraction index k < kc (clamped; what is past kc is replaced by zeros whose product is -0, which
+// leaves any sum as it is); done_a(i, v), done_b(q, i, v): what is made of it, when it is there (nothing may ask for a value before, or it
+// waits in front of the products).  beside(a): the step's A in LDS, behind its products.  ahead(k0): called a step before the fetches from
+// k0 on, for what these need of memory themselves.  DEPTH: steps whose loads are under way.
 template <int EDGE, int NB, bool A_LINES, bool B_LINES, int DEPTH, class FA, class FB, class DA, class DB, class BS, class AH = F32Nothing>
 __device__ __forceinline__ void f32_tile_sums(F32Lds<EDGE, NB>& l, int kc, FA&& fetch_a, FB&& fetch_b, DA&& done_a, DB&& done_b,
                                               typename F32Quarter<EDGE>::Acc (&acc)[NB], BS&& beside, AH&& ahead = AH{}) {

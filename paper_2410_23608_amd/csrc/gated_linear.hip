@@ -2,16 +2,17 @@
 //   g_j = x_row(j) Wg^T + bg,  u_j = x_row(j) Wu^T + bu,  h_j = act(g_j) * u_j          (W [2F][K]: Wg's rows, then Wu's)
 // and the step of its backward between the two products' gradients: with dh = dy W_down,
 //   d_g = dh * u * act'(g),  d_u = dh * act(g)
-// formed in the epilogue of that product, so that dh is never in memory.  The rest of the block are the projections of linear.hip and linear_bwd.hip: the
-// way back onto the residual stream, and from d_pre = (d_g, d_u) the gradients of x, W and the biases.
+// formed in the epilogue of that product, so that dh is never in memory.  The rest of the block are the projections of linear.hip and
+// linear_bwd.hip: the way back onto the residual stream, and from d_pre = (d_g, d_u) the gradients of x, W and the biases.
 //   act: SiLU g s(g), s = 1 / (1 + exp(-g)), slope s (1 + g (1 - s)); GELU g Phi(g), slope Phi(g) + g phi(g).
 //
-// Both are row GEMMs on the loop of gemm_async.h in the shapes of gemm_rows.h, chosen by its rules (2 F and F columns).  Forward, the rows of Wg and Wu lie
-// in turns of one matrix tile in LDS, so that a wave has a column's gate and its factor in the same register of neighbouring accumulators.
-// Rounded to bf16 are h and pre (from the same unrounded sums) and d_pre, the operands of the products that follow and what the backward keeps; act and its slope
-// are formed from pre as kept.
-// 6272 rows of 768 -> 2 x 2048 -> 768: forward 57 us (690 TFLOP/s; with 128 x 128 tiles 68), 1.8 rounds of tiles and 77 MB on their way out; backward 45 (50), 20
-// GFLOP and 102 MB of pre and d_pre behind the loop, when all units store at once.
+// Both are row GEMMs on the loop of gemm_async.h in the shapes of gemm_rows.h, chosen by its rules (2 F and F columns).  Forward, the rows
+// of Wg and Wu lie in turns of one matrix tile in LDS, so that a wave has a column's gate and its factor in the same register of
+// neighbouring accumulators.
+// Rounded to bf16 are h and pre (from the same unrounded sums) and d_pre, the operands of the products that follow and what the backward
+// keeps; act and its slope are formed from pre as kept. 6272 rows of 768 -> 2 x 2048 -> 768: forward 57 us (690 TFLOP/s; with 128 x 128
+// tiles 68), 1.8 rounds of tiles and 77 MB on their way out; backward 45 (50), 20 GFLOP and 102 MB of pre and d_pre behind the loop, when
+// all units store at once.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -35,9 +36,9 @@ struct GatedArgs {
   LargeRule rule;
 };
 
-// Phi and phi of the normal distribution.  bf16: erfc(x) exp(x^2) = t P(t), t = 1 / (1 + x / 2), P of degree 6 fitted so that erfc is off by at most 1.5e-7
-// absolute and 2^-12 relative for every x >= 0 (0.5e-7 and 2^-12.6 reached), Phi by half of the first: far below 0, too, the rounding of the result to
-// bf16 is what counts.  fp32: the library's.
+// Phi and phi of the normal distribution.  bf16: erfc(x) exp(x^2) = t P(t), t = 1 / (1 + x / 2), P of degree 6 fitted so that erfc is off
+// by at most 1.5e-7 absolute and 2^-12 relative for every x >= 0 (0.5e-7 and 2^-12.6 reached), Phi by half of the first: far below 0, too,
+// the rounding of the result to bf16 is what counts.  fp32: the library's.
 struct Normal {
   float cdf, density;
 };

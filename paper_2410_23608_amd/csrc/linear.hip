@@ -159,8 +159,9 @@ static int linear_common(const char* fn, const void* x, const int32_t* gather_id
     const bool wide = f32_wide(M_cap, N_out);
     const bool by_element = f32_by_element(F32Side::kForward, M_cap, N_out, K);
     const long most = std::max((long)M_cap, inv_pos != nullptr ? (long)rows : 0L);
+    const long copies = inv_pos != nullptr ? ((long)rows * N_out + 1023) / 1024 : 0L;
     const long wgs = std::min(by_element ? (most * N_out + kF32Threads - 1) / kF32Threads
-                                         : std::max(f32_tiles(M_cap, N_out, wide ? 64 : 32), inv_pos != nullptr ? ((long)rows * N_out + 1023) / 1024 : 0L), 8192L);
+                                         : std::max(f32_tiles(M_cap, N_out, wide ? 64 : 32), copies), 8192L);
 #define SPA_LIN_F32(G_, S_)                                                                                   \
   hipLaunchKernelGGL((by_element ? linear_f32_element_kernel<G_, S_> : wide ? linear_f32_kernel<G_, S_, 64> : linear_f32_kernel<G_, S_, 32>),                \
                      dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)x,                          \

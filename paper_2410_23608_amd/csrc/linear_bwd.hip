@@ -846,8 +846,9 @@ extern "C" int spa_linear_packed_bwd_input(const void* dout, const int32_t* dout
     const bool wide = f32_wide(M_cap, K);
     const bool by_element = f32_by_element(F32Side::kInput, M_cap, K, N_out);
     const long most = std::max((long)M_cap, inv_pos != nullptr ? (long)rows : 0L);
+    const long zeros = inv_pos != nullptr ? ((long)rows * K + 1023) / 1024 : 0L;
     const long wgs = std::min(by_element ? (most * K + kF32Threads - 1) / kF32Threads
-                                         : std::max(f32_tiles(M_cap, K, wide ? 64 : 32), inv_pos != nullptr ? ((long)rows * K + 1023) / 1024 : 0L), 8192L);
+                                         : std::max(f32_tiles(M_cap, K, wide ? 64 : 32), zeros), 8192L);
     const auto kernel = by_element ? linear_bwd_input_f32_element_kernel : wide ? linear_bwd_input_f32_kernel<64> : linear_bwd_input_f32_kernel<32>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)dout, dout_idx, (long)dout_row_stride, total, (const float*)W, M_cap, N_out, K, (float*)dx, (long)dx_row_stride,
                        dx_idx, inv_pos, (long)rows);
@@ -898,8 +899,12 @@ extern "C" int spa_linear_packed_bwd_weight(const void* dout, const int32_t* dou
     const bool wide = f32_wide(N_out, K);
     const bool by_element = f32_by_element(F32Side::kWeight, N_out, K, M_cap);
     const long wgs = std::min(by_element ? ((long)N_out * K + N_out + kF32Threads - 1) / kF32Threads : f32_tiles(N_out, K, wide ? 64 : 32), 8192L);
-    const auto scaled = by_element ? linear_bwd_weight_f32_element_kernel<true> : wide ? linear_bwd_weight_f32_kernel<64, true> : linear_bwd_weight_f32_kernel<32, true>;
-    const auto plain = by_element ? linear_bwd_weight_f32_element_kernel<false> : wide ? linear_bwd_weight_f32_kernel<64, false> : linear_bwd_weight_f32_kernel<32, false>;
+    const auto scaled = by_element ? linear_bwd_weight_f32_element_kernel<true>
+                        : wide     ? linear_bwd_weight_f32_kernel<64, true>
+                                   : linear_bwd_weight_f32_kernel<32, true>;
+    const auto plain = by_element ? linear_bwd_weight_f32_element_kernel<false>
+                       : wide     ? linear_bwd_weight_f32_kernel<64, false>
+                                  : linear_bwd_weight_f32_kernel<32, false>;
     const auto kernel = gate_scores != nullptr ? scaled : plain;
     hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(kF32Threads), 0, st, (const float*)dout, dout_idx,
                        (long)dout_row_stride, (const float*)x, x_idx, gate_scores, total, M_cap, K, N_out, dW, dbias);

@@ -4,10 +4,10 @@
 // axis) x (the pair's frequency), which a table holds by place and pair: rounded once, from 64 bits, however far the place.
 // Backward: du = the pairs of dy turned back,  g = gamma du,  dx = r (g - mean(g) - xh mean(g xh))  (RMS: without mean(g)),
 //   dgamma = sum du xh,  dbeta = sum du  over all rows and heads.
-// Bound by memory: a head is read once and kept in registers.  LH lanes share a head, a lane has whole pairs of
-// either layout (16 bytes; with 32 the backward of video clips took 46.5 us instead of 38); a thread takes up to four heads of a row and looks the
-// row's angles up once (two heads: 41).  Launches one by one, half of the tokens live: 64 x 196 tokens of 12 + 12 heads of 64 bf16 10.2 us forward (3.8 TB/s), 16.4
-// backward (3.5), 4.5 the sums; 8 clips of 8 x 28 x 28 of 16 + 4 heads 29.6 and 37.7; one image 4.0.
+// Bound by memory: a head is read once and kept in registers.  LH lanes share a head, a lane has whole pairs of either layout (16 bytes;
+// with 32 the backward of video clips took 46.5 us instead of 38); a thread takes up to four heads of a row and looks the row's angles up
+// once (two heads: 41).  Launches one by one, half of the tokens live: 64 x 196 tokens of 12 + 12 heads of 64 bf16 10.2 us forward (3.8
+// TB/s), 16.4 backward (3.5), 4.5 the sums; 8 clips of 8 x 28 x 28 of 16 + 4 heads 29.6 and 37.7; one image 4.0.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -353,8 +353,8 @@ static int rotary_groups(int heads, int Dh, int dtype) {
   const int lanes = rotary_lanes(Dh, dtype);
   return kRotaryThreads / (rotary_slots(heads, lanes) * lanes);
 }
-// Workgroups of a tensor: a row a group forward, up to eight a unit (video clips 33.6 us with 8192 workgroups at most, 29.8 with 2048, 30.7 with
-// 1024); four rows of the backward's, a partial row each
+// Workgroups of a tensor: a row a group forward, up to eight a unit (video clips 33.6 us with 8192 workgroups at most, 29.8 with 2048, 30.7
+// with 1024); four rows of the backward's, a partial row each
 static unsigned rotary_blocks(long rows, int heads, int Dh, int dtype) {
   const int groups = rotary_groups(heads, Dh, dtype);
   return heads == 0 ? 0 : (unsigned)std::min<long>((rows + groups - 1) / groups, 2048L);
