@@ -1,6 +1,6 @@
 // Tiles of fp32 products for the projections of small fp32 workloads (linear.hip, linear_bwd.hip, gated_linear.hip): every element is one
 // chain of fused multiply-adds in the order of the contraction, whatever the tile, so that neither its size nor the rest of the call
-// touches an element's bits.
+// touches an element's bits (the weight side adds up chains of 1024 rows).
 // Four waves have a quarter each of EDGE x EDGE elements, in fp32 matrix instructions, whose products are that chain (checked bit for bit,
 // with denormals, infinities and zeros of either sign; 1000 rows of 1400 -> 1000 108 us in vector instructions, 53 so).  Both operands of a
 // step of the contraction are in LDS, those of the next steps on their way in registers, eight loads of each operand a thread.

@@ -633,6 +633,9 @@ linear_bwd_weight_f32_element_kernel(const float* __restrict__ dout, const int32
   }
 }
 
+// The chain of an element is added up and begun anew every 1024 rows, whatever the tile (up to 1024 rows are one chain): over all rows its
+// error grows with their root, 66745 rows of 32 -> 96 4.5e-6 off, the bias' sums 4.8e-6, so 6e-7 and 6.7e-7, in the same time.
+constexpr int kF32FoldRows = 1024;
 template <int EDGE, bool kScale>
 __global__ void __launch_bounds__(kF32Threads, 2)
 linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __restrict__ dout_idx, long ldd,
@@ -641,6 +644,7 @@ linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __re
                              int n_out, float* __restrict__ dW, float* __restrict__ dbias) {
   using Out = F32Quarter<EDGE>;
   __shared__ F32Lds<EDGE, 1> l;
+  __shared__ float folded[Out::kCount + 1][kF32Threads];      // (in registers they spill beside the loads under way)
   const int M = total != nullptr ? min(total[0], m_cap) : m_cap, k_tiles = f32_steps(K, EDGE), n_tiles = f32_steps(n_out, EDGE);
   for (long tile = blockIdx.x; tile < (long)n_tiles * k_tiles; tile += gridDim.x) {
     const int n0 = (int)(tile / k_tiles) * EDGE, k0 = (int)(tile % k_tiles) * EDGE;
@@ -650,6 +654,8 @@ linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __re
     using Place = F32Place<EDGE, false>;
     typename Out::Acc acc[1] = {};
     float bias = 0.f, gate[Place::kCount];
+    const bool fold = M > kF32FoldRows;
+    unsigned rows = 0;
     int gr[Place::kCount], xr[Place::kCount];              // rows of the step to come
     f32_tile_sums<EDGE, 1, false, false, kScale ? 1 : 2>(
         l, M, [&](int i, int) { return gp[(long)gr[i] * ldd]; },
@@ -659,16 +665,26 @@ linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __re
         },
         F32AsIs{}, [&](int, int i, float v) { return kScale ? sigmoidf_dev(gate[i]) * v : v; }, acc,
         [&](const float (&a)[kF32Step<EDGE>][kF32Row<EDGE>], int ks) {
-          if (!sums) return;
-          int kk = 0;
-          for (; kk + 8 <= ks; kk += 8) {
-            float v[8];
+          if (sums) {
+            int kk = 0;
+            for (; kk + 8 <= ks; kk += 8) {
+              float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = a[kk + j][threadIdx.x];
+              for (int j = 0; j < 8; ++j) v[j] = a[kk + j][threadIdx.x];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) bias += v[j];
+              for (int j = 0; j < 8; ++j) bias += v[j];
+            }
+            for (; kk < ks; ++kk) bias += a[kk][threadIdx.x];
           }
-          for (; kk < ks; ++kk) bias += a[kk][threadIdx.x];
+          rows += kF32Step<EDGE>;
+          if (fold && rows % kF32FoldRows == 0) {             // (a thread's own place)
+            const bool first = rows == kF32FoldRows;
+#pragma unroll
+            for (int e = 0; e < Out::kCount; ++e) folded[e][threadIdx.x] = first ? acc[0][e] : folded[e][threadIdx.x] + acc[0][e];
+            folded[Out::kCount][threadIdx.x] = first ? bias : folded[Out::kCount][threadIdx.x] + bias;
+            acc[0] = {};
+            bias = 0.f;
+          }
         },
         [&](int m0) {
 #pragma unroll
@@ -678,6 +694,11 @@ linear_bwd_weight_f32_kernel(const float* __restrict__ dout, const int32_t* __re
             xr[i] = x_idx != nullptr ? x_idx[m] : m;
           }
         });
+    if (fold) {
+#pragma unroll
+      for (int e = 0; e < Out::kCount; ++e) acc[0][e] += folded[e][threadIdx.x];
+      bias += folded[Out::kCount][threadIdx.x];
+    }
     __syncthreads();                 // (the next tile's first step goes where this one's last may be read)
     if (sums && f32_inside(n0, threadIdx.x, n_out)) dbias[n0 + threadIdx.x] = bias;
 #pragma unroll
