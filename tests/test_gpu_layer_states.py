@@ -60,3 +60,19 @@ def test_all_states_without_lengths(pipeline, dtype):
         have = results(q)
         for name in want:
             assert torch.equal(have[name], want[name]), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_state_counts(pipeline, dtype):
+    """All lengths 0 and NaN in every state: the attention adds nothing, what belongs to the states has gradients of 0."""
+    i = Inputs(pipeline, "image", dtype)
+    i.key_lens.zero_()
+    i.states.fill_(float("nan"))
+    p, infer = i.make(pipeline, True), i.make(pipeline, False)
+    for _ in range(3):
+        p.run(*i.args(True))
+        have = results(p)
+        assert all(bool(torch.isfinite(t).all()) for t in have.values())
+        for name in ("gamma_cross_k", "W_cross_kv", "d_states", "gamma_cross_q", "W_cross_q", "W_cross_o"):
+            assert bool((have[name] == 0).all()), name
+        assert torch.equal(infer.run(*i.args(False)), have["y"])
