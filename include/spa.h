@@ -250,7 +250,7 @@ int spa_pack_shifted(const void* x, const uint8_t* mask, const int32_t* counts, 
  * The packing index of a padded batch: the first lens[b] (cut to 0 .. N) of the N places of every sequence b, as spa_pack without rows writes it
  * for a mask of these.  With it the rows that do not count are read by nothing: a projection takes the others through gather_idx, its backward
  * writes zeros in their places.
- * in:  lens [B] int32.   out: cu_seqlens [B+1], gather_idx [B*N] (first T valid, the others are not written), inv_pos [B*N], total [1] int32.  B*N < 2^31.
+ * in:  lens [B] int32.   out: cu_seqlens [B+1], gather_idx [B*N] (first T valid, the others are not written), inv_pos [B*N], total [1] int32.  B <= 65535, B*N < 2^31.
  */
 int spa_pack_lengths(const int32_t* lens, int B, int N, int32_t* cu_seqlens, int32_t* gather_idx, int32_t* inv_pos, int32_t* total, void* stream);
 

@@ -710,9 +710,9 @@ extern "C" int spa_pack_lengths(const int32_t* lens, int B, int N, int32_t* cu_s
   const char* fn = "spa_pack_lengths";
   SPA_REFUSE_IN_GROUP(fn);
   SPA_REQUIRE(lens && cu_seqlens && gather_idx && inv_pos && total, SPA_ERR_INVALID_ARG, "%s: null pointer", fn);
-  SPA_REQUIRE(B >= 1 && N >= 1 && (long)B * N < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B and N must be >= 1 and B*N < 2^31", fn);
+  // (every workgroup adds up the lengths before its own: as many sequences as the attention takes)
+  SPA_REQUIRE(B >= 1 && B <= 65535 && N >= 1 && (long)B * N < 2147483647L, SPA_ERR_INVALID_ARG, "%s: B must be in [1, 65535], N >= 1 and B*N < 2^31", fn);
   const int tiles = (int)(((long)N + kLengthsTile - 1) / kLengthsTile);
-  SPA_REQUIRE((long)B * tiles < 4294967296L / kPackThreads, SPA_ERR_INVALID_ARG, "%s: too many sequences", fn);
   hipLaunchKernelGGL(pack_lengths_kernel, dim3((unsigned)(B * tiles)), dim3(kPackThreads), 0, as_stream(stream), lens, B, N, tiles, cu_seqlens, gather_idx,
                      inv_pos, total);
   return check_launch(fn);

@@ -20,7 +20,7 @@ class Index:
         return self.cu, self.idx, self.inv, self.total
 
 
-@pytest.mark.parametrize("B,N", [(1, 1), (1, 5000), (3, 7), (64, 77), (5, 1024), (4, 1025), (300, 130), (2000, 3)])
+@pytest.mark.parametrize("B,N", [(1, 1), (1, 5000), (3, 7), (64, 77), (5, 1024), (4, 1025), (300, 130), (2000, 3), (65535, 2)])
 @pytest.mark.parametrize("kind", ["random", "none", "all", "past"])
 def test_index(spa, B, N, kind):
     g = torch.Generator().manual_seed(B * N)
